@@ -291,6 +291,89 @@ int lagkv_path_for(const lagkv_params* p, int64_t T);
  */
 const char* lagkv_kernel_for(const lagkv_params* p, int64_t T);
 
+/*
+ * ---- Operators that read a cache ------------------------------------------------------
+ *
+ * Attention of new tokens over a cache (compressed or not) and over themselves, over all of its rows or over
+ * blocks of them that a cheap score picks.  They take the rows as tensors with strides, so that a call can be made for one layer
+ * of a cache whose layers are folded into the batch.  Serving only: there is no backward pass.
+ *
+ * All strides are in ELEMENTS and taken as they are (0 repeats a row, a head or a batch entry; outputs must not
+ * overlap); channels are contiguous.  Q, K, V and the output share one type.  Addresses need the alignment of an
+ * element.  A call needs the device of its stream to be current, allocates nothing, keeps nothing and can be captured into a graph
+ * (two graphs that may run at the same time need a workspace each).  What `lengths`, `parents` and
+ * `blocks` hold is read on the device: any value there is safe, with the meaning given below.
+ */
+typedef struct {
+  int32_t B, H, G, N, D;    /* batch (x layers), KV heads, query heads of each KV head, new tokens, channels (8 .. 256) */
+  int32_t dtype;            /* lagkv_dtype of Q, K, V, K_new, V_new and out                             */
+  int32_t block, n_blocks;  /* lagkv_attend_blocks: rows of a block (a power of two, 16 .. 1024), entries of a list */
+  int64_t T;                /* rows of K and V                                                          */
+  double scale;             /* of the logits (1 / sqrt(D) as a rule)                                    */
+  int64_t q_stride_b, q_stride_h, q_stride_n;       /* Q    [B, H*G, N, D]; query head i reads KV head i / G */
+  int64_t kv_stride_b, kv_stride_h, kv_stride_t;    /* K, V [B, H, T, D]                                */
+  int64_t new_stride_b, new_stride_h, new_stride_n; /* K_new, V_new [B, H, N, D]                        */
+  int64_t out_stride_b, out_stride_h, out_stride_n; /* out  [B, H*G, N, D]                              */
+  int64_t parents_stride_b; /* parents [B, N]; 0: one tree for all                                      */
+} lagkv_attend_params;
+
+/* Tokens of a drafted tree (N of a call with parents). */
+#define LAGKV_TREE_MAX 256
+
+/*
+ * Device workspace, in bytes, of a lagkv_attend or (n_blocks > 0) lagkv_attend_blocks call with these parameters; 0 on
+ * invalid ones.  It depends on B, H, G, N, D, dtype, T (block, n_blocks) alone.  16-byte aligned; nothing in it has to be
+ * cleared, and nothing in it outlives the call.
+ */
+size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p);
+
+/*
+ * out = softmax(scale Q K^T) V over what each new token sees, and the logarithm of the softmax's denominator:
+ *   - rows 0 .. lengths[b]-1 of the cache (lengths: [B] device int32, values below 0 or above T count as 0 and T; NULL: all T);
+ *   - of the new tokens' rows K_new, V_new (NULL: none), with parents NULL those of tokens 0 .. n: a single token, or
+ *     a chunk of a prompt; else those of token n and of its ancestors in a drafted tree: parents[b,n] (device int32,
+ *     N <= LAGKV_TREE_MAX) is the token that n was drafted behind, an earlier one, or -1 behind the cache.  Any other
+ *     value says that n is no token (padding): it sees nothing, nothing sees it, and a path up the tree ends before it.
+ *   out  dtype of Q; a row that sees nothing is 0
+ *   lse  [B, H*G, N] device fp32, dense, or NULL: log sum exp of the logits, natural; -inf where nothing is seen
+ * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold.
+ * Logits, sums and products are held in fp32; results do not depend on anything but the arguments (no atomics).
+ * N = 0: LAGKV_OK, nothing is done.  T = 0 is allowed (K, V may be NULL then).
+ */
+int lagkv_attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
+                 const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse, void* ws,
+                 size_t ws_bytes, void* hip_stream);
+
+/*
+ * The same over listed blocks of the cache: `blocks` [B, H, N, n_blocks] device int32, dense, names for every token and KV
+ * head the blocks (rows j*block .. j*block+block-1) that its G query heads read, as lagkv_select_blocks writes them.  An
+ * entry outside the blocks that lengths[b] leaves (-1, say) stands for no rows; one that is listed twice counts twice.
+ */
+int lagkv_attend_blocks(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
+                        const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out,
+                        float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Smallest and largest key of every block of rows, channel by channel (Eq. 7-8 for each block): lo, hi [B, H,
+ * ceil(T / block), D] device, dense, type of K.  Of p the fields B, H, D, dtype, T, block and kv_stride_* are read.
+ * Only blocks from that of row `start` on are written (an update behind appended or compressed rows; 0: all).  A block with
+ * no row before lengths[b] gets +inf and -inf.
+ */
+int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_t* lengths, int64_t start, void* lo, void* hi,
+                       void* hip_stream);
+
+/*
+ * The n_blocks blocks that each new token reads in every KV head: those of the highest
+ *     sum over the head's G query rows and the channels of max(q lo, q hi),
+ * which no row of the block exceeds with its sum of q.k; of equal ones the lower.  The first `n_first` and the last `n_last`
+ * of the blocks that lengths[b] leaves are always among them (n_first + n_last <= n_blocks).  Scores are summed in 64 bits.
+ *   blocks [B, H, N, n_blocks] device int32, dense: ascending; -1 behind the last where there are fewer blocks
+ * Of p the fields B, H, G, N, D, dtype, T, block, n_blocks and q_stride_* are read.  Workspace: 8 * B * H * N * ceil(T /
+ * block) bytes, 16-byte aligned.
+ */
+int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void* lo, const void* hi, const int32_t* lengths,
+                        int32_t n_first, int32_t n_last, int32_t* blocks, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* Static, human readable text for a lagkv_status. */
 const char* lagkv_strerror(int status);
 

@@ -1,0 +1,259 @@
+// C ABI of the operators that read a cache (see include/lagkv.h): host-side validation, launch shapes and launches.
+#include <cmath>
+#include <cstring>
+
+#include "attend_internal.hpp"
+#include "compress_ws.h"
+#include "lagkv.h"
+#include "lagkv_internal.hpp"
+
+using namespace lagkv;
+
+namespace {
+
+constexpr int64_t kMost = 0x7fffffffLL;  // rows, and tokens times query heads
+
+int esize_of(const lagkv_attend_params* p) { return p->dtype == LAGKV_F32 ? 4 : 2; }
+bool known(int32_t dtype) { return dtype == LAGKV_F32 || dtype == LAGKV_BF16 || dtype == LAGKV_F16; }
+bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+int shift_of(int32_t block) { return __builtin_ctz((unsigned)block); }
+bool block_ok(int32_t block) { return block >= 16 && block <= 1024 && (block & (block - 1)) == 0; }
+
+int check_heads(const lagkv_attend_params* p) {
+  if (!p) return LAGKV_EINVAL;
+  if (!known(p->dtype)) return LAGKV_EDTYPE;
+  if (p->B < 1 || p->H < 1 || p->D < kMinHead || p->D > kMaxHead) return LAGKV_ESHAPE;
+  if ((int64_t)p->B * p->H > (1 << 24) || p->T < 0 || p->T > kMost) return LAGKV_ESHAPE;
+  return LAGKV_OK;
+}
+
+int check_tokens(const lagkv_attend_params* p) {
+  if (p->G < 1 || p->N < 0) return LAGKV_ESHAPE;
+  if ((int64_t)p->G * p->N > kMost || (int64_t)p->B * p->H * p->G > kMost) return LAGKV_ESHAPE;
+  if (p->q_stride_b < 0 || p->q_stride_h < 0 || p->q_stride_n < 0) return LAGKV_ESHAPE;
+  return LAGKV_OK;
+}
+
+// Rows [B, heads, N] of D channels that lie apart: with the axes of more than one entry from the smallest stride up, each
+// steps over all of what the ones before it span.
+bool apart(int64_t D, const int64_t (&n)[3], const int64_t (&stride)[3]) {
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[order[j]] < stride[order[i]]) {
+        const int t = order[i];
+        order[i] = order[j];
+        order[j] = t;
+      }
+  int64_t span = D;
+  for (int i : order) {
+    if (n[i] <= 1) continue;
+    if (stride[i] < span) return false;
+    span += stride[i] * (n[i] - 1);
+  }
+  return true;
+}
+
+int check_attend(const lagkv_attend_params* p, bool pick) {
+  int rc = check_heads(p);
+  if (rc != LAGKV_OK) return rc;
+  rc = check_tokens(p);
+  if (rc != LAGKV_OK) return rc;
+  if (!std::isfinite((float)p->scale)) return LAGKV_EINVAL;
+  if (pick && (!block_ok(p->block) || p->n_blocks < 1 || (int64_t)p->n_blocks * p->block > kMost)) return LAGKV_EINVAL;
+  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0 || p->new_stride_b < 0 || p->new_stride_h < 0 ||
+      p->new_stride_n < 0 || p->out_stride_b < 0 || p->out_stride_h < 0 || p->out_stride_n < 0 || p->parents_stride_b < 0)
+    return LAGKV_ESHAPE;
+  return LAGKV_OK;
+}
+
+// Query rows of a tile: as many as there are, up to what the registers hold.  Pieces of the cache: enough workgroups
+// for every compute unit to hold some, and no piece below four steps a wavefront.
+bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
+  pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
+  pl->rows = pick ? p->G : p->G * p->N;
+  pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
+  pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
+  const int64_t kt = p->dtype == LAGKV_F32 ? 16 : 32;
+  const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
+  const int64_t steps = (seen + kt - 1) / kt + (p->N + kt - 1) / kt;
+  const int64_t groups = pl->units * pl->row_tiles;
+  int64_t splits = 1024 / (groups > 0 ? groups : 1);
+  if (splits > steps / 16) splits = steps / 16;
+  if (splits > 256) splits = 256;
+  if (splits < 1) splits = 1;
+  pl->splits = (int)splits;
+  const int64_t parts = pl->units * splits * pl->rows, ld = (p->D + 3) & ~3;
+  pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
+  pl->ws_bytes = splits > 1 ? pl->off_ml + ws_align_up((size_t)parts * 8) : 0;
+  // the grids of the two kernels
+  return grid_fits((pl->units * splits + 7) / 8 * 8 * pl->row_tiles, 256) && grid_fits(pl->units * pl->rows, 256);
+}
+
+int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
+           const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse,
+           void* ws, size_t ws_bytes, void* hip_stream, bool pick) {
+  int rc = check_attend(p, pick);
+  if (rc != LAGKV_OK) return rc;
+  if (p->N == 0) return LAGKV_OK;
+  if (!Q || !out || (p->T > 0 && (!K || !V)) || (pick && !blocks) || !K_new != !V_new || (parents && !K_new)) return LAGKV_EINVAL;
+  if (parents && p->N > kMaxTree) return LAGKV_ESHAPE;
+  const int64_t n[3] = {p->B, (int64_t)p->H * p->G, p->N};
+  const int64_t st[3] = {p->out_stride_b, p->out_stride_h, p->out_stride_n};
+  if (!apart(p->D, n, st)) return LAGKV_ESHAPE;
+  const int es = esize_of(p);
+  if (!aligned(Q, es) || !aligned(K, es) || !aligned(V, es) || !aligned(K_new, es) || !aligned(V_new, es) || !aligned(out, es) ||
+      !aligned(lengths, 4) || !aligned(parents, 4) || !aligned(blocks, 4) || !aligned(lse, 4))
+    return LAGKV_EINVAL;
+  AttendPlan pl;
+  if (!plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
+  if (pl.ws_bytes > 0 && (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
+  AttendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.Q = (const char*)Q;
+  a.K = (const char*)K;
+  a.V = (const char*)V;
+  a.K_new = (const char*)K_new;
+  a.V_new = (const char*)V_new;
+  a.lengths = lengths;
+  a.parents = parents;
+  a.blocks = pick ? blocks : nullptr;
+  a.out = (char*)out;
+  a.lse = lse;
+  a.part_o = (float*)ws;
+  a.part_ml = (float*)((char*)ws + pl.off_ml);
+  a.qsb = p->q_stride_b * es;
+  a.qsh = p->q_stride_h * es;
+  a.qsn = p->q_stride_n * es;
+  a.ksb = p->kv_stride_b * es;
+  a.ksh = p->kv_stride_h * es;
+  a.kst = p->kv_stride_t * es;
+  a.nsb = p->new_stride_b * es;
+  a.nsh = p->new_stride_h * es;
+  a.nst = p->new_stride_n * es;
+  a.osb = p->out_stride_b * es;
+  a.osh = p->out_stride_h * es;
+  a.osn = p->out_stride_n * es;
+  a.psb = p->parents_stride_b;
+  a.T = p->T;
+  a.units = pl.units;
+  a.B = p->B;
+  a.H = p->H;
+  a.G = p->G;
+  a.N = p->N;
+  a.D = p->D;
+  a.n_new = K_new ? p->N : 0;
+  a.block = pick ? p->block : 0;
+  a.block_shift = pick ? shift_of(p->block) : 0;
+  a.n_blocks = pick ? p->n_blocks : 0;
+  a.part_ld = (p->D + 3) & ~3;
+  a.rows = pl.rows;
+  a.row_tiles = pl.row_tiles;
+  a.splits = pl.splits;
+  a.scale = (float)p->scale;
+  hipStream_t s = (hipStream_t)hip_stream;
+  hipError_t e = p->dtype == LAGKV_F32    ? launch_attend_f32(a, pl.row_tile, s)
+                 : p->dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, s)
+                                          : launch_attend_f16(a, pl.row_tile, s);
+  if (e == hipSuccess && pl.splits > 1) e = launch_attend_join(a, p->dtype, s);
+  return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p) {
+  if (!p) return 0;
+  const bool pick = p->n_blocks > 0;
+  AttendPlan pl;
+  if (check_attend(p, pick) != LAGKV_OK || p->N == 0 || !plan_of(p, pick, &pl)) return 0;
+  return pl.ws_bytes;
+}
+
+int lagkv_attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
+                 const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse, void* ws, size_t ws_bytes,
+                 void* hip_stream) {
+  return attend(p, Q, K, V, lengths, nullptr, K_new, V_new, parents, out, lse, ws, ws_bytes, hip_stream, false);
+}
+
+int lagkv_attend_blocks(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
+                        const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out,
+                        float* lse, void* ws, size_t ws_bytes, void* hip_stream) {
+  return attend(p, Q, K, V, lengths, blocks, K_new, V_new, parents, out, lse, ws, ws_bytes, hip_stream, true);
+}
+
+int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_t* lengths, int64_t start, void* lo, void* hi,
+                       void* hip_stream) {
+  int rc = check_heads(p);
+  if (rc != LAGKV_OK) return rc;
+  if (!block_ok(p->block) || start < 0) return LAGKV_EINVAL;
+  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0) return LAGKV_ESHAPE;
+  if (p->T == 0 || start >= p->T) return LAGKV_OK;
+  if (!K || !lo || !hi) return LAGKV_EINVAL;
+  const int es = esize_of(p);
+  if (!aligned(K, es) || !aligned(lo, es) || !aligned(hi, es) || !aligned(lengths, 4)) return LAGKV_EINVAL;
+  BoundsArgs a;
+  a.K = (const char*)K;
+  a.lengths = lengths;
+  a.lo = (char*)lo;
+  a.hi = (char*)hi;
+  a.ksb = p->kv_stride_b * es;
+  a.ksh = p->kv_stride_h * es;
+  a.kst = p->kv_stride_t * es;
+  a.T = p->T;
+  a.nb = (p->T + p->block - 1) / p->block;
+  a.first = start / p->block;
+  a.B = p->B;
+  a.H = p->H;
+  a.D = p->D;
+  a.block = p->block;
+  a.dtype = p->dtype;
+  if (!grid_fits(((int64_t)p->B * p->H * (a.nb - a.first) + 3) / 4, 256)) return LAGKV_ESHAPE;
+  return launch_block_bounds(a, (hipStream_t)hip_stream) == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
+}
+
+int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void* lo, const void* hi, const int32_t* lengths,
+                        int32_t n_first, int32_t n_last, int32_t* blocks, void* ws, size_t ws_bytes, void* hip_stream) {
+  int rc = check_heads(p);
+  if (rc != LAGKV_OK) return rc;
+  rc = check_tokens(p);
+  if (rc != LAGKV_OK) return rc;
+  if (!block_ok(p->block) || p->n_blocks < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > p->n_blocks)
+    return LAGKV_EINVAL;
+  if (p->N == 0) return LAGKV_OK;
+  if (!Q || !blocks || (p->T > 0 && (!lo || !hi))) return LAGKV_EINVAL;
+  const int es = esize_of(p);
+  if (!aligned(Q, es) || !aligned(lo, es) || !aligned(hi, es) || !aligned(lengths, 4) || !aligned(blocks, 4)) return LAGKV_EINVAL;
+  SelectArgs a;
+  a.Q = (const char*)Q;
+  a.lo = (const char*)lo;
+  a.hi = (const char*)hi;
+  a.lengths = lengths;
+  a.score = (double*)ws;
+  a.blocks = blocks;
+  a.qsb = p->q_stride_b * es;
+  a.qsh = p->q_stride_h * es;
+  a.qsn = p->q_stride_n * es;
+  a.T = p->T;
+  a.nb = (p->T + p->block - 1) / p->block;
+  a.B = p->B;
+  a.H = p->H;
+  a.G = p->G;
+  a.N = p->N;
+  a.D = p->D;
+  a.block = p->block;
+  a.k = p->n_blocks;
+  a.first = n_first;
+  a.last = n_last;
+  a.dtype = p->dtype;
+  const int64_t units = (int64_t)p->B * p->H * p->N;
+  if (!grid_fits(units, 256) || !grid_fits((int64_t)p->B * p->H * (a.nb + 1), 256)) return LAGKV_ESHAPE;
+  if (a.nb > 0 && (!ws || ws_bytes < 8 * (size_t)(units * a.nb) || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
+  hipStream_t s = (hipStream_t)hip_stream;
+  hipError_t e = a.nb > 0 ? launch_block_scores(a, s) : hipSuccess;
+  if (e == hipSuccess) e = launch_block_select(a, s);
+  return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
+}
+
+}  // extern "C"

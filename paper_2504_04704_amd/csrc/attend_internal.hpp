@@ -1,0 +1,71 @@
+// Internal interface between the host layer of the cache-reading operators (attend_api.hip) and their kernels
+// (attend_pass.hpp, block_pass.hip).  Not part of the public ABI.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lagkv.h"
+
+namespace lagkv {
+
+// A unit is what one list of cache rows is for: a stream (b, h) with its G*N query rows, token-major (row n*G + g), or
+// with blocks listed for each token, (b, h, n) with its G query rows.  Strides are in BYTES here.
+struct AttendArgs {
+  const char *Q, *K, *V, *K_new, *V_new;
+  const int32_t* lengths;  // [B] or nullptr
+  const int32_t* parents;  // [B,N] (or [N]) or nullptr
+  const int32_t* blocks;   // [B,H,N,n_blocks] or nullptr
+  char* out;
+  float* lse;      // [B,H*G,N] or nullptr
+  float* part_o;   // [units, splits, rows, part_ld], where splits > 1
+  float* part_ml;  // [units, splits, rows, 2]: maximum (base 2), sum
+  int64_t qsb, qsh, qsn, ksb, ksh, kst, nsb, nsh, nst, osb, osh, osn, psb;
+  int64_t T, units;
+  int32_t B, H, G, N, D;
+  int32_t n_new;  // N with K_new, else 0
+  int32_t block, block_shift, n_blocks;
+  int32_t part_ld;  // D, rounded up to 4
+  int32_t rows;    // of a unit
+  int32_t row_tiles, splits;
+  float scale;
+};
+
+// Launch shape, a pure function of the parameters: rows of a tile, tiles of a unit, pieces the cache is cut into.
+struct AttendPlan {
+  int row_tile, row_tiles, splits;
+  int64_t units;
+  int32_t rows;
+  size_t off_ml, ws_bytes;
+};
+
+hipError_t launch_attend_f32(const AttendArgs& a, int row_tile, hipStream_t s);
+hipError_t launch_attend_bf16(const AttendArgs& a, int row_tile, hipStream_t s);
+hipError_t launch_attend_f16(const AttendArgs& a, int row_tile, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);
+
+struct BoundsArgs {
+  const char* K;
+  const int32_t* lengths;
+  char *lo, *hi;  // [B,H,nb,D]
+  int64_t ksb, ksh, kst;
+  int64_t T, nb, first;  // first block that is written
+  int32_t B, H, D, block, dtype;
+};
+hipError_t launch_block_bounds(const BoundsArgs& a, hipStream_t s);
+
+struct SelectArgs {
+  const char *Q, *lo, *hi;
+  const int32_t* lengths;
+  double* score;     // [B,H,N,nb]
+  int32_t* blocks;   // [B,H,N,k]
+  int64_t qsb, qsh, qsn;
+  int64_t T, nb;
+  int32_t B, H, G, N, D, block, k, first, last, dtype;
+};
+hipError_t launch_block_scores(const SelectArgs& a, hipStream_t s);
+hipError_t launch_block_select(const SelectArgs& a, hipStream_t s);
+
+constexpr int kMaxTree = 256;  // tokens of a drafted tree
+constexpr int kMinHead = 8, kMaxHead = 256;
+
+}  // namespace lagkv

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import importlib
+import math
 import os
 import warnings
 from dataclasses import dataclass
@@ -35,7 +36,9 @@ EXPORTS = ("lagkv_plan", "lagkv_keep_for_compression", "lagkv_workspace_bytes", 
            "lagkv_prefill_rows",
            "lagkv_append_and_compress", "lagkv_prefill", "lagkv_launch_hint", "lagkv_launch_hint_ex", "lagkv_path_for",
            "lagkv_kernel_for", "lagkv_strerror",
-           "lagkv_version")
+           "lagkv_version",
+           "lagkv_attend_workspace_bytes", "lagkv_attend", "lagkv_attend_blocks", "lagkv_block_bounds",
+           "lagkv_select_blocks")
 
 
 class LagKVError(RuntimeError):
@@ -62,6 +65,14 @@ class CacheT(C.Structure):
     _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("pos", C.c_void_p),
                 ("capacity", C.c_int64), ("n_static", C.c_int64), ("n_tail", C.c_int64),
                 ("n_seen", C.c_int64)]
+
+
+class AttendParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("G", C.c_int32), ("N", C.c_int32), ("D", C.c_int32),
+                ("dtype", C.c_int32), ("block", C.c_int32), ("n_blocks", C.c_int32),
+                ("T", C.c_int64), ("scale", C.c_double),
+                ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3), ("new_stride", C.c_int64 * 3),
+                ("out_stride", C.c_int64 * 3), ("parents_stride_b", C.c_int64)]
 
 
 def lib_path() -> str:
@@ -114,6 +125,17 @@ def load():
     lib.lagkv_strerror.restype = C.c_char_p
     lib.lagkv_version.argtypes = []
     lib.lagkv_version.restype = C.c_int
+    ap = C.POINTER(AttendParams)
+    lib.lagkv_attend_workspace_bytes.argtypes = [ap]
+    lib.lagkv_attend_workspace_bytes.restype = sz
+    lib.lagkv_attend.argtypes = [ap] + [vp] * 10 + [sz, vp]
+    lib.lagkv_attend.restype = C.c_int
+    lib.lagkv_attend_blocks.argtypes = [ap] + [vp] * 11 + [sz, vp]
+    lib.lagkv_attend_blocks.restype = C.c_int
+    lib.lagkv_block_bounds.argtypes = [ap, vp, vp, i64, vp, vp, vp]
+    lib.lagkv_block_bounds.restype = C.c_int
+    lib.lagkv_select_blocks.argtypes = [ap, vp, vp, vp, vp, C.c_int32, C.c_int32, vp, vp, sz, vp]
+    lib.lagkv_select_blocks.restype = C.c_int
     _lib = lib
     _native = _load_native(lib)
     return lib
@@ -362,6 +384,205 @@ def compress_static(K: torch.Tensor, V: torch.Tensor, S: int, L: int, r: float, 
                                         Vo.data_ptr(), _ptr(idx_out), _ptr(scores_out),
                                         _stream_ptr(K.device)), "lagkv_compress_static")
     return pl
+
+
+# ---- operators that read a cache (include/lagkv.h, "Operators that read a cache") ----
+
+TREE_MAX = 256
+
+
+@dataclass
+class Attended:
+    out: torch.Tensor               # [B,H*G,N,D], layout of q
+    lse: Optional[torch.Tensor]     # [B,H*G,N] fp32
+
+
+def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """A [.., .., rows, D] device tensor with contiguous channels, of the type and on the device of `like`."""
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+        raise ValueError(f"{name} must be a 4-dimensional tensor with contiguous channels")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    if not t.is_cuda:
+        raise RuntimeError(f"{name} must be a device tensor; there is no CPU path")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must share dtype and device with the others")
+
+
+def _ints(name: str, t: torch.Tensor, shape, device):
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a dense int32 tensor {list(shape)} on the device of q")
+
+
+def _no_grad(*tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise RuntimeError("the operators that read a cache have no backward pass: call them under torch.no_grad()")
+
+
+class _on:
+    """The device of a call made current for it, where it is not."""
+
+    def __init__(self, device):
+        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *a):
+        if self.guard is not None:
+            self.guard.__exit__(*a)
+
+
+def _bytes(ws: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tensor]:
+    if ws is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
+        raise ValueError("ws must be a dense uint8 tensor on the device of the inputs")
+    return ws
+
+
+def _attend(where, q, K, V, blocks, block, K_new, V_new, parents, lengths, scale, out, want_lse, ws) -> Attended:
+    _rows("q", q)
+    _rows("K", K, q)
+    _same_layout(K, V)
+    _no_grad(q, K, V, K_new, V_new)
+    B, H, T, D = K.shape
+    heads, N = q.shape[1], q.shape[2]
+    if q.shape[0] != B or q.shape[3] != D or H == 0 or heads % H:
+        raise ValueError("q must be [B,H*G,N,D] for K, V [B,H,T,D]")
+    p = AttendParams(B, H, heads // H, N, D, _DTYPES[q.dtype], block, 0, T, 1.0 / math.sqrt(D) if scale is None else float(scale))
+    p.q_stride[:] = q.stride()[:3]
+    p.kv_stride[:] = K.stride()[:3]
+    device = q.device
+    if (K_new is None) != (V_new is None) or (parents is not None and K_new is None):
+        raise ValueError("K_new and V_new go together, and parents with them")
+    if K_new is not None:
+        _rows("K_new", K_new, q)
+        _same_layout(K_new, V_new)
+        if tuple(K_new.shape) != (B, H, N, D):
+            raise ValueError("K_new, V_new must be [B,H,N,D]")
+        p.new_stride[:] = K_new.stride()[:3]
+    if parents is not None:
+        if parents.dim() == 2:
+            _ints("parents", parents, (B, N), device)
+            p.parents_stride_b = N
+        else:
+            _ints("parents", parents, (N,), device)
+    if lengths is not None:
+        _ints("lengths", lengths, (B,), device)
+    if blocks is not None:
+        if blocks.dim() != 4:
+            raise ValueError("blocks must be [B,H,N,k]")
+        _ints("blocks", blocks, (B, H, N, blocks.shape[3]), device)
+        p.n_blocks = blocks.shape[3]
+    if out is None:
+        out = torch.empty_like(q)
+        if out.stride(3) != 1 and D > 1:
+            out = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        _rows("out", out, q)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    p.out_stride[:] = out.stride()[:3]
+    lse = torch.empty((B, heads, N), dtype=torch.float32, device=device) if want_lse else None
+    lib = load()
+    ref = C.byref(p)
+    with _on(device):
+        ws = _bytes(ws, lib.lagkv_attend_workspace_bytes(ref), device)
+        args = (_ptr(K_new), _ptr(V_new), _ptr(parents), out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
+                _stream_ptr(device))
+        if blocks is None:
+            rc = lib.lagkv_attend(ref, q.data_ptr(), K.data_ptr(), V.data_ptr(), _ptr(lengths), *args)
+        else:
+            rc = lib.lagkv_attend_blocks(ref, q.data_ptr(), K.data_ptr(), V.data_ptr(), _ptr(lengths), blocks.data_ptr(), *args)
+    _check(rc, where)
+    return Attended(out, lse)
+
+
+def attend(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, K_new: Optional[torch.Tensor] = None,
+           V_new: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
+           lengths: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+           want_lse: bool = False, ws: Optional[torch.Tensor] = None) -> Attended:
+    """lagkv_attend: attention of N new tokens, q [B,H*G,N,D], over a cache K, V [B,H,T,D] (its first lengths[b] rows) and,
+    with K_new, V_new [B,H,N,D], over themselves: each the ones before it and itself or, with parents [N] or [B,N], its
+    ancestors in a drafted tree and itself.  Tensors may have any strides with contiguous channels; `out` takes the
+    layout of q unless it is given.  There is no backward pass."""
+    return _attend("lagkv_attend", q, K, V, None, 0, K_new, V_new, parents, lengths, scale, out, want_lse, ws)
+
+
+def attend_blocks(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, blocks: torch.Tensor, block: int,
+                  K_new: Optional[torch.Tensor] = None, V_new: Optional[torch.Tensor] = None,
+                  parents: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None, want_lse: bool = False,
+                  ws: Optional[torch.Tensor] = None) -> Attended:
+    """lagkv_attend_blocks: `attend` over the listed blocks of `block` cache rows alone; blocks [B,H,N,k] int32, as
+    select_blocks gives them."""
+    if blocks is None:
+        raise ValueError("blocks must be [B,H,N,k]")
+    return _attend("lagkv_attend_blocks", q, K, V, blocks, index(block), K_new, V_new, parents, lengths, scale, out, want_lse, ws)
+
+
+def block_bounds(K: torch.Tensor, block: int, lengths: Optional[torch.Tensor] = None, start: int = 0,
+                 out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """lagkv_block_bounds: smallest and largest key (lo, hi) [B,H,ceil(T/block),D] of every block of rows, channel by
+    channel; with `start` and `out` only the blocks from that of row `start` on are written."""
+    _rows("K", K)
+    _no_grad(K)
+    B, H, T, D = K.shape
+    block, start = index(block), index(start)
+    if block < 1:
+        raise LagKVError(EINVAL, "lagkv_block_bounds")
+    shape = (B, H, -(-T // block), D)
+    if out is None:
+        if start > 0:
+            raise ValueError("start needs out: the blocks before it are left as they are")
+        out = (torch.empty(shape, dtype=K.dtype, device=K.device), torch.empty(shape, dtype=K.dtype, device=K.device))
+    lo, hi = out
+    for t in out:
+        if tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != K.dtype or t.device != K.device:
+            raise ValueError("output buffers must be dense [B,H,ceil(T/block),D] of the input dtype")
+    if lengths is not None:
+        _ints("lengths", lengths, (B,), K.device)
+    p = AttendParams(B=B, H=H, D=D, dtype=_DTYPES[K.dtype], block=block, T=T)
+    p.kv_stride[:] = K.stride()[:3]
+    with _on(K.device):
+        _check(load().lagkv_block_bounds(C.byref(p), K.data_ptr(), _ptr(lengths), start, lo.data_ptr(), hi.data_ptr(),
+                                         _stream_ptr(K.device)), "lagkv_block_bounds")
+    return lo, hi
+
+
+def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, block: int, k: int, first: int = 0,
+                  last: int = 0, lengths: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """lagkv_select_blocks: for every new token and KV head the k blocks of a cache of T rows whose bounds allow the
+    largest logits, the first `first` and last `last` always among them; int32 [B,H,N,k], ascending, -1 behind."""
+    _rows("q", q)
+    _rows("lo", lo, q)
+    _no_grad(q, lo, hi)
+    B, H, nb, D = lo.shape
+    heads, N = q.shape[1], q.shape[2]
+    T, block, k = index(T), index(block), index(k)
+    if block < 1 or k < 1 or T < 0:
+        raise LagKVError(EINVAL, "lagkv_select_blocks")
+    if q.shape[0] != B or q.shape[3] != D or H == 0 or heads % H or nb != -(-T // block):
+        raise ValueError("q must be [B,H*G,N,D] for lo, hi [B,H,ceil(T/block),D]")
+    if hi.shape != lo.shape or hi.dtype != lo.dtype or hi.device != lo.device or not lo.is_contiguous() or not hi.is_contiguous():
+        raise ValueError("lo and hi must be dense and share shape, dtype and device")
+    if lengths is not None:
+        _ints("lengths", lengths, (B,), q.device)
+    if out is None:
+        out = torch.empty((B, H, N, k), dtype=torch.int32, device=q.device)
+    else:
+        _ints("out", out, (B, H, N, k), q.device)
+    p = AttendParams(B=B, H=H, G=heads // H, N=N, D=D, dtype=_DTYPES[q.dtype], block=block, n_blocks=k, T=T)
+    p.q_stride[:] = q.stride()[:3]
+    with _on(q.device):
+        ws = _bytes(ws, 8 * B * H * N * nb, q.device)
+        _check(load().lagkv_select_blocks(C.byref(p), q.data_ptr(), lo.data_ptr(), hi.data_ptr(), _ptr(lengths), index(first),
+                                          index(last), out.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
+                                          _stream_ptr(q.device)), "lagkv_select_blocks")
+    return out
 
 
 class Cache:
