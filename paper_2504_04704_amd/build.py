@@ -17,7 +17,8 @@ SOURCES = ["lagkv_api.hip", "split_pass.hip", "hold_pass.hip", "append_pass.hip"
            "chunk_f32.hip", "chunk_bf16.hip", "chunk_f16.hip",
            "ring_f32.hip", "ring_bf16.hip", "ring_f16.hip",
            "round_f32.hip", "round_bf16.hip", "round_f16.hip", "static_scratch.hip",
-           "attend_api.hip", "attend_f32.hip", "attend_bf16.hip", "attend_f16.hip", "attend_join.hip", "block_pass.hip"]
+           "attend_api.hip", "attend_f32.hip", "attend_bf16.hip", "attend_f16.hip", "attend_wide_bf16.hip", "attend_wide_f16.hip",
+           "attend_join.hip", "block_pass.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

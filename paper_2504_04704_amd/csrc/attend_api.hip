@@ -59,7 +59,7 @@ int check_attend(const lagkv_attend_params* p, bool pick) {
   if (rc != LAGKV_OK) return rc;
   rc = check_tokens(p);
   if (rc != LAGKV_OK) return rc;
-  if (!std::isfinite((float)p->scale)) return LAGKV_EINVAL;
+  if (!std::isfinite((float)(p->scale * 1.4426950408889634))) return LAGKV_EINVAL;
   if (pick && (!block_ok(p->block) || p->n_blocks < 1 || (int64_t)p->n_blocks * p->block > kMost)) return LAGKV_EINVAL;
   if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0 || p->new_stride_b < 0 || p->new_stride_h < 0 ||
       p->new_stride_n < 0 || p->out_stride_b < 0 || p->out_stride_h < 0 || p->out_stride_n < 0 || p->parents_stride_b < 0)
@@ -72,14 +72,15 @@ int check_attend(const lagkv_attend_params* p, bool pick) {
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
-  pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
+  pl->wide = !pick && p->dtype != LAGKV_F32 && pl->rows > 32;
+  pl->row_tile = pl->wide ? (pl->rows <= 128 || p->D > 128 ? 128 : 256) : pl->rows <= 16 || p->D > 128 ? 16 : 32;
   pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
-  const int64_t kt = p->dtype == LAGKV_F32 ? 16 : 32;
+  const int64_t kt = pl->wide ? 64 : p->dtype == LAGKV_F32 ? 16 : 32;
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
   const int64_t steps = (seen + kt - 1) / kt + (p->N + kt - 1) / kt;
   const int64_t groups = pl->units * pl->row_tiles;
-  int64_t splits = 1024 / (groups > 0 ? groups : 1);
-  if (splits > steps / 16) splits = steps / 16;
+  int64_t splits = (pl->wide ? (pl->row_tile == 128 ? 512 : 256) : 1024) / (groups > 0 ? groups : 1);
+  if (splits > steps / (pl->wide ? 4 : 16)) splits = steps / (pl->wide ? 4 : 16);
   if (splits > 256) splits = 256;
   if (splits < 1) splits = 1;
   pl->splits = (int)splits;
@@ -87,7 +88,7 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
   pl->ws_bytes = splits > 1 ? pl->off_ml + ws_align_up((size_t)parts * 8) : 0;
   // the grids of the two kernels
-  return grid_fits((pl->units * splits + 7) / 8 * 8 * pl->row_tiles, 256) && grid_fits(pl->units * pl->rows, 256);
+  return grid_fits((pl->units * splits + 7) / 8 * 8 * pl->row_tiles, 512) && grid_fits(pl->units * pl->rows, 256);
 }
 
 int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
@@ -150,9 +151,10 @@ int attend(const lagkv_attend_params* p, const void* Q, const void* K, const voi
   a.rows = pl.rows;
   a.row_tiles = pl.row_tiles;
   a.splits = pl.splits;
-  a.scale = (float)p->scale;
+  a.scale = (float)(p->dtype == LAGKV_F32 ? p->scale : p->scale * 1.4426950408889634);
   hipStream_t s = (hipStream_t)hip_stream;
-  hipError_t e = p->dtype == LAGKV_F32    ? launch_attend_f32(a, pl.row_tile, s)
+  hipError_t e = pl.wide ? (p->dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))
+                 : p->dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, s)
                  : p->dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, s)
                                           : launch_attend_f16(a, pl.row_tile, s);
   if (e == hipSuccess && pl.splits > 1) e = launch_attend_join(a, p->dtype, s);

@@ -27,11 +27,12 @@ struct AttendArgs {
   int32_t part_ld;  // D, rounded up to 4
   int32_t rows;    // of a unit
   int32_t row_tiles, splits;
-  float scale;
+  float scale;  // times log2 e for the 16-bit types
 };
 
 // Launch shape, a pure function of the parameters: rows of a tile, tiles of a unit, pieces the cache is cut into.
 struct AttendPlan {
+  bool wide;
   int row_tile, row_tiles, splits;
   int64_t units;
   int32_t rows;
@@ -41,6 +42,8 @@ struct AttendPlan {
 hipError_t launch_attend_f32(const AttendArgs& a, int row_tile, hipStream_t s);
 hipError_t launch_attend_bf16(const AttendArgs& a, int row_tile, hipStream_t s);
 hipError_t launch_attend_f16(const AttendArgs& a, int row_tile, hipStream_t s);
+hipError_t launch_wide_bf16(const AttendArgs& a, int row_tile, hipStream_t s);
+hipError_t launch_wide_f16(const AttendArgs& a, int row_tile, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);
 
 struct BoundsArgs {

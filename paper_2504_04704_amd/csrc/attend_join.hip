@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     const int64_t at = first + (int64_t)s * a.rows;
     const float mx = a.part_ml[at * 2];
     if (mx == -INFINITY) continue;  // (nothing seen: its outputs were written as zeros)
-    const float f = __builtin_amdgcn_exp2f((mx - top) * 1.44269504088896f);
+    const float f = __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
     sum += f * a.part_ml[at * 2 + 1];
     if (lane * 4 < a.D) v += f * *(const f32x4*)(a.part_o + at * a.part_ld + lane * 4);
   }
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     else *(uint16_t*)(op + c * 2) = (uint16_t)E::pack(y, 0.f);
   }
   if (threadIdx.x == 0 && a.lse)
-    a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : top + (__builtin_amdgcn_logf(sum) - E::LIFT) * 0.693147180559945f;
+    a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s) {

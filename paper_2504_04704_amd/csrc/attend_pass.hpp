@@ -45,11 +45,13 @@ struct AElem;
 template <>
 struct AElem<LAGKV_F32> {
   static constexpr int SIZE = 4, SUBS = 1, PAD = 16;
+  static constexpr float UNIT = 1.44269504088896f;  // logits in natural units: the difference is scaled, not each of them
   static constexpr float LIFT = 0.f;
 };
 template <>
 struct AElem<LAGKV_BF16> {
   static constexpr int SIZE = 2, SUBS = 2, PAD = 32;
+  static constexpr float UNIT = 1.f;  // logits in base 2 (the scale holds the factor)
   static constexpr float LIFT = 0.f;
   static __device__ __forceinline__ f32x4 mma(u32v4 a, u32v4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -63,6 +65,7 @@ struct AElem<LAGKV_BF16> {
 template <>
 struct AElem<LAGKV_F16> {
   static constexpr int SIZE = 2, SUBS = 2, PAD = 32;
+  static constexpr float UNIT = 1.f;  // logits in base 2 (the scale holds the factor)
   // exp(x - m) is held times 2^14: binary16 has no numbers between 0 and 2^-24, and a million rows of 2^-25 are no
   // trifle beside one of 1.  (l carries the same factor.)
   static constexpr float LIFT = 14.f;
@@ -75,6 +78,14 @@ struct AElem<LAGKV_F16> {
   static __device__ __forceinline__ f32x2 unpack(uint32_t v) { return __builtin_convertvector(__builtin_bit_cast(f16x2, v), f32x2); }
   static __device__ __forceinline__ float one(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
 };
+
+// lse of a state, natural
+template <int DT>
+__device__ __forceinline__ float lse_of(float m, float l) {
+  using E = AElem<DT>;
+  if constexpr (DT == LAGKV_F32) return m + __builtin_amdgcn_logf(l) * 0.693147180559945f;
+  return (m + __builtin_amdgcn_logf(l) - E::LIFT) * 0.693147180559945f;
+}
 
 // Channel at which the c-th 16-byte slice of a row of D begins: the last one of a row that is no whole number of slices
 // is taken from the row's end, so that nothing behind the row is read.  The channels it shares with the slice before it
@@ -329,14 +340,14 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       const float before = m[rt], now = fmaxf(before, top);
       m[rt] = now;
       const float at = now == -INFINITY ? 0.f : now;
-      const float keep = __builtin_amdgcn_exp2f((before - at) * 1.44269504088896f);
+      const float keep = __builtin_amdgcn_exp2f((before - at) * E::UNIT);
       float sum = 0.f;
 #pragma unroll
       for (int s = 0; s < SUBS; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // (the difference first: its rounding is that of a number near zero)
-          const float e = __builtin_amdgcn_exp2f((p[rt][s][i] - at) * 1.44269504088896f + E::LIFT);
+          const float e = __builtin_amdgcn_exp2f((p[rt][s][i] - at) * E::UNIT + E::LIFT);
           p[rt][s][i] = e;
           sum += e;
         }
@@ -437,7 +448,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
-        const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * 1.44269504088896f);
+        const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
         const bool none = m[rt] == -INFINITY;
 #pragma unroll
         for (int d = 0; d < DT16; ++d) {
@@ -462,7 +473,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) {
       const float mx = sh_ml[x][rl][0];
-      if (mx != -INFINITY) sum += sh_ml[x][rl][1] * __builtin_amdgcn_exp2f((mx - top) * 1.44269504088896f);
+      if (mx != -INFINITY) sum += sh_ml[x][rl][1] * __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
     }
     const f32x4 v = *(const f32x4*)(ol + rl * LDO + quad * 4);
     const int slot = quad * 4, slice = slot / PER, own_at = slice * PER;
@@ -504,7 +515,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       }
     }
     if (quad == 0 && a.lse)
-      a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : top + (__builtin_amdgcn_logf(sum) - E::LIFT) * 0.693147180559945f;
+      a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
   }
 }
 

@@ -1,0 +1,372 @@
+// Attention of many query rows over all rows of a cache (lagkv_attend, 16-bit types; the mathematics is attend_pass.hpp's).
+//
+// Where a stream has tens of query rows (a drafted tree under grouped heads, a chunk of a prompt) the matrix cores are the
+// bound, not memory: 256 rows make 256 flop of a cache byte.  A workgroup of four or eight wavefronts goes over 64 cache
+// rows (32 beyond 128 channels) at a time, which lie in LDS for all of them (the next ones are on their way through registers meanwhile); each wavefront
+// keeps 32 query rows to itself, so that nothing is exchanged between wavefronts.  32x32 products: a lane holds one
+// query row (of S^T, P^T and O^T), so that maxima and sums need one exchange between the lane's halves only.
+//
+// P is put in rounded to the type: two numbers, as in the narrow kernel, would cost half as many products again.  The
+// rounding of a weight is independent of the others' and of the output's own; together they are off by sqrt(2) times what
+// the output's rounding alone is.
+//
+// The reference m of the exponentials is only moved when a row's maximum leaves it by more than SLACK (base 2): exp(x - m) is then
+// up to 2^SLACK, which costs nothing in a floating-point number, and the outputs are rescaled in a few steps, not most.
+#pragma once
+#include "attend_pass.hpp"
+
+namespace lagkv {
+
+typedef uint32_t u32v2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DT>
+struct Wide;
+template <>
+struct Wide<LAGKV_BF16> {
+  static constexpr float LIFT = 0.f, SLACK = 8.f;
+  static constexpr uint32_t EXP = 0x7f80u;
+  static __device__ __forceinline__ f32x16 mma(u32v4 a, u32v4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Wide<LAGKV_F16> {
+  // 2^(LIFT + SLACK) is in binary16's range; weights down to 2^-34 of the largest are not lost
+  static constexpr float LIFT = 10.f, SLACK = 4.f;
+  static constexpr uint32_t EXP = 0x7c00u;
+  static __device__ __forceinline__ f32x16 mma(u32v4 a, u32v4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+
+// 1 in each half of a pair of 16-bit numbers whose exponent is all ones (an infinity or no number)
+template <uint32_t EXP>
+__device__ __forceinline__ uint32_t odd_halves(uint32_t v) {
+  return ((v & EXP) == EXP ? 0x0000ffffu : 0u) | ((v >> 16 & EXP) == EXP ? 0xffff0000u : 0u);
+}
+
+template <int DP>
+struct WideShape {
+  static constexpr int KT = DP > 128 ? 32 : 64, CPR = DP / 8;  // (the registers hold no more of long rows)
+  static constexpr int LDK = DP * 2 + 16, LDV = DP * 2 + 64;  // bytes between rows: sixteen lanes' reads on different banks
+  static constexpr int BUF = KT * (LDK + LDV);
+};
+
+template <int DT, int DP, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_kernel(const AttendArgs a) {
+  using E = AElem<DT>;
+  using W = Wide<DT>;
+  using Sh = WideShape<DP>;
+  constexpr int KT = Sh::KT, CPR = Sh::CPR, LDK = Sh::LDK, LDV = Sh::LDV, THREADS = WAVES * 64, ROWS = WAVES * 32;
+  constexpr int HALVES = KT / 32, KS = DP / 16, DT32 = DP / 32, PASSES = KT * CPR / THREADS;
+  static_assert(KT * CPR % THREADS == 0, "");
+  extern __shared__ __attribute__((aligned(16))) char wide_lds[];  // two buffers of [K rows][V rows]
+  __shared__ int32_t sh_parent[kMaxTree];
+  __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
+  __shared__ int sh_odd[2];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+
+  const WorkItem w = work_item(a);
+  if (!w.any) return;
+  const int64_t b = w.unit / a.H, h = w.unit % a.H;
+  const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
+  int64_t len = a.lengths ? a.lengths[b] : a.T;
+  len = len < 0 ? 0 : len > a.T ? a.T : len;
+  const int cache_steps = (int)((len + KT - 1) / KT);
+  const int token0 = row0 / a.G, last_token = (row1 - 1) / a.G, tokens = last_token - token0 + 1;
+  const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
+  const int steps = cache_steps + (seen_new + KT - 1) / KT;
+  const int share = (steps + a.splits - 1) / a.splits;
+  const int step0 = w.split * share, step1 = min(step0 + share, steps);
+
+  const int words = (seen_new + 31) / 32;
+  if (a.parents && step1 > cache_steps && step0 < step1) {
+    const int32_t* parents = a.parents + b * a.psb;
+    for (int i = tid; i < a.N; i += THREADS) sh_parent[i] = parents[i];
+    for (int i = tid; i < tokens * words; i += THREADS) sh_mask[i] = 0;
+    __syncthreads();
+    if (tid < tokens) {
+      for (int at = token0 + tid; at >= 0;) {  // a parent comes before its child: the walk ends
+        const int up = sh_parent[at];
+        if (up < -1 || up >= at) break;
+        sh_mask[tid * words + (at >> 5)] |= 1u << (at & 31);
+        at = up;
+      }
+    }
+  }
+  if (tid < 2) sh_odd[tid] = 0;
+
+  // q, with the scale's sign: what is left of it is not negative, and the largest logit that of the largest product
+  const int r = row0 + wave * 32 + col;
+  const bool mine = r < row1, idle = row0 + wave * 32 >= row1;  // (a wavefront without rows loads for the others)
+  const int rr = mine ? r : row0, token = rr / a.G, head = (int)h * a.G + rr % a.G;
+  const float c = fmaxf(fabsf(a.scale), 1e-30f);
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  u32v4 q[KS];
+  {
+    const char* p = a.Q + b * a.qsb + head * a.qsh + (int64_t)token * a.qsn;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int slice = 2 * k + half, begin = slice * 8;
+      u32v4 v = {0, 0, 0, 0};
+      if (mine && begin < a.D) {
+        const int at = slice_at(slice, a.D, 8), dup = begin - at;
+        v = *(const u32v4_any*)(p + at * 2) ^ flip;
+        if (dup > 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < dup) v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+        }
+      }
+      q[k] = v;
+    }
+  }
+
+  const char* kb = a.K + b * a.ksb + h * a.ksh;
+  const char* vb = a.V + b * a.ksb + h * a.ksh;
+  const char* knb = a.K_new + b * a.nsb + h * a.nsh;
+  const char* vnb = a.V_new + b * a.nsb + h * a.nsh;
+  // this thread's slice of each row it loads
+  const int lslice = tid % CPR, lrow = tid / CPR;
+  const bool lhave = lslice * 8 < a.D;
+  const int loff = lhave ? slice_at(lslice, a.D, 8) * 2 : 0;
+  u32v4 kr[PASSES], vr[PASSES];
+  auto load = [&](int step) {
+    const bool fresh = step >= cache_steps;
+    const int64_t first = (int64_t)(fresh ? step - cache_steps : step) * KT, limit = fresh ? seen_new : len;
+    const char* kp = (fresh ? knb : kb) + loff;
+    const char* vp = (fresh ? vnb : vb) + loff;
+    const int64_t st = fresh ? a.nst : a.kst;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      int64_t row = first + lrow + i * (THREADS / CPR);
+      row = row < limit ? row : limit - 1;
+      kr[i] = *(const u32v4_any*)(kp + row * st);
+      vr[i] = *(const u32v4_any*)(vp + row * st);
+    }
+  };
+  auto store = [&](int step, int buf) {
+    const bool fresh = step >= cache_steps;
+    const int64_t first = (int64_t)(fresh ? step - cache_steps : step) * KT, limit = fresh ? seen_new : len;
+    char* kl = wide_lds + buf * Sh::BUF;
+    char* vl = kl + KT * LDK;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int row = lrow + i * (THREADS / CPR);
+      u32v4 k = kr[i], v = vr[i];
+      if (!lhave) k = u32v4{0, 0, 0, 0};
+      if (!lhave || first + row >= limit) v = u32v4{0, 0, 0, 0};
+      if (fresh) {
+        // what is no finite number is put in as 0 (0 * inf is not) and added to the rows that see it afterwards
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t o = odd_halves<W::EXP>(v[e]);
+          odd = odd || o;
+          v[e] &= ~o;
+        }
+      }
+      *(u32v4*)(kl + row * LDK + lslice * 16) = k;
+      *(u32v4*)(vl + row * LDV + lslice * 16) = v;
+    }
+    if (fresh && odd) sh_odd[buf] = 1;
+  };
+
+  float m = -INFINITY, l = 0.f;  // m in units of base 2
+  f32x16 o[DT32];
+#pragma unroll
+  for (int d = 0; d < DT32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  int buf = 0;
+  if (step0 < step1) {
+    load(step0);
+    __syncthreads();  // (sh_odd is cleared)
+    store(step0, 0);
+  }
+  __syncthreads();
+  for (int step = step0; step < step1; ++step, buf ^= 1) {
+    if (step + 1 < step1) load(step + 1);
+    if (!idle) {
+    const char* kl = wide_lds + buf * Sh::BUF;
+    const char* vl = kl + KT * LDK;
+    const bool fresh = step >= cache_steps;
+    const int64_t first = (int64_t)(fresh ? step - cache_steps : step) * KT, limit = fresh ? seen_new : len;
+
+    f32x16 s[HALVES];
+#pragma unroll
+    for (int t = 0; t < HALVES; ++t) {
+      f32x16 x;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) x = W::mma(*(const u32v4*)(kl + (t * 32 + col) * LDK + (2 * k + half) * 16), q[k], x);
+      s[t] = x;
+      __builtin_amdgcn_sched_barrier(0);  // (the next half's operands are not fetched ahead: they would not fit)
+    }
+    uint32_t vis[HALVES];  // bit j: row 32 t + j of the step is seen
+    if (fresh || first + KT > limit) {
+#pragma unroll
+      for (int t = 0; t < HALVES; ++t) {
+        const int64_t left = limit - (first + t * 32);
+        uint32_t bits = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
+        if (fresh) {
+          const int j = (int)first + t * 32;
+          if (a.parents) {
+            bits &= (j >> 5) < words ? sh_mask[(token - token0) * words + (j >> 5)] : 0u;
+          } else {
+            const int upto = token - j + 1;
+            bits &= upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
+          }
+        }
+        vis[t] = bits;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!((bits >> (4 * half)) >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < HALVES; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+    top = fmaxf(top, __shfl_xor(top, 32)) * c;
+    if (__any(top > m + W::SLACK)) {
+      const float now = fmaxf(m, top);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DT32; ++d) o[d] *= keep;
+    }
+    const float at = m == -INFINITY ? 0.f : m - W::LIFT;
+    float sum0 = 0.f, sum1 = 0.f;
+    u32v4 p[2 * HALVES];  // steps of 16 rows
+#pragma unroll
+    for (int t = 0; t < HALVES; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, -at));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], c, -at));
+        sum0 += x;
+        sum1 += y;
+        p[t * 2 + i / 8][i % 8 / 2] = E::pack(x, y);
+      }
+    l += sum0 + sum1;
+#pragma unroll
+    for (int k = 0; k < 2 * HALVES; ++k) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < DT32; ++d) {
+        const char* from = vl + (k * 16 + half * 4 + (lane & 15) / 4) * LDV + (d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+        const u32v2 x = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from));
+        const u32v2 y = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8 * LDV)));
+        o[d] = W::mma(u32v4{x.x, x.y, y.x, y.y}, p[k], o[d]);
+      }
+    }
+    if (fresh && sh_odd[buf]) {
+      for (int t = 0; t < KT && first + t < limit; ++t) {
+        if (!((HALVES == 2 && t >= 32 ? vis[HALVES - 1] : vis[0]) >> (t & 31) & 1)) continue;
+        const char* row = vnb + (first + t) * a.nst + half * 8;
+#pragma unroll
+        for (int d = 0; d < DT32; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int slice = d * 4 + e;
+            if (slice * 8 >= a.D) continue;
+            const u32v2 v = *(const u32v2_any*)(row + slice_at(slice, a.D, 8) * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint16_t x = (uint16_t)(v[i / 2] >> (16 * (i % 2)));
+              if ((x & W::EXP) == W::EXP) o[d][4 * e + i] += E::one(x);
+            }
+          }
+      }
+    }
+    }
+    if (step + 1 < step1) store(step + 1, buf ^ 1);
+    __syncthreads();
+  }
+
+  if (!mine) return;
+  l += __shfl_xor(l, 32);
+  const bool whole = a.D % 8 == 0;
+  if (a.splits > 1) {
+    const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
+    float* po = a.part_o + at * a.part_ld;
+#pragma unroll
+    for (int d = 0; d < DT32; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int slot = d * 32 + 8 * e + 4 * half, begin = slot & ~7;
+        if (begin >= a.D) continue;
+        const f32x4 v = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+        if (whole) {
+          *(f32x4*)(po + slot) = v;
+        } else {
+          const int base = slice_at(begin / 8, a.D, 8), dup = begin - base;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if ((slot & 7) + i >= dup) po[base + (slot & 7) + i] = v[i];
+        }
+      }
+    if (half == 0) {
+      a.part_ml[at * 2] = m - W::LIFT + E::LIFT;  // (the same state, with the factor that the join counts on)
+      a.part_ml[at * 2 + 1] = l;
+    }
+    return;
+  }
+  bool blind = m == -INFINITY;
+  if (a.parents) {
+    const int up = a.parents[b * a.psb + token];
+    blind = blind || up < -1 || up >= token;
+  }
+  const float inv = blind ? 0.f : 1.f / l;
+  char* op = a.out + b * a.osb + head * a.osh + (int64_t)token * a.osn;
+  const bool wide_out = whole && !(((uintptr_t)a.out | a.osb | a.osh | a.osn) & 7);
+#pragma unroll
+  for (int d = 0; d < DT32; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int slot = d * 32 + 8 * e + 4 * half, begin = slot & ~7;
+      if (begin >= a.D) continue;
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = blind ? 0.f : o[d][4 * e + i] * inv;
+      const u32v2 y = {E::pack(v[0], v[1]), E::pack(v[2], v[3])};
+      if (wide_out) {
+        *(u32v2*)(op + slot * 2) = y;
+      } else {
+        const int base = slice_at(begin / 8, a.D, 8), dup = begin - base;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((slot & 7) + i >= dup) *(uint16_t*)(op + (base + (slot & 7) + i) * 2) = (uint16_t)(y[i / 2] >> (16 * (i % 2)));
+      }
+    }
+  if (half == 0 && a.lse)
+    a.lse[(b * a.H * a.G + head) * a.N + token] = blind ? -INFINITY : (m + __builtin_amdgcn_logf(l) - W::LIFT) * 0.693147180559945f;
+}
+
+template <int DT, int DP, int WAVES>
+hipError_t launch_wide_as(const AttendArgs& a, hipStream_t s) {
+  const int64_t groups = (a.units * a.splits + 7) / 8 * 8 * a.row_tiles;
+  constexpr size_t lds = 2 * WideShape<DP>::BUF;
+  auto kernel = attend_wide_kernel<DT, DP, WAVES>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((uint32_t)groups), dim3(WAVES * 64), lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_wide_of(const AttendArgs& a, int row_tile, hipStream_t s) {
+  if (a.D <= 64) return row_tile == 128 ? launch_wide_as<DT, 64, 4>(a, s) : launch_wide_as<DT, 64, 8>(a, s);
+  if (a.D <= 128) return row_tile == 128 ? launch_wide_as<DT, 128, 4>(a, s) : launch_wide_as<DT, 128, 8>(a, s);
+  return launch_wide_as<DT, 256, 4>(a, s);
+}
+
+}  // namespace lagkv

@@ -60,6 +60,16 @@ SIZES = [  # B, H, G, N, D, T, new
     (1, 1, 1, 1, 128, 3000, "chain"),     # the cache in pieces
     (1, 1, 4, 16, 128, 2500, "tree"),
     (2, 1, 130, 1, 64, 90, "chain"),      # more query heads than a tile
+    (1, 2, 4, 40, 128, 700, "tree"),      # many query rows: 160, of 256
+    (1, 1, 5, 60, 128, 190, "chain"),     # 300: two tiles
+    (1, 1, 2, 130, 64, 129, "chain"),
+    (1, 1, 3, 12, 41, 100, "tree"),       # rows on odd addresses
+    (1, 2, 7, 21, 100, 230, "chain"),
+    (1, 1, 4, 20, 250, 150, "tree"),
+    (1, 1, 2, 65, 256, 60, "chain"),
+    (1, 1, 8, 16, 128, 3000, "tree"),     # the cache in pieces
+    (1, 1, 1, 256, 64, 10, "tree"),       # the largest tree
+    (1, 2, 8, 6, 96, 0, "tree"),
 ]
 
 
@@ -77,10 +87,11 @@ def test_attend(size, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, FL], ids=["bf16", "f32"])
 @pytest.mark.parametrize("new", ["none", "chain", "tree"])
-def test_ragged_lengths_and_what_lies_behind_them(dtype, new):
+@pytest.mark.parametrize("N", [5, 20])
+def test_ragged_lengths_and_what_lies_behind_them(dtype, new, N):
     """Lengths of nothing, of one row, inside and at the end of a step, and beyond the rows there are; the rows behind
     them, which a cache has not written yet, hold NaN and infinities."""
-    T, N = 200, 5
+    T = 200
     lens = [0, 1, 16, 33, 100, 200, 1000, -7]
     q, K, V, Kn, Vn = problem(dtype, len(lens), 2, 4, N, 64, T, new, seed=3)
     lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
