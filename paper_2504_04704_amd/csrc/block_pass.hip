@@ -97,18 +97,53 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsArgs a, i
   }
 }
 
-__device__ __forceinline__ double add_from(double x, int far) {
-  const long long u = __builtin_bit_cast(long long, x);
-  return x + __builtin_bit_cast(double, ((long long)__shfl_xor((int)(u >> 32), far) << 32) | (uint32_t)__shfl_xor((int)u, far));
+// x of the lane that FAR (1, 2, 4 or 8) lanes or the mirror image away is, within a row of sixteen lanes
+template <int CTRL>
+__device__ __forceinline__ double dpp_mov_d(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)dpp_mov_i<CTRL>((int)(u >> 32)) << 32 | (uint32_t)dpp_mov_i<CTRL>((int)u));
+}
+__device__ __forceinline__ double far_d(double x, int far) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__shfl_xor((int)(u >> 32), far) << 32 | (uint32_t)__shfl_xor((int)u, far));
+}
+// Sum over groups of lpr lanes, in every lane of the group.
+__device__ __forceinline__ double lanes_sum(double x, int lpr) {
+  if (lpr >= 2) x += dpp_mov_d<0xB1>(x);
+  if (lpr >= 4) x += dpp_mov_d<0x4E>(x);
+  if (lpr >= 8) x += dpp_mov_d<0x141>(x);
+  if (lpr >= 16) x += dpp_mov_d<0x140>(x);
+  if (lpr >= 32) x += far_d(x, 16);
+  if (lpr >= 64) x += far_d(x, 32);
+  return x;
 }
 
-// A workgroup takes up to 64 blocks of a stream and all its tokens: P and M of a token in LDS, LPR lanes a block.
-constexpr int kScoreBlocks = 64;
+// P and M (above) of a token: channel d
+template <int DT>
+__device__ __forceinline__ void query_parts(const SelectArgs& a, int64_t b, int64_t h, int n, int d, double* p, double* m) {
+  constexpr int SIZE = AElem<DT>::SIZE;
+  const char* q = a.Q + b * a.qsb + h * a.G * a.qsh + (int64_t)n * a.qsn + (int64_t)d * SIZE;
+  double ps = 0, ms = 0;
+  for (int g = 0; g < a.G; ++g, q += a.qsh) {
+    float x;
+    if constexpr (DT == LAGKV_F32) x = *(const float*)q;
+    else x = AElem<DT>::one(*(const uint16_t*)q);
+    ps += x > 0.f ? (double)x : 0.0;
+    ms += x > 0.f ? 0.0 : (double)x;
+  }
+  *p = ps;
+  *m = ms;
+}
+
+// Scores of one, two or three tokens: a wavefront takes 16 blocks, LPR lanes a block; the bounds are on their way while P
+// and M are made.  Bound by reading the bounds (65536 blocks of 128 16-bit channels: see the figures at the launch).
+constexpr int kScoreBlocks = 64;  // of a workgroup
+constexpr int kFewTokens = 3;
 template <int DT>
 __global__ __launch_bounds__(256) void block_scores_kernel(const SelectArgs a, int lpr) {
   using ET = typename Of<DT>::T;
-  constexpr int VEC = ET::VEC, SIZE = 16 / VEC;
-  __shared__ double sh_p[kMaxHead], sh_m[kMaxHead];
+  constexpr int VEC = ET::VEC, SIZE = 16 / VEC, AHEAD = 4;
+  __shared__ double sh_p[kFewTokens][kMaxHead], sh_m[kFewTokens][kMaxHead];
   const int64_t tiles = (a.nb + kScoreBlocks - 1) / kScoreBlocks;
   const int64_t stream = blockIdx.x / tiles, j0 = blockIdx.x % tiles * kScoreBlocks;
   const int64_t b = stream / a.H, h = stream % a.H;
@@ -116,114 +151,260 @@ __global__ __launch_bounds__(256) void block_scores_kernel(const SelectArgs a, i
   const int slice = lane % lpr, sub = lane / lpr, step = 64 / lpr;
   const bool have = slice * VEC < a.D;
   const int at = have ? slice_at(slice, a.D, VEC) : 0, dup = have ? slice * VEC - at : 0;
-  for (int n = 0; n < a.N; ++n) {
-    __syncthreads();
-    for (int d = threadIdx.x; d < a.D; d += 256) {
-      double p = 0, m = 0;
-      for (int g = 0; g < a.G; ++g) {
-        const char* q = a.Q + b * a.qsb + (h * a.G + g) * a.qsh + (int64_t)n * a.qsn + (int64_t)d * SIZE;
-        float x;
-        if constexpr (DT == LAGKV_F32) x = *(const float*)q;
-        else x = AElem<DT>::one(*(const uint16_t*)q);
-        p += x > 0.f ? (double)x : 0.0;
-        m += x > 0.f ? 0.0 : (double)x;
-      }
-      sh_p[d] = p;
-      sh_m[d] = m;
+  const int64_t jw = j0 + wave * 16;
+  const int passes = (16 + step - 1) / step;  // of `step` blocks
+  bool first = true;
+  for (int p0 = 0; p0 < passes; p0 += AHEAD) {
+    uint4 lo4[AHEAD], hi4[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int64_t j = jw + (p0 + i) * step + sub, jj = j < a.nb ? j : a.nb - 1;
+      const int64_t from = ((stream * a.nb + jj) * a.D + at) * SIZE;
+      lo4[i] = ld16_any(a.lo + from);
+      hi4[i] = ld16_any(a.hi + from);
     }
-    __syncthreads();
-    for (int i = wave * step + sub; i < kScoreBlocks; i += 4 * step) {
-      const int64_t j = j0 + i;
-      double s = 0;
-      if (j < a.nb && have) {
-        const int64_t from = ((stream * a.nb + j) * a.D + at) * SIZE;
-        float lo[VEC], hi[VEC];
-        unpack<ET>(ld16_any(a.lo + from), lo);
-        unpack<ET>(ld16_any(a.hi + from), hi);
+    if (first) {
+      for (int i = threadIdx.x; i < a.N * a.D; i += 256) {
+        const int n = i / a.D, d = i % a.D;
+        query_parts<DT>(a, b, h, n, d, &sh_p[n][d], &sh_m[n][d]);
+      }
+      __syncthreads();
+      first = false;
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int of = (p0 + i) * step + sub;
+      const int64_t j = jw + of;
+      const bool ok = of < 16 && j < a.nb;
+      float lo[VEC], hi[VEC];
+      unpack<ET>(lo4[i], lo);
+      unpack<ET>(hi4[i], hi);
+      for (int n = 0; n < a.N; ++n) {
+        double s0 = 0, s1 = 0;
 #pragma unroll
         for (int c = 0; c < VEC; ++c)
-          if (c >= dup) {
-            s = __builtin_fma(sh_p[at + c], (double)hi[c], s);
-            s = __builtin_fma(sh_m[at + c], (double)lo[c], s);
+          if (have && c >= dup) {
+            s0 = __builtin_fma(sh_p[n][at + c], (double)hi[c], s0);
+            s1 = __builtin_fma(sh_m[n][at + c], (double)lo[c], s1);
           }
+        const double s = lanes_sum(s0 + s1, lpr);
+        if (slice == 0 && ok) a.score[(stream * a.N + n) * a.nb + j] = s;
       }
-      for (int far = 1; far < lpr; far <<= 1) s = add_from(s, far);
-      if (slice == 0 && j < a.nb) a.score[((stream * a.N) + n) * a.nb + j] = s;
     }
   }
 }
 
-// 64-bit key in the order of the scores: blocks that are always taken first, equal scores equal (-0 like 0).
-__device__ __forceinline__ uint64_t score_key(double s, bool always) {
-  if (always) return ~0ull;
+// Scores of more tokens: sixteen blocks times sixteen tokens at a time on the matrix cores (64-bit), whose operand of
+// the blocks is the bounds as they lie in memory (lane l: block l % 16, a slice of its channels), and that of the tokens is
+// P and M, in LDS for the workgroup's 64 blocks.  A product takes what 64-bit vector arithmetic takes, but nothing has to be
+// summed across lanes.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs a) {
+  using ET = typename Of<DT>::T;
+  constexpr int VEC = ET::VEC, SIZE = 16 / VEC, NC = DP / VEC / 4;
+  constexpr int LD = DP + 2;  // doubles between tokens: lanes of one channel slice on different banks
+  extern __shared__ __attribute__((aligned(16))) double sh_pm[];  // [16][LD] of P, then of M
+  const int64_t tiles = (a.nb + kScoreBlocks - 1) / kScoreBlocks;
+  const int64_t stream = blockIdx.x / tiles, j0 = blockIdx.x % tiles * kScoreBlocks;
+  const int64_t b = stream / a.H, h = stream % a.H;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+  const int64_t jw = j0 + wave * 16, j = jw + col, jj = j < a.nb ? j : a.nb - 1;
+  uint4 lo4[NC], hi4[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int slice = c * 4 + grp;
+    const int64_t from = ((stream * a.nb + jj) * a.D + (slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0)) * SIZE;
+    lo4[c] = ld16_any(a.lo + from);
+    hi4[c] = ld16_any(a.hi + from);
+  }
+  for (int n0 = 0; n0 < a.N; n0 += 16) {
+    __syncthreads();
+    // by slots: those that repeat channels of the slice before, and those behind the last, are 0
+    for (int i = threadIdx.x; i < 16 * DP; i += 256) {
+      const int n = n0 + i / DP, slot = i % DP, begin = slot / VEC * VEC;
+      double p = 0, m = 0;
+      if (n < a.N && begin < a.D) {
+        const int at = slice_at(slot / VEC, a.D, VEC);
+        if (slot - begin >= begin - at) query_parts<DT>(a, b, h, n, at + slot - begin, &p, &m);
+      }
+      sh_pm[i / DP * LD + slot] = p;
+      sh_pm[(16 + i / DP) * LD + slot] = m;
+    }
+    __syncthreads();
+    f64x4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float lo[VEC], hi[VEC];
+      unpack<ET>(lo4[c], lo);
+      unpack<ET>(hi4[c], hi);
+      const bool have = (c * 4 + grp) * VEC < a.D;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int slot = (c * 4 + grp) * VEC + i;
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(have ? (double)hi[i] : 0.0, sh_pm[col * LD + slot], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(have ? (double)lo[i] : 0.0, sh_pm[(16 + col) * LD + slot], s, 0, 0, 0);
+      }
+    }
+    // s[i]: block grp + 4 i of the sixteen, token col
+    const int n = n0 + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t to = jw + grp + 4 * i;
+      if (n < a.N && to < a.nb) a.score[(stream * a.N + n) * a.nb + to] = s[i];
+    }
+  }
+}
+
+// 64-bit key in the order of the scores (-0 like 0, what is no number below all); 0 is no key.
+__device__ __forceinline__ uint64_t score_key(double s) {
+  if (s != s) return 1;
   const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// A workgroup takes a token's list: the k-th largest key digit by digit (eight bits a pass, a histogram in LDS), then
-// the blocks above it and the first of those equal to it, in order.
-__global__ __launch_bounds__(256) void block_select_kernel(const SelectArgs a) {
+// A workgroup takes a token's list.  The k-th largest key is found eight bits at a time (a histogram in LDS of the keys that
+// share the digits found), from the highest bit in which two keys differ down to where the keys that share all digits found are as many as are
+// still wanted: two or three passes as a rule.  Then the blocks above it, and the first of those equal to it, are written in
+// order.  E keys a thread in registers; E = 0: read again in every pass.
+constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
+template <int E>
+__global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const SelectArgs a) {
   __shared__ uint32_t sh_hist[256];
-  __shared__ uint64_t sh_prefix;
-  __shared__ int32_t sh_need;
-  __shared__ int32_t sh_count[2][4];
+  __shared__ uint64_t sh_edge, sh_wave[2][kSelectWaves];
+  __shared__ uint32_t sh_need, sh_in;
+  __shared__ uint32_t sh_count[2][2][kSelectWaves];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t unit = blockIdx.x, b = unit / a.N / a.H;
   const int64_t len = rows_held(a.lengths, b, a.T), nb = (len + a.block - 1) / a.block;
   const double* score = a.score + unit * a.nb;
   int32_t* to = a.blocks + unit * a.k;
   if (nb <= a.k) {
-    for (int64_t i = tid; i < a.k; i += 256) to[i] = i < nb ? (int32_t)i : -1;
+    for (int64_t i = tid; i < a.k; i += kSelectThreads) to[i] = i < nb ? (int32_t)i : -1;
     return;
   }
-  auto key = [&](int64_t j) { return score_key(score[j], j < a.first || j >= nb - a.last); };
-  if (tid == 0) {
-    sh_prefix = 0;
-    sh_need = a.k;
+  const int64_t free0 = a.first, free1 = nb - a.last;  // the others are taken anyway
+  uint64_t mine[E ? E : 1];
+  const int64_t slabs = (nb + kSelectThreads - 1) / kSelectThreads;
+  auto read = [&](int64_t e) {
+    const int64_t j = e * kSelectThreads + tid;
+    return j >= free0 && j < free1 ? score_key(score[j]) : 0;
+  };
+  auto each = [&](auto f) {
+    if constexpr (E > 0) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) f(e, mine[e]);
+    } else {
+      for (int64_t e = 0; e < slabs; ++e) f(e, read(e));
+    }
+  };
+  if constexpr (E > 0) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) mine[e] = read(e);
   }
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    sh_hist[tid] = 0;
-    __syncthreads();
-    const uint64_t prefix = sh_prefix;
-    for (int64_t j = tid; j < nb; j += 256) {
-      const uint64_t u = key(j);
-      if (shift == 56 || (u >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&sh_hist[(u >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (tid == 0) {
-      int need = sh_need, digit = 255;
-      while (digit > 0 && (int)sh_hist[digit] < need) need -= (int)sh_hist[digit--];
-      sh_need = need;
-      sh_prefix = prefix | (uint64_t)digit << shift;
-    }
-    __syncthreads();
+  // bits in which keys differ: those that some have and not all
+  uint64_t some = 0, all = ~0ull;
+  each([&](int64_t, uint64_t u) {
+    some |= u;
+    all &= u ? u : ~0ull;
+  });
+#pragma unroll
+  for (int far = 1; far < 64; far <<= 1) {
+    some |= __shfl_xor(some, far);
+    all &= __shfl_xor(all, far);
   }
-  const uint64_t edge = sh_prefix;
-  const int ties = sh_need;  // of the keys equal to the edge, this many are taken
-  int taken = 0, equal = 0;
-  for (int64_t j0 = 0; j0 < nb; j0 += 256) {
-    const int64_t j = j0 + tid;
-    const uint64_t u = j < nb ? key(j) : 0;
-    const uint64_t above = __ballot(j < nb && u > edge), same = __ballot(j < nb && u == edge);
-    if (lane == 0) {
-      sh_count[0][wave] = __popcll(above);
-      sh_count[1][wave] = __popcll(same);
-    }
-    __syncthreads();
-    int before_a = taken, before_s = equal;
-    for (int x = 0; x < 4; ++x) {
-      if (x < wave) {
-        before_a += sh_count[0][x];
-        before_s += sh_count[1][x];
+  if (lane == 0) {
+    sh_wave[0][wave] = some;
+    sh_wave[1][wave] = all;
+  }
+  if (tid < 256) sh_hist[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kSelectWaves; ++x) {
+    some |= sh_wave[0][x];
+    all &= sh_wave[1][x];
+  }
+  const uint64_t differ = some & ~all;
+  uint32_t need = (uint32_t)(a.k - a.first - a.last);
+  uint64_t edge = all & some, above_edge = 0;  // taken: keys above `edge`, and `need` of the equal ones; keys at or above `above_edge`, if set
+  if (need == 0) {
+    edge = ~0ull;
+  } else if (differ != 0) {
+    int low = 63 - __builtin_clzll(differ);  // the highest differing bit, then the lowest one found
+    edge = low == 63 ? 0 : edge >> (low + 1) << (low + 1);
+    int high = low;
+    for (;;) {
+      const int width = high + 1 < 8 ? high + 1 : 8;
+      low = high + 1 - width;
+      each([&](int64_t, uint64_t u) {
+        if (u && (high == 63 || (u >> (high + 1)) == (edge >> (high + 1)))) atomicAdd(&sh_hist[(u >> low) & ((1u << width) - 1)], 1u);
+      });
+      __syncthreads();
+      if (wave == 0) {
+        // digits from the top: lane l has 255 - 4 l down to 252 - 4 l
+        uint32_t c[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          c[i] = sh_hist[255 - 4 * lane - i];
+          sum += c[i];
+        }
+        uint32_t upto = sum;
+#pragma unroll
+        for (int far = 1; far < 64; far <<= 1) {
+          const uint32_t x = __shfl_up(upto, far);
+          if (lane >= far) upto += x;
+        }
+        uint32_t before = upto - sum;
+        if (before < need && upto >= need) {
+          int i = 0;
+          while (i < 3 && before + c[i] < need) before += c[i++];
+          sh_edge = edge | (uint64_t)(255 - 4 * lane - i) << low;
+          sh_need = need - before;
+          sh_in = c[i];
+        }
       }
-      taken += sh_count[0][x];
-      equal += sh_count[1][x];
+      __syncthreads();
+      edge = sh_edge;
+      need = sh_need;
+      const bool done = sh_in == need;
+      if (tid < 256) sh_hist[tid] = 0;
+      if (done) above_edge = edge;
+      if (done || low == 0) break;
+      high = low - 1;
+      __syncthreads();
     }
-    before_a += prefix_popc(above);
-    before_s += prefix_popc(same);
-    if (j < nb && (u > edge || (u == edge && before_s < ties))) to[before_a + (before_s < ties ? before_s : ties)] = (int32_t)j;
-    __syncthreads();
   }
+  // (all keys equal: the first `need` of them)
+  uint32_t taken = 0, equal = 0;
+  int turn = 0;
+  each([&](int64_t e, uint64_t u) {
+    if (e >= slabs) return;  // (uniform)
+    const int64_t j = e * kSelectThreads + tid;
+    const bool forced = j < free0 || (j >= free1 && j < nb);
+    const bool over = forced || (u && (above_edge ? u >= above_edge : u > edge));
+    const bool tie = !forced && u && !above_edge && u == edge;
+    const uint64_t overs = __ballot(over), ties = __ballot(tie);
+    if (lane == 0) {
+      sh_count[turn][0][wave] = __popcll(overs);
+      sh_count[turn][1][wave] = __popcll(ties);
+    }
+    __syncthreads();
+    uint32_t before_o = taken, before_t = equal;
+#pragma unroll
+    for (int x = 0; x < kSelectWaves; ++x) {
+      const uint32_t o = sh_count[turn][0][x], t = sh_count[turn][1][x];
+      if (x < wave) {
+        before_o += o;
+        before_t += t;
+      }
+      taken += o;
+      equal += t;
+    }
+    before_o += prefix_popc(overs);
+    before_t += prefix_popc(ties);
+    if (over || (tie && before_t < need)) to[before_o + (before_t < need ? before_t : need)] = (int32_t)j;
+    turn ^= 1;
+  });
 }
 
 int lanes_a_row(int D, int dtype) {
@@ -245,18 +426,33 @@ hipError_t launch_block_bounds(const BoundsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_block_scores(const SelectArgs& a, hipStream_t s) {
-  const int64_t groups = (int64_t)a.B * a.H * ((a.nb + kScoreBlocks - 1) / kScoreBlocks);
-  const int lpr = lanes_a_row(a.D, a.dtype);
-  const dim3 grid((uint32_t)groups), group(256);
-  if (a.dtype == LAGKV_F32) block_scores_kernel<LAGKV_F32><<<grid, group, 0, s>>>(a, lpr);
-  else if (a.dtype == LAGKV_BF16) block_scores_kernel<LAGKV_BF16><<<grid, group, 0, s>>>(a, lpr);
-  else block_scores_kernel<LAGKV_F16><<<grid, group, 0, s>>>(a, lpr);
+namespace {
+template <int DT>
+hipError_t launch_scores(const SelectArgs& a, hipStream_t s) {
+  const dim3 grid((uint32_t)((int64_t)a.B * a.H * ((a.nb + kScoreBlocks - 1) / kScoreBlocks))), group(256);
+  auto lds = [](int dp) { return (size_t)32 * (dp + 2) * 8; };
+  if (a.N <= kFewTokens) block_scores_kernel<DT><<<grid, group, 0, s>>>(a, lanes_a_row(a.D, DT));
+  else if (a.D <= 64) block_scores_many_kernel<DT, 64><<<grid, group, lds(64), s>>>(a);
+  else if (a.D <= 128) block_scores_many_kernel<DT, 128><<<grid, group, lds(128), s>>>(a);
+  else {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(block_scores_many_kernel<DT, 256>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds(256));
+    if (e != hipSuccess) return e;
+    block_scores_many_kernel<DT, 256><<<grid, group, lds(256), s>>>(a);
+  }
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_block_scores(const SelectArgs& a, hipStream_t s) {
+  return a.dtype == LAGKV_F32 ? launch_scores<LAGKV_F32>(a, s) : a.dtype == LAGKV_BF16 ? launch_scores<LAGKV_BF16>(a, s) : launch_scores<LAGKV_F16>(a, s);
 }
 
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t s) {
-  block_select_kernel<<<dim3((uint32_t)((int64_t)a.B * a.H * a.N)), dim3(256), 0, s>>>(a);
+  const dim3 grid((uint32_t)((int64_t)a.B * a.H * a.N)), group(kSelectThreads);
+  if (a.nb <= 4 * kSelectThreads) block_select_kernel<4><<<grid, group, 0, s>>>(a);
+  else if (a.nb <= 16 * kSelectThreads) block_select_kernel<16><<<grid, group, 0, s>>>(a);
+  else block_select_kernel<0><<<grid, group, 0, s>>>(a);
   return hipGetLastError();
 }
 
