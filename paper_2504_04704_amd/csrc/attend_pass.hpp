@@ -103,86 +103,189 @@ struct WorkItem {
   bool any;
 };
 __device__ __forceinline__ WorkItem work_item(const AttendArgs& a) {
-  const int64_t id = blockIdx.x, slot = id % 8, rest = id / 8;
-  const int64_t us = rest / a.row_tiles * 8 + slot;
+  const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, us = rest / (uint32_t)a.row_tiles * 8 + slot;
   WorkItem w;
-  w.tile = (int)(rest % a.row_tiles);
-  w.any = us < a.units * a.splits;
-  w.unit = us / a.splits;
-  w.split = (int)(us % a.splits);
+  w.tile = (int)(rest % (uint32_t)a.row_tiles);
+  w.any = us < (uint32_t)(a.units * a.splits);
+  w.unit = us / (uint32_t)a.splits;
+  w.split = (int)(us % (uint32_t)a.splits);
   return w;
 }
 
-template <int DT, int DP, int RT, bool PICK>
+// Which new tokens each of a tile's tokens sees, as bits: `words` words a token.  A parent comes before its child: the walk ends.
+__device__ __forceinline__ void ancestors(const int32_t* parents, int N, int token0, int tokens, int words, int32_t* sh_parent,
+                                          uint32_t* sh_mask, int tid, int threads) {
+  for (int i = tid; i < N; i += threads) sh_parent[i] = parents[i];
+  for (int i = tid; i < tokens * words; i += threads) sh_mask[i] = 0;
+  __syncthreads();
+  if (tid < tokens)
+    for (int at = token0 + tid; at >= 0;) {
+      const int up = sh_parent[at];
+      if (up < -1 || up >= at) break;  // not a token
+      sh_mask[tid * words + (at >> 5)] |= 1u << (at & 31);
+      at = up;
+    }
+}
+
+// All ones in each number of a pair (fp32: in the number) that is infinite or none
+template <int DT>
+__device__ __forceinline__ uint32_t odd_bits(uint32_t v) {
+  constexpr uint32_t EXP = DT == LAGKV_F32 ? 0x7f800000u : DT == LAGKV_BF16 ? 0x7f80u : 0x7c00u;
+  if constexpr (DT == LAGKV_F32) return (v & EXP) == EXP ? ~0u : 0u;
+  return ((v & EXP) == EXP ? 0x0000ffffu : 0u) | ((v >> 16 & EXP) == EXP ? 0xffff0000u : 0u);
+}
+// What four channels of a row have of such numbers, added to o
+template <int DT>
+__device__ __forceinline__ void add_odd(const char* at, float* o) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == LAGKV_F32) {
+      const float v = ((const float*)at)[i];
+      if (odd_bits<DT>(__float_as_uint(v))) o[i] += v;
+    } else {
+      const uint16_t v = ((const uint16_t*)at)[i];
+      if (odd_bits<DT>(v)) o[i] += AElem<DT>::one(v);
+    }
+  }
+}
+
+template <int DT, int DP, int RT, int WAVES>
 struct AttendShape {
   using E = AElem<DT>;
-  static constexpr int WAVES = 4;
-  static constexpr int PER = 16 / E::SIZE;         // elements of a slice
-  static constexpr int NC = DP * E::SIZE / 64;     // slices of a row a lane holds
-  static constexpr int KT = 16 * E::SUBS;          // cache rows of a step
+  static constexpr int PER = 16 / E::SIZE;           // elements of a slice
+  static constexpr int CPR = DP / PER;               // slices of a row
+  static constexpr int NC = CPR / 4;                 // of those, a lane holds of K
+  static constexpr int KT = 16 * E::SUBS;            // cache rows of a step
   static constexpr int ROWS = 16 * RT;
   static constexpr int LDV = DP * E::SIZE + E::PAD;  // bytes between rows of V in LDS
-  static constexpr int LDO = DP + 4;                 // floats between rows of the joined output
-  static constexpr int V_BYTES = WAVES * KT * LDV;
-  static constexpr int O_BYTES = ROWS * LDO * 4;
-  static constexpr int MASK_WORDS = ROWS * (kMaxTree / 32);
+  static constexpr int LDO = DP + 4;                 // floats between rows of the outputs in LDS
+  static constexpr int V_BYTES = WAVES * KT * LDV, O_BYTES = WAVES * ROWS * LDO * 4;
   static constexpr int MAIN = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
 };
 
-template <int DT, int DP, int RT, bool PICK>
-__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
+template <int DT, int DP, int RT, int WAVES, bool PICK>
+__global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) {
   using E = AElem<DT>;
-  using Sh = AttendShape<DT, DP, RT, PICK>;
-  constexpr int PER = Sh::PER, NC = Sh::NC, SUBS = E::SUBS, KT = Sh::KT, ROWS = Sh::ROWS, WAVES = Sh::WAVES;
-  constexpr int LDV = Sh::LDV, LDO = Sh::LDO, DT16 = DP / 16;
-  __shared__ __attribute__((aligned(16))) char lds[Sh::MAIN];
+  using Sh = AttendShape<DT, DP, RT, WAVES>;
+  constexpr int PER = Sh::PER, NC = Sh::NC, CPR = Sh::CPR, SUBS = E::SUBS, KT = Sh::KT, ROWS = Sh::ROWS, THREADS = WAVES * 64;
+  constexpr int LDV = Sh::LDV, LDO = Sh::LDO, DT16 = DP / 16, NV = SUBS * NC, VROWS = 64 / CPR;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float sh_ml[WAVES][ROWS][2];
   __shared__ int32_t sh_parent[kMaxTree];
-  __shared__ uint32_t sh_mask[Sh::MASK_WORDS];
+  __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
   const WorkItem w = work_item(a);
   if (!w.any) return;
-  const int n_fixed = PICK ? (int)(w.unit % a.N) : 0;
-  const int64_t stream = PICK ? w.unit / a.N : w.unit;
-  const int64_t b = stream / a.H, h = stream % a.H;
+  const int n_fixed = PICK ? (int)((uint32_t)w.unit % (uint32_t)a.N) : 0;
+  const uint32_t stream = PICK ? (uint32_t)w.unit / (uint32_t)a.N : (uint32_t)w.unit;
+  const int64_t b = stream / (uint32_t)a.H, h = stream % (uint32_t)a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);  // query rows of this tile
-  auto token_of = [&](int r) { return PICK ? n_fixed : r / a.G; };
-  auto group_of = [&](int r) { return PICK ? r : r % a.G; };
+  auto token_of = [&](int r) { return PICK ? n_fixed : (int)((uint32_t)r / (uint32_t)a.G); };
+  auto group_of = [&](int r) { return PICK ? r : (int)((uint32_t)r % (uint32_t)a.G); };
 
   // rows this tile may see, in steps: of the cache, then of the new tokens (up to the tile's last one, where each sees
   // those before it)
-  int64_t len = a.lengths ? a.lengths[b] : a.T;
-  len = len < 0 ? 0 : len > a.T ? a.T : len;
-  const int64_t listed = PICK ? (int64_t)a.n_blocks * a.block : len;
-  const int64_t cache_steps = len > 0 ? (listed + KT - 1) / KT : 0;
-  const int last_token = token_of(row1 - 1);
-  const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
-  const int64_t steps = cache_steps + (seen_new + KT - 1) / KT;
-  const int64_t share = ((steps + a.splits - 1) / a.splits + WAVES - 1) / WAVES * WAVES;
-  const int64_t step0 = w.split * share, step1 = step0 + share < steps ? step0 + share : steps;
-
-  // which new tokens each of the tile's tokens sees, as bits
-  const int words = (seen_new + 31) / 32, token0 = token_of(row0), tokens = last_token - token0 + 1;
-  if (a.parents && step1 > cache_steps) {  // (uniform in the workgroup)
-    const int32_t* parents = a.parents + b * a.psb;
-    for (int i = tid; i < a.N; i += 256) sh_parent[i] = parents[i];
-    for (int i = tid; i < tokens * words; i += 256) sh_mask[i] = 0;
+  int64_t held = a.lengths ? a.lengths[b] : a.T;
+  const int len = (int)(held < 0 ? 0 : held > a.T ? a.T : held);
+  const int listed = PICK ? a.n_blocks << a.block_shift : len;
+  const int cache_steps = len > 0 ? (int)(((int64_t)listed + KT - 1) / KT) : 0;
+  const int last_token = token_of(row1 - 1), token0 = token_of(row0), tokens = last_token - token0 + 1;
+  const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0, words = (seen_new + 31) / 32;
+  const int steps = cache_steps + (seen_new + KT - 1) / KT;
+  const int share = ((steps + a.splits - 1) / a.splits + WAVES - 1) / WAVES * WAVES;
+  const int step0 = w.split * share, step1 = min(step0 + share, steps);
+  if (a.parents && step1 > cache_steps && step0 < step1) {  // (uniform in the workgroup)
+    ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
     __syncthreads();
-    if (tid < tokens) {
-      // a parent comes before its child: the walk ends
-      for (int at = token0 + tid; at >= 0;) {
-        const int up = sh_parent[at];
-        if (up < -1 || up >= at) break;  // not a token
-        sh_mask[tid * words + (at >> 5)] |= 1u << (at & 31);
-        at = up;
+  }
+
+  const char* kb = a.K + b * a.ksb + h * a.ksh;
+  const char* vb = a.V + b * a.ksb + h * a.ksh;
+  const char* knb = a.K_new + b * a.nsb + h * a.nsh;
+  const char* vnb = a.V_new + b * a.nsb + h * a.nsh;
+  const int32_t* list = PICK ? a.blocks + w.unit * a.n_blocks : nullptr;
+  const int n_full = PICK ? (int)(((int64_t)len + a.block - 1) >> a.block_shift) : 0;
+  char* vl = lds + wave * (KT * LDV);
+
+  // A step: the first row of each sixteen, and how many rows there are.  The list's entries are read a step ahead.
+  struct Step {
+    int first[SUBS], limit[SUBS];
+    int fresh;  // (of the new tokens)
+  };
+  auto entries = [&](int step, int (&id)[SUBS]) {
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      if constexpr (PICK) {
+        const int e = (step * KT + s * 16) >> a.block_shift;
+        id[s] = step < cache_steps && e < a.n_blocks ? list[e] : -1;
+      } else {
+        id[s] = 0;
       }
     }
-    __syncthreads();
+  };
+  auto step_of = [&](int step, const int (&id)[SUBS]) {
+    Step x;
+    x.fresh = step >= cache_steps;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      if (x.fresh) {
+        x.first[s] = (step - cache_steps) * KT + s * 16;
+        x.limit[s] = seen_new;
+      } else if (!PICK) {
+        x.first[s] = step * KT + s * 16;
+        x.limit[s] = len;
+      } else {
+        const bool ok = id[s] >= 0 && id[s] < n_full;
+        x.first[s] = ok ? (id[s] << a.block_shift) + ((step * KT + s * 16) & (a.block - 1)) : 0;
+        x.limit[s] = ok ? len : 0;
+      }
+    }
+    return x;
+  };
+  // K: lane (col, grp) has row col of each sixteen, slices grp, 4 + grp, ...: what its operand takes.  V: whole rows.
+  u32v4 kf[SUBS][NC], vf[NV];
+  const int vslice = lane % CPR, vrow = lane / CPR;
+  const bool vhave = vslice * PER < a.D;
+  const int voff = vhave ? slice_at(vslice, a.D, PER) * E::SIZE : 0;
+  auto load_k = [&](const Step& x) {
+    const char* p = x.fresh ? knb : kb;
+    const int64_t st = x.fresh ? a.nst : a.kst;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      const int row = x.first[s] + col;
+      const char* at = p + (int64_t)(row < x.limit[s] ? row : 0) * st;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int slice = c * 4 + grp;
+        kf[s][c] = *(const u32v4_any*)(at + (slice * PER < a.D ? slice_at(slice, a.D, PER) : 0) * E::SIZE);
+      }
+    }
+  };
+  auto load_v = [&](const Step& x) {
+    const char* p = (x.fresh ? vnb : vb) + voff;
+    const int64_t st = x.fresh ? a.nst : a.kst;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int s = i * VROWS / 16, row = x.first[s] + i * VROWS % 16 + vrow;
+      vf[i] = *(const u32v4_any*)(p + (int64_t)(row < x.limit[s] ? row : 0) * st);
+    }
+  };
+
+  int ids[SUBS], next_ids[SUBS];
+  int step = step0 + wave;
+  Step now;
+  if (step < step1) {
+    entries(step, ids);
+    now = step_of(step, ids);
+    load_k(now);
+    load_v(now);
+    entries(step + WAVES, next_ids);
   }
 
   // q: one row a lane
   u32v4 q[RT][NC];
+#pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + rt * 16 + col;
     const bool ok = r < row1;
@@ -191,19 +294,16 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int slice = c * 4 + grp, begin = slice * PER;
-      u32v4 v = {0, 0, 0, 0};
-      if (ok && begin < a.D) {
-        const int at = slice_at(slice, a.D, PER);
-        v = *(const u32v4_any*)(p + at * E::SIZE);
-        const int dup = begin - at;  // leading channels that the slice before has
-        if (dup > 0) {
+      const int at = begin < a.D ? slice_at(slice, a.D, PER) : 0, dup = begin - at;
+      u32v4 v = *(const u32v4_any*)(p + at * E::SIZE);
+      if (!ok || begin >= a.D) v = u32v4{0, 0, 0, 0};
+      if (dup > 0) {  // leading channels that the slice before has
 #pragma unroll
-          for (int i = 0; i < PER; ++i)
-            if (i < dup) {
-              if constexpr (E::SIZE == 4) v[i] = 0;
-              else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
-            }
-        }
+        for (int i = 0; i < PER; ++i)
+          if (i < dup) {
+            if constexpr (E::SIZE == 4) v[i] = 0;
+            else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+          }
       }
       q[rt][c] = v;
     }
@@ -219,74 +319,32 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
     for (int d = 0; d < DT16; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const char* kb = a.K + b * a.ksb + h * a.ksh;
-  const char* vb = a.V + b * a.ksb + h * a.ksh;
-  const char* knb = a.K_new + b * a.nsb + h * a.nsh;
-  const char* vnb = a.V_new + b * a.nsb + h * a.nsh;
-  const int32_t* list = PICK ? a.blocks + w.unit * a.n_blocks : nullptr;
-  const int64_t n_full = PICK ? (len + a.block - 1) >> a.block_shift : 0;
-  char* vl = lds + wave * (KT * LDV);
-
-  for (int64_t step = step0 + wave; step < step1; step += WAVES) {
-    const bool fresh = step >= cache_steps;  // rows of the new tokens
-    // first row of each 16 and how many rows there are
-    int64_t first[SUBS], limit[SUBS];
+  for (; step < step1; step += WAVES) {
+    const bool more = step + WAVES < step1;
+    Step next = now;
+    if (more) next = step_of(step + WAVES, next_ids);
+    // V into LDS, rows that are not there as zeros, and the next step's on its way
+    bool odd = false;
+    wave_order();
 #pragma unroll
-    for (int s = 0; s < SUBS; ++s) {
-      if (fresh) {
-        first[s] = (step - cache_steps) * KT + s * 16;
-        limit[s] = seen_new;
-      } else if (!PICK) {
-        first[s] = step * KT + s * 16;
-        limit[s] = len;
-      } else {
-        const int64_t at = step * KT + s * 16;
-        const int64_t e = at >> a.block_shift;
-        const int id = e < a.n_blocks ? list[e] : -1;
-        const bool ok = id >= 0 && id < n_full;
-        first[s] = ok ? ((int64_t)id << a.block_shift) + (at & (a.block - 1)) : 0;
-        limit[s] = ok ? len : 0;
-      }
-    }
-    bool whole = true;
+    for (int i = 0; i < NV; ++i) {
+      const int s = i * VROWS / 16, row = i * VROWS + vrow;
+      u32v4 v = vf[i];
+      if (!vhave || now.first[s] + row % 16 >= now.limit[s]) v = u32v4{0, 0, 0, 0};
+      if (now.fresh) {
+        // what is no finite number goes in as 0 (0 * inf is not) and is added to the query rows that see it afterwards
 #pragma unroll
-    for (int s = 0; s < SUBS; ++s) whole = whole && first[s] + 16 <= limit[s];
-    const char* kp = fresh ? knb : kb;
-    const char* vp = fresh ? vnb : vb;
-    const int64_t st = fresh ? a.nst : a.kst;
-    u32v4 kf[SUBS][NC], vf[SUBS][NC];
-    bool odd = false;  // a value that is no number, or infinite
-#pragma unroll
-    for (int s = 0; s < SUBS; ++s) {
-      int64_t row = first[s] + col;
-      const bool in = row < limit[s];
-      row = in ? row : 0;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int slice = c * 4 + grp;
-        const bool have = slice * PER < a.D;
-        const int64_t off = row * st + (have ? slice_at(slice, a.D, PER) : 0) * E::SIZE;
-        kf[s][c] = *(const u32v4_any*)(kp + off);
-        u32v4 v = *(const u32v4_any*)(vp + off);
-        if (!in) v = u32v4{0, 0, 0, 0};
-        vf[s][c] = v;
-        if (fresh) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (DT == LAGKV_F32) odd = odd || (v[i] & 0x7f800000u) == 0x7f800000u;
-            if constexpr (DT == LAGKV_BF16) odd = odd || (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-            if constexpr (DT == LAGKV_F16) odd = odd || (v[i] & 0x7c00u) == 0x7c00u || (v[i] & 0x7c000000u) == 0x7c000000u;
-          }
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bits = odd_bits<DT>(v[e]);
+          odd = odd || bits;
+          v[e] &= ~bits;
         }
       }
+      *(u32v4*)(vl + row * LDV + vslice * 16) = v;
     }
     wave_order();
-#pragma unroll
-    for (int s = 0; s < SUBS; ++s)
-#pragma unroll
-      for (int c = 0; c < NC; ++c) *(u32v4*)(vl + (s * 16 + col) * LDV + (c * 4 + grp) * 16) = vf[s][c];
-    wave_order();
-    odd = __any(odd);
+    if (more) load_v(next);
+    __builtin_amdgcn_sched_barrier(0);
 
     f32x4 p[RT][SUBS];
 #pragma unroll
@@ -309,40 +367,49 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
         }
         p[rt][s] = x;
       }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) {
+      load_k(next);
+      entries(step + 2 * WAVES, next_ids);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 
-    uint32_t seen[RT][SUBS];  // bits of the four cache rows a lane holds, for its query row
+    bool whole = !now.fresh;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) whole = whole && now.first[s] + 16 <= now.limit[s];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float top = -INFINITY;
 #pragma unroll
-      for (int s = 0; s < SUBS; ++s) {
-        uint32_t bits = 15u;
-        if (!whole) {
-          const int64_t left = limit[s] - (first[s] + grp * 4);
-          bits = left >= 4 ? 15u : left <= 0 ? 0u : (1u << left) - 1u;
-        }
-        if (fresh) {
-          const int r = min(row0 + rt * 16 + col, row1 - 1), n = token_of(r), j = (int)first[s] + grp * 4;
-          if (a.parents) {
-            bits &= sh_mask[(n - token0) * words + (j >> 5 < words ? j >> 5 : 0)] >> (j & 31);
-          } else {
-            const int upto = n - j + 1;
-            bits &= upto >= 4 ? 15u : upto <= 0 ? 0u : (1u << upto) - 1u;
+      for (int s = 0; s < SUBS; ++s) p[rt][s] *= a.scale;
+      if (!whole) {
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+          const int j = now.first[s] + grp * 4, left = now.limit[s] - j;
+          uint32_t bits = left >= 4 ? 15u : left <= 0 ? 0u : (1u << left) - 1u;
+          if (now.fresh) {
+            const int n = token_of(min(row0 + rt * 16 + col, row1 - 1));
+            if (a.parents) {
+              bits &= sh_mask[(n - token0) * words + min(j >> 5, words - 1)] >> (j & 31);
+            } else {
+              const int upto = n - j + 1;
+              bits &= upto >= 4 ? 15u : upto <= 0 ? 0u : (1u << upto) - 1u;
+            }
           }
-        }
-        seen[rt][s] = bits;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = p[rt][s][i] * a.scale;
-          p[rt][s][i] = (bits >> i) & 1 ? x : -INFINITY;
-          top = fmaxf(top, p[rt][s][i]);
+          for (int i = 0; i < 4; ++i)
+            if (!(bits >> i & 1)) p[rt][s][i] = -INFINITY;
         }
       }
+      float top = p[rt][0][0];
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, p[rt][s][i]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float before = m[rt], now = fmaxf(before, top);
-      m[rt] = now;
-      const float at = now == -INFINITY ? 0.f : now;
+      const float before = m[rt];
+      m[rt] = fmaxf(before, top);
+      const float at = m[rt] == -INFINITY ? 0.f : m[rt];
       const float keep = __builtin_amdgcn_exp2f((before - at) * E::UNIT);
       float sum = 0.f;
 #pragma unroll
@@ -361,33 +428,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       }
     }
 
-    if (odd) {
-      // an infinite or undefined value in a new token's row must not reach those that do not see it, as 0 * inf would
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          float w4[SUBS];
-#pragma unroll
-          for (int s = 0; s < SUBS; ++s) {
-            const int i = t & 3;
-            w4[s] = i == 0 ? p[rt][s][0] : i == 1 ? p[rt][s][1] : i == 2 ? p[rt][s][2] : p[rt][s][3];
-          }
-          const int from = ((t & 15) >> 2) * 16 + col;
-          const float e = __shfl(SUBS == 2 && t >= 16 ? w4[SUBS - 1] : w4[0], from);
-          const uint32_t bits = __shfl(SUBS == 2 && t >= 16 ? seen[rt][SUBS - 1] : seen[rt][0], from);
-          const bool see = (bits >> (t & 3)) & 1;
-#pragma unroll
-          for (int d = 0; d < DT16; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const char* at = vl + t * LDV + (d * 16 + grp * 4 + i) * E::SIZE;
-              float v;
-              if constexpr (DT == LAGKV_F32) v = *(const float*)at;
-              else v = E::one(*(const uint16_t*)at);
-              if (see) o[rt][d][i] += e * v;
-            }
-        }
-    } else if constexpr (DT == LAGKV_F32) {
+    if constexpr (DT == LAGKV_F32) {
 #pragma unroll
       for (int d = 0; d < DT16; ++d)
 #pragma unroll
@@ -428,10 +469,28 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
         }
       }
     }
+    if (now.fresh && __any(odd)) {
+      for (int j = now.first[0]; j < now.first[0] + KT && j < seen_new; ++j) {
+        const char* row = vnb + (int64_t)j * a.nst;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const int n = token_of(min(row0 + rt * 16 + col, row1 - 1));
+          if (!(a.parents ? sh_mask[(n - token0) * words + (j >> 5)] >> (j & 31) & 1 : j <= n)) continue;
+#pragma unroll
+          for (int d = 0; d < DT16; ++d) {
+            const int slot = d * 16 + grp * 4;
+            if (slot / PER * PER >= a.D) continue;
+            float v[4] = {o[rt][d][0], o[rt][d][1], o[rt][d][2], o[rt][d][3]};
+            add_odd<DT>(row + (slice_at(slot / PER, a.D, PER) + slot % PER) * E::SIZE, v);
+            o[rt][d] = f32x4{v[0], v[1], v[2], v[3]};
+          }
+        }
+      }
+    }
+    now = next;
   }
 
-  // the four states join: maxima and sums first, then the outputs one wavefront after another
-  __syncthreads();
+  // the wavefronts' states join: maxima and sums, then each writes its outputs, scaled to the common maximum
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float sum = l[rt];
@@ -442,53 +501,45 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       sh_ml[wave][rt * 16 + col][1] = sum;
     }
   }
-  __syncthreads();
+  __syncthreads();  // (V of all wavefronts is done with as well)
   float* ol = (float*)lds;
-  for (int turn = 0; turn < WAVES; ++turn) {
-    if (wave == turn) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float top = -INFINITY;
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
-        const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
-        const bool none = m[rt] == -INFINITY;
+    for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
+    const bool none = m[rt] == -INFINITY;
+    const float f = none ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
 #pragma unroll
-        for (int d = 0; d < DT16; ++d) {
-          f32x4* at = (f32x4*)(ol + (rt * 16 + col) * LDO + d * 16 + grp * 4);
-          f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][d] * f;
-          if (turn > 0) v += *at;
-          *at = v;
-        }
-      }
-    }
-    __syncthreads();
+    for (int d = 0; d < DT16; ++d)
+      *(f32x4*)(ol + (wave * ROWS + rt * 16 + col) * LDO + d * 16 + grp * 4) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][d] * f;
   }
+  __syncthreads();
 
-  // out: a row's slices, four slots of them a thread
+  // out: four slots of a row a thread
   constexpr int QUADS = DP / 4;
-  for (int i = tid; i < ROWS * QUADS; i += 256) {
+  for (int i = tid; i < ROWS * QUADS; i += THREADS) {
     const int rl = i / QUADS, quad = i % QUADS, r = row0 + rl;
     if (r >= row1) continue;
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rl][0]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) {
       const float mx = sh_ml[x][rl][0];
       if (mx != -INFINITY) sum += sh_ml[x][rl][1] * __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
+      v += *(const f32x4*)(ol + (x * ROWS + rl) * LDO + quad * 4);
     }
-    const f32x4 v = *(const f32x4*)(ol + rl * LDO + quad * 4);
-    const int slot = quad * 4, slice = slot / PER, own_at = slice * PER;
+    // the slots' channels: `dup` leading ones of a slice are the slice before's
+    const int slot = quad * 4, begin = slot / PER * PER;
+    const int base = begin < a.D ? slice_at(slot / PER, a.D, PER) : 0, dup = begin - base, within = slot - begin;
     if (a.splits > 1) {
       const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
-      if (own_at < a.D) {
-        const int shift = own_at - slice_at(slice, a.D, PER);
+      if (begin < a.D) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int ch = slot + e - shift;
-          if (slot + e - own_at >= shift && ch < a.D) a.part_o[at * a.part_ld + ch] = v[e];
-        }
+        for (int e = 0; e < 4; ++e)
+          if (within + e >= dup) a.part_o[at * a.part_ld + base + within + e] = v[e];
       }
       if (quad == 0) {
         a.part_ml[at * 2] = top;
@@ -504,39 +555,45 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       blind = blind || up < -1 || up >= n;
     }
     const float inv = blind ? 0.f : 1.f / sum;
-    if (own_at < a.D) {
-      const int shift = own_at - slice_at(slice, a.D, PER);
+    if (begin < a.D) {
       char* op = a.out + b * a.osb + head * a.osh + (int64_t)n * a.osn;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int ch = slot + e - shift;
-        if (slot + e - own_at >= shift && ch < a.D) {
+      for (int e = 0; e < 4; ++e)
+        if (within + e >= dup) {
           const float y = blind ? 0.f : v[e] * inv;
+          const int ch = base + within + e;
           if constexpr (DT == LAGKV_F32) *(float*)(op + ch * 4) = y;
           else *(uint16_t*)(op + ch * 2) = (uint16_t)E::pack(y, 0.f);
         }
-      }
     }
-    if (quad == 0 && a.lse)
-      a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
+    if (quad == 0 && a.lse) a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
   }
 }
 
-// Row tiles by the registers they take: 16 query rows of 256 channels or 32 of 128 are what a lane holds without spilling.
-template <int DT, int DP, int RT>
-hipError_t launch_attend_as(const AttendArgs& a, hipStream_t s) {
+template <int DT, int DP, int RT, int WAVES, bool PICK>
+hipError_t launch_attend_one(const AttendArgs& a, hipStream_t s) {
   const int64_t groups = (a.units * a.splits + 7) / 8 * 8 * a.row_tiles;
-  if (a.blocks) attend_kernel<DT, DP, RT, true><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(a);
-  else attend_kernel<DT, DP, RT, false><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(a);
+  constexpr size_t lds = AttendShape<DT, DP, RT, WAVES>::MAIN;
+  auto kernel = attend_kernel<DT, DP, RT, WAVES, PICK>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((uint32_t)groups), dim3(WAVES * 64), lds, s>>>(a);
   return hipGetLastError();
 }
+template <int DT, int DP, int RT, int WAVES>
+hipError_t launch_attend_as(const AttendArgs& a, hipStream_t s) {
+  return a.blocks ? launch_attend_one<DT, DP, RT, WAVES, true>(a, s) : launch_attend_one<DT, DP, RT, WAVES, false>(a, s);
+}
 
+// Row tiles by the registers they take: 16 query rows of 256 channels or 32 of 128 are what a lane holds without spilling.
 template <int DT>
 hipError_t launch_attend_of(const AttendArgs& a, int row_tile, hipStream_t s) {
-  const int rt = row_tile / 16;
-  if (a.D <= 64) return rt == 1 ? launch_attend_as<DT, 64, 1>(a, s) : launch_attend_as<DT, 64, 2>(a, s);
-  if (a.D <= 128) return rt == 1 ? launch_attend_as<DT, 128, 1>(a, s) : launch_attend_as<DT, 128, 2>(a, s);
-  return launch_attend_as<DT, 256, 1>(a, s);
+  const bool one = row_tile == 16;
+  if (a.D <= 64) return one ? launch_attend_as<DT, 64, 1, 4>(a, s) : launch_attend_as<DT, 64, 2, 4>(a, s);
+  if (a.D <= 128) return one ? launch_attend_as<DT, 128, 1, 4>(a, s) : launch_attend_as<DT, 128, 2, 4>(a, s);
+  return launch_attend_as<DT, 256, 1, 4>(a, s);
 }
 
 }  // namespace lagkv

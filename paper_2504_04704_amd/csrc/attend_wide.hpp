@@ -17,7 +17,6 @@
 
 namespace lagkv {
 
-typedef uint32_t u32v2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int DT>
@@ -25,7 +24,6 @@ struct Wide;
 template <>
 struct Wide<LAGKV_BF16> {
   static constexpr float LIFT = 0.f, SLACK = 8.f;
-  static constexpr uint32_t EXP = 0x7f80u;
   static __device__ __forceinline__ f32x16 mma(u32v4 a, u32v4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
@@ -34,17 +32,10 @@ template <>
 struct Wide<LAGKV_F16> {
   // 2^(LIFT + SLACK) is in binary16's range; weights down to 2^-34 of the largest are not lost
   static constexpr float LIFT = 10.f, SLACK = 4.f;
-  static constexpr uint32_t EXP = 0x7c00u;
   static __device__ __forceinline__ f32x16 mma(u32v4 a, u32v4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
 };
-
-// 1 in each half of a pair of 16-bit numbers whose exponent is all ones (an infinity or no number)
-template <uint32_t EXP>
-__device__ __forceinline__ uint32_t odd_halves(uint32_t v) {
-  return ((v & EXP) == EXP ? 0x0000ffffu : 0u) | ((v >> 16 & EXP) == EXP ? 0xffff0000u : 0u);
-}
 
 template <int DP>
 struct WideShape {
@@ -69,7 +60,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 
   const WorkItem w = work_item(a);
   if (!w.any) return;
-  const int64_t b = w.unit / a.H, h = w.unit % a.H;
+  const int64_t b = (uint32_t)w.unit / (uint32_t)a.H, h = (uint32_t)w.unit % (uint32_t)a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
   int64_t len = a.lengths ? a.lengths[b] : a.T;
   len = len < 0 ? 0 : len > a.T ? a.T : len;
@@ -82,18 +73,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 
   const int words = (seen_new + 31) / 32;
   if (a.parents && step1 > cache_steps && step0 < step1) {
-    const int32_t* parents = a.parents + b * a.psb;
-    for (int i = tid; i < a.N; i += THREADS) sh_parent[i] = parents[i];
-    for (int i = tid; i < tokens * words; i += THREADS) sh_mask[i] = 0;
-    __syncthreads();
-    if (tid < tokens) {
-      for (int at = token0 + tid; at >= 0;) {  // a parent comes before its child: the walk ends
-        const int up = sh_parent[at];
-        if (up < -1 || up >= at) break;
-        sh_mask[tid * words + (at >> 5)] |= 1u << (at & 31);
-        at = up;
-      }
-    }
+    ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
   }
   if (tid < 2) sh_odd[tid] = 0;
 
@@ -162,7 +142,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
         // what is no finite number is put in as 0 (0 * inf is not) and added to the rows that see it afterwards
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t o = odd_halves<W::EXP>(v[e]);
+          const uint32_t o = odd_bits<DT>(v[e]);
           odd = odd || o;
           v[e] &= ~o;
         }
@@ -276,12 +256,10 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
           for (int e = 0; e < 4; ++e) {
             const int slice = d * 4 + e;
             if (slice * 8 >= a.D) continue;
-            const u32v2 v = *(const u32v2_any*)(row + slice_at(slice, a.D, 8) * 2);
+            float v[4] = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+            add_odd<DT>(row + slice_at(slice, a.D, 8) * 2, v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint16_t x = (uint16_t)(v[i / 2] >> (16 * (i % 2)));
-              if ((x & W::EXP) == W::EXP) o[d][4 * e + i] += E::one(x);
-            }
+            for (int i = 0; i < 4; ++i) o[d][4 * e + i] = v[i];
           }
       }
     }

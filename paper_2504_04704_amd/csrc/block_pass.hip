@@ -118,42 +118,60 @@ __device__ __forceinline__ double lanes_sum(double x, int lpr) {
   return x;
 }
 
-// P and M (above) of a token: channel d
-template <int DT>
-__device__ __forceinline__ void query_parts(const SelectArgs& a, int64_t b, int64_t h, int n, int d, double* p, double* m) {
-  constexpr int SIZE = AElem<DT>::SIZE;
-  const char* q = a.Q + b * a.qsb + h * a.G * a.qsh + (int64_t)n * a.qsn + (int64_t)d * SIZE;
-  double ps = 0, ms = 0;
-  for (int g = 0; g < a.G; ++g, q += a.qsh) {
-    float x;
-    if constexpr (DT == LAGKV_F32) x = *(const float*)q;
-    else x = AElem<DT>::one(*(const uint16_t*)q);
-    ps += x > 0.f ? (double)x : 0.0;
-    ms += x > 0.f ? 0.0 : (double)x;
+// P and M (above) of U slots of tokens: entry i of the workgroup's list of slots, 256 apart.  A slot is a channel of a slice;
+// those that repeat channels of the slice before, those behind the last, and tokens behind the last are 0.
+template <int DT, int U, typename Put>
+__device__ __forceinline__ void query_parts(const SelectArgs& a, int64_t b, int64_t h, int n0, int width, int from, int count, Put put) {
+  constexpr int SIZE = AElem<DT>::SIZE, VEC = 16 / SIZE;
+  const char* base = a.Q + b * a.qsb + h * a.G * a.qsh;
+  for (int i0 = from; i0 < count; i0 += 256 * U) {
+    int64_t at[U];
+    bool real[U];
+    double p[U], m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 256 * u, n = n0 + i / width, slot = i % width, begin = slot / VEC * VEC;
+      const int ch = begin < a.D ? slice_at(slot / VEC, a.D, VEC) + slot - begin : 0;
+      real[u] = i < count && n < a.N && begin < a.D && ch >= begin;
+      at[u] = real[u] ? (int64_t)n * a.qsn + (int64_t)ch * SIZE : 0;
+      p[u] = m[u] = 0;
+    }
+#pragma unroll 4
+    for (int g = 0; g < a.G; ++g) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const char* q = base + g * a.qsh + at[u];
+        float x;
+        if constexpr (DT == LAGKV_F32) x = *(const float*)q;
+        else x = AElem<DT>::one(*(const uint16_t*)q);
+        p[u] += x > 0.f ? (double)x : 0.0;
+        m[u] += x > 0.f ? 0.0 : (double)x;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 256 * u;
+      if (i < count) put(i / width, i % width, real[u] ? p[u] : 0.0, real[u] ? m[u] : 0.0);
+    }
   }
-  *p = ps;
-  *m = ms;
 }
 
 // Scores of one, two or three tokens: a wavefront takes 16 blocks, LPR lanes a block; the bounds are on their way while P
-// and M are made.  Bound by reading the bounds (65536 blocks of 128 16-bit channels: see the figures at the launch).
+// and M are made.  Bound by reading the bounds.
 constexpr int kScoreBlocks = 64;  // of a workgroup
 constexpr int kFewTokens = 3;
 template <int DT>
-__global__ __launch_bounds__(256) void block_scores_kernel(const SelectArgs a, int lpr) {
+__global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a, int lpr) {
   using ET = typename Of<DT>::T;
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC, AHEAD = 4;
-  __shared__ double sh_p[kFewTokens][kMaxHead], sh_m[kFewTokens][kMaxHead];
-  const int64_t tiles = (a.nb + kScoreBlocks - 1) / kScoreBlocks;
-  const int64_t stream = blockIdx.x / tiles, j0 = blockIdx.x % tiles * kScoreBlocks;
-  const int64_t b = stream / a.H, h = stream % a.H;
+  __shared__ double sh_p[kFewTokens][kMaxHead], sh_m[kFewTokens][kMaxHead];  // of a token: [channel of a slice][slice]
+  const uint32_t tiles = (uint32_t)((a.nb + kScoreBlocks - 1) / kScoreBlocks), st = blockIdx.x / tiles;
+  const int64_t stream = st, j0 = (int64_t)(blockIdx.x % tiles) * kScoreBlocks, b = st / (uint32_t)a.H, h = st % (uint32_t)a.H;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int slice = lane % lpr, sub = lane / lpr, step = 64 / lpr;
-  const bool have = slice * VEC < a.D;
-  const int at = have ? slice_at(slice, a.D, VEC) : 0, dup = have ? slice * VEC - at : 0;
+  const int at = slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0;
   const int64_t jw = j0 + wave * 16;
   const int passes = (16 + step - 1) / step;  // of `step` blocks
-  bool first = true;
   for (int p0 = 0; p0 < passes; p0 += AHEAD) {
     uint4 lo4[AHEAD], hi4[AHEAD];
 #pragma unroll
@@ -163,32 +181,35 @@ __global__ __launch_bounds__(256) void block_scores_kernel(const SelectArgs a, i
       lo4[i] = ld16_any(a.lo + from);
       hi4[i] = ld16_any(a.hi + from);
     }
-    if (first) {
-      for (int i = threadIdx.x; i < a.N * a.D; i += 256) {
-        const int n = i / a.D, d = i % a.D;
-        query_parts<DT>(a, b, h, n, d, &sh_p[n][d], &sh_m[n][d]);
-      }
+    if (p0 == 0) {
+      query_parts<DT, 1>(a, b, h, 0, lpr * VEC, threadIdx.x, a.N * lpr * VEC, [&](int n, int slot, double p, double m) {
+        sh_p[n][slot % VEC * lpr + slot / VEC] = p;
+        sh_m[n][slot % VEC * lpr + slot / VEC] = m;
+      });
       __syncthreads();
-      first = false;
     }
+    for (int n = 0; n < a.N; ++n) {
+      double p[VEC], m[VEC];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int of = (p0 + i) * step + sub;
-      const int64_t j = jw + of;
-      const bool ok = of < 16 && j < a.nb;
-      float lo[VEC], hi[VEC];
-      unpack<ET>(lo4[i], lo);
-      unpack<ET>(hi4[i], hi);
-      for (int n = 0; n < a.N; ++n) {
+      for (int c = 0; c < VEC; ++c) {
+        p[c] = sh_p[n][c * lpr + slice];
+        m[c] = sh_m[n][c * lpr + slice];
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int of = (p0 + i) * step + sub;
+        const int64_t j = jw + of;
+        float lo[VEC], hi[VEC];
+        unpack<ET>(lo4[i], lo);
+        unpack<ET>(hi4[i], hi);
         double s0 = 0, s1 = 0;
 #pragma unroll
-        for (int c = 0; c < VEC; ++c)
-          if (have && c >= dup) {
-            s0 = __builtin_fma(sh_p[n][at + c], (double)hi[c], s0);
-            s1 = __builtin_fma(sh_m[n][at + c], (double)lo[c], s1);
-          }
+        for (int c = 0; c < VEC; ++c) {
+          s0 = __builtin_fma(p[c], (double)hi[c], s0);
+          s1 = __builtin_fma(m[c], (double)lo[c], s1);
+        }
         const double s = lanes_sum(s0 + s1, lpr);
-        if (slice == 0 && ok) a.score[(stream * a.N + n) * a.nb + j] = s;
+        if (slice == 0 && of < 16 && j < a.nb) a.score[(stream * a.N + n) * a.nb + j] = s;
       }
     }
   }
@@ -203,11 +224,10 @@ template <int DT, int DP>
 __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs a) {
   using ET = typename Of<DT>::T;
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC, NC = DP / VEC / 4;
-  constexpr int LD = DP + 2;  // doubles between tokens: lanes of one channel slice on different banks
+  constexpr int LD = DP + 1;  // doubles between tokens: sixteen lanes' reads on different banks
   extern __shared__ __attribute__((aligned(16))) double sh_pm[];  // [16][LD] of P, then of M
-  const int64_t tiles = (a.nb + kScoreBlocks - 1) / kScoreBlocks;
-  const int64_t stream = blockIdx.x / tiles, j0 = blockIdx.x % tiles * kScoreBlocks;
-  const int64_t b = stream / a.H, h = stream % a.H;
+  const uint32_t tiles = (uint32_t)((a.nb + kScoreBlocks - 1) / kScoreBlocks), st = blockIdx.x / tiles;
+  const int64_t stream = st, j0 = (int64_t)(blockIdx.x % tiles) * kScoreBlocks, b = st / (uint32_t)a.H, h = st % (uint32_t)a.H;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int64_t jw = j0 + wave * 16, j = jw + col, jj = j < a.nb ? j : a.nb - 1;
   uint4 lo4[NC], hi4[NC];
@@ -220,17 +240,10 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
   }
   for (int n0 = 0; n0 < a.N; n0 += 16) {
     __syncthreads();
-    // by slots: those that repeat channels of the slice before, and those behind the last, are 0
-    for (int i = threadIdx.x; i < 16 * DP; i += 256) {
-      const int n = n0 + i / DP, slot = i % DP, begin = slot / VEC * VEC;
-      double p = 0, m = 0;
-      if (n < a.N && begin < a.D) {
-        const int at = slice_at(slot / VEC, a.D, VEC);
-        if (slot - begin >= begin - at) query_parts<DT>(a, b, h, n, at + slot - begin, &p, &m);
-      }
-      sh_pm[i / DP * LD + slot] = p;
-      sh_pm[(16 + i / DP) * LD + slot] = m;
-    }
+    query_parts<DT, 4>(a, b, h, n0, DP, threadIdx.x, 16 * DP, [&](int n, int slot, double p, double m) {
+      sh_pm[n * LD + slot] = p;
+      sh_pm[(16 + n) * LD + slot] = m;
+    });
     __syncthreads();
     f64x4 s = {0, 0, 0, 0};
 #pragma unroll
@@ -430,7 +443,7 @@ namespace {
 template <int DT>
 hipError_t launch_scores(const SelectArgs& a, hipStream_t s) {
   const dim3 grid((uint32_t)((int64_t)a.B * a.H * ((a.nb + kScoreBlocks - 1) / kScoreBlocks))), group(256);
-  auto lds = [](int dp) { return (size_t)32 * (dp + 2) * 8; };
+  auto lds = [](int dp) { return (size_t)32 * (dp + 1) * 8; };
   if (a.N <= kFewTokens) block_scores_kernel<DT><<<grid, group, 0, s>>>(a, lanes_a_row(a.D, DT));
   else if (a.D <= 64) block_scores_many_kernel<DT, 64><<<grid, group, lds(64), s>>>(a);
   else if (a.D <= 128) block_scores_many_kernel<DT, 128><<<grid, group, lds(128), s>>>(a);
