@@ -1,62 +1,91 @@
 // Joins the pieces that a unit's cache rows were cut into (see attend_pass.hpp for how two states join): a workgroup
-// takes one query row, its four wavefronts every fourth piece, its lanes four channels each.  Bound by the launch
+// or a wavefront takes one query row, a lane four channels of every so many pieces.  Bound by the launch
 // and the latency of two dependent reads: there are at most some hundred pieces of a row.
 #include "attend_pass.hpp"
 
 namespace lagkv {
 
-template <int DT>
+template <int DT, int WAVES>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
   using E = AElem<DT>;
   __shared__ float sh_o[4][kMaxHead];
   __shared__ float sh_l[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t unit = blockIdx.x / a.rows;
-  const int r = (int)(blockIdx.x % a.rows);
+  const uint32_t id = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, rows = (uint32_t)a.rows;
+  const int64_t unit = id / rows;
+  if (unit >= a.units) return;
+  const int r = (int)(id % rows);
   const bool pick = a.blocks != nullptr;
-  const int64_t stream = pick ? unit / a.N : unit;
-  const int n = pick ? (int)(unit % a.N) : r / a.G, g = pick ? r : r % a.G;
-  const int64_t b = stream / a.H, h = stream % a.H, head = h * a.G + g;
+  const uint32_t stream = pick ? (uint32_t)unit / (uint32_t)a.N : (uint32_t)unit;
+  const int n = pick ? (int)((uint32_t)unit % (uint32_t)a.N) : (int)((uint32_t)r / (uint32_t)a.G);
+  const int g = pick ? r : (int)((uint32_t)r % (uint32_t)a.G);
+  const int64_t b = stream / (uint32_t)a.H, h = stream % (uint32_t)a.H, head = h * a.G + g;
   const int64_t first = unit * a.splits * a.rows + r;  // of the pieces' rows, `rows` apart
+  // lanes: four channels each, of one piece or of two or four
+  const int per = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, quad = lane % per, sub = lane / per, pieces = 64 / per;
+  const bool have = quad * 4 < a.D;
   float top = -INFINITY;
   for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(first + (int64_t)s * a.rows) * 2]);
   top = wave_max(top);
   float sum = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s = wave; s < a.splits; s += 4) {
+  const int turn = (WAVES == 1 ? 0 : wave * pieces) + sub;
+#pragma unroll 4
+  for (int s = turn; s < a.splits; s += WAVES * pieces) {
     const int64_t at = first + (int64_t)s * a.rows;
-    const float mx = a.part_ml[at * 2];
-    if (mx == -INFINITY) continue;  // (nothing seen: its outputs were written as zeros)
-    const float f = __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
-    sum += f * a.part_ml[at * 2 + 1];
-    if (lane * 4 < a.D) v += f * *(const f32x4*)(a.part_o + at * a.part_ld + lane * 4);
+    const f32x4 x = *(const f32x4*)(a.part_o + at * a.part_ld + (have ? quad * 4 : 0));
+    const float mx = a.part_ml[at * 2], lx = a.part_ml[at * 2 + 1];
+    // (a piece that saw nothing has zeros)
+    const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
+    sum += f * lx;
+    v += f * x;
   }
-  if (lane * 4 < a.D) *(f32x4*)(&sh_o[wave][lane * 4]) = v;
-  if (lane == 0) sh_l[wave] = sum;
-  __syncthreads();
-  sum = sh_l[0] + sh_l[1] + sh_l[2] + sh_l[3];
+  for (int far = per; far < 64; far <<= 1) {
+    sum += __shfl_xor(sum, far);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], far);
+  }
+  if constexpr (WAVES > 1) {
+    if (sub == 0) {
+      if (have) *(f32x4*)(&sh_o[wave][quad * 4]) = v;
+      if (lane == 0) sh_l[wave] = sum;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    sum = (sh_l[0] + sh_l[1]) + (sh_l[2] + sh_l[3]);
+    if (have) v = (*(const f32x4*)&sh_o[0][quad * 4] + *(const f32x4*)&sh_o[1][quad * 4]) +
+                  (*(const f32x4*)&sh_o[2][quad * 4] + *(const f32x4*)&sh_o[3][quad * 4]);
+  }
   bool blind = sum == 0.f;
   if (a.parents) {
     const int up = a.parents[b * a.psb + n];
     blind = blind || up < -1 || up >= n;
   }
   const float inv = blind ? 0.f : 1.f / sum;
-  char* op = a.out + b * a.osb + head * a.osh + (int64_t)n * a.osn;
-  for (int c = threadIdx.x; c < a.D; c += 256) {
-    const float y = blind ? 0.f : (sh_o[0][c] + sh_o[1][c] + sh_o[2][c] + sh_o[3][c]) * inv;
-    if constexpr (DT == LAGKV_F32) *(float*)(op + c * 4) = y;
-    else *(uint16_t*)(op + c * 2) = (uint16_t)E::pack(y, 0.f);
+  if (sub == 0 && have) {
+    char* op = a.out + b * a.osb + head * a.osh + (int64_t)n * a.osn;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (quad * 4 + e < a.D) {
+        const float y = blind ? 0.f : v[e] * inv;
+        if constexpr (DT == LAGKV_F32) *(float*)(op + (quad * 4 + e) * 4) = y;
+        else *(uint16_t*)(op + (quad * 4 + e) * 2) = (uint16_t)E::pack(y, 0.f);
+      }
   }
-  if (threadIdx.x == 0 && a.lse)
-    a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
+  if (lane == 0 && a.lse) a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
+}
+
+// A wavefront a row where there are rows for all compute units, else a workgroup.
+template <int DT>
+static hipError_t launch_join_of(const AttendArgs& a, hipStream_t s) {
+  const int64_t rows = a.units * a.rows;
+  if (rows >= 2048) attend_join_kernel<DT, 1><<<dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
+  else attend_join_kernel<DT, 4><<<dim3((uint32_t)rows), dim3(256), 0, s>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s) {
-  const dim3 grid((uint32_t)(a.units * a.rows)), group(256);
-  if (dtype == LAGKV_F32) attend_join_kernel<LAGKV_F32><<<grid, group, 0, s>>>(a);
-  else if (dtype == LAGKV_BF16) attend_join_kernel<LAGKV_BF16><<<grid, group, 0, s>>>(a);
-  else attend_join_kernel<LAGKV_F16><<<grid, group, 0, s>>>(a);
-  return hipGetLastError();
+  return dtype == LAGKV_F32 ? launch_join_of<LAGKV_F32>(a, s) : dtype == LAGKV_BF16 ? launch_join_of<LAGKV_BF16>(a, s) : launch_join_of<LAGKV_F16>(a, s);
 }
 
 }  // namespace lagkv

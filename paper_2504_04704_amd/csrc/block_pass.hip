@@ -199,6 +199,9 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
       for (int i = 0; i < AHEAD; ++i) {
         const int of = (p0 + i) * step + sub;
         const int64_t j = jw + of;
+        // (unpacked in every turn: all of them at once, as 64-bit numbers ahead of the turns, would not fit the registers)
+        asm volatile("" : "+v"(lo4[i].x), "+v"(lo4[i].y), "+v"(lo4[i].z), "+v"(lo4[i].w));
+        asm volatile("" : "+v"(hi4[i].x), "+v"(hi4[i].y), "+v"(hi4[i].z), "+v"(hi4[i].w));
         float lo[VEC], hi[VEC];
         unpack<ET>(lo4[i], lo);
         unpack<ET>(hi4[i], hi);

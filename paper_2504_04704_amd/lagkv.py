@@ -153,8 +153,10 @@ def _load_native(lib):
     except ImportError as e:  # built for another torch or Python
         warnings.warn(f"_lagkv_native.so does not load and calls go through ctypes, some microseconds more each: {e}", RuntimeWarning)
         return None
-    native.init(*(C.cast(f, C.c_void_p).value for f in (lib.lagkv_plan, lib.lagkv_workspace_bytes, lib.lagkv_compress,
-                                                        lib.lagkv_append_and_compress)), raw_stream)
+    native.init(*(C.cast(f, C.c_void_p).value for f in (
+        lib.lagkv_plan, lib.lagkv_workspace_bytes, lib.lagkv_compress, lib.lagkv_append_and_compress,
+        lib.lagkv_attend_workspace_bytes, lib.lagkv_attend, lib.lagkv_attend_blocks, lib.lagkv_block_bounds,
+        lib.lagkv_select_blocks)), raw_stream)
     return native
 
 
@@ -443,6 +445,12 @@ def _bytes(ws: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tens
 
 
 def _attend(where, q, K, V, blocks, block, K_new, V_new, parents, lengths, scale, out, want_lse, ws) -> Attended:
+    if _native is not None:
+        got = _native.attend(q, K, V, K_new, V_new, parents, lengths, scale, out, want_lse, ws, blocks, block)
+        if isinstance(got, int):
+            raise LagKVError(got, where)
+        if got is not None:
+            return Attended(*got)
     _rows("q", q)
     _rows("K", K, q)
     _same_layout(K, V)
@@ -527,6 +535,12 @@ def block_bounds(K: torch.Tensor, block: int, lengths: Optional[torch.Tensor] = 
                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """lagkv_block_bounds: smallest and largest key (lo, hi) [B,H,ceil(T/block),D] of every block of rows, channel by
     channel; with `start` and `out` only the blocks from that of row `start` on are written."""
+    if _native is not None:
+        got = _native.block_bounds(K, block, lengths, start, *(out if out is not None else (None, None)))
+        if isinstance(got, int):
+            raise LagKVError(got, "lagkv_block_bounds")
+        if got is not None:
+            return got
     _rows("K", K)
     _no_grad(K)
     B, H, T, D = K.shape
@@ -557,6 +571,12 @@ def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, b
                   ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """lagkv_select_blocks: for every new token and KV head the k blocks of a cache of T rows whose bounds allow the
     largest logits, the first `first` and last `last` always among them; int32 [B,H,N,k], ascending, -1 behind."""
+    if _native is not None and out is None and ws is None:
+        got = _native.select_blocks(q, lo, hi, T, block, k, first, last, lengths)
+        if isinstance(got, int):
+            raise LagKVError(got, "lagkv_select_blocks")
+        if got is not None:
+            return got
     _rows("q", q)
     _rows("lo", lo, q)
     _no_grad(q, lo, hi)
