@@ -40,6 +40,20 @@ typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
 __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+// x of this lane and of the lane 32 (16) away, joined
+__device__ __forceinline__ float max_across_32(float x) {
+  const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float max_across_16(float x) {
+  const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float sum_across_32(float x) {
+  const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+
 template <int DT>
 struct AElem;
 template <>
@@ -246,8 +260,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
   // K: lane (col, grp) has row col of each sixteen, slices grp, 4 + grp, ...: what its operand takes.  V: whole rows.
   u32v4 kf[SUBS][NC], vf[NV];
   const int vslice = lane % CPR, vrow = lane / CPR;
-  const bool vhave = vslice * PER < a.D;
-  const int voff = vhave ? slice_at(vslice, a.D, PER) * E::SIZE : 0;
+  const int voff = (vslice * PER < a.D ? slice_at(vslice, a.D, PER) : 0) * E::SIZE;  // (slices behind the last are not stored)
   auto load_k = [&](const Step& x) {
     const char* p = x.fresh ? knb : kb;
     const int64_t st = x.fresh ? a.nst : a.kst;
@@ -330,7 +343,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     for (int i = 0; i < NV; ++i) {
       const int s = i * VROWS / 16, row = i * VROWS + vrow;
       u32v4 v = vf[i];
-      if (!vhave || now.first[s] + row % 16 >= now.limit[s]) v = u32v4{0, 0, 0, 0};
+      if (now.first[s] + row % 16 >= now.limit[s]) v = u32v4{0, 0, 0, 0};
       if (now.fresh) {
         // what is no finite number goes in as 0 (0 * inf is not) and is added to the query rows that see it afterwards
 #pragma unroll
@@ -405,8 +418,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
       for (int s = 0; s < SUBS; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, p[rt][s][i]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = max_across_32(max_across_16(top));
       const float before = m[rt];
       m[rt] = fmaxf(before, top);
       const float at = m[rt] == -INFINITY ? 0.f : m[rt];

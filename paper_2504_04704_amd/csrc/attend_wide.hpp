@@ -10,6 +10,13 @@
 // rounding of a weight is independent of the others' and of the output's own; together they are off by sqrt(2) times what
 // the output's rounding alone is.
 //
+// Products and exponentials take about the same time (32 products of 32 cycles, 32 elements a lane of some 35), on
+// different units.  So the eight wavefronts go in two halves, one of each on every SIMD, between barriers: while one half
+// multiplies (the scores of its step, the outputs of the step before), the other makes weights and moves rows.  With
+// h counting the phases, the first half multiplies for step i in h = 2i and makes weights in 2i + 1, the other one phase later.
+// K of step i and V of step i - 1 are read in 2i and 2i + 1; K(i+1) and V(i) are written into the other buffers in
+// 2i + 1 by the first half and in 2i by the second, when nobody reads these any more.
+//
 // The reference m of the exponentials is only moved when a row's maximum leaves it by more than SLACK (base 2): exp(x - m) is then
 // up to 2^SLACK, which costs nothing in a floating-point number, and the outputs are rescaled in a few steps, not most.
 #pragma once
@@ -37,6 +44,22 @@ struct Wide<LAGKV_F16> {
   }
 };
 
+// N products, of what the reads of LDS give that are made AHEAD products before.  (Left to itself the compiler reads, waits
+// and multiplies in turn, in one set of registers.)
+template <int N, int AHEAD, typename Read, typename Mul>
+__device__ __forceinline__ void products(Read read, Mul mul) {
+  u32v4 f[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) f[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    mul(i, f[i % AHEAD]);
+    if (i + AHEAD < N) f[i % AHEAD] = read(i + AHEAD);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int DP>
 struct WideShape {
   static constexpr int KT = DP > 128 ? 32 : 64, CPR = DP / 8;  // (the registers hold no more of long rows)
@@ -56,7 +79,8 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   __shared__ int32_t sh_parent[kMaxTree];
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   __shared__ int sh_odd[2];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int late = wave >> 2;  // (of the half of eight wavefronts that is a phase behind)
 
   const WorkItem w = work_item(a);
   if (!w.any) return;
@@ -69,10 +93,10 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
   const int share = (steps + a.splits - 1) / a.splits;
-  const int step0 = w.split * share, step1 = min(step0 + share, steps);
+  const int step0 = w.split * share, step1 = min(step0 + share, steps), n = max(step1 - step0, 0);
 
   const int words = (seen_new + 31) / 32;
-  if (a.parents && step1 > cache_steps && step0 < step1) {
+  if (a.parents && step1 > cache_steps && n > 0) {
     ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
   }
   if (tid < 2) sh_odd[tid] = 0;
@@ -107,112 +131,164 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   const char* vb = a.V + b * a.ksb + h * a.ksh;
   const char* knb = a.K_new + b * a.nsb + h * a.nsh;
   const char* vnb = a.V_new + b * a.nsb + h * a.nsh;
-  // this thread's slice of each row it loads
+  // This thread's slice of each row it loads, and where it is in the next step's first row.  (Slices behind a row's last
+  // repeat its last: q is 0 there, and what V gives for them is not stored.)
   const int lslice = tid % CPR, lrow = tid / CPR;
-  const bool lhave = lslice * 8 < a.D;
-  const int loff = lhave ? slice_at(lslice, a.D, 8) * 2 : 0;
-  u32v4 kr[PASSES], vr[PASSES];
-  auto load = [&](int step) {
+  const int loff = (lslice * 8 < a.D ? slice_at(lslice, a.D, 8) : 0) * 2;
+  constexpr int LROWS = THREADS / CPR;
+  struct Tile {
+    int64_t first;
+    int limit;
+    bool fresh;  // of the new tokens
+  };
+  auto tile_of = [&](int i) {  // i-th step of this piece
+    const int step = step0 + i;
     const bool fresh = step >= cache_steps;
-    const int64_t first = (int64_t)(fresh ? step - cache_steps : step) * KT, limit = fresh ? seen_new : len;
-    const char* kp = (fresh ? knb : kb) + loff;
-    const char* vp = (fresh ? vnb : vb) + loff;
-    const int64_t st = fresh ? a.nst : a.kst;
+    return Tile{(int64_t)(fresh ? step - cache_steps : step) * KT, fresh ? seen_new : (int)len, fresh};
+  };
+  const int n_whole = min(n, (int)(len / KT) - step0);  // steps of rows of the cache that are all there
+  const char* kp = kb + loff + ((int64_t)step0 * KT + lrow) * a.kst;
+  const char* vp = vb + loff + ((int64_t)step0 * KT + lrow) * a.kst;
+  const int64_t pass = a.kst * LROWS, stride = a.kst * KT;
+  u32v4 kr[PASSES], vr[PASSES];
+  auto load_edge = [&](int i, const char* cache, const char* tokens_at, u32v4 (&to)[PASSES]) {
+    const Tile x = tile_of(i);
+    const char* p = (x.fresh ? tokens_at : cache) + loff;
+    const int64_t st = x.fresh ? a.nst : a.kst;
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      int64_t row = first + lrow + i * (THREADS / CPR);
-      row = row < limit ? row : limit - 1;
-      kr[i] = *(const u32v4_any*)(kp + row * st);
-      vr[i] = *(const u32v4_any*)(vp + row * st);
+    for (int k = 0; k < PASSES; ++k) {
+      const int64_t row = x.first + lrow + k * LROWS;
+      to[k] = *(const u32v4_any*)(p + (row < x.limit ? row : x.limit - 1) * st);
     }
   };
-  auto store = [&](int step, int buf) {
-    const bool fresh = step >= cache_steps;
-    const int64_t first = (int64_t)(fresh ? step - cache_steps : step) * KT, limit = fresh ? seen_new : len;
-    char* kl = wide_lds + buf * Sh::BUF;
-    char* vl = kl + KT * LDK;
-    bool odd = false;
+  // (called for one step after another)
+  auto load_k = [&](int i) {
+    if (i < n_whole) {
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int row = lrow + i * (THREADS / CPR);
-      u32v4 k = kr[i], v = vr[i];
-      if (!lhave) k = u32v4{0, 0, 0, 0};
-      if (!lhave || first + row >= limit) v = u32v4{0, 0, 0, 0};
-      if (fresh) {
-        // what is no finite number is put in as 0 (0 * inf is not) and added to the rows that see it afterwards
+      for (int k = 0; k < PASSES; ++k) kr[k] = *(const u32v4_any*)(kp + k * pass);
+      kp += stride;
+    } else if (i < n) {
+      load_edge(i, kb, knb, kr);
+    }
+  };
+  auto load_v = [&](int i) {
+    if (i < n_whole) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t o = odd_bits<DT>(v[e]);
-          odd = odd || o;
-          v[e] &= ~o;
+      for (int k = 0; k < PASSES; ++k) vr[k] = *(const u32v4_any*)(vp + k * pass);
+      vp += stride;
+    } else if (i < n) {
+      load_edge(i, vb, vnb, vr);
+    }
+  };
+  auto k_at = [&](int i) { return wide_lds + (i & 1) * (KT * LDK); };
+  auto v_at = [&](int i) { return wide_lds + 2 * KT * LDK + (i & 1) * (KT * LDV); };
+  auto store_k = [&](int i) {
+    char* at = k_at(i) + lrow * LDK + lslice * 16;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) *(u32v4*)(at + k * LROWS * LDK) = kr[k];  // (behind the last step: what was there)
+  };
+  auto store_v = [&](int i) {
+    char* at = v_at(i) + lrow * LDV + lslice * 16;
+    if (i >= n_whole && i < n) {
+      const Tile x = tile_of(i);
+      bool odd = false;
+#pragma unroll
+      for (int k = 0; k < PASSES; ++k) {
+        if (x.first + lrow + k * LROWS >= x.limit) vr[k] = u32v4{0, 0, 0, 0};
+        if (x.fresh) {
+          // what is no finite number is put in as 0 (0 * inf is not) and added to the rows that see it afterwards
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = odd_bits<DT>(vr[k][e]);
+            odd = odd || bits;
+            vr[k][e] &= ~bits;
+          }
         }
       }
-      *(u32v4*)(kl + row * LDK + lslice * 16) = k;
-      *(u32v4*)(vl + row * LDV + lslice * 16) = v;
+      if (x.fresh && odd) sh_odd[i & 1] = 1;
     }
-    if (fresh && odd) sh_odd[buf] = 1;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) *(u32v4*)(at + k * LROWS * LDV) = vr[k];
+  };
+  // which of 32 rows from first + 32 t on this lane's query row sees
+  auto sees = [&](const Tile& x, int t) {
+    const int64_t left = x.limit - (x.first + t * 32);
+    uint32_t bits = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
+    if (x.fresh) {
+      const int j = (int)x.first + t * 32;
+      if (a.parents) {
+        bits &= (j >> 5) < words ? sh_mask[(token - token0) * words + (j >> 5)] : 0u;
+      } else {
+        const int upto = token - j + 1;
+        bits &= upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
+      }
+    }
+    return bits;
   };
 
   float m = -INFINITY, l = 0.f;  // m in units of base 2
-  f32x16 o[DT32];
+  f32x16 o[DT32], s[HALVES];
+  u32v4 p[2 * HALVES];  // P, in steps of 16 rows
 #pragma unroll
   for (int d = 0; d < DT32; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  int buf = 0;
-  if (step0 < step1) {
-    load(step0);
-    __syncthreads();  // (sh_odd is cleared)
-    store(step0, 0);
-  }
-  __syncthreads();
-  for (int step = step0; step < step1; ++step, buf ^= 1) {
-    if (step + 1 < step1) load(step + 1);
-    if (!idle) {
-    const char* kl = wide_lds + buf * Sh::BUF;
-    const char* vl = kl + KT * LDK;
-    const bool fresh = step >= cache_steps;
-    const int64_t first = (int64_t)(fresh ? step - cache_steps : step) * KT, limit = fresh ? seen_new : len;
-
-    f32x16 s[HALVES];
+  auto scores = [&](int i) {
+    const char* kl = k_at(i) + col * LDK + half * 16;
 #pragma unroll
-    for (int t = 0; t < HALVES; ++t) {
-      f32x16 x;
+    for (int t = 0; t < HALVES; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+    products<KS * HALVES, 6>([&](int j) { return *(const u32v4*)(kl + j % HALVES * 32 * LDK + j / HALVES * 32); },
+                             [&](int j, u32v4 f) { s[j % HALVES] = W::mma(f, q[j / HALVES], s[j % HALVES]); });
+  };
+  auto outputs = [&](int i) {
+    const char* vl = v_at(i) + (half * 4 + (lane & 15) / 4) * LDV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+    products<2 * HALVES * DT32, 4>(
+        [&](int j) {
+          const char* from = vl + j / DT32 * 16 * LDV + j % DT32 * 64;
+          const u32v2 x = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from));
+          const u32v2 y = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8 * LDV)));
+          return u32v4{x.x, x.y, y.x, y.y};
+        },
+        [&](int j, u32v4 f) { o[j % DT32] = W::mma(f, p[j / DT32], o[j % DT32]); });
+    if (i >= n_whole && tile_of(i).fresh && sh_odd[i & 1]) {
+      const Tile x = tile_of(i);
+      for (int t = 0; t < KT && x.first + t < x.limit; ++t) {
+        if (!(sees(x, t >> 5) >> (t & 31) & 1)) continue;
+        const char* row = vnb + (x.first + t) * a.nst + half * 8;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) x = W::mma(*(const u32v4*)(kl + (t * 32 + col) * LDK + (2 * k + half) * 16), q[k], x);
-      s[t] = x;
-      __builtin_amdgcn_sched_barrier(0);  // (the next half's operands are not fetched ahead: they would not fit)
+        for (int d = 0; d < DT32; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int slice = d * 4 + e;
+            if (slice * 8 >= a.D) continue;
+            float v[4] = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+            add_odd<DT>(row + slice_at(slice, a.D, 8) * 2, v);
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) o[d][4 * e + i4] = v[i4];
+          }
+      }
     }
-    uint32_t vis[HALVES];  // bit j: row 32 t + j of the step is seen
-    if (fresh || first + KT > limit) {
+  };
+  auto weights = [&](int i) {
+    if (i >= n_whole) {
+      const Tile x = tile_of(i);
 #pragma unroll
       for (int t = 0; t < HALVES; ++t) {
-        const int64_t left = limit - (first + t * 32);
-        uint32_t bits = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
-        if (fresh) {
-          const int j = (int)first + t * 32;
-          if (a.parents) {
-            bits &= (j >> 5) < words ? sh_mask[(token - token0) * words + (j >> 5)] : 0u;
-          } else {
-            const int upto = token - j + 1;
-            bits &= upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
-          }
-        }
-        vis[t] = bits;
+        const uint32_t bits = sees(x, t) >> (4 * half);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!((bits >> (4 * half)) >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
+        for (int e = 0; e < 16; ++e)
+          if (!(bits >> (8 * (e / 4) + e % 4) & 1)) s[t][e] = -INFINITY;
       }
     }
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < HALVES; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-    top = fmaxf(top, __shfl_xor(top, 32)) * c;
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+    top = max_across_32(top) * c;
     if (__any(top > m + W::SLACK)) {
       const float now = fmaxf(m, top);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
@@ -223,53 +299,51 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     }
     const float at = m == -INFINITY ? 0.f : m - W::LIFT;
     float sum0 = 0.f, sum1 = 0.f;
-    u32v4 p[2 * HALVES];  // steps of 16 rows
 #pragma unroll
     for (int t = 0; t < HALVES; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, -at));
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], c, -at));
-        sum0 += x;
-        sum1 += y;
-        p[t * 2 + i / 8][i % 8 / 2] = E::pack(x, y);
+      for (int e = 0; e < 16; e += 2) {
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], c, -at));
+        const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e + 1], c, -at));
+        sum0 += y;
+        sum1 += z;
+        p[t * 2 + e / 8][e % 8 / 2] = E::pack(y, z);
       }
     l += sum0 + sum1;
-#pragma unroll
-    for (int k = 0; k < 2 * HALVES; ++k) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int d = 0; d < DT32; ++d) {
-        const char* from = vl + (k * 16 + half * 4 + (lane & 15) / 4) * LDV + (d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
-        const u32v2 x = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from));
-        const u32v2 y = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8 * LDV)));
-        o[d] = W::mma(u32v4{x.x, x.y, y.x, y.y}, p[k], o[d]);
-      }
-    }
-    if (fresh && sh_odd[buf]) {
-      for (int t = 0; t < KT && first + t < limit; ++t) {
-        if (!((HALVES == 2 && t >= 32 ? vis[HALVES - 1] : vis[0]) >> (t & 31) & 1)) continue;
-        const char* row = vnb + (first + t) * a.nst + half * 8;
-#pragma unroll
-        for (int d = 0; d < DT32; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int slice = d * 4 + e;
-            if (slice * 8 >= a.D) continue;
-            float v[4] = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
-            add_odd<DT>(row + slice_at(slice, a.D, 8) * 2, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[d][4 * e + i] = v[i];
-          }
-      }
-    }
-    }
-    if (step + 1 < step1) store(step + 1, buf ^ 1);
+  };
+
+  if (n > 0) {
+    load_k(0);
+    store_k(0);
+    load_k(1);
+    load_v(0);
     __syncthreads();
+    if (late) {
+      store_k(1);
+      store_v(0);
+      load_k(2);
+      load_v(1);
+      __syncthreads();
+    }
+    for (int i = 0; i < n; ++i) {
+      if (!idle) {
+        scores(i);
+        if (i > 0) outputs(i - 1);
+      }
+      __syncthreads();
+      if (!idle) weights(i);
+      store_k(i + late + 1);
+      store_v(i + late);
+      load_k(i + late + 2);
+      load_v(i + late + 1);
+      __syncthreads();
+    }
+    if (!idle) outputs(n - 1);
+    if (!late) __syncthreads();
   }
 
   if (!mine) return;
-  l += __shfl_xor(l, 32);
+  l = sum_across_32(l);
   const bool whole = a.D % 8 == 0;
   if (a.splits > 1) {
     const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
