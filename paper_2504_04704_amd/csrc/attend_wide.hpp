@@ -161,34 +161,28 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
       to[k] = *(const u32v4_any*)(p + (row < x.limit ? row : x.limit - 1) * st);
     }
   };
+  auto load_next = [&](const char*& p, u32v4 (&to)[PASSES]) {
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) to[k] = *(const u32v4_any*)(p + k * pass);
+    p += stride;
+  };
   // (called for one step after another)
   auto load_k = [&](int i) {
-    if (i < n_whole) {
-#pragma unroll
-      for (int k = 0; k < PASSES; ++k) kr[k] = *(const u32v4_any*)(kp + k * pass);
-      kp += stride;
-    } else if (i < n) {
-      load_edge(i, kb, knb, kr);
-    }
+    if (i < n_whole) load_next(kp, kr);
+    else if (i < n) load_edge(i, kb, knb, kr);
   };
   auto load_v = [&](int i) {
-    if (i < n_whole) {
-#pragma unroll
-      for (int k = 0; k < PASSES; ++k) vr[k] = *(const u32v4_any*)(vp + k * pass);
-      vp += stride;
-    } else if (i < n) {
-      load_edge(i, vb, vnb, vr);
-    }
+    if (i < n_whole) load_next(vp, vr);
+    else if (i < n) load_edge(i, vb, vnb, vr);
   };
   auto k_at = [&](int i) { return wide_lds + (i & 1) * (KT * LDK); };
   auto v_at = [&](int i) { return wide_lds + 2 * KT * LDK + (i & 1) * (KT * LDV); };
-  auto store_k = [&](int i) {
-    char* at = k_at(i) + lrow * LDK + lslice * 16;
+  auto store = [&](const u32v4 (&from)[PASSES], char* to, int ld) {
+    to += lrow * ld + lslice * 16;
 #pragma unroll
-    for (int k = 0; k < PASSES; ++k) *(u32v4*)(at + k * LROWS * LDK) = kr[k];  // (behind the last step: what was there)
+    for (int k = 0; k < PASSES; ++k) *(u32v4*)(to + k * LROWS * ld) = from[k];
   };
   auto store_v = [&](int i) {
-    char* at = v_at(i) + lrow * LDV + lslice * 16;
     if (i >= n_whole && i < n) {
       const Tile x = tile_of(i);
       bool odd = false;
@@ -207,8 +201,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
       }
       if (x.fresh && odd) sh_odd[i & 1] = 1;
     }
-#pragma unroll
-    for (int k = 0; k < PASSES; ++k) *(u32v4*)(at + k * LROWS * LDV) = vr[k];
+    store(vr, v_at(i), LDV);
   };
   // which of 32 rows from first + 32 t on this lane's query row sees
   auto sees = [&](const Tile& x, int t) {
@@ -234,27 +227,33 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  auto scores = [&](int i) {
+  // Scores of step i and outputs of step i - 1, in one stream of products.  (Before the first step P and V are 0; behind the
+  // last the scores are not used.)
+  constexpr int NS = KS * HALVES, NO = 2 * HALVES * DT32;
+  auto multiply = [&](int i) {
     const char* kl = k_at(i) + col * LDK + half * 16;
+    const char* vl = v_at(i - 1) + (half * 4 + (lane & 15) / 4) * LDV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
 #pragma unroll
     for (int t = 0; t < HALVES; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-    products<KS * HALVES, 6>([&](int j) { return *(const u32v4*)(kl + j % HALVES * 32 * LDK + j / HALVES * 32); },
-                             [&](int j, u32v4 f) { s[j % HALVES] = W::mma(f, q[j / HALVES], s[j % HALVES]); });
-  };
-  auto outputs = [&](int i) {
-    const char* vl = v_at(i) + (half * 4 + (lane & 15) / 4) * LDV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-    products<2 * HALVES * DT32, 4>(
+    products<NS + NO, 4>(
         [&](int j) {
-          const char* from = vl + j / DT32 * 16 * LDV + j % DT32 * 64;
-          const u32v2 x = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from));
-          const u32v2 y = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8 * LDV)));
-          return u32v4{x.x, x.y, y.x, y.y};
+          if (j < NS) return *(const u32v4*)(kl + j % HALVES * 32 * LDK + j / HALVES * 32);
+          const char* at = vl + (j - NS) / DT32 * 16 * LDV + (j - NS) % DT32 * 64;
+          const u32v2 y = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at));
+          const u32v2 z = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 8 * LDV)));
+          return u32v4{y.x, y.y, z.x, z.y};
         },
-        [&](int j, u32v4 f) { o[j % DT32] = W::mma(f, p[j / DT32], o[j % DT32]); });
-    if (i >= n_whole && tile_of(i).fresh && sh_odd[i & 1]) {
-      const Tile x = tile_of(i);
+        [&](int j, u32v4 f) {
+          if (j < NS) s[j % HALVES] = W::mma(f, q[j < NS ? j / HALVES : 0], s[j % HALVES]);
+          else o[(j - NS) % DT32] = W::mma(f, p[(j - NS) / DT32], o[(j - NS) % DT32]);
+        });
+  };
+  // infinities of the rows of step i
+  auto strays = [&](int i) {
+    const Tile x = tile_of(i);
+    if (x.fresh && sh_odd[i & 1]) {
       for (int t = 0; t < KT && x.first + t < x.limit; ++t) {
         if (!(sees(x, t >> 5) >> (t & 31) & 1)) continue;
         const char* row = vnb + (x.first + t) * a.nst + half * 8;
@@ -313,32 +312,39 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   };
 
   if (n > 0) {
+#pragma unroll
+    for (int k = 0; k < 2 * HALVES; ++k) p[k] = u32v4{0, 0, 0, 0};
+    for (int k = tid; k < KT * LDV / 16; k += THREADS) *(u32v4*)(v_at(1) + k * 16) = u32v4{0, 0, 0, 0};
     load_k(0);
-    store_k(0);
-    load_k(1);
     load_v(0);
+    // (q is used here, so that it is waited for here and not, with what else is on its way, in every step)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));
+    store(kr, k_at(0), LDK);
+    load_k(1);
     __syncthreads();
     if (late) {
-      store_k(1);
+      store(kr, k_at(1), LDK);
       store_v(0);
       load_k(2);
       load_v(1);
       __syncthreads();
     }
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i <= n; ++i) {
       if (!idle) {
-        scores(i);
-        if (i > 0) outputs(i - 1);
+        multiply(i);
+        if (i > n_whole) strays(i - 1);
       }
       __syncthreads();
-      if (!idle) weights(i);
-      store_k(i + late + 1);
-      store_v(i + late);
-      load_k(i + late + 2);
-      load_v(i + late + 1);
+      if (i < n) {
+        if (!idle) weights(i);
+        store(kr, k_at(i + late + 1), LDK);  // (behind the last step: what was there)
+        store_v(i + late);
+        load_k(i + late + 2);
+        load_v(i + late + 1);
+      }
       __syncthreads();
     }
-    if (!idle) outputs(n - 1);
     if (!late) __syncthreads();
   }
 
