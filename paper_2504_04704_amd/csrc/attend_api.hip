@@ -79,8 +79,8 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
   const int64_t steps = (seen + kt - 1) / kt + (p->N + kt - 1) / kt;
   const int64_t groups = pl->units * pl->row_tiles;
-  int64_t splits = (pl->wide ? (pl->row_tile == 128 ? 512 : 256) : 1024) / (groups > 0 ? groups : 1);
-  if (splits > steps / 4) splits = steps / 4;
+  int64_t splits = (pl->wide ? (pl->row_tile == 128 ? 512 : 256) : 512) / (groups > 0 ? groups : 1);
+  if (splits > steps / (pl->wide ? 2 : 4)) splits = steps / (pl->wide ? 2 : 4);
   if (splits > 256) splits = 256;
   if (splits < 1) splits = 1;
   pl->splits = (int)splits;

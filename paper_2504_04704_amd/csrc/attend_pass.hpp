@@ -209,11 +209,6 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
   const int share = ((steps + a.splits - 1) / a.splits + WAVES - 1) / WAVES * WAVES;
   const int step0 = w.split * share, step1 = min(step0 + share, steps);
-  if (a.parents && step1 > cache_steps && step0 < step1) {  // (uniform in the workgroup)
-    ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
-    __syncthreads();
-  }
-
   const char* kb = a.K + b * a.ksb + h * a.ksh;
   const char* vb = a.V + b * a.ksb + h * a.ksh;
   const char* knb = a.K_new + b * a.nsb + h * a.nsh;
@@ -285,17 +280,6 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     }
   };
 
-  int ids[SUBS], next_ids[SUBS];
-  int step = step0 + wave;
-  Step now;
-  if (step < step1) {
-    entries(step, ids);
-    now = step_of(step, ids);
-    load_k(now);
-    load_v(now);
-    entries(step + WAVES, next_ids);
-  }
-
   // q: one row a lane
   u32v4 q[RT][NC];
 #pragma unroll
@@ -322,6 +306,17 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     }
   }
 
+  int ids[SUBS], next_ids[SUBS];
+  int step = step0 + wave;
+  Step now;
+  if (step < step1) {
+    entries(step, ids);
+    now = step_of(step, ids);
+    load_k(now);
+    load_v(now);
+    entries(step + WAVES, next_ids);
+  }
+
   float m[RT], l[RT];
   f32x4 o[RT][DT16];
 #pragma unroll
@@ -331,6 +326,15 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
 #pragma unroll
     for (int d = 0; d < DT16; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+
+  if (a.parents && step1 > cache_steps && step0 < step1) {  // (uniform in the workgroup)
+    ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(q[rt][c]));  // (waited for here, not in every step)
 
   for (; step < step1; step += WAVES) {
     const bool more = step + WAVES < step1;

@@ -96,9 +96,6 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   const int step0 = w.split * share, step1 = min(step0 + share, steps), n = max(step1 - step0, 0);
 
   const int words = (seen_new + 31) / 32;
-  if (a.parents && step1 > cache_steps && n > 0) {
-    ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
-  }
   if (tid < 2) sh_odd[tid] = 0;
 
   // q, with the scale's sign: what is left of it is not negative, and the largest logit that of the largest product
@@ -317,6 +314,8 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     for (int k = tid; k < KT * LDV / 16; k += THREADS) *(u32v4*)(v_at(1) + k * 16) = u32v4{0, 0, 0, 0};
     load_k(0);
     load_v(0);
+    if (a.parents && step1 > cache_steps)
+      ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
     // (q is used here, so that it is waited for here and not, with what else is on its way, in every step)
 #pragma unroll
     for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));
