@@ -82,6 +82,12 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   int64_t splits = (pl->wide ? (pl->row_tile == 128 ? 512 : 256) : 512) / (groups > 0 ? groups : 1);
   if (splits > steps / (pl->wide ? 2 : 4)) splits = steps / (pl->wide ? 2 : 4);
   if (splits > 256) splits = 256;
+  // short caches whole, by twice the wavefronts: a second kernel costs more than these steps
+  pl->waves = 4;
+  if (pl->wide ? steps <= 6 : steps <= 32 && groups <= 256 && pl->row_tile == 16 && p->D <= 128) {
+    splits = 1;
+    pl->waves = 8;
+  }
   if (splits < 1) splits = 1;
   pl->splits = (int)splits;
   const int64_t parts = pl->units * splits * pl->rows, ld = (p->D + 3) & ~3;
@@ -154,9 +160,9 @@ int attend(const lagkv_attend_params* p, const void* Q, const void* K, const voi
   a.scale = (float)(p->dtype == LAGKV_F32 ? p->scale : p->scale * 1.4426950408889634);
   hipStream_t s = (hipStream_t)hip_stream;
   hipError_t e = pl.wide ? (p->dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))
-                 : p->dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, s)
-                 : p->dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, s)
-                                          : launch_attend_f16(a, pl.row_tile, s);
+                 : p->dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, pl.waves, s)
+                 : p->dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, pl.waves, s)
+                                          : launch_attend_f16(a, pl.row_tile, pl.waves, s);
   if (e == hipSuccess && pl.splits > 1) e = launch_attend_join(a, p->dtype, s);
   return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
 }

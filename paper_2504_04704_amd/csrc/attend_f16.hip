@@ -2,6 +2,8 @@
 
 namespace lagkv {
 
-hipError_t launch_attend_f16(const AttendArgs& a, int row_tile, hipStream_t s) { return launch_attend_of<LAGKV_F16>(a, row_tile, s); }
+hipError_t launch_attend_f16(const AttendArgs& a, int row_tile, int waves, hipStream_t s) {
+  return launch_attend_of<LAGKV_F16>(a, row_tile, waves, s);
+}
 
 }  // namespace lagkv

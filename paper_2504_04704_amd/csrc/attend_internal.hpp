@@ -33,15 +33,15 @@ struct AttendArgs {
 // Launch shape, a pure function of the parameters: rows of a tile, tiles of a unit, pieces the cache is cut into.
 struct AttendPlan {
   bool wide;
-  int row_tile, row_tiles, splits;
+  int row_tile, row_tiles, waves, splits;
   int64_t units;
   int32_t rows;
   size_t off_ml, ws_bytes;
 };
 
-hipError_t launch_attend_f32(const AttendArgs& a, int row_tile, hipStream_t s);
-hipError_t launch_attend_bf16(const AttendArgs& a, int row_tile, hipStream_t s);
-hipError_t launch_attend_f16(const AttendArgs& a, int row_tile, hipStream_t s);
+hipError_t launch_attend_f32(const AttendArgs& a, int row_tile, int waves, hipStream_t s);
+hipError_t launch_attend_bf16(const AttendArgs& a, int row_tile, int waves, hipStream_t s);
+hipError_t launch_attend_f16(const AttendArgs& a, int row_tile, int waves, hipStream_t s);
 hipError_t launch_wide_bf16(const AttendArgs& a, int row_tile, hipStream_t s);
 hipError_t launch_wide_f16(const AttendArgs& a, int row_tile, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int dtype, hipStream_t s);

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
   __shared__ float sh_ml[WAVES][ROWS][2];
   __shared__ int32_t sh_parent[kMaxTree];
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
   const WorkItem w = work_item(a);
   if (!w.any) return;
@@ -207,8 +207,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
   const int last_token = token_of(row1 - 1), token0 = token_of(row0), tokens = last_token - token0 + 1;
   const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0, words = (seen_new + 31) / 32;
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
-  const int share = ((steps + a.splits - 1) / a.splits + WAVES - 1) / WAVES * WAVES;
-  const int step0 = w.split * share, step1 = min(step0 + share, steps);
+  const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
   const char* kb = a.K + b * a.ksb + h * a.ksh;
   const char* vb = a.V + b * a.ksb + h * a.ksh;
   const char* knb = a.K_new + b * a.nsb + h * a.nsh;
@@ -217,23 +216,24 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
   const int n_full = PICK ? (int)(((int64_t)len + a.block - 1) >> a.block_shift) : 0;
   char* vl = lds + wave * (KT * LDV);
 
-  // A step: the first row of each sixteen, and how many rows there are.  The list's entries are read a step ahead.
+  // A step: the first row of each sixteen, and how many rows there are.
   struct Step {
     int first[SUBS], limit[SUBS];
     int fresh;  // (of the new tokens)
+    int whole;  // rows of the cache, all there
   };
-  auto entries = [&](int step, int (&id)[SUBS]) {
+  // (lane i has the entries of this wavefront's step i, or 64 + i, ...: one wait for all of them)
+  int ids[SUBS];
+  auto entries = [&](int step) {
+    if constexpr (PICK) {
 #pragma unroll
-    for (int s = 0; s < SUBS; ++s) {
-      if constexpr (PICK) {
-        const int e = (step * KT + s * 16) >> a.block_shift;
-        id[s] = step < cache_steps && e < a.n_blocks ? list[e] : -1;
-      } else {
-        id[s] = 0;
+      for (int s = 0; s < SUBS; ++s) {
+        const int at = step + lane * WAVES, e = (int)(((int64_t)at * KT + s * 16) >> a.block_shift);
+        ids[s] = at < cache_steps && e < a.n_blocks ? list[e] : -1;
       }
     }
   };
-  auto step_of = [&](int step, const int (&id)[SUBS]) {
+  auto step_of = [&](int step, int turn) {  // the turn-th of this wavefront
     Step x;
     x.fresh = step >= cache_steps;
 #pragma unroll
@@ -245,18 +245,37 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
         x.first[s] = step * KT + s * 16;
         x.limit[s] = len;
       } else {
-        const bool ok = id[s] >= 0 && id[s] < n_full;
-        x.first[s] = ok ? (id[s] << a.block_shift) + ((step * KT + s * 16) & (a.block - 1)) : 0;
+        const int id = __builtin_amdgcn_readlane(ids[s], turn & 63);
+        const bool ok = id >= 0 && id < n_full;
+        x.first[s] = ok ? (id << a.block_shift) + ((step * KT + s * 16) & (a.block - 1)) : 0;
         x.limit[s] = ok ? len : 0;
       }
     }
+    x.whole = !x.fresh;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) x.whole = x.whole && x.first[s] + 16 <= x.limit[s];
     return x;
   };
-  // K: lane (col, grp) has row col of each sixteen, slices grp, 4 + grp, ...: what its operand takes.  V: whole rows.
+  // K: lane (col, grp) has row col of each sixteen, slices grp, 4 + grp, ...: what its operand takes.  V: whole rows, a slice
+  // a lane.  Slices behind a row's last repeat another: q is 0 there, and what V gives for them is not stored.
   u32v4 kf[SUBS][NC], vf[NV];
   const int vslice = lane % CPR, vrow = lane / CPR;
-  const int voff = (vslice * PER < a.D ? slice_at(vslice, a.D, PER) : 0) * E::SIZE;  // (slices behind the last are not stored)
+  auto offset = [&](int slice) { return (slice * PER < a.D ? slice_at(slice, a.D, PER) : 0) * E::SIZE; };
+  int koff[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) koff[c] = offset(c * 4 + grp);
+  const int64_t klane = (int64_t)col * a.kst, vlane = (int64_t)vrow * a.kst + offset(vslice), vpass = a.kst * VROWS;
   auto load_k = [&](const Step& x) {
+    if (x.whole) {
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s) {
+        const char* at = kb + (int64_t)x.first[s] * a.kst + klane;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          kf[s][c] = *(const u32v4_any*)(at + (DP > 64 && c < NC / 2 ? koff[0] + c * 64 : koff[c]));  // (D is more than DP / 2 there)
+      }
+      return;
+    }
     const char* p = x.fresh ? knb : kb;
     const int64_t st = x.fresh ? a.nst : a.kst;
 #pragma unroll
@@ -264,14 +283,19 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
       const int row = x.first[s] + col;
       const char* at = p + (int64_t)(row < x.limit[s] ? row : 0) * st;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int slice = c * 4 + grp;
-        kf[s][c] = *(const u32v4_any*)(at + (slice * PER < a.D ? slice_at(slice, a.D, PER) : 0) * E::SIZE);
-      }
+      for (int c = 0; c < NC; ++c) kf[s][c] = *(const u32v4_any*)(at + koff[c]);
     }
   };
   auto load_v = [&](const Step& x) {
-    const char* p = (x.fresh ? vnb : vb) + voff;
+    if (x.whole) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int s = i * VROWS / 16;
+        vf[i] = *(const u32v4_any*)(vb + (int64_t)x.first[s] * a.kst + (i - s * 16 / VROWS) * vpass + vlane);
+      }
+      return;
+    }
+    const char* p = (x.fresh ? vnb : vb) + offset(vslice);
     const int64_t st = x.fresh ? a.nst : a.kst;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -280,41 +304,24 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     }
   };
 
+  entries(step0 + wave);
   // q: one row a lane
   u32v4 q[RT][NC];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + rt * 16 + col;
-    const bool ok = r < row1;
-    const int rr = ok ? r : row0;
+    const int rr = r < row1 ? r : row0;
     const char* p = a.Q + b * a.qsb + (h * a.G + group_of(rr)) * a.qsh + (int64_t)token_of(rr) * a.qsn;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int slice = c * 4 + grp, begin = slice * PER;
-      const int at = begin < a.D ? slice_at(slice, a.D, PER) : 0, dup = begin - at;
-      u32v4 v = *(const u32v4_any*)(p + at * E::SIZE);
-      if (!ok || begin >= a.D) v = u32v4{0, 0, 0, 0};
-      if (dup > 0) {  // leading channels that the slice before has
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (i < dup) {
-            if constexpr (E::SIZE == 4) v[i] = 0;
-            else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
-          }
-      }
-      q[rt][c] = v;
-    }
+    for (int c = 0; c < NC; ++c) q[rt][c] = *(const u32v4_any*)(p + koff[c]);
   }
 
-  int ids[SUBS], next_ids[SUBS];
-  int step = step0 + wave;
+  int step = step0 + wave, turn = 0;
   Step now;
   if (step < step1) {
-    entries(step, ids);
-    now = step_of(step, ids);
+    now = step_of(step, 0);
     load_k(now);
     load_v(now);
-    entries(step + WAVES, next_ids);
   }
 
   float m[RT], l[RT];
@@ -331,34 +338,56 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
     __syncthreads();
   }
+  // q's channels that the slice before has, and those behind its row's end, are 0.  (It is waited for here, behind the
+  // first rows' loads, and not in every step.)
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(q[rt][c]));  // (waited for here, not in every step)
+    for (int c = 0; c < NC; ++c) {
+      const int begin = (c * 4 + grp) * PER, dup = begin - koff[c] / E::SIZE;
+      u32v4 v = q[rt][c];
+      if (row0 + rt * 16 + col >= row1 || begin >= a.D) v = u32v4{0, 0, 0, 0};
+      if (a.D % PER != 0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i < dup) {
+            if constexpr (E::SIZE == 4) v[i] = 0;
+            else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+          }
+      }
+      asm volatile("" : "+v"(v));
+      q[rt][c] = v;
+    }
 
   for (; step < step1; step += WAVES) {
     const bool more = step + WAVES < step1;
     Step next = now;
-    if (more) next = step_of(step + WAVES, next_ids);
+    ++turn;
+    if (more) {
+      if (PICK && (turn & 63) == 0) entries(step + WAVES);
+      next = step_of(step + WAVES, turn);
+    }
     // V into LDS, rows that are not there as zeros, and the next step's on its way
     bool odd = false;
     wave_order();
+    if (!now.whole) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int s = i * VROWS / 16, row = i * VROWS + vrow;
-      u32v4 v = vf[i];
-      if (now.first[s] + row % 16 >= now.limit[s]) v = u32v4{0, 0, 0, 0};
-      if (now.fresh) {
-        // what is no finite number goes in as 0 (0 * inf is not) and is added to the query rows that see it afterwards
+      for (int i = 0; i < NV; ++i) {
+        const int s = i * VROWS / 16;
+        if (now.first[s] + i * VROWS % 16 + vrow >= now.limit[s]) vf[i] = u32v4{0, 0, 0, 0};
+        if (now.fresh) {
+          // what is no finite number goes in as 0 (0 * inf is not) and is added to the query rows that see it afterwards
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t bits = odd_bits<DT>(v[e]);
-          odd = odd || bits;
-          v[e] &= ~bits;
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = odd_bits<DT>(vf[i][e]);
+            odd = odd || bits;
+            vf[i][e] &= ~bits;
+          }
         }
       }
-      *(u32v4*)(vl + row * LDV + vslice * 16) = v;
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) *(u32v4*)(vl + (i * VROWS + vrow) * LDV + vslice * 16) = vf[i];
     wave_order();
     if (more) load_v(next);
     __builtin_amdgcn_sched_barrier(0);
@@ -385,20 +414,14 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
         p[rt][s] = x;
       }
     __builtin_amdgcn_sched_barrier(0);
-    if (more) {
-      load_k(next);
-      entries(step + 2 * WAVES, next_ids);
-    }
+    if (more) load_k(next);
     __builtin_amdgcn_sched_barrier(0);
 
-    bool whole = !now.fresh;
-#pragma unroll
-    for (int s = 0; s < SUBS; ++s) whole = whole && now.first[s] + 16 <= now.limit[s];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
       for (int s = 0; s < SUBS; ++s) p[rt][s] *= a.scale;
-      if (!whole) {
+      if (!now.whole) {
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
           const int j = now.first[s] + grp * 4, left = now.limit[s] - j;
@@ -534,6 +557,8 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
 
   // out: four slots of a row a thread
   constexpr int QUADS = DP / 4;
+  const bool slices = a.D % PER == 0;
+  const bool wide_out = slices && !(((uintptr_t)a.out | a.osb | a.osh | a.osn) & (4 * E::SIZE - 1));
   for (int i = tid; i < ROWS * QUADS; i += THREADS) {
     const int rl = i / QUADS, quad = i % QUADS, r = row0 + rl;
     if (r >= row1) continue;
@@ -552,7 +577,9 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     const int base = begin < a.D ? slice_at(slot / PER, a.D, PER) : 0, dup = begin - base, within = slot - begin;
     if (a.splits > 1) {
       const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
-      if (begin < a.D) {
+      if (slices && begin < a.D) {
+        *(f32x4*)(a.part_o + at * a.part_ld + slot) = v;
+      } else if (begin < a.D) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (within + e >= dup) a.part_o[at * a.part_ld + base + within + e] = v[e];
@@ -573,14 +600,19 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
     const float inv = blind ? 0.f : 1.f / sum;
     if (begin < a.D) {
       char* op = a.out + b * a.osb + head * a.osh + (int64_t)n * a.osn;
+      const f32x4 y = blind ? f32x4{0.f, 0.f, 0.f, 0.f} : v * inv;
+      if (wide_out) {
+        if constexpr (DT == LAGKV_F32) *(f32x4*)(op + slot * 4) = y;
+        else *(u32v2*)(op + slot * 2) = u32v2{E::pack(y[0], y[1]), E::pack(y[2], y[3])};
+      } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (within + e >= dup) {
-          const float y = blind ? 0.f : v[e] * inv;
-          const int ch = base + within + e;
-          if constexpr (DT == LAGKV_F32) *(float*)(op + ch * 4) = y;
-          else *(uint16_t*)(op + ch * 2) = (uint16_t)E::pack(y, 0.f);
-        }
+        for (int e = 0; e < 4; ++e)
+          if (within + e >= dup) {
+            const int ch = base + within + e;
+            if constexpr (DT == LAGKV_F32) *(float*)(op + ch * 4) = y[e];
+            else *(uint16_t*)(op + ch * 2) = (uint16_t)E::pack(y[e], 0.f);
+          }
+      }
     }
     if (quad == 0 && a.lse) a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
   }
@@ -605,8 +637,9 @@ hipError_t launch_attend_as(const AttendArgs& a, hipStream_t s) {
 
 // Row tiles by the registers they take: 16 query rows of 256 channels or 32 of 128 are what a lane holds without spilling.
 template <int DT>
-hipError_t launch_attend_of(const AttendArgs& a, int row_tile, hipStream_t s) {
+hipError_t launch_attend_of(const AttendArgs& a, int row_tile, int waves, hipStream_t s) {
   const bool one = row_tile == 16;
+  if (one && waves == 8) return a.D <= 64 ? launch_attend_as<DT, 64, 1, 8>(a, s) : launch_attend_as<DT, 128, 1, 8>(a, s);
   if (a.D <= 64) return one ? launch_attend_as<DT, 64, 1, 4>(a, s) : launch_attend_as<DT, 64, 2, 4>(a, s);
   if (a.D <= 128) return one ? launch_attend_as<DT, 128, 1, 4>(a, s) : launch_attend_as<DT, 128, 2, 4>(a, s);
   return launch_attend_as<DT, 256, 1, 4>(a, s);

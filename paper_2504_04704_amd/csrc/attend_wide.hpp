@@ -92,8 +92,8 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   const int token0 = row0 / a.G, last_token = (row1 - 1) / a.G, tokens = last_token - token0 + 1;
   const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
-  const int share = (steps + a.splits - 1) / a.splits;
-  const int step0 = w.split * share, step1 = min(step0 + share, steps), n = max(step1 - step0, 0);
+  const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
+  const int n = step1 - step0;
 
   const int words = (seen_new + 31) / 32;
   if (tid < 2) sh_odd[tid] = 0;
