@@ -157,6 +157,12 @@ int attend(const lagkv_attend_params* p, const void* Q, const void* K, const voi
   a.rows = pl.rows;
   a.row_tiles = pl.row_tiles;
   a.splits = pl.splits;
+  a.by_tiles = Divide::by(pl.row_tiles);
+  a.by_splits = Divide::by(pl.splits);
+  a.by_n = Divide::by(p->N);
+  a.by_h = Divide::by(p->H);
+  a.by_g = Divide::by(p->G);
+  a.by_rows = Divide::by(pl.rows);
   a.scale = (float)(p->dtype == LAGKV_F32 ? p->scale : p->scale * 1.4426950408889634);
   hipStream_t s = (hipStream_t)hip_stream;
   hipError_t e = pl.wide ? (p->dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))

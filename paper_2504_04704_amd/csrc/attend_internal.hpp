@@ -8,6 +8,20 @@
 
 namespace lagkv {
 
+// n / d for n below 2^31 by a product (a division takes some twenty instructions, one behind the other, and the kernels
+// begin with several).  With l the smallest for which d <= 2^l, and m = floor(2^32 (2^l - d) / d) + 1, the quotient is
+// (floor(m n / 2^32) + n) / 2^l: m + 2^32 is 2^(32+l) / d rounded up by less than 2^l.
+struct Divide {
+  uint32_t m, l;
+  __host__ static Divide by(uint32_t d) {
+    Divide x = {0, 0};
+    while ((uint64_t(1) << x.l) < d) ++x.l;
+    x.m = (uint32_t)((((uint64_t(1) << x.l) - d) << 32) / d + 1);
+    return x;
+  }
+  __host__ __device__ uint32_t of(uint32_t n) const { return ((uint32_t)((uint64_t)m * n >> 32) + n) >> l; }
+};
+
 // A unit is what one list of cache rows is for: a stream (b, h) with its G*N query rows, token-major (row n*G + g), or
 // with blocks listed for each token, (b, h, n) with its G query rows.  Strides are in BYTES here.
 struct AttendArgs {
@@ -27,6 +41,7 @@ struct AttendArgs {
   int32_t part_ld;  // D, rounded up to 4
   int32_t rows;    // of a unit
   int32_t row_tiles, splits;
+  Divide by_tiles, by_splits, by_n, by_h, by_g, by_rows;  // row_tiles, splits, N, H, G, rows
   float scale;  // times log2 e for the 16-bit types
 };
 

@@ -11,15 +11,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
   __shared__ float sh_o[4][kMaxHead];
   __shared__ float sh_l[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const uint32_t id = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, rows = (uint32_t)a.rows;
-  const int64_t unit = id / rows;
+  const uint32_t id = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, at_unit = a.by_rows.of(id);
+  const int64_t unit = at_unit;
   if (unit >= a.units) return;
-  const int r = (int)(id % rows);
+  const int r = (int)(id - at_unit * a.rows);
   const bool pick = a.blocks != nullptr;
-  const uint32_t stream = pick ? (uint32_t)unit / (uint32_t)a.N : (uint32_t)unit;
-  const int n = pick ? (int)((uint32_t)unit % (uint32_t)a.N) : (int)((uint32_t)r / (uint32_t)a.G);
-  const int g = pick ? r : (int)((uint32_t)r % (uint32_t)a.G);
-  const int64_t b = stream / (uint32_t)a.H, h = stream % (uint32_t)a.H, head = h * a.G + g;
+  const uint32_t stream = pick ? a.by_n.of(at_unit) : at_unit, bu = a.by_h.of(stream);
+  const int n = pick ? (int)(at_unit - stream * a.N) : (int)a.by_g.of(r), g = pick ? r : r - n * a.G;
+  const int64_t b = bu, h = stream - bu * a.H, head = h * a.G + g;
   const int64_t first = unit * a.splits * a.rows + r;  // of the pieces' rows, `rows` apart
   // lanes: four channels each, of one piece or of two or four
   const int per = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, quad = lane % per, sub = lane / per, pieces = 64 / per;

@@ -117,12 +117,13 @@ struct WorkItem {
   bool any;
 };
 __device__ __forceinline__ WorkItem work_item(const AttendArgs& a) {
-  const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, us = rest / (uint32_t)a.row_tiles * 8 + slot;
+  const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, many = a.by_tiles.of(rest), us = many * 8 + slot;
+  const uint32_t unit = a.by_splits.of(us);
   WorkItem w;
-  w.tile = (int)(rest % (uint32_t)a.row_tiles);
-  w.any = us < (uint32_t)(a.units * a.splits);
-  w.unit = us / (uint32_t)a.splits;
-  w.split = (int)(us % (uint32_t)a.splits);
+  w.tile = (int)(rest - many * a.row_tiles);
+  w.any = unit < (uint32_t)a.units;
+  w.unit = unit;
+  w.split = (int)(us - unit * a.splits);
   return w;
 }
 
@@ -191,12 +192,12 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
 
   const WorkItem w = work_item(a);
   if (!w.any) return;
-  const int n_fixed = PICK ? (int)((uint32_t)w.unit % (uint32_t)a.N) : 0;
-  const uint32_t stream = PICK ? (uint32_t)w.unit / (uint32_t)a.N : (uint32_t)w.unit;
-  const int64_t b = stream / (uint32_t)a.H, h = stream % (uint32_t)a.H;
+  const uint32_t stream = PICK ? a.by_n.of((uint32_t)w.unit) : (uint32_t)w.unit, bu = a.by_h.of(stream);
+  const int n_fixed = PICK ? (int)((uint32_t)w.unit - stream * a.N) : 0;
+  const int64_t b = bu, h = stream - bu * a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);  // query rows of this tile
-  auto token_of = [&](int r) { return PICK ? n_fixed : (int)((uint32_t)r / (uint32_t)a.G); };
-  auto group_of = [&](int r) { return PICK ? r : (int)((uint32_t)r % (uint32_t)a.G); };
+  auto token_of = [&](int r) { return PICK ? n_fixed : (int)a.by_g.of(r); };
+  auto group_of = [&](int r) { return PICK ? r : r - (int)a.by_g.of(r) * a.G; };
 
   // rows this tile may see, in steps: of the cache, then of the new tokens (up to the tile's last one, where each sees
   // those before it)

@@ -84,12 +84,13 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 
   const WorkItem w = work_item(a);
   if (!w.any) return;
-  const int64_t b = (uint32_t)w.unit / (uint32_t)a.H, h = (uint32_t)w.unit % (uint32_t)a.H;
+  const uint32_t bu = a.by_h.of((uint32_t)w.unit);
+  const int64_t b = bu, h = (uint32_t)w.unit - bu * a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
   int64_t len = a.lengths ? a.lengths[b] : a.T;
   len = len < 0 ? 0 : len > a.T ? a.T : len;
   const int cache_steps = (int)((len + KT - 1) / KT);
-  const int token0 = row0 / a.G, last_token = (row1 - 1) / a.G, tokens = last_token - token0 + 1;
+  const int token0 = (int)a.by_g.of(row0), last_token = (int)a.by_g.of(row1 - 1), tokens = last_token - token0 + 1;
   const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
   const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
@@ -101,27 +102,14 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   // q, with the scale's sign: what is left of it is not negative, and the largest logit that of the largest product
   const int r = row0 + wave * 32 + col;
   const bool mine = r < row1, idle = row0 + wave * 32 >= row1;  // (a wavefront without rows loads for the others)
-  const int rr = mine ? r : row0, token = rr / a.G, head = (int)h * a.G + rr % a.G;
+  const int rr = mine ? r : row0, token = (int)a.by_g.of(rr), head = (int)h * a.G + rr - token * a.G;
   const float c = fmaxf(fabsf(a.scale), 1e-30f);
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   u32v4 q[KS];
   {
     const char* p = a.Q + b * a.qsb + head * a.qsh + (int64_t)token * a.qsn;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const int slice = 2 * k + half, begin = slice * 8;
-      u32v4 v = {0, 0, 0, 0};
-      if (mine && begin < a.D) {
-        const int at = slice_at(slice, a.D, 8), dup = begin - at;
-        v = *(const u32v4_any*)(p + at * 2) ^ flip;
-        if (dup > 0) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < dup) v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
-        }
-      }
-      q[k] = v;
-    }
+    for (int k = 0; k < KS; ++k) q[k] = *(const u32v4_any*)(p + ((2 * k + half) * 8 < a.D ? slice_at(2 * k + half, a.D, 8) : 0) * 2);
   }
 
   const char* kb = a.K + b * a.ksb + h * a.ksh;
@@ -316,9 +304,20 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     load_v(0);
     if (a.parents && step1 > cache_steps)
       ancestors(a.parents + b * a.psb, a.N, token0, tokens, words, sh_parent, sh_mask, tid, THREADS);
-    // (q is used here, so that it is waited for here and not, with what else is on its way, in every step)
+    // q's channels that the slice before has, and those behind its row's end, are 0.  (It is waited for here, behind the
+    // first rows' loads, and not with what else is on its way in every step.)
 #pragma unroll
-    for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));
+    for (int k = 0; k < KS; ++k) {
+      const int begin = (2 * k + half) * 8, dup = begin < a.D ? begin - slice_at(2 * k + half, a.D, 8) : 0;
+      u32v4 v = mine && begin < a.D ? q[k] ^ flip : u32v4{0, 0, 0, 0};
+      if (a.D % 8 != 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < dup) v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+      }
+      asm volatile("" : "+v"(v));
+      q[k] = v;
+    }
     store(kr, k_at(0), LDK);
     load_k(1);
     __syncthreads();
