@@ -355,9 +355,9 @@ int lagkv_attend_blocks(const lagkv_attend_params* p, const void* Q, const void*
 
 /*
  * Smallest and largest key of every block of rows, channel by channel (Eq. 7-8 for each block): lo, hi [B, H,
- * ceil(T / block), D] device, dense, type of K.  Of p the fields B, H, D, dtype, T, block and kv_stride_* are read.
- * Only blocks from that of row `start` on are written (an update behind appended or compressed rows; 0: all).  A block with
- * no row before lengths[b] gets +inf and -inf.
+ * ceil(T / block), D] device, type of K, both with out_stride_*.  Of p the fields B, H, D, dtype, T, block, kv_stride_* and
+ * out_stride_* (b, h, block) are read.  Only blocks from that of row `start` on are written (an update behind appended or
+ * compressed rows; 0: all).  A block with no row before lengths[b] gets +inf and -inf.
  */
 int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_t* lengths, int64_t start, void* lo, void* hi,
                        void* hip_stream);
@@ -367,9 +367,10 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
  *     sum over the head's G query rows and the channels of max(q lo, q hi),
  * which no row of the block exceeds with its sum of q.k; of equal ones the lower.  The first `n_first` and the last `n_last`
  * of the blocks that lengths[b] leaves are always among them (n_first + n_last <= n_blocks).  Scores are summed in 64 bits.
+ *   lo, hi [B, H, ceil(T / block), D] device, type of Q, both with kv_stride_* (b, h, block)
  *   blocks [B, H, N, n_blocks] device int32, dense: ascending; -1 behind the last where there are fewer blocks
- * Of p the fields B, H, G, N, D, dtype, T, block, n_blocks and q_stride_* are read.  Workspace: 8 * B * H * N * ceil(T /
- * block) bytes, 16-byte aligned.
+ * Of p the fields B, H, G, N, D, dtype, T, block, n_blocks, q_stride_* and kv_stride_* are read.  Workspace: 8 * B * H * N *
+ * ceil(T / block) bytes, 16-byte aligned.
  */
 int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void* lo, const void* hi, const int32_t* lengths,
                         int32_t n_first, int32_t n_last, int32_t* blocks, void* ws, size_t ws_bytes, void* hip_stream);

@@ -202,12 +202,20 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
   int rc = check_heads(p);
   if (rc != LAGKV_OK) return rc;
   if (!block_ok(p->block) || start < 0) return LAGKV_EINVAL;
-  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0) return LAGKV_ESHAPE;
+  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0 || p->out_stride_b < 0 || p->out_stride_h < 0 ||
+      p->out_stride_n < 0)
+    return LAGKV_ESHAPE;
   if (p->T == 0 || start >= p->T) return LAGKV_OK;
   if (!K || !lo || !hi) return LAGKV_EINVAL;
   const int es = esize_of(p);
   if (!aligned(K, es) || !aligned(lo, es) || !aligned(hi, es) || !aligned(lengths, 4)) return LAGKV_EINVAL;
+  const int64_t nb = (p->T + p->block - 1) / p->block;
+  const int64_t n[3] = {p->B, p->H, nb}, st[3] = {p->out_stride_b, p->out_stride_h, p->out_stride_n};
+  if (!apart(p->D, n, st)) return LAGKV_ESHAPE;
   BoundsArgs a;
+  a.osb = p->out_stride_b * es;
+  a.osh = p->out_stride_h * es;
+  a.ost = p->out_stride_n * es;
   a.K = (const char*)K;
   a.lengths = lengths;
   a.lo = (char*)lo;
@@ -216,7 +224,7 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
   a.ksh = p->kv_stride_h * es;
   a.kst = p->kv_stride_t * es;
   a.T = p->T;
-  a.nb = (p->T + p->block - 1) / p->block;
+  a.nb = nb;
   a.first = start / p->block;
   a.B = p->B;
   a.H = p->H;
@@ -235,6 +243,7 @@ int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void*
   if (rc != LAGKV_OK) return rc;
   if (!block_ok(p->block) || p->n_blocks < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > p->n_blocks)
     return LAGKV_EINVAL;
+  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0) return LAGKV_ESHAPE;
   if (p->N == 0) return LAGKV_OK;
   if (!Q || !blocks || (p->T > 0 && (!lo || !hi))) return LAGKV_EINVAL;
   const int es = esize_of(p);
@@ -249,6 +258,9 @@ int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void*
   a.qsb = p->q_stride_b * es;
   a.qsh = p->q_stride_h * es;
   a.qsn = p->q_stride_n * es;
+  a.bsb = p->kv_stride_b * es;
+  a.bsh = p->kv_stride_h * es;
+  a.bst = p->kv_stride_t * es;
   a.T = p->T;
   a.nb = (p->T + p->block - 1) / p->block;
   a.B = p->B;

@@ -65,7 +65,7 @@ struct BoundsArgs {
   const char* K;
   const int32_t* lengths;
   char *lo, *hi;  // [B,H,nb,D]
-  int64_t ksb, ksh, kst;
+  int64_t ksb, ksh, kst, osb, osh, ost;
   int64_t T, nb, first;  // first block that is written
   int32_t B, H, D, block, dtype;
 };
@@ -76,7 +76,7 @@ struct SelectArgs {
   const int32_t* lengths;
   double* score;     // [B,H,N,nb]
   int32_t* blocks;   // [B,H,N,k]
-  int64_t qsb, qsh, qsn;
+  int64_t qsb, qsh, qsn, bsb, bsh, bst;
   int64_t T, nb;
   int32_t B, H, G, N, D, block, k, first, last, dtype;
 };

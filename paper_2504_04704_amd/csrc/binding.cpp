@@ -320,8 +320,8 @@ PyObject* select_blocks(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   try {
     int32_t dq, dl, dh, first, last, T;
     const at::Tensor *q = rows_of(args[0], &dq), *lo = rows_of(args[1], &dl), *hi = rows_of(args[2], &dh), *lengths;
-    if (!q || !lo || !hi || dq != dl || dq != dh || q->device() != lo->device() || !alike(*lo, *hi) || !lo->is_contiguous() ||
-        !hi->is_contiguous() || !small(*q) || !small(*lo))
+    if (!q || !lo || !hi || dq != dl || dq != dh || q->device() != lo->device() || !alike(*lo, *hi) || !small(*q) ||
+        !small(*lo))
       return none();
     lagkv_attend_params p = {};
     if (!to_int(args[3], &T) || !to_int(args[4], &p.block) || !to_int(args[5], &p.n_blocks) || !to_int(args[6], &first) ||
@@ -340,6 +340,9 @@ PyObject* select_blocks(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     p.q_stride_b = q->stride(0);
     p.q_stride_h = q->stride(1);
     p.q_stride_n = q->stride(2);
+    p.kv_stride_b = lo->stride(0);
+    p.kv_stride_h = lo->stride(1);
+    p.kv_stride_t = lo->stride(2);
     void* stream;
     if (!stream_of(*q, &stream)) return none();
     const auto opt = q->options().requires_grad(false);
@@ -386,12 +389,14 @@ PyObject* block_bounds(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       hi = at::empty({p.B, p.H, nb, p.D}, opt);
     } else {
       const at::Tensor *l = rows_of(args[4], &dl), *u = rows_of(args[5], &dh);
-      if (!l || !u || dl != dk || dh != dk || l->device() != K->device() || u->device() != K->device() || l->sizes() != u->sizes() ||
-          !l->is_contiguous() || !u->is_contiguous() || l->size(0) != p.B || l->size(1) != p.H || l->size(2) != nb || l->size(3) != p.D)
+      if (!l || !u || dl != dk || dh != dk || l->device() != K->device() || !alike(*l, *u) || l->size(0) != p.B || l->size(1) != p.H || l->size(2) != nb || l->size(3) != p.D)
         return none();
       lo = *l;
       hi = *u;
     }
+    p.out_stride_b = lo.stride(0);
+    p.out_stride_h = lo.stride(1);
+    p.out_stride_n = lo.stride(2);
     void* stream;
     if (!stream_of(*K, &stream)) return none();
     const void* kp = K->data_ptr();

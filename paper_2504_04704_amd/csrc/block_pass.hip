@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsArgs a, i
       hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], far));
     }
   if (sub == 0 && have) {
-    const int64_t to = ((stream * a.nb + j) * a.D + at) * SIZE;
+    const int64_t to = b * a.osb + h * a.osh + j * a.ost + at * SIZE;
     const uint4 l4 = repack<ET>(lo), h4 = repack<ET>(hi);
     *(u32v4_any*)(a.lo + to) = u32v4{l4.x, l4.y, l4.z, l4.w};
     *(u32v4_any*)(a.hi + to) = u32v4{h4.x, h4.y, h4.z, h4.w};
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       const int64_t j = jw + (p0 + i) * step + sub, jj = j < a.nb ? j : a.nb - 1;
-      const int64_t from = ((stream * a.nb + jj) * a.D + at) * SIZE;
+      const int64_t from = b * a.bsb + h * a.bsh + jj * a.bst + at * SIZE;
       lo4[i] = ld16_any(a.lo + from);
       hi4[i] = ld16_any(a.hi + from);
     }
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int slice = c * 4 + grp;
-    const int64_t from = ((stream * a.nb + jj) * a.D + (slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0)) * SIZE;
+    const int64_t from = b * a.bsb + h * a.bsh + jj * a.bst + (slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0) * SIZE;
     lo4[c] = ld16_any(a.lo + from);
     hi4[c] = ld16_any(a.hi + from);
   }

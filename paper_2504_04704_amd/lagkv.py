@@ -554,12 +554,14 @@ def block_bounds(K: torch.Tensor, block: int, lengths: Optional[torch.Tensor] = 
         out = (torch.empty(shape, dtype=K.dtype, device=K.device), torch.empty(shape, dtype=K.dtype, device=K.device))
     lo, hi = out
     for t in out:
-        if tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != K.dtype or t.device != K.device:
-            raise ValueError("output buffers must be dense [B,H,ceil(T/block),D] of the input dtype")
+        _rows("out", t, K)
+        if tuple(t.shape) != shape or t.stride() != lo.stride():
+            raise ValueError("output buffers must be two [B,H,ceil(T/block),D] tensors of the input dtype with the same strides")
     if lengths is not None:
         _ints("lengths", lengths, (B,), K.device)
     p = AttendParams(B=B, H=H, D=D, dtype=_DTYPES[K.dtype], block=block, T=T)
     p.kv_stride[:] = K.stride()[:3]
+    p.out_stride[:] = lo.stride()[:3]
     with _on(K.device):
         _check(load().lagkv_block_bounds(C.byref(p), K.data_ptr(), _ptr(lengths), start, lo.data_ptr(), hi.data_ptr(),
                                          _stream_ptr(K.device)), "lagkv_block_bounds")
@@ -587,8 +589,7 @@ def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, b
         raise LagKVError(EINVAL, "lagkv_select_blocks")
     if q.shape[0] != B or q.shape[3] != D or H == 0 or heads % H or nb != -(-T // block):
         raise ValueError("q must be [B,H*G,N,D] for lo, hi [B,H,ceil(T/block),D]")
-    if hi.shape != lo.shape or hi.dtype != lo.dtype or hi.device != lo.device or not lo.is_contiguous() or not hi.is_contiguous():
-        raise ValueError("lo and hi must be dense and share shape, dtype and device")
+    _same_layout(lo, hi)
     if lengths is not None:
         _ints("lengths", lengths, (B,), q.device)
     if out is None:
@@ -597,6 +598,7 @@ def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, b
         _ints("out", out, (B, H, N, k), q.device)
     p = AttendParams(B=B, H=H, G=heads // H, N=N, D=D, dtype=_DTYPES[q.dtype], block=block, n_blocks=k, T=T)
     p.q_stride[:] = q.stride()[:3]
+    p.kv_stride[:] = lo.stride()[:3]
     with _on(q.device):
         ws = _bytes(ws, 8 * B * H * N * nb, q.device)
         _check(load().lagkv_select_blocks(C.byref(p), q.data_ptr(), lo.data_ptr(), hi.data_ptr(), _ptr(lengths), index(first),
@@ -621,6 +623,7 @@ class Cache:
         self.c = CacheT(self.K.data_ptr(), self.V.data_ptr(), _ptr(self.pos), capacity, 0, 0, 0)
         self._ws = None
         self._prepared = {}
+        self._bounds = {}  # rows of a block -> [lo, hi, first row that they are behind of]
 
     @classmethod
     def from_compressed(cls, comp: Compressed, T: int, capacity: int, S: int, L: int, r: float,
@@ -645,6 +648,7 @@ class Cache:
         """lagkv_cache_after_compress: the buffers now hold the output of compress() on T rows."""
         _check(load().lagkv_cache_after_compress(C.byref(self._params()), T, C.byref(self.c)),
                "lagkv_cache_after_compress")
+        self.changed_from(0)
 
     @property
     def n_static(self) -> int:
@@ -680,6 +684,8 @@ class Cache:
         return self._ws
 
     def append_and_compress(self, K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]) -> None:
+        if self._bounds:
+            return self._append_tracked(K_new, V_new)
         K = self.K
         if _native is not None:
             rc = _native.append(self.c, K, self.S, self.L, self.r, self.variant, self.std_ddof, self.launch, self._ws, K_new, V_new)
@@ -712,6 +718,7 @@ class Cache:
         number of calls."""
         T, have = K.shape[2], self.K.shape
         strides = K.stride()
+        self.changed_from(self.c.n_static)
         if T and isinstance(V, torch.Tensor) and K.shape == (have[0], have[1], T, have[3]) and strides[3] == 1 \
                 and 0 not in strides and (V.shape, V.stride(), V.dtype, V.device) == (K.shape, strides, K.dtype, K.device) \
                 and (K.dtype, K.device) == (self.K.dtype, self.K.device):
@@ -735,3 +742,58 @@ class Cache:
     def view(self) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
         n = self.length
         return self.K[:, :, :n], self.V[:, :, :n], None if self.pos is None else self.pos[:, :, :n]
+
+    # ---- the operators that read a cache, over the rows held; `batch`: a slice of the batch (one layer of those folded into it) ----
+
+    def attend(self, q: torch.Tensor, K_new: Optional[torch.Tensor] = None, V_new: Optional[torch.Tensor] = None,
+               parents: Optional[torch.Tensor] = None, batch: slice = slice(None), **kw) -> Attended:
+        """attend() of new tokens over the rows held.  The tokens' own rows, K_new and V_new, are not in the cache yet: those
+        of the accepted ones are what append_and_compress takes afterwards."""
+        n = self.length
+        return attend(q, self.K[batch, :, :n], self.V[batch, :, :n], K_new, V_new, parents, **kw)
+
+    def _append_tracked(self, K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]) -> None:
+        # (a round rewrites the rows behind the static part; a call that makes none, those behind the tail)
+        kept, static, held = self._bounds, self.c.n_static, self.length
+        self._bounds = {}
+        try:
+            self.append_and_compress(K_new, V_new)
+        finally:
+            self._bounds = kept
+            self.changed_from(held if self.c.n_static == static else static)
+
+    def changed_from(self, row: int) -> None:
+        """Says that rows from `row` on were written past this object's calls: block_bounds() works them out again."""
+        for kept in self._bounds.values():
+            kept[2] = min(kept[2], max(int(row), 0))
+
+    def block_bounds(self, block: int) -> Tuple[torch.Tensor, torch.Tensor]:
+        """block_bounds() of the rows held, kept from call to call: only blocks whose rows have changed are gone over."""
+        n, block = self.length, index(block)
+        kept = self._bounds.get(block)
+        if kept is None:
+            if block < 1:
+                raise LagKVError(EINVAL, "lagkv_block_bounds")
+            B, H, capacity, D = self.K.shape
+            lo, hi = (torch.empty((B, H, -(-capacity // block), D), dtype=self.K.dtype, device=self.K.device) for _ in range(2))
+            kept = [lo, hi, 0]
+        nb = -(-n // block)
+        lo, hi = kept[0][:, :, :nb], kept[1][:, :, :nb]
+        if kept[2] < n:
+            block_bounds(self.K[:, :, :n], block, start=kept[2], out=(lo, hi))
+        kept[2] = n
+        self._bounds[block] = kept
+        return lo, hi
+
+    def select_blocks(self, q: torch.Tensor, block: int, k: int, first: int = 0, last: int = 0,
+                      batch: slice = slice(None)) -> torch.Tensor:
+        """select_blocks() among the blocks of the rows held."""
+        lo, hi = self.block_bounds(block)
+        return select_blocks(q, lo[batch], hi[batch], self.length, block, k, first, last)
+
+    def attend_blocks(self, q: torch.Tensor, blocks: torch.Tensor, block: int, K_new: Optional[torch.Tensor] = None,
+                      V_new: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
+                      batch: slice = slice(None), **kw) -> Attended:
+        """attend_blocks() over listed blocks of the rows held, as select_blocks() gives them."""
+        n = self.length
+        return attend_blocks(q, self.K[batch, :, :n], self.V[batch, :, :n], blocks, block, K_new, V_new, parents, **kw)

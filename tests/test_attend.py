@@ -317,6 +317,25 @@ def test_bounds_update_leaves_the_blocks_before_it():
     assert torch.equal(lo, before)
 
 
+@pytest.mark.parametrize("dtype", [BF, FL], ids=["bf16", "f32"])
+def test_bounds_between_other_rows(dtype):
+    """Bounds in buffers with room, one layer of several, and read from there."""
+    T, block = 300, 32
+    K, q = rand(2, 3, T, 72, dtype=dtype, seed=61), rand(2, 6, 2, 72, dtype=dtype, seed=62)
+    room = torch.full((2, 4, 3, 15, 75), 5.0, dtype=dtype, device=DEV)
+    lo, hi = room[0, 1:3, :, 2:12, 1:73], room[1, 1:3, :, 2:12, 1:73]
+    lagkv.block_bounds(K, block, out=(lo, hi))
+    wl, wh = A.bounds(K, block)
+    assert torch.equal(lo.cpu(), wl) and torch.equal(hi.cpu(), wh)
+    for n in (1, 2):
+        got = lagkv.select_blocks(q[:, :, :n], lo, hi, T, block, 4)
+        assert torch.equal(got.cpu(), A.select(q[:, :, :n], wl, wh, T, block, 4))
+    q5 = rand(2, 6, 5, 72, dtype=dtype, seed=63)
+    assert torch.equal(lagkv.select_blocks(q5, lo, hi, T, block, 4).cpu(), A.select(q5, wl, wh, T, block, 4))
+    lo.fill_(5.0), hi.fill_(5.0)
+    assert bool((room == 5).all())
+
+
 def test_equal_scores_go_to_the_lower_block():
     """Blocks of equal bounds, and of scores 0 and -0: the lower index is taken."""
     lo = torch.ones(1, 1, 700, 16, device=DEV)

@@ -103,7 +103,9 @@ def test_bounds_and_selection_refuse(lib):
     assert bounds(params(T=0), K=None) == lagkv.OK and bounds(params(), start=1000) == lagkv.OK
     for kw in [dict(K=None), dict(lo=None), dict(hi=None), dict(start=-1), dict(K=P + 1), dict(lengths=P + 1), dict(hi=P + 1)]:
         assert bounds(params(), **kw) == E, kw
-    assert bounds(params(block=12)) == E and bounds(params(kv=(0, 0, -1))) == S and bounds(params(dtype=9)) == lagkv.EDTYPE
+    wide = (1 << 20, 1 << 19, 64)
+    assert bounds(params()) == S and bounds(params(out=(1 << 20, 1 << 19, 63))) == S and bounds(params(out=(-1, 0, 0))) == S
+    assert bounds(params(out=wide, block=12)) == E and bounds(params(kv=(0, 0, -1))) == S and bounds(params(dtype=9)) == lagkv.EDTYPE
 
     def select(p, Q=P, lo=P, hi=P, lengths=None, first=0, last=0, blocks=P, ws=P, n=1 << 40):
         return lib.lagkv_select_blocks(C.byref(p), Q, lo, hi, lengths, first, last, blocks, ws, n, None)
@@ -113,6 +115,7 @@ def test_bounds_and_selection_refuse(lib):
     for kw in [dict(Q=None), dict(lo=None), dict(hi=None), dict(blocks=None), dict(first=-1), dict(last=-1), dict(first=3, last=2),
                dict(first=(1 << 31) - 1, last=(1 << 31) - 1), dict(Q=P + 1), dict(blocks=P + 1)]:
         assert select(ok, **kw) == E, kw
+    assert select(params(n_blocks=4, kv=(0, 0, -1))) == S
     assert select(params(n_blocks=0)) == E and select(params(n_blocks=4, block=20)) == E
     need = 8 * 2 * 2 * 3 * 32
     for kw in [dict(ws=None), dict(n=need - 1), dict(ws=P + 8)]:
