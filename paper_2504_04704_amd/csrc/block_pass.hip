@@ -279,6 +279,27 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
+// Bits that any lane has.
+__device__ __forceinline__ uint32_t wave_or(uint32_t v) {
+  v |= (uint32_t)dpp_mov_i<0xB1>((int)v);
+  v |= (uint32_t)dpp_mov_i<0x4E>((int)v);
+  v |= (uint32_t)dpp_mov_i<0x141>((int)v);
+  v |= (uint32_t)dpp_mov_i<0x140>((int)v);
+  const int x = (int)v;
+  return (uint32_t)(__builtin_amdgcn_readlane(x, 0) | __builtin_amdgcn_readlane(x, 16) | __builtin_amdgcn_readlane(x, 32) |
+                    __builtin_amdgcn_readlane(x, 48));
+}
+__device__ __forceinline__ uint64_t wave_or(uint64_t v) { return (uint64_t)wave_or((uint32_t)(v >> 32)) << 32 | wave_or((uint32_t)v); }
+// Sum over the lanes up to this one (row_shr: 0 where a row begins).
+__device__ __forceinline__ uint32_t sum_upto(uint32_t v, int lane) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+  const uint32_t a = __builtin_amdgcn_readlane((int)v, 15), b = __builtin_amdgcn_readlane((int)v, 31), c = __builtin_amdgcn_readlane((int)v, 47);
+  return v + (lane >= 16 ? a : 0) + (lane >= 32 ? b : 0) + (lane >= 48 ? c : 0);
+}
+
 // A workgroup takes a token's list.  The k-th largest key is found eight bits at a time (a histogram in LDS of the keys that
 // share the digits found), from the highest bit in which two keys differ down to where the keys that share all digits found are as many as are
 // still wanted: two or three passes as a rule.  Then the blocks above it, and the first of those equal to it, are written in
@@ -286,7 +307,7 @@ __device__ __forceinline__ uint64_t score_key(double s) {
 constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
 template <int E>
 __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const SelectArgs a) {
-  __shared__ uint32_t sh_hist[256];
+  __shared__ uint32_t sh_hist[2][256];
   __shared__ uint64_t sh_edge, sh_wave[2][kSelectWaves];
   __shared__ uint32_t sh_need, sh_in;
   __shared__ uint32_t sh_count[2][2][kSelectWaves];
@@ -324,16 +345,13 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
     some |= u;
     all &= u ? u : ~0ull;
   });
-#pragma unroll
-  for (int far = 1; far < 64; far <<= 1) {
-    some |= __shfl_xor(some, far);
-    all &= __shfl_xor(all, far);
-  }
+  some = wave_or(some);
+  all = ~wave_or(~all);
   if (lane == 0) {
     sh_wave[0][wave] = some;
     sh_wave[1][wave] = all;
   }
-  if (tid < 256) sh_hist[tid] = 0;
+  (&sh_hist[0][0])[tid] = 0;  // (kSelectThreads bins)
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < kSelectWaves; ++x) {
@@ -348,12 +366,12 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
   } else if (differ != 0) {
     int low = 63 - __builtin_clzll(differ);  // the highest differing bit, then the lowest one found
     edge = low == 63 ? 0 : edge >> (low + 1) << (low + 1);
-    int high = low;
+    int high = low, turn = 0;
     for (;;) {
       const int width = high + 1 < 8 ? high + 1 : 8;
       low = high + 1 - width;
       each([&](int64_t, uint64_t u) {
-        if (u && (high == 63 || (u >> (high + 1)) == (edge >> (high + 1)))) atomicAdd(&sh_hist[(u >> low) & ((1u << width) - 1)], 1u);
+        if (u && (high == 63 || (u >> (high + 1)) == (edge >> (high + 1)))) atomicAdd(&sh_hist[turn][(u >> low) & ((1u << width) - 1)], 1u);
       });
       __syncthreads();
       if (wave == 0) {
@@ -361,66 +379,91 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
         uint32_t c[4], sum = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          c[i] = sh_hist[255 - 4 * lane - i];
+          c[i] = sh_hist[turn][255 - 4 * lane - i];
           sum += c[i];
         }
-        uint32_t upto = sum;
-#pragma unroll
-        for (int far = 1; far < 64; far <<= 1) {
-          const uint32_t x = __shfl_up(upto, far);
-          if (lane >= far) upto += x;
-        }
+        const uint32_t upto = sum_upto(sum, lane);
         uint32_t before = upto - sum;
         if (before < need && upto >= need) {
           int i = 0;
           while (i < 3 && before + c[i] < need) before += c[i++];
           sh_edge = edge | (uint64_t)(255 - 4 * lane - i) << low;
           sh_need = need - before;
-          sh_in = c[i];
+          sh_in = i == 0 ? c[0] : i == 1 ? c[1] : i == 2 ? c[2] : c[3];
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sh_hist[turn][255 - 4 * lane - i] = 0;  // (for the pass after the next)
       }
       __syncthreads();
       edge = sh_edge;
       need = sh_need;
       const bool done = sh_in == need;
-      if (tid < 256) sh_hist[tid] = 0;
       if (done) above_edge = edge;
       if (done || low == 0) break;
       high = low - 1;
-      __syncthreads();
+      turn ^= 1;
     }
   }
   // (all keys equal: the first `need` of them)
-  uint32_t taken = 0, equal = 0;
-  int turn = 0;
-  each([&](int64_t e, uint64_t u) {
-    if (e >= slabs) return;  // (uniform)
-    const int64_t j = e * kSelectThreads + tid;
-    const bool forced = j < free0 || (j >= free1 && j < nb);
-    const bool over = forced || (u && (above_edge ? u >= above_edge : u > edge));
-    const bool tie = !forced && u && !above_edge && u == edge;
-    const uint64_t overs = __ballot(over), ties = __ballot(tie);
-    if (lane == 0) {
-      sh_count[turn][0][wave] = __popcll(overs);
-      sh_count[turn][1][wave] = __popcll(ties);
+  auto over_of = [&](int64_t j, uint64_t u) {
+    return j < free0 || (j >= free1 && j < nb) || (u && (above_edge ? u >= above_edge : u > edge));
+  };
+  auto tie_of = [&](int64_t j, uint64_t u) { return u && !above_edge && u == edge && j >= free0 && j < free1; };
+  auto put = [&](int64_t j, bool over, bool tie, uint32_t before_o, uint32_t before_t) {
+    if (over || (tie && before_t < need)) to[before_o + (before_t < need ? before_t : need)] = (int32_t)j;
+  };
+  if constexpr (E * kSelectWaves <= 64 && E > 0) {
+    // the slabs' counts by wavefront, a lane each
+    __shared__ uint32_t sh_all[2][E * kSelectWaves];
+    uint64_t overs[E], ties[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int64_t j = (int64_t)e * kSelectThreads + tid;
+      overs[e] = __ballot(over_of(j, mine[e]));
+      ties[e] = __ballot(tie_of(j, mine[e]));
+      if (lane == 0) {
+        sh_all[0][e * kSelectWaves + wave] = __popcll(overs[e]);
+        sh_all[1][e * kSelectWaves + wave] = __popcll(ties[e]);
+      }
     }
     __syncthreads();
-    uint32_t before_o = taken, before_t = equal;
+    const uint32_t o = lane < E * kSelectWaves ? sh_all[0][lane] : 0, t = lane < E * kSelectWaves ? sh_all[1][lane] : 0;
+    const uint32_t upto_o = sum_upto(o, lane) - o, upto_t = sum_upto(t, lane) - t;
+    const int w = __builtin_amdgcn_readfirstlane(wave);
 #pragma unroll
-    for (int x = 0; x < kSelectWaves; ++x) {
-      const uint32_t o = sh_count[turn][0][x], t = sh_count[turn][1][x];
-      if (x < wave) {
-        before_o += o;
-        before_t += t;
-      }
-      taken += o;
-      equal += t;
+    for (int e = 0; e < E; ++e) {
+      const uint32_t before_o = (uint32_t)__builtin_amdgcn_readlane((int)upto_o, e * kSelectWaves + w) + prefix_popc(overs[e]);
+      const uint32_t before_t = (uint32_t)__builtin_amdgcn_readlane((int)upto_t, e * kSelectWaves + w) + prefix_popc(ties[e]);
+      put((int64_t)e * kSelectThreads + tid, overs[e] >> lane & 1, ties[e] >> lane & 1, before_o, before_t);
     }
-    before_o += prefix_popc(overs);
-    before_t += prefix_popc(ties);
-    if (over || (tie && before_t < need)) to[before_o + (before_t < need ? before_t : need)] = (int32_t)j;
-    turn ^= 1;
-  });
+  } else {
+    uint32_t taken = 0, equal = 0;
+    int slab = 0;
+    each([&](int64_t e, uint64_t u) {
+      if (e >= slabs) return;  // (uniform)
+      const int64_t j = e * kSelectThreads + tid;
+      const bool over = over_of(j, u), tie = tie_of(j, u);
+      const uint64_t overs = __ballot(over), ties = __ballot(tie);
+      if (lane == 0) {
+        sh_count[slab][0][wave] = __popcll(overs);
+        sh_count[slab][1][wave] = __popcll(ties);
+      }
+      __syncthreads();
+      uint32_t before_o = taken, before_t = equal;
+#pragma unroll
+      for (int x = 0; x < kSelectWaves; ++x) {
+        const uint32_t o = sh_count[slab][0][x], t = sh_count[slab][1][x];
+        if (x < wave) {
+          before_o += o;
+          before_t += t;
+        }
+        taken += o;
+        equal += t;
+      }
+      put(j, over, tie, before_o + prefix_popc(overs), before_t + prefix_popc(ties));
+      slab ^= 1;
+    });
+  }
 }
 
 int lanes_a_row(int D, int dtype) {
