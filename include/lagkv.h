@@ -334,7 +334,7 @@ size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p);
  *     a chunk of a prompt; else those of token n and of its ancestors in a drafted tree: parents[b,n] (device int32,
  *     N <= LAGKV_TREE_MAX) is the token that n was drafted behind, an earlier one, or -1 behind the cache.  Any other
  *     value says that n is no token (padding): it sees nothing, nothing sees it, and a path up the tree ends before it.
- *   out  dtype of Q; a row that sees nothing is 0
+ *   out  dtype of Q; a row that sees nothing is 0.  May be Q itself (with Q's strides), and overlap no other input.
  *   lse  [B, H*G, N] device fp32, dense, or NULL: log sum exp of the logits, natural; -inf where nothing is seen
  * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold.
  * Logits, sums and products are held in fp32; results do not depend on anything but the arguments (no atomics).

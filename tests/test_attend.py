@@ -106,6 +106,19 @@ def test_ragged_lengths_and_what_lies_behind_them(dtype, new, N):
         assert bool((got.out[0] == 0).all()) and bool((got.lse[7] == -math.inf).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, FL], ids=["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 12], ids=["few_rows", "many_rows"])
+def test_ragged_lengths_of_a_cache_in_pieces(dtype, N):
+    """Pieces that are cut for the longest length there may be: most have no row of a shorter one."""
+    T, lens = 5000, [0, 1, 70, 4999]
+    q, K, V, Kn, Vn = problem(dtype, len(lens), 1, 4, N, 64, T, "chain", seed=15)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    want = A.attend(q, K, V, Kn, Vn, None, lengths)
+    for b, n in enumerate(lens):
+        K[b, :, n:], V[b, :, n:] = math.nan, math.nan
+    A.check(lagkv.attend(q, K, V, Kn, Vn, lengths=lengths, want_lse=True), want)
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("chain", [True, False])
@@ -275,6 +288,54 @@ def test_bounds_select_and_attend_blocks(size, dtype):
     assert torch.equal(blocks.cpu(), A.select(q, lo, hi, T, block, k, first, last, lengths))
     got = lagkv.attend_blocks(q, K, V, blocks, block, Kn, Vn, parents, lengths, want_lse=True)
     A.check(got, A.attend(q, K, V, Kn, Vn, parents, lengths, blocks=blocks.cpu(), block=block), str(size))
+
+
+@pytest.mark.parametrize("dtype", [BF, FL], ids=["bf16", "f32"])
+def test_long_lists_of_many_tokens(dtype):
+    """More steps of a list than a wavefront reads entries for at once, in lists that are not cut into pieces."""
+    B, H, N, T, block, k = 8, 8, 8, 9000, 64, 140
+    q, K, V, Kn, Vn = problem(dtype, B, H, 1, N, 32, T, "chain", seed=44)
+    g = torch.Generator().manual_seed(3)
+    blocks = torch.rand(B, H, N, 141, generator=g).argsort(-1)[..., :k].to(torch.int32)
+    got = lagkv.attend_blocks(q, K, V, blocks.to(DEV), block, Kn, Vn, want_lse=True)
+    one = slice(3, 4)
+    want = A.attend(q[one], K[one], V[one], Kn[one], Vn[one], blocks=blocks[one], block=block)
+    A.check(lagkv.Attended(got.out[one], got.lse[one]), want)
+
+
+def test_nothing_to_do_and_the_output_in_place_of_the_queries():
+    q, K, V, Kn, Vn = problem(BF, 2, 2, 4, 0, 64, 50, "chain", seed=45)
+    got = lagkv.attend(q, K, V, Kn, Vn, want_lse=True)
+    assert got.out.shape == (2, 8, 0, 64) and got.lse.shape == (2, 8, 0)
+    for N, T in ((1, 50), (3, 4000), (40, 500)):
+        q, K, V, Kn, Vn = problem(BF, 2, 2, 4, N, 64, T, "chain", seed=46)
+        want = A.attend(q, K, V, Kn, Vn)
+        assert lagkv.attend(q, K, V, Kn, Vn, out=q).out is q
+        A.check(lagkv.Attended(q, None), want)
+
+
+def test_two_threads():
+    """Calls from two threads, each on a stream of its own."""
+    import threading
+    sets = [problem(BF, 1, 2, 4, 3, 128, 3000, "chain", seed=47 + i) for i in range(2)]
+    want = [lagkv.attend(*s).out for s in sets]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(50):
+                out = lagkv.attend(*sets[i]).out
+            torch.cuda.current_stream().synchronize()
+            if not torch.equal(out, want[i]):
+                wrong.append(i)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert wrong == []
 
 
 def test_all_blocks_are_all_rows():

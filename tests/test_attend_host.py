@@ -62,7 +62,7 @@ def test_attend_refuses(lib):
     assert attend(lib, None) == E
     assert attend(lib, params(N=0), Q=None, out=None) == lagkv.OK           # nothing to do
     for kw, want in [(dict(dtype=3), D), (dict(dtype=-1), D), (dict(B=0), S), (dict(H=0), S), (dict(G=0), S), (dict(N=-1), S),
-                     (dict(D=7), S), (dict(D=257), S), (dict(T=-1), S), (dict(T=1 << 31), S), (dict(scale=math.inf), E),
+                     (dict(D=7), S), (dict(D=257), S), (dict(T=-1), S), (dict(T=(1 << 31) - 1), S), (dict(scale=math.inf), E),
                      (dict(scale=math.nan), E), (dict(scale=1e39), E), (dict(B=1 << 20, H=1 << 10), S), (dict(G=1 << 16, N=1 << 16), S),
                      (dict(q=(-1, 0, 0)), S), (dict(kv=(0, -1, 0)), S), (dict(new=(0, 0, -1)), S), (dict(psb=-1), S),
                      # rows of the output on one another
