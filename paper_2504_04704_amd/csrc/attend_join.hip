@@ -11,6 +11,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
   __shared__ float sh_o[4][kMaxHead];
   __shared__ float sh_l[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  fetch_arguments<AttendArgs>();
   const uint32_t id = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, at_unit = a.by_rows.of(id);
   const int64_t unit = at_unit;
   if (unit >= a.units) return;

@@ -109,6 +109,22 @@ __device__ __forceinline__ int slice_at(int c, int D, int per) {
   return at + per <= D ? at : D - per;
 }
 
+// Asks for every line of the kernel's arguments at once.  They lie in host memory, and the compiler loads them where they
+// are used: one line after another, each a trip of its own for the first workgroups of a compute unit.
+template <typename T>
+__device__ __forceinline__ void fetch_arguments() {
+  typedef const __attribute__((address_space(4))) uint32_t* args_t;
+  const args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+  constexpr int LINES = (int)(sizeof(T) + 63) / 64;
+  uint32_t x[LINES];
+#pragma unroll
+  for (int i = 0; i < LINES; ++i) x[i] = p[16 * i];
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < LINES; ++i) any |= x[i];
+  asm volatile("" ::"s"(any));
+}
+
 // The workgroup's unit, row tile and piece.  Tiles of one unit and piece read the same cache rows: they are dealt to
 // workgroups whose numbers differ by multiples of eight, which share an L2.
 struct WorkItem {
@@ -190,6 +206,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) 
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
+  fetch_arguments<AttendArgs>();
   const WorkItem w = work_item(a);
   if (!w.any) return;
   const uint32_t stream = PICK ? a.by_n.of((uint32_t)w.unit) : (uint32_t)w.unit, bu = a.by_h.of(stream);

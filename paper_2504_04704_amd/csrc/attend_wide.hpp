@@ -82,6 +82,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int late = wave >> 2;  // (of the half of eight wavefronts that is a phase behind)
 
+  fetch_arguments<AttendArgs>();
   const WorkItem w = work_item(a);
   if (!w.any) return;
   const uint32_t bu = a.by_h.of((uint32_t)w.unit);
