@@ -68,26 +68,60 @@ int check_attend(const lagkv_attend_params* p, bool pick) {
   return LAGKV_OK;
 }
 
-// Query rows of a tile: as many as there are, up to what the registers hold.  Pieces of the cache: enough workgroups
-// for every compute unit to hold some, and no piece below four steps a wavefront.
+// Tiles of many rows: 128 query rows (four wavefronts, two workgroups a compute unit) or 256 (eight, one), and the pieces that
+// the cache is cut into, by the microseconds that they take: a step of 64 cache rows, the beginning and end of a workgroup,
+// and, with pieces, a second kernel and every piece of a row written and read.  A step takes longer the more compute
+// units are at work, and less where wavefronts of the eight have no rows.  Measured, 128 channels, model beside it (us):
+//    8 streams,  256 query rows, 1000 rows   128 in 1 32 (32)   128 in 6 17 (17)   256 in 1 37 (37)   256 in 6 22 (22)
+//   32 streams,  256 query rows, 8000 rows   128 in 4 65 (65)   128 in 8 53 (53)   256 in 4 64 (69)   256 in 8 51 (51)
+//    8 streams, 2048 query rows, 8000 rows   128 in 2 121 (119)   128 in 4 91 (92)   256 in 2 119 (122)   256 in 4 87 (82)
+//   64 streams,  160 query rows, 8000 rows   128 in 4 79 (85)   256 in 4 63 (65)
+void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_tile, int64_t* pieces) {
+  const double by_d4 = D <= 64 ? 0.62 : D <= 128 ? 1 : 1.7, by_d8 = D <= 64 ? 0.7 : 1;
+  double least = 1e30;
+  for (int tile = 128; tile <= (D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
+    const int64_t groups = units * ((rows + tile - 1) / tile), places = tile == 256 || D > 128 ? 256 : 512;
+    const double full = (double)(units * rows) / (double)(groups * tile);
+    for (int64_t s = 1; s <= 256 && s <= steps; s += s < 4 ? 1 : s % 3 == 0 ? s / 3 : s / 2) {  // 1 2 3 4 6 8 12 16 24 ...
+      const int64_t all = groups * s;
+      const double busy = all < 256 ? (double)all / 256 : 1;
+      const double step = tile == 256 ? by_d8 * (0.85 + (0.5 + 0.35 * busy) * full) : by_d4 * (all > 256 && D <= 128 ? 2.15 : 1.35 + 0.2 * busy);
+      const double ends = tile == 256 ? (D <= 64 ? 10 : 14) : D <= 64 ? 6.7 : 8.8;
+      const double us = (double)((all + places - 1) / places) * ((double)((steps + s - 1) / s) * step + ends) +
+                        (s > 1 ? 2.5 + (double)(units * rows * s) * (double)D * 8 / 9e6 : 0);
+      if (us < least) {
+        least = us;
+        *row_tile = tile;
+        *pieces = s;
+      }
+    }
+  }
+}
+
+// Query rows of a tile: as many as there are, up to what the registers hold.  Pieces of the cache: for tiles of few rows as many
+// as make a round of workgroups, two a compute unit, and none below a step a wavefront.
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
   pl->wide = !pick && p->dtype != LAGKV_F32 && pl->rows > 32;
-  pl->row_tile = pl->wide ? (pl->rows <= 128 || p->D > 128 ? 128 : 256) : pl->rows <= 16 || p->D > 128 ? 16 : 32;
-  pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
   const int64_t kt = pl->wide ? 64 : p->dtype == LAGKV_F32 ? 16 : 32;
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
   const int64_t steps = (seen + kt - 1) / kt + (p->N + kt - 1) / kt;
+  int64_t splits = 1;
+  if (pl->wide) wide_shape(pl->units, pl->rows, p->D, steps, &pl->row_tile, &splits);
+  else pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
+  pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
   const int64_t groups = pl->units * pl->row_tiles;
-  int64_t splits = (pl->wide ? (pl->row_tile == 128 ? 512 : 256) : 512) / (groups > 0 ? groups : 1);
-  if (splits > steps / (pl->wide ? 2 : 4)) splits = steps / (pl->wide ? 2 : 4);
-  if (splits > 256) splits = 256;
+  if (!pl->wide) {
+    splits = 512 / (groups > 0 ? groups : 1);
+    if (splits > steps / 4) splits = steps / 4;
+    if (splits > 256) splits = 256;
+  }
   // Short caches whole, by twice the wavefronts in one kernel: up to two steps a wavefront.  (One token over 300 rows of 128
   // 16-bit channels 7.1 us, in pieces about 8; over 640 rows, three steps, 9.5 us, over 1000 12.9 us and in pieces 8.4 us.
   // Rows of 64 fp32 channels: 300 rows 7.6 us, 640 rows 11.2 us and in pieces 7.6 us.)
   pl->waves = 4;
-  if (pl->wide ? steps <= 6 : steps <= 16 && groups <= 256 && pl->row_tile == 16 && p->D <= 128) {
+  if (!pl->wide && steps <= 16 && groups <= 256 && pl->row_tile == 16 && p->D <= 128) {
     splits = 1;
     pl->waves = 8;
   }

@@ -132,6 +132,8 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     const bool fresh = step >= cache_steps;
     return Tile{(int64_t)(fresh ? step - cache_steps : step) * KT, fresh ? seen_new : (int)len, fresh};
   };
+  // (rows of new tokens that every query row of the tile sees, in a chunk of a prompt, need no masks either)
+  auto seen_by_all = [&](const Tile& x) { return x.fresh && !a.parents && x.first + KT <= token0 + 1; };
   const int n_whole = min(n, (int)(len / KT) - step0);  // steps of rows of the cache that are all there
   const char* kp = kb + loff + ((int64_t)step0 * KT + lrow) * a.kst;
   const char* vp = vb + loff + ((int64_t)step0 * KT + lrow) * a.kst;
@@ -171,9 +173,11 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   auto store_v = [&](int i) {
     if (i >= n_whole && i < n) {
       const Tile x = tile_of(i);
+      const bool all = seen_by_all(x);
       bool odd = false;
 #pragma unroll
       for (int k = 0; k < PASSES; ++k) {
+        if (all) break;
         if (x.first + lrow + k * LROWS >= x.limit) vr[k] = u32v4{0, 0, 0, 0};
         if (x.fresh) {
           // what is no finite number is put in as 0 (0 * inf is not) and added to the rows that see it afterwards
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   // infinities of the rows of step i
   auto strays = [&](int i) {
     const Tile x = tile_of(i);
-    if (x.fresh && sh_odd[i & 1]) {
+    if (x.fresh && sh_odd[i & 1] && !seen_by_all(x)) {
       for (int t = 0; t < KT && x.first + t < x.limit; ++t) {
         if (!(sees(x, t >> 5) >> (t & 31) & 1)) continue;
         const char* row = vnb + (x.first + t) * a.nst + half * 8;
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     }
   };
   auto weights = [&](int i) {
-    if (i >= n_whole) {
+    if (i >= n_whole && !seen_by_all(tile_of(i))) {
       const Tile x = tile_of(i);
 #pragma unroll
       for (int t = 0; t < HALVES; ++t) {
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
         multiply(i);
         if (i > n_whole) strays(i - 1);
       }
-      __syncthreads();
+      if (WAVES == 8) __syncthreads();  // (four wavefronts write buffers that nobody reads in this step)
       if (i < n) {
         if (!idle) weights(i);
         store(kr, k_at(i + late + 1), LDK);  // (behind the last step: what was there)
