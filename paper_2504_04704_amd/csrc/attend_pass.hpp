@@ -194,8 +194,13 @@ struct AttendShape {
   static constexpr int MAIN = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
 };
 
+// Two wavefronts a SIMD where 256 registers do for each (the compiler then keeps all in vector registers; with 512 it
+// moves the outputs in and out of the accumulators' in every step).
+template <int DT, int DP, int RT>
+constexpr int kAttendWaves = DP > 128 || (DT == LAGKV_F32 && DP == 128 && RT == 2) ? 1 : 2;
+
 template <int DT, int DP, int RT, int WAVES, bool PICK>
-__global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend_kernel(const AttendArgs a) {
   using E = AElem<DT>;
   using Sh = AttendShape<DT, DP, RT, WAVES>;
   constexpr int PER = Sh::PER, NC = Sh::NC, CPR = Sh::CPR, SUBS = E::SUBS, KT = Sh::KT, ROWS = Sh::ROWS, THREADS = WAVES * 64;
