@@ -336,7 +336,8 @@ size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p);
  *     value says that n is no token (padding): it sees nothing, nothing sees it, and a path up the tree ends before it.
  *   out  dtype of Q; a row that sees nothing is 0.  May be Q itself (with Q's strides), and overlap no other input.
  *   lse  [B, H*G, N] device fp32, dense, or NULL: log sum exp of the logits, natural; -inf where nothing is seen
- * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold.
+ * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold;
+ * one that it sees does: an output with a logit that is no number is none.
  * Logits, sums and products are held in fp32; results do not depend on anything but the arguments (no atomics).
  * N = 0: LAGKV_OK, nothing is done.  T = 0 is allowed (K, V may be NULL then).
  */
@@ -357,7 +358,7 @@ int lagkv_attend_blocks(const lagkv_attend_params* p, const void* Q, const void*
  * Smallest and largest key of every block of rows, channel by channel (Eq. 7-8 for each block): lo, hi [B, H,
  * ceil(T / block), D] device, type of K, both with out_stride_*.  Of p the fields B, H, D, dtype, T, block, kv_stride_* and
  * out_stride_* (b, h, block) are read.  Only blocks from that of row `start` on are written (an update behind appended or
- * compressed rows; 0: all).  A block with no row before lengths[b] gets +inf and -inf.
+ * compressed rows; 0: all).  A block with no row before lengths[b] gets +inf and -inf.  Keys that are no number are passed over.
  */
 int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_t* lengths, int64_t start, void* lo, void* hi,
                        void* hip_stream);

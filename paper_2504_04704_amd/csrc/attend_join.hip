@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
     const f32x4 x = *(const f32x4*)(a.part_o + at * a.part_ld + (have ? quad * 4 : 0));
     const float mx = a.part_ml[at * 2], lx = a.part_ml[at * 2 + 1];
     // (a piece that saw nothing has zeros)
-    const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
+    const float f = lx == 0.f ? 0.f : __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
     sum += f * lx;
     v += f * x;
   }

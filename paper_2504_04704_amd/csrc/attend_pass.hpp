@@ -570,7 +570,7 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
-    const bool none = m[rt] == -INFINITY;
+    const bool none = sh_ml[wave][rt * 16 + col][1] == 0.f;  // (what is no number has a maximum of -inf too, and is not dropped)
     const float f = none ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
 #pragma unroll
     for (int d = 0; d < DT16; ++d)
@@ -591,8 +591,8 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) {
-      const float mx = sh_ml[x][rl][0];
-      if (mx != -INFINITY) sum += sh_ml[x][rl][1] * __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
+      const float lx = sh_ml[x][rl][1];
+      if (lx != 0.f) sum += lx * __builtin_amdgcn_exp2f((sh_ml[x][rl][0] - top) * E::UNIT);
       v += *(const f32x4*)(ol + (x * ROWS + rl) * LDO + quad * 4);
     }
     // the slots' channels: `dup` leading ones of a slice are the slice before's

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   __shared__ int sh_odd[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
-    const int late = wave >> 2;  // (of the half of eight wavefronts that is a phase behind)
+  const int late = wave >> 2;  // (of the half of eight wavefronts that is a phase behind)
 
   fetch_arguments<AttendArgs>();
   const WorkItem w = work_item(a);
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     }
     return;
   }
-  bool blind = m == -INFINITY;
+  bool blind = l == 0.f;
   if (a.parents) {
     const int up = a.parents[b * a.psb + token];
     blind = blind || up < -1 || up >= token;

@@ -143,6 +143,38 @@ def test_values_of_tokens_that_are_not_seen(dtype, bad, chain):
     A.check(lagkv.Attended(keep, None), want)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("N,T", [(1, 32), (1, 0), (1, 3000), (24, 64), (24, 3000)])
+def test_what_is_no_number_and_is_seen(dtype, N, T):
+    """A query row, or the row of a token that sees little else, with NaN: its outputs are NaN, and no others."""
+    q, K, V, Kn, Vn = problem(dtype, 1, 2, 3, N, 128, T, "chain", seed=31)
+    want = A.attend(q, K, V, Kn, Vn)
+
+    def nan_in(got, bad):
+        assert bool(torch.isnan(got.out[0, bad]).all()) and bool(torch.isnan(got.lse[0, bad]).all())
+        got.out[0, bad], got.lse[0, bad] = want[0][0, bad].to(dtype).to(DEV), want[1][0, bad].float().to(DEV)
+        A.check(got, want)
+
+    q2 = q.clone()
+    q2[0, 4, N - 1, 5] = math.nan
+    got = lagkv.attend(q2, K, V, Kn, Vn, want_lse=True)
+    bad = torch.zeros(6, N, dtype=torch.bool)
+    bad[4, N - 1] = True
+    nan_in(got, bad)
+    Kn[0, 1, N - 1, 9] = math.nan
+    got = lagkv.attend(q, K, V, Kn, Vn, want_lse=True)
+    bad[3:, N - 1] = True
+    nan_in(got, bad)
+    if T > 32:
+        K[0, 0, :, 3] = math.nan
+        got = lagkv.attend(q, K, V, Kn, Vn, want_lse=True)
+        assert bool(torch.isnan(got.out[0, :3]).all()) and bool(torch.isnan(got.lse[0, :3]).all())
+        lo, hi = lagkv.block_bounds(K, 16)
+        blocks = lagkv.select_blocks(q, lo, hi, T, 16, 4, 1, 1)
+        got = lagkv.attend_blocks(q, K, V, blocks, 16, want_lse=True)
+        assert bool(torch.isnan(got.out[0, :3]).all()) and bool(torch.isfinite(got.out[0, 3:]).all())
+
+
 def test_padded_trees():
     """Trees of several sizes in one batch: what is no token sees nothing and is not seen, nor is what lies before it on a
     path, and its rows may hold anything."""
