@@ -2,7 +2,7 @@
 
 Argument marshalling only: every step of the pass runs in the HIP kernels.
 Functions carry the C names (`plan`, `workspace_bytes`, `score`, `select`,
-`compress`, `append_and_compress`, `launch_hint`, ...).  torch is used for device memory
+`compress`, `append_and_compress`, `attend`, `select_blocks`, `launch_hint`, ...).  torch is used for device memory
 and the current HIP stream; there is no CPU fallback: if the library is
 missing or a call fails, an exception is raised.
 """
@@ -623,7 +623,7 @@ class Cache:
         self.c = CacheT(self.K.data_ptr(), self.V.data_ptr(), _ptr(self.pos), capacity, 0, 0, 0)
         self._ws = None
         self._prepared = {}
-        self._bounds = {}  # rows of a block -> [lo, hi, first row that they are behind of]
+        self._bounds = {}  # rows of a block -> [lo, hi, first row that they are behind of, stream of the last call (raw), itself]
 
     @classmethod
     def from_compressed(cls, comp: Compressed, T: int, capacity: int, S: int, L: int, r: float,
@@ -768,15 +768,26 @@ class Cache:
             kept[2] = min(kept[2], max(int(row), 0))
 
     def block_bounds(self, block: int) -> Tuple[torch.Tensor, torch.Tensor]:
-        """block_bounds() of the rows held, kept from call to call: only blocks whose rows have changed are gone over."""
+        """block_bounds() of the rows held, kept from call to call: only blocks whose rows have changed are gone over.  A
+        call on another stream than the last one's waits for that stream.  In a captured graph all are gone over, into
+        tensors of the graph: what a replay finds in the kept ones would be those of another step."""
         n, block = self.length, index(block)
         kept = self._bounds.get(block)
         if kept is None:
             if block < 1:
                 raise LagKVError(EINVAL, "lagkv_block_bounds")
+        if self.K.is_cuda and torch.cuda.is_current_stream_capturing():
+            return block_bounds(self.K[:, :, :n], block)
+        device = self.K.device
+        stream = _stream_ptr(device)
+        if kept is None:
             B, H, capacity, D = self.K.shape
-            lo, hi = (torch.empty((B, H, -(-capacity // block), D), dtype=self.K.dtype, device=self.K.device) for _ in range(2))
-            kept = [lo, hi, 0]
+            lo, hi = (torch.empty((B, H, -(-capacity // block), D), dtype=self.K.dtype, device=device) for _ in range(2))
+            kept = [lo, hi, 0, stream, torch.cuda.current_stream(device)]
+        elif kept[3] != stream:
+            now = torch.cuda.current_stream(device)
+            now.wait_stream(kept[4])
+            kept[3:] = stream, now
         nb = -(-n // block)
         lo, hi = kept[0][:, :, :nb], kept[1][:, :, :nb]
         if kept[2] < n:

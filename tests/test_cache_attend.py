@@ -58,6 +58,59 @@ def test_steps_of_a_model(dtype, D):
 
 
 @pytest.mark.gpu
+def test_bounds_on_two_streams():
+    """The stream of a call that finds the bounds kept does not run ahead of the one that they are made on."""
+    cache = lagkv.Cache(2, 2, 128, 4096, 4, 128, 0.25)
+    x = rand(2, 2, 4000, 128, dtype=torch.bfloat16, seed=8)
+    cache.K[:, :, :4000].copy_(x)
+    cache.c.n_static, cache.c.n_seen = 4000, 4000
+    q = rand(2, 4, 1, 128, dtype=torch.bfloat16, seed=9)
+    want = lagkv.select_blocks(q, *lagkv.block_bounds(x, 16), 4000, 16, 20)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    busy = torch.zeros(4096, 4096, device=DEV)
+    torch.mm(busy, busy)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(a):
+        for _ in range(20):
+            busy = torch.mm(busy, busy)
+        first = cache.select_blocks(q, 16, 20)
+    with torch.cuda.stream(b):
+        second = cache.select_blocks(q, 16, 20)
+    torch.cuda.synchronize()
+    assert torch.equal(first, want) and torch.equal(second, want)
+
+
+@pytest.mark.gpu
+def test_bounds_in_a_captured_step():
+    """A captured step works the bounds out in every replay, and leaves those of the steps outside it alone."""
+    cache = lagkv.Cache(1, 2, 64, 700, 4, 32, 0.5)
+    x = rand(1, 2, 600, 64, dtype=torch.bfloat16, seed=8)
+    cache.K.zero_()
+    cache.V.zero_()
+    cache.c.n_static, cache.c.n_seen = 600, 600
+    q = rand(1, 4, 1, 64, dtype=torch.bfloat16, seed=9)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        lagkv.select_blocks(q, *lagkv.block_bounds(x, 16), 600, 16, 5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        picked = cache.select_blocks(q, 16, 5)
+    for turn in range(3):
+        rows = x * (turn - 1.5)
+        cache.K[:, :, :600].copy_(rows)
+        cache.changed_from(0)
+        want = lagkv.select_blocks(q, *lagkv.block_bounds(rows, 16), 600, 16, 5)
+        assert torch.equal(cache.select_blocks(q, 16, 5), want)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(picked, want), turn
+        lo, hi = cache.block_bounds(16)
+        wl, wh = A.bounds(rows, 16)
+        assert torch.equal(lo.cpu(), wl) and torch.equal(hi.cpu(), wh)
+
+
+@pytest.mark.gpu
 def test_a_refused_append_leaves_the_bounds_right():
     cache = lagkv.Cache(1, 1, 64, 40, 2, 16, 0.5)
     x = rand(1, 1, 30, 64, dtype=torch.bfloat16, seed=5)
