@@ -68,6 +68,12 @@ int check_attend(const lagkv_attend_params* p, bool pick) {
   return LAGKV_OK;
 }
 
+// Workgroups of the fullest of the eight XCDs (work_item deals units and pieces to them in turn, with all their tiles).
+int64_t fullest_xcd(int64_t units, int64_t pieces, int64_t row_tiles) { return (units * pieces + 7) / 8 * row_tiles; }
+
+// 1 2 3 4 6 8 12 16 24 ...
+int64_t next_pieces(int64_t s) { return s + (s < 4 ? 1 : s % 3 == 0 ? s / 3 : s / 2); }
+
 // Tiles of many rows: 128 query rows (four wavefronts, two workgroups a compute unit) or 256 (eight, one), and the pieces that
 // the cache is cut into, by the microseconds that they take: a step of 64 cache rows, the beginning and end of a workgroup,
 // and, with pieces, a second kernel and every piece of a row written and read.  A step takes longer the more compute
@@ -82,8 +88,8 @@ void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_
   for (int tile = 128; tile <= (D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
     const int64_t groups = units * ((rows + tile - 1) / tile), places = tile == 256 || D > 128 ? 256 : 512;
     const double full = (double)(units * rows) / (double)(groups * tile);
-    for (int64_t s = 1; s <= 256 && s <= steps; s += s < 4 ? 1 : s % 3 == 0 ? s / 3 : s / 2) {  // 1 2 3 4 6 8 12 16 24 ...
-      const int64_t all = groups * s;
+    for (int64_t s = 1; s <= 256 && s <= steps; s = next_pieces(s)) {
+      const int64_t all = 8 * fullest_xcd(units, s, (rows + tile - 1) / tile);
       const double busy = all < 256 ? (double)all / 256 : 1;
       const double step = tile == 256 ? by_d8 * (0.85 + (0.5 + 0.35 * busy) * full) : by_d4 * (all > 256 && D <= 128 ? 2.15 : 1.35 + 0.2 * busy);
       const double ends = tile == 256 ? (D <= 64 ? 10 : 14) : D <= 64 ? 6.7 : 8.8;
@@ -98,11 +104,40 @@ void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_
   }
 }
 
-// Query rows of a tile: as many as there are, up to what the registers hold.  Pieces of the cache: for tiles of few rows as many
-// as make a round of workgroups, two a compute unit, and none below a step a wavefront.
+// Tiles of 16 or 32 query rows: the pieces of the cache by the microseconds that they take, none below a step a wavefront.
+// A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them,
+// and one where the outputs fill its registers.  All rows together pass memory at 6 TB/s, less where some compute
+// units have a workgroup more than others.  With pieces, a second kernel and every piece of a row written and read.
+// Over 205 shapes (16-bit and fp32, 64 to 256 channels, 4 to 600 query rows, 1 to 1000 workgroups, 200 to 50000 rows) the
+// time is 1.1 % above that of the best number of pieces in the mean and 26 % in the worst; with as many pieces as make
+// 512 workgroups, 11.9 % and 73 %.  Where lengths differ within a batch (a quarter of T to T; 54 shapes) 3.9 % and 23 %, and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4 115; 192 streams in 1 70, in 2 79;
+// fp32, 64 streams x 64 rows x 8000 in 4 108, in 8 121.)
+int64_t narrow_pieces(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps) {
+  const bool heavy = f32 && row_tile == 32;  // (bound by the products)
+  const int64_t tiles = (rows + row_tile - 1) / row_tile, places = heavy || D > 128 ? 32 : 64;  // of an XCD
+  const double step = (heavy ? 0.75 : 0.45) * (D <= 64 ? 0.5 : D <= 128 ? 1 : 2), ends = 5.5;
+  const double memory = (double)units * (double)steps * (double)D * 128 / 6e6;
+  int64_t best = 1;
+  double least = 1e30;
+  for (int64_t s = 1; s <= 256 && (s == 1 || s <= steps / 4); s = next_pieces(s)) {
+    const int64_t load = fullest_xcd(units, s, tiles);
+    const double uneven = load > 32 ? (double)((load + 31) / 32 * 32) / (double)load - 1 : 0;
+    const double go = (double)((load + places - 1) / places) * ((double)((steps + s - 1) / s) * step + ends);
+    const double pass = memory * (1 + 0.35 * uneven) + ends;
+    const double us = (go > pass ? go : pass) + (s > 1 ? 3.5 + (double)(units * rows * s) * (double)D * 8 / 3e6 : 0);
+    if (us < least) {
+      least = us;
+      best = s;
+    }
+  }
+  return best;
+}
+
+// Query rows of a tile: as many as there are, up to what the registers hold.
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
+  if (pl->units > kMost) return false;  // (more than a grid takes, and products of what follows stay in 64 bits)
   pl->wide = !pick && p->dtype != LAGKV_F32 && pl->rows > 32;
   const int64_t kt = pl->wide ? 64 : p->dtype == LAGKV_F32 ? 16 : 32;
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
@@ -112,11 +147,7 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   else pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
   pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
   const int64_t groups = pl->units * pl->row_tiles;
-  if (!pl->wide) {
-    splits = 512 / (groups > 0 ? groups : 1);
-    if (splits > steps / 4) splits = steps / 4;
-    if (splits > 256) splits = 256;
-  }
+  if (!pl->wide) splits = narrow_pieces(pl->units, pl->rows, pl->row_tile, p->D, p->dtype == LAGKV_F32, steps);
   // Short caches whole, by twice the wavefronts in one kernel: up to two steps a wavefront.  (One token over 300 rows of 128
   // 16-bit channels 7.1 us, in pieces about 8; over 640 rows, three steps, 9.5 us, over 1000 12.9 us and in pieces 8.4 us.
   // Rows of 64 fp32 channels: 300 rows 7.6 us, 640 rows 11.2 us and in pieces 7.6 us.)
@@ -125,7 +156,6 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
     splits = 1;
     pl->waves = 8;
   }
-  if (splits < 1) splits = 1;
   pl->splits = (int)splits;
   const int64_t parts = pl->units * splits * pl->rows, ld = (p->D + 3) & ~3;
   pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
