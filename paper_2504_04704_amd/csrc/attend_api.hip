@@ -110,7 +110,7 @@ void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_
 // units have a workgroup more than others.  With pieces, a second kernel and every piece of a row written and read.
 // Over 205 shapes (16-bit and fp32, 64 to 256 channels, 4 to 600 query rows, 1 to 1000 workgroups, 200 to 50000 rows) the
 // time is 1.1 % above that of the best number of pieces in the mean and 26 % in the worst; with as many pieces as make
-// 512 workgroups, 11.9 % and 73 %.  Where lengths differ within a batch (a quarter of T to T; 54 shapes) 3.9 % and 23 %, and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4 115; 192 streams in 1 70, in 2 79;
+// 512 workgroups, 11.9 % and 73 %.  Where lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 23 %, and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4 115; 192 streams in 1 70, in 2 79;
 // fp32, 64 streams x 64 rows x 8000 in 4 108, in 8 121.)
 int64_t narrow_pieces(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps) {
   const bool heavy = f32 && row_tile == 32;  // (bound by the products)
@@ -341,7 +341,9 @@ int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void*
   a.last = n_last;
   a.dtype = p->dtype;
   const int64_t units = (int64_t)p->B * p->H * p->N;
-  if (!grid_fits(units, 256) || !grid_fits((int64_t)p->B * p->H * (a.nb + 1), 256)) return LAGKV_ESHAPE;
+  if (!grid_fits(units, 512) || !grid_fits((int64_t)p->B * p->H * (a.nb + 1), 256) ||
+      !grid_fits(((int64_t)p->B * p->H * ((a.nb + 63) / 64) + 7) * (((int64_t)p->N + 15) / 16), 256))
+    return LAGKV_ESHAPE;
   if (a.nb > 0 && (!ws || ws_bytes < 8 * (size_t)(units * a.nb) || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
   hipStream_t s = (hipStream_t)hip_stream;
   hipError_t e = a.nb > 0 ? launch_block_scores(a, s) : hipSuccess;

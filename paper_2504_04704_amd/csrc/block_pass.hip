@@ -118,41 +118,73 @@ __device__ __forceinline__ double lanes_sum(double x, int lpr) {
   return x;
 }
 
-// P and M (above) of U slots of tokens: entry i of the workgroup's list of slots, 256 apart.  A slot is a channel of a slice;
-// those that repeat channels of the slice before, those behind the last, and tokens behind the last are 0.
-template <int DT, int U, typename Put>
-__device__ __forceinline__ void query_parts(const SelectArgs& a, int64_t b, int64_t h, int n0, int width, int from, int count, Put put) {
+// P and M (above) of `count` slots of tokens 0, 1, ...  A slot is a channel of a slice; those that repeat channels of the slice
+// before, and those behind the last, are 0.
+template <int DT, typename Put>
+__device__ __forceinline__ void query_parts(const SelectArgs& a, int64_t b, int64_t h, int width, int from, int count, Put put) {
   constexpr int SIZE = AElem<DT>::SIZE, VEC = 16 / SIZE;
   const char* base = a.Q + b * a.qsb + h * a.G * a.qsh;
-  for (int i0 = from; i0 < count; i0 += 256 * U) {
-    int64_t at[U];
-    bool real[U];
-    double p[U], m[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + 256 * u, n = n0 + i / width, slot = i % width, begin = slot / VEC * VEC;
-      const int ch = begin < a.D ? slice_at(slot / VEC, a.D, VEC) + slot - begin : 0;
-      real[u] = i < count && n < a.N && begin < a.D && ch >= begin;
-      at[u] = real[u] ? (int64_t)n * a.qsn + (int64_t)ch * SIZE : 0;
-      p[u] = m[u] = 0;
-    }
+  for (int i = from; i < count; i += 256) {
+    const int slot = i % width, begin = slot / VEC * VEC;
+    const int ch = begin < a.D ? slice_at(slot / VEC, a.D, VEC) + slot - begin : 0;
+    const bool real = begin < a.D && ch >= begin;
+    const char* at = base + (int64_t)(i / width) * a.qsn + (real ? ch * SIZE : 0);
+    double p = 0, m = 0;
 #pragma unroll 4
     for (int g = 0; g < a.G; ++g) {
+      const char* q = at + g * a.qsh;
+      float x;
+      if constexpr (DT == LAGKV_F32) x = *(const float*)q;
+      else x = AElem<DT>::one(*(const uint16_t*)q);
+      p += x > 0.f ? (double)x : 0.0;
+      m += x > 0.f ? 0.0 : (double)x;
+    }
+    put(i / width, slot, real ? p : 0.0, real ? m : 0.0);
+  }
+}
+// The same of sixteen tokens from n0 on, by slices: a thread asks for what four query heads have of its slices in one go.
+// (Channel by channel the loads, four or eight times as many, were a third of the kernel.)  Tokens behind the last are 0.
+template <int DT, int DP, typename Put>
+__device__ __forceinline__ void query_slices(const SelectArgs& a, int64_t b, int64_t h, int n0, int tid, Put put) {
+  using ET = typename Of<DT>::T;
+  constexpr int VEC = ET::VEC, SIZE = 16 / VEC, CPR = DP / VEC, U = 16 * CPR > 256 ? 16 * CPR / 256 : 1;
+  if (tid >= 16 * CPR) return;
+  const char* at[U];
+  double p[U][VEC], m[U][VEC];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = tid + 256 * u, n = i / CPR, slice = i % CPR;
+    at[u] = a.Q + b * a.qsb + h * a.G * a.qsh + (int64_t)(n0 + n < a.N ? n0 + n : 0) * a.qsn + (slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0) * SIZE;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) p[u][e] = m[u][e] = 0;
+  }
+  for (int g0 = 0; g0 < a.G; g0 += 4) {
+    uint4 v[4][U];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[g][u] = ld16_any(at[u] + (g0 + g < a.G ? g0 + g : g0) * a.qsh);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g0 + g >= a.G) break;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const char* q = base + g * a.qsh + at[u];
-        float x;
-        if constexpr (DT == LAGKV_F32) x = *(const float*)q;
-        else x = AElem<DT>::one(*(const uint16_t*)q);
-        p[u] += x > 0.f ? (double)x : 0.0;
-        m[u] += x > 0.f ? 0.0 : (double)x;
+        float x[VEC];
+        unpack<ET>(v[g][u], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          p[u][e] += x[e] > 0.f ? (double)x[e] : 0.0;
+          m[u][e] += x[e] > 0.f ? 0.0 : (double)x[e];
+        }
       }
     }
+  }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + 256 * u;
-      if (i < count) put(i / width, i % width, real[u] ? p[u] : 0.0, real[u] ? m[u] : 0.0);
-    }
+  for (int u = 0; u < U; ++u) {
+    const int i = tid + 256 * u, n = i / CPR, begin = i % CPR * VEC, dup = begin < a.D ? begin - slice_at(i % CPR, a.D, VEC) : 0;
+    const bool real = n0 + n < a.N && begin < a.D;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) put(n, begin + e, real && e >= dup ? p[u][e] : 0.0, real && e >= dup ? m[u][e] : 0.0);
   }
 }
 
@@ -160,6 +192,7 @@ __device__ __forceinline__ void query_parts(const SelectArgs& a, int64_t b, int6
 // and M are made.  Bound by reading the bounds.
 constexpr int kScoreBlocks = 64;  // of a workgroup
 constexpr int kFewTokens = 3;
+constexpr int kManyGroups = 512;  // (two a compute unit)
 template <int DT>
 __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a, int lpr) {
   using ET = typename Of<DT>::T;
@@ -182,7 +215,7 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
       hi4[i] = ld16_any(a.hi + from);
     }
     if (p0 == 0) {
-      query_parts<DT, 1>(a, b, h, 0, lpr * VEC, threadIdx.x, a.N * lpr * VEC, [&](int n, int slot, double p, double m) {
+      query_parts<DT>(a, b, h, lpr * VEC, threadIdx.x, a.N * lpr * VEC, [&](int n, int slot, double p, double m) {
         sh_p[n][slot % VEC * lpr + slot / VEC] = p;
         sh_m[n][slot % VEC * lpr + slot / VEC] = m;
       });
@@ -220,37 +253,47 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
 
 // Scores of more tokens: sixteen blocks times sixteen tokens at a time on the matrix cores (64-bit), whose operand of
 // the blocks is the bounds as they lie in memory (lane l: block l % 16, a slice of its channels), and that of the tokens is
-// P and M, in LDS for the workgroup's 64 blocks.  A product takes what 64-bit vector arithmetic takes, but nothing has to be
-// summed across lanes.
+// P and M, in LDS for the workgroup's sixteen tokens and `sets` of 64 blocks; the next set is on its way while one is
+// multiplied.  Workgroups of other tokens and the same blocks follow on the same XCD, whose L2 has the bounds.  A product
+// takes what 64-bit vector arithmetic takes, but nothing has to be summed across lanes.
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 template <int DT, int DP>
-__global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs a) {
+__global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs a, int sets) {
   using ET = typename Of<DT>::T;
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC, NC = DP / VEC / 4;
   constexpr int LD = DP + 1;  // doubles between tokens: sixteen lanes' reads on different banks
   extern __shared__ __attribute__((aligned(16))) double sh_pm[];  // [16][LD] of P, then of M
-  const uint32_t tiles = (uint32_t)((a.nb + kScoreBlocks - 1) / kScoreBlocks), st = blockIdx.x / tiles;
-  const int64_t stream = st, j0 = (int64_t)(blockIdx.x % tiles) * kScoreBlocks, b = st / (uint32_t)a.H, h = st % (uint32_t)a.H;
+  const uint32_t tiles = (uint32_t)((a.nb + kScoreBlocks * sets - 1) / (kScoreBlocks * sets)), token_groups = (uint32_t)(a.N + 15) / 16;
+  const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, of = rest / token_groups, id = of * 8 + slot, st = id / tiles;
+  if (st >= (uint32_t)a.B * (uint32_t)a.H) return;
+  const int n0 = (int)(rest - of * token_groups) * 16;
+  const int64_t stream = st, b = st / (uint32_t)a.H, h = st % (uint32_t)a.H;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-  const int64_t jw = j0 + wave * 16, j = jw + col, jj = j < a.nb ? j : a.nb - 1;
+  const int64_t j0 = (int64_t)(id - st * tiles) * kScoreBlocks * sets + wave * 16;
+  int here = 0;  // sets that are there
+  while (here < sets && j0 - wave * 16 + here * kScoreBlocks < a.nb) ++here;
   uint4 lo4[NC], hi4[NC];
+  auto load = [&](int set) {
+    const int64_t j = j0 + set * kScoreBlocks + col, jj = j < a.nb ? j : a.nb - 1;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int slice = c * 4 + grp;
-    const int64_t from = b * a.bsb + h * a.bsh + jj * a.bst + (slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0) * SIZE;
-    lo4[c] = ld16_any(a.lo + from);
-    hi4[c] = ld16_any(a.hi + from);
-  }
-  for (int n0 = 0; n0 < a.N; n0 += 16) {
-    __syncthreads();
-    query_parts<DT, 4>(a, b, h, n0, DP, threadIdx.x, 16 * DP, [&](int n, int slot, double p, double m) {
-      sh_pm[n * LD + slot] = p;
-      sh_pm[(16 + n) * LD + slot] = m;
-    });
-    __syncthreads();
+    for (int c = 0; c < NC; ++c) {
+      const int slice = c * 4 + grp;
+      const int64_t from = b * a.bsb + h * a.bsh + jj * a.bst + (slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0) * SIZE;
+      lo4[c] = ld16_any(a.lo + from);
+      hi4[c] = ld16_any(a.hi + from);
+    }
+  };
+  load(0);
+  query_slices<DT, DP>(a, b, h, n0, threadIdx.x, [&](int n, int slot, double p, double m) {
+    sh_pm[n * LD + slot] = p;
+    sh_pm[(16 + n) * LD + slot] = m;
+  });
+  __syncthreads();
+  for (int set = 0; set < here; ++set) {
     f64x4 s = {0, 0, 0, 0};
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+      __builtin_amdgcn_sched_barrier(0);  // (not all bounds as 64-bit numbers at once: half the wavefronts a SIMD)
       float lo[VEC], hi[VEC];
       unpack<ET>(lo4[c], lo);
       unpack<ET>(hi4[c], hi);
@@ -262,11 +305,12 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
         s = __builtin_amdgcn_mfma_f64_16x16x4f64(have ? (double)lo[i] : 0.0, sh_pm[(16 + col) * LD + slot], s, 0, 0, 0);
       }
     }
+    if (set + 1 < here) load(set + 1);
     // s[i]: block grp + 4 i of the sixteen, token col
     const int n = n0 + col;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t to = jw + grp + 4 * i;
+      const int64_t to = j0 + set * kScoreBlocks + grp + 4 * i;
       if (n < a.N && to < a.nb) a.score[(stream * a.N + n) * a.nb + to] = s[i];
     }
   }
@@ -488,16 +532,22 @@ hipError_t launch_block_bounds(const BoundsArgs& a, hipStream_t s) {
 namespace {
 template <int DT>
 hipError_t launch_scores(const SelectArgs& a, hipStream_t s) {
-  const dim3 grid((uint32_t)((int64_t)a.B * a.H * ((a.nb + kScoreBlocks - 1) / kScoreBlocks))), group(256);
+  const int64_t streams = (int64_t)a.B * a.H, token_groups = (a.N + 15) / 16;
+  auto tiles = [&](int sets) { return streams * ((a.nb + kScoreBlocks * sets - 1) / (kScoreBlocks * sets)); };
+  // (several sets of blocks a workgroup where there are workgroups enough, as each makes P and M for itself: 16 tokens of 32
+  // streams over 2048 blocks 31 us with two sets and 39 with one, over 512 blocks of 64 tokens 36 with one and 37 with two)
+  int sets = 1;
+  while (sets < 8 && tiles(2 * sets) * token_groups >= kManyGroups) sets *= 2;
+  const dim3 grid((uint32_t)(a.N <= kFewTokens ? tiles(1) : (tiles(sets) + 7) / 8 * 8 * token_groups)), group(256);
   auto lds = [](int dp) { return (size_t)32 * (dp + 1) * 8; };
   if (a.N <= kFewTokens) block_scores_kernel<DT><<<grid, group, 0, s>>>(a, lanes_a_row(a.D, DT));
-  else if (a.D <= 64) block_scores_many_kernel<DT, 64><<<grid, group, lds(64), s>>>(a);
-  else if (a.D <= 128) block_scores_many_kernel<DT, 128><<<grid, group, lds(128), s>>>(a);
+  else if (a.D <= 64) block_scores_many_kernel<DT, 64><<<grid, group, lds(64), s>>>(a, sets);
+  else if (a.D <= 128) block_scores_many_kernel<DT, 128><<<grid, group, lds(128), s>>>(a, sets);
   else {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(block_scores_many_kernel<DT, 256>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds(256));
     if (e != hipSuccess) return e;
-    block_scores_many_kernel<DT, 256><<<grid, group, lds(256), s>>>(a);
+    block_scores_many_kernel<DT, 256><<<grid, group, lds(256), s>>>(a, sets);
   }
   return hipGetLastError();
 }
