@@ -197,7 +197,10 @@ struct AttendShape {
 // Two wavefronts a SIMD where 256 registers do for each (the compiler then keeps all in vector registers; with 512 it
 // moves the outputs in and out of the accumulators' in every step).
 template <int DT, int DP, int RT>
-constexpr int kAttendWaves = DP > 128 || (DT == LAGKV_F32 && DP == 128 && RT == 2) ? 1 : 2;
+constexpr int kAttendWaves = DP > 128 ? 1 : 2;
+// 32 fp32 rows of 128 channels: q in LDS, one copy for the workgroup, where V's rows leave room beside them, for 256 to do.
+template <int DT, int DP, int RT>
+constexpr bool kQueryInLds = DT == LAGKV_F32 && DP == 128 && RT == 2;
 
 template <int DT, int DP, int RT, int WAVES, bool PICK>
 __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend_kernel(const AttendArgs a) {
@@ -381,6 +384,21 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
       asm volatile("" : "+v"(v));
       q[rt][c] = v;
     }
+  constexpr bool QLDS = kQueryInLds<DT, DP, RT>;
+  char* ql = lds + Sh::V_BYTES + lane * 16;
+  if constexpr (QLDS) {
+    static_assert(Sh::V_BYTES + RT * NC * 1024 <= Sh::MAIN, "");
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c % WAVES == wave) *(u32v4*)(ql + (rt * NC + c) * 1024) = q[rt][c];
+    __syncthreads();
+  }
+  auto query = [&](int rt, int c) {
+    if constexpr (QLDS) return *(const u32v4*)(ql + (rt * NC + c) * 1024);
+    else return q[rt][c];
+  };
 
   for (; step < step1; step += WAVES) {
     const bool more = step + WAVES < step1;
@@ -425,14 +443,16 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
           // four sums of a quarter of the channels each: shorter chains, of steps and of roundings
           f32x4 y[4] = {x, x, x, x};
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+          for (int c = 0; c < NC; ++c) {
+            const u32v4 qv = query(rt, c);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              y[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[s][c][i]), __uint_as_float(q[rt][c][i]), y[i], 0, 0, 0);
+              y[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[s][c][i]), __uint_as_float(qv[i]), y[i], 0, 0, 0);
+          }
           x = (y[0] + y[1]) + (y[2] + y[3]);
         } else {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) x = E::mma(kf[s][c], q[rt][c], x);
+          for (int c = 0; c < NC; ++c) x = E::mma(kf[s][c], query(rt, c), x);
         }
         p[rt][s] = x;
       }

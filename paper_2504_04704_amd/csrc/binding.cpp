@@ -1,7 +1,7 @@
 // The Python calls of a serving loop without ctypes: parameters read from the tensors, outputs allocated and the C
 // function called in one step.  A call costs what its launch costs, and ctypes, the attribute reads and four
 // torch.empty cost more than that: 14.8 us for a compress call whose kernel takes 9 us, 6.2 us for a token in
-// decode whose kernel takes 3 us.
+// decode whose kernel takes 3 us.  An attend call takes the host 5.7 us here with one kernel and 9 with two.
 //
 // It takes the plain forms only (exact tensors of one device, four dimensions, integers and floats as such).  Anything
 // else - and what lagkv_plan refuses or an allocator throws - it leaves alone and says so (None, or -1): lagkv.py

@@ -535,7 +535,7 @@ hipError_t launch_scores(const SelectArgs& a, hipStream_t s) {
   const int64_t streams = (int64_t)a.B * a.H, token_groups = (a.N + 15) / 16;
   auto tiles = [&](int sets) { return streams * ((a.nb + kScoreBlocks * sets - 1) / (kScoreBlocks * sets)); };
   // (several sets of blocks a workgroup where there are workgroups enough, as each makes P and M for itself: 16 tokens of 32
-  // streams over 2048 blocks 31 us with two sets and 39 with one, over 512 blocks of 64 tokens 36 with one and 37 with two)
+  // streams over 2048 blocks 29.9 us with two sets and 31.3 with one, fp32 34 and 38, 64 tokens over 512 blocks 35.3 and 37.3)
   int sets = 1;
   while (sets < 8 && tiles(2 * sets) * token_groups >= kManyGroups) sets *= 2;
   const dim3 grid((uint32_t)(a.N <= kFewTokens ? tiles(1) : (tiles(sets) + 7) / 8 * 8 * token_groups)), group(256);
