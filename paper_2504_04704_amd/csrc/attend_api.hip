@@ -105,24 +105,28 @@ void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_
 }
 
 // Tiles of 16 or 32 query rows: the pieces of the cache by the microseconds that they take, none below a step a wavefront.
-// A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them,
-// and one where the outputs fill its registers.  All rows together pass memory at 6 TB/s, less where some compute
+// A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them, at
+// no cost to each other but memory's where that is the bound (32 fp32 rows: 0.75 us alone, 1.4 us beside another), and one where
+// the outputs fill its registers.  All rows together pass memory at 6 TB/s, less where some compute
 // units have a workgroup more than others.  With pieces, a second kernel and every piece of a row written and read.
 // Over 205 shapes (16-bit and fp32, 64 to 256 channels, 4 to 600 query rows, 1 to 1000 workgroups, 200 to 50000 rows) the
-// time is 1.1 % above that of the best number of pieces in the mean and 26 % in the worst; with as many pieces as make
-// 512 workgroups, 11.9 % and 73 %.  Where lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 23 %, and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4 115; 192 streams in 1 70, in 2 79;
-// fp32, 64 streams x 64 rows x 8000 in 4 108, in 8 121.)
+// time is 1 % above that of the best number of pieces in the mean; with as many pieces as make 512 workgroups, 11.9 %.  Where
+// lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4
+// 115; 192 streams in 1 70, in 2 79.)
 int64_t narrow_pieces(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps) {
   const bool heavy = f32 && row_tile == 32;  // (bound by the products)
-  const int64_t tiles = (rows + row_tile - 1) / row_tile, places = heavy || D > 128 ? 32 : 64;  // of an XCD
-  const double step = (heavy ? 0.75 : 0.45) * (D <= 64 ? 0.5 : D <= 128 ? 1 : 2), ends = 5.5;
+  const int64_t tiles = (rows + row_tile - 1) / row_tile, places = D > 128 ? 32 : 64;  // of an XCD
+  const double channels = D <= 64 ? 0.5 : D <= 128 ? 1 : 2, alone = (heavy ? 0.75 : 0.45) * channels, both = (heavy ? 1.4 : 0.45) * channels;
+  const double ends = 5.5;
   const double memory = (double)units * (double)steps * (double)D * 128 / 6e6;
   int64_t best = 1;
   double least = 1e30;
   for (int64_t s = 1; s <= 256 && (s == 1 || s <= steps / 4); s = next_pieces(s)) {
     const int64_t load = fullest_xcd(units, s, tiles);
     const double uneven = load > 32 ? (double)((load + 31) / 32 * 32) / (double)load - 1 : 0;
-    const double go = (double)((load + places - 1) / places) * ((double)((steps + s - 1) / s) * step + ends);
+    const int64_t full = load / places, rest = load - full * places;
+    const double each = (double)((steps + s - 1) / s);
+    const double go = (double)full * (each * both + ends) + (rest > 32 ? each * both + ends : rest > 0 ? each * alone + ends : 0);
     const double pass = memory * (1 + 0.35 * uneven) + ends;
     const double us = (go > pass ? go : pass) + (s > 1 ? 3.5 + (double)(units * rows * s) * (double)D * 8 / 3e6 : 0);
     if (us < least) {
@@ -137,7 +141,7 @@ int64_t narrow_pieces(int64_t units, int64_t rows, int64_t row_tile, int64_t D, 
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
-  if (pl->units > kMost) return false;  // (more than a grid takes, and products of what follows stay in 64 bits)
+  if (pl->units > kMost || !grid_fits(pl->units * pl->rows, 256)) return false;  // (the second kernel's grid)
   pl->wide = !pick && p->dtype != LAGKV_F32 && pl->rows > 32;
   const int64_t kt = pl->wide ? 64 : p->dtype == LAGKV_F32 ? 16 : 32;
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
@@ -160,8 +164,7 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   const int64_t parts = pl->units * splits * pl->rows, ld = (p->D + 3) & ~3;
   pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
   pl->ws_bytes = splits > 1 ? pl->off_ml + ws_align_up((size_t)parts * 8) : 0;
-  // the grids of the two kernels
-  return grid_fits((pl->units * splits + 7) / 8 * 8 * pl->row_tiles, 512) && grid_fits(pl->units * pl->rows, 256);
+  return grid_fits((pl->units * splits + 7) / 8 * 8 * pl->row_tiles, 512);
 }
 
 int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
