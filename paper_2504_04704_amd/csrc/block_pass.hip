@@ -51,7 +51,9 @@ __device__ __forceinline__ int64_t rows_held(const int32_t* lengths, int64_t b, 
   return n < 0 ? 0 : n > T ? T : n;
 }
 
-// A wavefront takes a block: LPR lanes a row (a power of two), one slice each, 64 / LPR rows at a time.
+// A wavefront takes a block: LPR lanes a row (a power of two), one slice each, 64 / LPR rows at a time.  A value is
+// unpacked, compared twice and never summed, so that this is exact.  Bound by memory: 1.07 GB of keys (32 streams x
+// 131072 rows, bf16) in 201 us, 5.5 TB/s; the last 200 rows of 32 streams in 4 us, the launch.
 template <int DT>
 __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsArgs a, int lpr) {
   using ET = typename Of<DT>::T;
@@ -189,7 +191,9 @@ __device__ __forceinline__ void query_slices(const SelectArgs& a, int64_t b, int
 }
 
 // Scores of one, two or three tokens: a wavefront takes 16 blocks, LPR lanes a block; the bounds are on their way while P
-// and M are made.  Bound by reading the bounds.
+// and M are made.  Bound by reading the bounds (34 MB, 32 streams x 2048 blocks: 9 us traced, 6.6 at a copy's rate) and the
+// latency of q, of the sums and of the launch; 64-bit products of two tokens take as long as that (beyond three tokens the
+// matrix cores are faster or as fast: four 26.8 us and 24.8, fp32 29.9 and 30.8, five 26.8 and 27.8, fp32 29.9 and 34.1).
 constexpr int kScoreBlocks = 64;  // of a workgroup
 constexpr int kFewTokens = 3;
 constexpr int kManyGroups = 512;  // (two a compute unit)
@@ -255,7 +259,9 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
 // the blocks is the bounds as they lie in memory (lane l: block l % 16, a slice of its channels), and that of the tokens is
 // P and M, in LDS for the workgroup's sixteen tokens and `sets` of 64 blocks; the next set is on its way while one is
 // multiplied.  Workgroups of other tokens and the same blocks follow on the same XCD, whose L2 has the bounds.  A product
-// takes what 64-bit vector arithmetic takes, but nothing has to be summed across lanes.
+// takes what 64-bit vector arithmetic takes, but nothing has to be summed across lanes.  Bound by the products: 16 tokens of
+// 32 streams x 2048 blocks 20 us, 9 at the rate of a large 64-bit product (the rest are P and M, 64-bit conversions and
+// the launch).
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 template <int DT, int DP>
 __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs a, int sets) {
@@ -323,6 +329,25 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
+__device__ __forceinline__ double key_score(uint64_t u) { return __builtin_bit_cast(double, u >> 63 ? u ^ 1ull << 63 : ~u); }
+
+// Largest of all lanes.
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_max(uint64_t v) {
+  const uint64_t far = __builtin_bit_cast(uint64_t, dpp_mov_d<CTRL>(__builtin_bit_cast(double, v)));
+  return far > v ? far : v;
+}
+__device__ __forceinline__ uint64_t wave_largest(uint64_t v) {
+  v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
+  uint64_t most = 0;
+#pragma unroll
+  for (int row = 0; row < 64; row += 16) {
+    const uint64_t x = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), row) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, row);
+    most = x > most ? x : most;
+  }
+  return most;
+}
+
 // Bits that any lane has.
 __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
   v |= (uint32_t)dpp_mov_i<0xB1>((int)v);
@@ -344,17 +369,21 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t v, int lane) {
   return v + (lane >= 16 ? a : 0) + (lane >= 32 ? b : 0) + (lane >= 48 ? c : 0);
 }
 
-// A workgroup takes a token's list.  The k-th largest key is found eight bits at a time (a histogram in LDS of the keys that
-// share the digits found), from the highest bit in which two keys differ down to where the keys that share all digits found are as many as are
-// still wanted: two or three passes as a rule.  Then the blocks above it, and the first of those equal to it, are written in
-// order.  E keys a thread in registers; E = 0: read again in every pass.
+// A workgroup takes a token's list.  The k-th largest score is found eight bits at a time (a histogram in LDS of the keys that
+// share the digits found), down to where the keys that share all digits found are as many as are still wanted: two
+// passes as a rule.  The digits are those of where a score lies between the least and the largest, as a 32-bit fraction: its own
+// leading bits are its exponent, which nearly all scores share.  Where more scores than wanted share a fraction, or the
+// range is not finite, those scores' keys are gone through in the same way, from the highest bit in which two differ.
+// Then the blocks above, and the first of those that are equal, are written in order.  Bound by latency: a chain of
+// barriers for short lists (32 lists of 2048 blocks 6 us, 2048 lists of 512 12 us), one compute unit's instructions for
+// long ones (8192 blocks 16 us; in digits of the keys alone 18).  E keys a thread in registers; E = 0: read again in every pass.
 constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
 template <int E>
 __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const SelectArgs a) {
   __shared__ uint32_t sh_hist[2][256];
-  __shared__ uint64_t sh_edge, sh_wave[2][kSelectWaves];
-  __shared__ uint32_t sh_need, sh_in;
-  __shared__ uint32_t sh_count[2][2][kSelectWaves];
+  __shared__ uint64_t sh_wave[4][kSelectWaves];
+  __shared__ uint32_t sh_digit, sh_need, sh_in;
+  __shared__ uint32_t sh_count[2][kSelectWaves];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t unit = blockIdx.x, b = unit / a.N / a.H;
   const int64_t len = rows_held(a.lengths, b, a.T), nb = (len + a.block - 1) / a.block;
@@ -364,150 +393,194 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
     for (int64_t i = tid; i < a.k; i += kSelectThreads) to[i] = i < nb ? (int32_t)i : -1;
     return;
   }
-  const int64_t free0 = a.first, free1 = nb - a.last;  // the others are taken anyway
+  const int free0 = a.first, free1 = (int)nb - a.last;  // the others are taken anyway
   uint64_t mine[E ? E : 1];
-  const int64_t slabs = (nb + kSelectThreads - 1) / kSelectThreads;
-  auto read = [&](int64_t e) {
-    const int64_t j = e * kSelectThreads + tid;
+  uint32_t lies[E ? E : 1];  // (fractions)
+  // a wavefront takes `slabs` times 64 blocks, one behind the other: what it writes lies together
+  const int slabs = (int)((nb + kSelectThreads - 1) / kSelectThreads);
+  auto block_of = [&](int e) { return e < slabs ? (wave * slabs + e) * 64 + lane : (int)nb; };
+  auto read = [&](int e) {
+    const int j = block_of(e);
     return j >= free0 && j < free1 ? score_key(score[j]) : 0;
   };
-  auto each = [&](auto f) {
+  bool linear = false;
+  uint64_t first_key = 0;
+  double least = 0, scale = 0;
+  auto fraction = [&](uint64_t u) { return linear ? (uint32_t)((key_score(u ? u : first_key) - least) * scale) : 0u; };
+  auto each = [&](auto f) {  // key and fraction
     if constexpr (E > 0) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) f(e, mine[e]);
+      for (int e = 0; e < E; ++e) f(e, mine[e], lies[e]);
     } else {
-      for (int64_t e = 0; e < slabs; ++e) f(e, read(e));
+      for (int e0 = 0; e0 < slabs; e0 += 8) {  // (eight on their way together; behind the last: no keys)
+        uint64_t u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = read(e0 + i);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(e0 + i, u[i], fraction(u[i]));
+      }
     }
   };
   if constexpr (E > 0) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) mine[e] = read(e);
+    for (int e = 0; e < E; ++e) {
+      mine[e] = read(e);
+      lies[e] = 0;
+    }
   }
-  // bits in which keys differ: those that some have and not all
-  uint64_t some = 0, all = ~0ull;
-  each([&](int64_t, uint64_t u) {
-    some |= u;
-    all &= u ? u : ~0ull;
+  // the two ends of the keys
+  uint64_t top = 0, low_end = 0;  // (the least as its complement)
+  each([&](int, uint64_t u, uint32_t) {
+    top = u > top ? u : top;
+    const uint64_t c = u ? ~u : 0;
+    low_end = c > low_end ? c : low_end;
   });
-  some = wave_or(some);
-  all = ~wave_or(~all);
+  top = wave_largest(top);
+  low_end = wave_largest(low_end);
   if (lane == 0) {
-    sh_wave[0][wave] = some;
-    sh_wave[1][wave] = all;
+    sh_wave[0][wave] = top;
+    sh_wave[1][wave] = low_end;
   }
   (&sh_hist[0][0])[tid] = 0;  // (kSelectThreads bins)
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < kSelectWaves; ++x) {
-    some |= sh_wave[0][x];
-    all &= sh_wave[1][x];
+    top = sh_wave[0][x] > top ? sh_wave[0][x] : top;
+    low_end = sh_wave[1][x] > low_end ? sh_wave[1][x] : low_end;
   }
-  const uint64_t differ = some & ~all;
   uint32_t need = (uint32_t)(a.k - a.first - a.last);
-  uint64_t edge = all & some, above_edge = 0;  // taken: keys above `edge`, and `need` of the equal ones; keys at or above `above_edge`, if set
-  if (need == 0) {
-    edge = ~0ull;
-  } else if (differ != 0) {
-    int low = 63 - __builtin_clzll(differ);  // the highest differing bit, then the lowest one found
-    edge = low == 63 ? 0 : edge >> (low + 1) << (low + 1);
-    int high = low, turn = 0;
-    for (;;) {
-      const int width = high + 1 < 8 ? high + 1 : 8;
-      low = high + 1 - width;
-      each([&](int64_t, uint64_t u) {
-        if (u && (high == 63 || (u >> (high + 1)) == (edge >> (high + 1)))) atomicAdd(&sh_hist[turn][(u >> low) & ((1u << width) - 1)], 1u);
-      });
-      __syncthreads();
-      if (wave == 0) {
-        // digits from the top: lane l has 255 - 4 l down to 252 - 4 l
-        uint32_t c[4], sum = 0;
+  int turn = 0;
+  // One digit of the keys that f counts: the one at which `need` keys are reached from the top.  The keys above it are taken
+  // off `need`; true where all that have it are wanted.
+  auto digit_of = [&](auto count, uint32_t* digit) {
+    count(&sh_hist[turn][0]);
+    __syncthreads();
+    if (wave == 0) {
+      // digits from the top: lane l has 255 - 4 l down to 252 - 4 l
+      uint32_t c[4], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = sh_hist[turn][255 - 4 * lane - i];
-          sum += c[i];
-        }
-        const uint32_t upto = sum_upto(sum, lane);
-        uint32_t before = upto - sum;
-        if (before < need && upto >= need) {
-          int i = 0;
-          while (i < 3 && before + c[i] < need) before += c[i++];
-          sh_edge = edge | (uint64_t)(255 - 4 * lane - i) << low;
-          sh_need = need - before;
-          sh_in = i == 0 ? c[0] : i == 1 ? c[1] : i == 2 ? c[2] : c[3];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sh_hist[turn][255 - 4 * lane - i] = 0;  // (for the pass after the next)
+      for (int i = 0; i < 4; ++i) {
+        c[i] = sh_hist[turn][255 - 4 * lane - i];
+        sum += c[i];
       }
-      __syncthreads();
-      edge = sh_edge;
-      need = sh_need;
-      const bool done = sh_in == need;
-      if (done) above_edge = edge;
-      if (done || low == 0) break;
-      high = low - 1;
-      turn ^= 1;
-    }
-  }
-  // (all keys equal: the first `need` of them)
-  auto over_of = [&](int64_t j, uint64_t u) {
-    return j < free0 || (j >= free1 && j < nb) || (u && (above_edge ? u >= above_edge : u > edge));
-  };
-  auto tie_of = [&](int64_t j, uint64_t u) { return u && !above_edge && u == edge && j >= free0 && j < free1; };
-  auto put = [&](int64_t j, bool over, bool tie, uint32_t before_o, uint32_t before_t) {
-    if (over || (tie && before_t < need)) to[before_o + (before_t < need ? before_t : need)] = (int32_t)j;
-  };
-  if constexpr (E * kSelectWaves <= 64 && E > 0) {
-    // the slabs' counts by wavefront, a lane each
-    __shared__ uint32_t sh_all[2][E * kSelectWaves];
-    uint64_t overs[E], ties[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int64_t j = (int64_t)e * kSelectThreads + tid;
-      overs[e] = __ballot(over_of(j, mine[e]));
-      ties[e] = __ballot(tie_of(j, mine[e]));
-      if (lane == 0) {
-        sh_all[0][e * kSelectWaves + wave] = __popcll(overs[e]);
-        sh_all[1][e * kSelectWaves + wave] = __popcll(ties[e]);
+      const uint32_t upto = sum_upto(sum, lane);
+      uint32_t before = upto - sum;
+      if (before < need && upto >= need) {
+        int i = 0;
+        while (i < 3 && before + c[i] < need) before += c[i++];
+        sh_digit = 255 - 4 * lane - i;
+        sh_need = need - before;
+        sh_in = i == 0 ? c[0] : i == 1 ? c[1] : i == 2 ? c[2] : c[3];
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sh_hist[turn][255 - 4 * lane - i] = 0;  // (for the pass after the next)
     }
     __syncthreads();
-    const uint32_t o = lane < E * kSelectWaves ? sh_all[0][lane] : 0, t = lane < E * kSelectWaves ? sh_all[1][lane] : 0;
-    const uint32_t upto_o = sum_upto(o, lane) - o, upto_t = sum_upto(t, lane) - t;
-    const int w = __builtin_amdgcn_readfirstlane(wave);
+    *digit = sh_digit;
+    need = sh_need;
+    turn ^= 1;
+    return sh_in == need;
+  };
+  // Taken: scores whose fraction is above `at`; of those at it, keys above `edge` or (if set) at or above `above_edge`, and the
+  // first `need` of the keys at `edge`.
+  first_key = ~low_end;
+  least = key_score(first_key);
+  const double range = key_score(top) - least;
+  linear = range >= 1e-290 && range <= 1.7e308;  // (and a number)
+  scale = linear ? 4294967295.0 / range : 0;
+  if constexpr (E > 0) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const uint32_t before_o = (uint32_t)__builtin_amdgcn_readlane((int)upto_o, e * kSelectWaves + w) + prefix_popc(overs[e]);
-      const uint32_t before_t = (uint32_t)__builtin_amdgcn_readlane((int)upto_t, e * kSelectWaves + w) + prefix_popc(ties[e]);
-      put((int64_t)e * kSelectThreads + tid, overs[e] >> lane & 1, ties[e] >> lane & 1, before_o, before_t);
-    }
+    for (int e = 0; e < E; ++e) lies[e] = fraction(mine[e]);
+  }
+  uint32_t at = 0;
+  uint64_t edge = ~0ull, above_edge = 0;
+  if (need == 0) {
+    at = ~0u;
   } else {
-    uint32_t taken = 0, equal = 0;
-    int slab = 0;
-    each([&](int64_t e, uint64_t u) {
-      if (e >= slabs) return;  // (uniform)
-      const int64_t j = e * kSelectThreads + tid;
-      const bool over = over_of(j, u), tie = tie_of(j, u);
-      const uint64_t overs = __ballot(over), ties = __ballot(tie);
+    bool done = false;
+    for (int shift = 24; linear && shift >= 0 && !done; shift -= 8) {
+      uint32_t digit;
+      done = digit_of([&](uint32_t* hist) {
+        each([&](int, uint64_t u, uint32_t f) {
+          if (u && (shift == 24 || f >> (shift + 8) == at >> (shift + 8))) atomicAdd(&hist[f >> shift & 255], 1u);
+        });
+      }, &digit);
+      at |= digit << shift;
+      if (done) --at;  // (not all keys are taken: it was not 0)
+    }
+    if (!done) {
+      // bits in which the keys at this fraction differ: those that some have and not all
+      uint64_t some = 0, all = ~0ull;
+      each([&](int, uint64_t u, uint32_t f) {
+        if (u && f == at) {
+          some |= u;
+          all &= u;
+        }
+      });
+      some = wave_or(some);
+      all = ~wave_or(~all);
       if (lane == 0) {
-        sh_count[slab][0][wave] = __popcll(overs);
-        sh_count[slab][1][wave] = __popcll(ties);
+        sh_wave[2][wave] = some;
+        sh_wave[3][wave] = all;
       }
       __syncthreads();
-      uint32_t before_o = taken, before_t = equal;
 #pragma unroll
       for (int x = 0; x < kSelectWaves; ++x) {
-        const uint32_t o = sh_count[slab][0][x], t = sh_count[slab][1][x];
-        if (x < wave) {
-          before_o += o;
-          before_t += t;
-        }
-        taken += o;
-        equal += t;
+        some |= sh_wave[2][x];
+        all &= sh_wave[3][x];
       }
-      put(j, over, tie, before_o + prefix_popc(overs), before_t + prefix_popc(ties));
-      slab ^= 1;
-    });
+      const uint64_t differ = some & ~all;
+      edge = some & all;
+      if (differ != 0) {
+        int low = 63 - __builtin_clzll(differ);  // the highest differing bit, then the lowest one found
+        edge = low == 63 ? 0 : edge >> (low + 1) << (low + 1);
+        for (int high = low;; high = low - 1) {
+          const int width = high + 1 < 8 ? high + 1 : 8;
+          low = high + 1 - width;
+          uint32_t digit;
+          done = digit_of([&](uint32_t* hist) {
+            each([&](int, uint64_t u, uint32_t f) {
+              if (u && f == at && (high == 63 || (u >> (high + 1)) == (edge >> (high + 1)))) atomicAdd(&hist[(u >> low) & ((1u << width) - 1)], 1u);
+            });
+          }, &digit);
+          edge |= (uint64_t)digit << low;
+          if (done) above_edge = edge;
+          if (done || low == 0) break;
+        }
+      }
+    }
   }
+  // (keys from `from` on at the fraction `at`; no key is all ones)
+  const uint64_t from = above_edge ? above_edge : edge == ~0ull ? edge : edge + 1, tied = above_edge ? ~0ull : edge;
+  auto over_of = [&](int j, uint64_t u, uint32_t f) {
+    return (j < free0) | ((j >= free1) & (j < (int)nb)) | ((u != 0) & ((f > at) | ((f == at) & (u >= from))));
+  };
+  auto tie_of = [&](uint64_t u, uint32_t f) { return (u == tied) & (f == at); };
+  uint32_t n_over = 0, n_tie = 0;  // of the wavefront
+  each([&](int e, uint64_t u, uint32_t f) {
+    n_over += __popcll(__ballot(over_of(block_of(e), u, f)));
+    n_tie += __popcll(__ballot(tie_of(u, f)));
+  });
+  if (lane == 0) {
+    sh_count[0][wave] = n_over;
+    sh_count[1][wave] = n_tie;
+  }
+  __syncthreads();
+  uint32_t before_o = 0, before_t = 0;
+#pragma unroll
+  for (int x = 0; x < kSelectWaves; ++x) {
+    before_o += x < wave ? sh_count[0][x] : 0;
+    before_t += x < wave ? sh_count[1][x] : 0;
+  }
+  each([&](int e, uint64_t u, uint32_t f) {
+    const int j = block_of(e);
+    const bool over = over_of(j, u, f), tie = tie_of(u, f);
+    const uint64_t overs = __ballot(over), ties = __ballot(tie);
+    const uint32_t o = before_o + prefix_popc(overs), t = before_t + prefix_popc(ties);
+    if (over || (tie && t < need)) to[o + (t < need ? t : need)] = j;
+    before_o += __popcll(overs);
+    before_t += __popcll(ties);
+  });
 }
 
 int lanes_a_row(int D, int dtype) {
@@ -559,7 +632,8 @@ hipError_t launch_block_scores(const SelectArgs& a, hipStream_t s) {
 
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t s) {
   const dim3 grid((uint32_t)((int64_t)a.B * a.H * a.N)), group(kSelectThreads);
-  if (a.nb <= 4 * kSelectThreads) block_select_kernel<4><<<grid, group, 0, s>>>(a);
+  if (a.nb <= kSelectThreads) block_select_kernel<1><<<grid, group, 0, s>>>(a);
+  else if (a.nb <= 4 * kSelectThreads) block_select_kernel<4><<<grid, group, 0, s>>>(a);
   else if (a.nb <= 16 * kSelectThreads) block_select_kernel<16><<<grid, group, 0, s>>>(a);
   else block_select_kernel<0><<<grid, group, 0, s>>>(a);
   return hipGetLastError();

@@ -444,6 +444,40 @@ def test_equal_scores_go_to_the_lower_block():
     assert got[0, 0, 0].tolist() == list(range(298)) + [698, 699]
 
 
+@pytest.mark.parametrize("nb,k", [(70, 33), (512, 1), (513, 200), (2049, 64), (8200, 500), (20000, 4096)])
+@pytest.mark.parametrize("kind", ["normal", "near", "far", "few", "one", "huge", "wide", "none"])
+def test_scores_that_are_hard_to_part(nb, k, kind):
+    """Scores that differ in their last bits beside some far away, few distinct ones, the largest range, and some that are no
+    numbers ("huge": of infinite bounds; they are q times a bound of either sign, 0 and infinity among them)."""
+    g = torch.Generator().manual_seed(nb + k)
+    x = torch.randn(nb, generator=g)
+    if kind == "near":
+        x = 1 + torch.randint(0, 9, (nb,), generator=g) * 2.0 ** -23
+    elif kind == "far":
+        x = torch.where(torch.rand(nb, generator=g) < 0.9, 1 + torch.randint(0, 99, (nb,), generator=g) * 2.0 ** -23, -3e38 * torch.rand(nb, generator=g))
+    elif kind == "few":
+        x = torch.randint(-2, 3, (nb,), generator=g).float() * 0.5
+    elif kind == "one":
+        x = torch.full((nb,), -2.5)
+    elif kind == "huge":
+        x = x * 3e38 / x.abs().max()
+    elif kind == "wide":
+        x = x / x.abs().max() * 3e38
+    elif kind == "none":
+        x[torch.rand(nb, generator=g) < 0.5] = math.nan
+    D, N, block = 8, 5, 16
+    bound = torch.zeros(1, 1, nb, D)
+    bound[0, 0, :, 0] = x
+    q = torch.zeros(1, 1, N, D)
+    q[0, 0, :, 0] = 1
+    first = min(2, k)
+    order = sorted(range(nb), key=lambda j: (j >= first, j < first or (-float(x[j]) if math.isfinite(x[j]) else math.inf), j))
+    want = torch.tensor(sorted(order[:k]), dtype=torch.int32)
+    for n in (1, N):
+        got = lagkv.select_blocks(q[:, :, :n].to(DEV), bound.to(DEV), bound.to(DEV), nb * block, block, k, first).cpu()
+        assert bool((got == want).all()), (kind, n)
+
+
 @pytest.mark.parametrize("dtype", [BF, FL], ids=["bf16", "f32"])
 def test_selection_at_size(dtype):
     """Thousands of blocks, several tokens, every count of heads of a group; near the border scores are close."""
