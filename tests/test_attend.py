@@ -119,6 +119,16 @@ def test_ragged_lengths_of_a_cache_in_pieces(dtype, N):
     A.check(lagkv.attend(q, K, V, Kn, Vn, lengths=lengths, want_lse=True), want)
 
 
+@pytest.mark.parametrize("dtype", [BF, FL], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 1, 8, 1, 128, 60001), (1, 1, 4, 30, 64, 20000), (3, 5, 2, 1, 64, 5000), (1, 3, 4, 9, 128, 7000),
+                                  (1, 7, 32, 1, 100, 3001), (1, 1, 2, 17, 256, 9000)], ids=lambda s: "x".join(map(str, s)))
+def test_many_pieces_of_few_streams(dtype, size):
+    """Caches that are cut into numbers of pieces that are no multiples of the eight chiplets', of one stream and more."""
+    B, H, G, N, D, T = size
+    q, K, V, Kn, Vn = problem(dtype, B, H, G, N, D, T, "chain", seed=T)
+    A.check(lagkv.attend(q, K, V, Kn, Vn, want_lse=True), A.attend(q, K, V, Kn, Vn))
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("chain", [True, False])
