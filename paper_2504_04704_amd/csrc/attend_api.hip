@@ -82,7 +82,7 @@ int64_t next_pieces(int64_t s) { return s + (s < 4 ? 1 : s % 3 == 0 ? s / 3 : s 
 //   32 streams,  256 query rows, 8000 rows   128 in 4 65 (65)   128 in 8 53 (53)   256 in 4 64 (69)   256 in 8 51 (51)
 //    8 streams, 2048 query rows, 8000 rows   128 in 2 121 (119)   128 in 4 91 (92)   256 in 2 119 (122)   256 in 4 87 (82)
 //   64 streams,  160 query rows, 8000 rows   128 in 4 79 (85)   256 in 4 63 (65)
-void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_tile, int64_t* pieces) {
+double wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_tile, int64_t* pieces) {
   const double by_d4 = D <= 64 ? 0.62 : D <= 128 ? 1 : 1.7, by_d8 = D <= 64 ? 0.7 : 1;
   double least = 1e30;
   for (int tile = 128; tile <= (D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
@@ -102,24 +102,25 @@ void wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_
       }
     }
   }
+  return least;
 }
 
 // Tiles of 16 or 32 query rows: the pieces of the cache by the microseconds that they take, none below a step a wavefront.
 // A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them, at
-// no cost to each other but memory's where that is the bound (32 fp32 rows: 0.75 us alone, 1.4 us beside another), and one where
+// no cost to each other but memory's with 16 query rows (32: 0.75 us beside another, in fp32 0.75 alone and 1.4), and one where
 // the outputs fill its registers.  All rows together pass memory at 6 TB/s, less where some compute
 // units have a workgroup more than others.  With pieces, a second kernel and every piece of a row written and read.
 // Over 205 shapes (16-bit and fp32, 64 to 256 channels, 4 to 600 query rows, 1 to 1000 workgroups, 200 to 50000 rows) the
 // time is 1 % above that of the best number of pieces in the mean; with as many pieces as make 512 workgroups, 11.9 %.  Where
 // lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4
 // 115; 192 streams in 1 70, in 2 79.)
-int64_t narrow_pieces(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps) {
+double narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces) {
   const bool heavy = f32 && row_tile == 32;  // (bound by the products)
   const int64_t tiles = (rows + row_tile - 1) / row_tile, places = D > 128 ? 32 : 64;  // of an XCD
-  const double channels = D <= 64 ? 0.5 : D <= 128 ? 1 : 2, alone = (heavy ? 0.75 : 0.45) * channels, both = (heavy ? 1.4 : 0.45) * channels;
+  const double channels = D <= 64 ? 0.5 : D <= 128 ? 1 : 2, alone = (heavy ? 0.75 : 0.45) * channels;
+  const double both = (heavy ? 1.4 : row_tile == 32 ? 0.75 : 0.45) * channels;  // (beside another workgroup)
   const double ends = 5.5;
   const double memory = (double)units * (double)steps * (double)D * 128 / 6e6;
-  int64_t best = 1;
   double least = 1e30;
   for (int64_t s = 1; s <= 256 && (s == 1 || s <= steps / 4); s = next_pieces(s)) {
     const int64_t load = fullest_xcd(units, s, tiles);
@@ -131,27 +132,40 @@ int64_t narrow_pieces(int64_t units, int64_t rows, int64_t row_tile, int64_t D, 
     const double us = (go > pass ? go : pass) + (s > 1 ? 3.5 + (double)(units * rows * s) * (double)D * 8 / 3e6 : 0);
     if (us < least) {
       least = us;
-      best = s;
+      *pieces = s;
     }
   }
-  return best;
+  return least;
 }
 
-// Query rows of a tile: as many as there are, up to what the registers hold.
+// Tiles of few query rows: as many as there are, up to what the registers hold.  Of many (16-bit types): tiles of 128 or 256
+// where they take less time, by the two models.  (Over 299 shapes with trees, 40 to 600 query rows of 2 to 128 streams, 100 to
+// 6000 cache rows, the time is 1.6 % above that of the better kernel, with tiles of many rows for all of them 4.3 %; over 392
+// without new tokens, to 2000 query rows and 400 streams, 2.2 % and 7.9 %.  us, few and many: 8 streams, 256 query rows,
+// 300 rows 12.4 and 15.3, 2000 rows 23.5 and 23.0; 32 streams, 256, 2000 rows 38 and 29.)
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
   if (pl->units > kMost || !grid_fits(pl->units * pl->rows, 256)) return false;  // (the second kernel's grid)
-  pl->wide = !pick && p->dtype != LAGKV_F32 && pl->rows > 32;
-  const int64_t kt = pl->wide ? 64 : p->dtype == LAGKV_F32 ? 16 : 32;
+  const bool f32 = p->dtype == LAGKV_F32;
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
-  const int64_t steps = (seen + kt - 1) / kt + (p->N + kt - 1) / kt;
+  auto steps_of = [&](int64_t kt) { return (seen + kt - 1) / kt + (p->N + kt - 1) / kt; };
+  const int64_t steps = steps_of(f32 ? 16 : 32);
   int64_t splits = 1;
-  if (pl->wide) wide_shape(pl->units, pl->rows, p->D, steps, &pl->row_tile, &splits);
-  else pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
+  pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
+  const double us = narrow_shape(pl->units, pl->rows, pl->row_tile, p->D, f32, steps, &splits);
+  pl->wide = false;
+  if (!pick && !f32 && pl->rows > 32) {
+    int row_tile;
+    int64_t pieces;
+    pl->wide = wide_shape(pl->units, pl->rows, p->D, steps_of(64), &row_tile, &pieces) < us;
+    if (pl->wide) {
+      pl->row_tile = row_tile;
+      splits = pieces;
+    }
+  }
   pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
   const int64_t groups = pl->units * pl->row_tiles;
-  if (!pl->wide) splits = narrow_pieces(pl->units, pl->rows, pl->row_tile, p->D, p->dtype == LAGKV_F32, steps);
   // Short caches whole, by twice the wavefronts in one kernel: up to two steps a wavefront.  (One token over 300 rows of 128
   // 16-bit channels 7.1 us, in pieces about 8; over 640 rows, three steps, 9.5 us, over 1000 12.9 us and in pieces 8.4 us.
   // Rows of 64 fp32 channels: 300 rows 7.6 us, 640 rows 11.2 us and in pieces 7.6 us.)

@@ -1,4 +1,5 @@
-// Attention of many query rows over all rows of a cache (lagkv_attend, 16-bit types; the mathematics is attend_pass.hpp's).
+// Attention of many query rows over all rows of a cache (lagkv_attend, 16-bit types; the mathematics is attend_pass.hpp's; when
+// it is taken, plan_of says).
 //
 // Where a stream has tens of query rows (a drafted tree under grouped heads, a chunk of a prompt) the matrix cores are the
 // bound, not memory: 256 rows make 256 flop of a cache byte.  A workgroup of four or eight wavefronts goes over 64 cache

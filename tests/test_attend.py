@@ -185,6 +185,112 @@ def test_what_is_no_number_and_is_seen(dtype, N, T):
         assert bool(torch.isnan(got.out[0, :3]).all()) and bool(torch.isfinite(got.out[0, 3:]).all())
 
 
+# Tiles of many rows are taken where there is much to multiply: the same shapes, of many streams.  (One problem, read by all: its
+# strides along the batch are 0.)
+MANY = 1200
+
+
+def copies(*tensors):
+    return [None if t is None else t[:1].expand(MANY, *t.shape[1:]) for t in tensors]
+
+
+def the_first_of(got):
+    """The first copy's result; that of all the others is the same, bit for bit."""
+    same = got.out.nan_to_num(7.0) == got.out[:1].nan_to_num(7.0)
+    assert bool(same.all())
+    if got.lse is not None:
+        assert bool((got.lse.nan_to_num(7.0) == got.lse[:1].nan_to_num(7.0)).all())
+    return lagkv.Attended(got.out[:1].clone(), None if got.lse is None else got.lse[:1].clone())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@pytest.mark.parametrize("size", [s for s in SIZES if s[2] * s[3] > 32 and s[1] * s[2] * s[3] <= 420 and s[3] > 1], ids=lambda s: "x".join(map(str, s)))
+def test_attend_of_many_streams(size, dtype):
+    _, H, G, N, D, T, new = size
+    print("[gpu-test] attend, many streams", size, dtype, flush=True)
+    q, K, V, Kn, Vn = problem(dtype, 1, H, G, N, D, T, new, seed=D + T)
+    parents = tree(N, T) if new == "tree" else None
+    got = lagkv.attend(*copies(q, K, V, Kn, Vn), parents, want_lse=True)
+    A.check(the_first_of(got), A.attend(q, K, V, Kn, Vn, parents), str(size))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("chain", [True, False])
+def test_values_of_tokens_that_are_not_seen_of_many_streams(dtype, bad, chain):
+    N, T, at = 70, 90, 40
+    q, K, V, Kn, Vn = problem(dtype, 1, 1, 2, N, 128, T, "tree", seed=9)
+    parents = None if chain else tree(N, 5)
+    want = A.attend(q, K, V, Kn, Vn, parents)
+    see = A.tree_visible(parents.cpu(), N)[:, at] if not chain else torch.arange(N) >= at
+    assert bool(see.any()) and bool((~see).any())
+    Vn[0, 0, at, 7] = bad
+    for row in (None, Kn):
+        if row is not None:
+            row[0, 0, at] = bad
+        got = the_first_of(lagkv.attend(*copies(q, K, V, Kn, Vn), parents))
+        if row is None:
+            assert not bool(torch.isfinite(got.out[0, :, see, 7]).any())
+        got.out[0, :, see] = want[0][0, :, see].to(dtype).to(DEV)
+        A.check(got, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+def test_what_is_no_number_and_is_seen_of_many_streams(dtype):
+    N, T = 70, 64
+    q, K, V, Kn, Vn = problem(dtype, 1, 1, 2, N, 128, T, "chain", seed=31)
+    want = A.attend(q, K, V, Kn, Vn)
+    for what in ("query", "key", "keys"):
+        q2, Kn2, K2, bad = q.clone(), Kn.clone(), K.clone(), torch.zeros(2, N, dtype=torch.bool)
+        if what == "query":
+            q2[0, 1, 3, 5] = math.nan
+            bad[1, 3] = True
+        elif what == "key":
+            Kn2[0, 0, N - 1, 9] = math.nan
+            bad[:, N - 1] = True
+        else:
+            K2[0, 0, :, 3] = math.nan
+            bad[:] = True
+        got = the_first_of(lagkv.attend(*copies(q2, K2, V, Kn2, Vn), want_lse=True))
+        assert bool(torch.isnan(got.out[0, bad]).all()) and bool(torch.isnan(got.lse[0, bad]).all())
+        got.out[0, bad], got.lse[0, bad] = want[0][0, bad].to(dtype).to(DEV), want[1][0, bad].float().to(DEV)
+        A.check(got, want)
+
+
+@pytest.mark.parametrize("new", ["none", "chain", "tree"])
+def test_ragged_lengths_of_many_streams(new):
+    """Lengths as above, and trees of several sizes, 150 times each; what lies behind is NaN and infinite."""
+    T, N = 200, 20
+    lens = [0, 1, 64, 65, 127, 200, 1000, -7]
+    q, K, V, Kn, Vn = problem(BF, len(lens), 2, 4, N, 64, T, new, seed=3)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    parents = tree(N, 1, len(lens), padded=3) if new == "tree" else None
+    clean = A.attend(q, K, V, Kn, Vn, parents, lengths)
+    for b, n in enumerate(lens):
+        n = min(max(n, 0), T)
+        K[b, :, n:], V[b, :, n:] = math.nan, math.inf
+    r = lambda t: None if t is None else t.repeat(150, *[1] * (t.dim() - 1))
+    got = lagkv.attend(r(q), r(K), r(V), r(Kn), r(Vn), r(parents), r(lengths), want_lse=True)
+    A.check(lagkv.Attended(got.out[:8], got.lse[:8]), clean)
+    assert torch.equal(got.out, r(got.out[:8])) and torch.equal(got.lse, r(got.lse[:8]))
+
+
+@pytest.mark.parametrize("size", [(4, 8, 4, 64, 128, 2100, "tree"), (1, 8, 4, 150, 256, 2000, "chain"), (2, 4, 8, 200, 100, 3000, "chain")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_many_rows_of_long_caches(size):
+    B, H, G, N, D, T, new = size
+    q, K, V, Kn, Vn = problem(BF, B, H, G, N, D, T, new, seed=D + T)
+    parents = tree(N, T, B) if new == "tree" else None
+    got = lagkv.attend(q, K, V, Kn, Vn, parents, want_lse=True)
+    # (every few heads of every batch entry)
+    heads = [0, H * G // 2, H * G - 1]
+    for b in range(B):
+        for i in heads:
+            pick = lambda t, j: None if t is None else t[b:b + 1, j:j + 1]
+            want = A.attend(pick(q, i), *(pick(t, i // G) for t in (K, V, Kn, Vn)), None if parents is None else parents[b:b + 1])
+            A.check(lagkv.Attended(pick(got.out, i), pick(got.lse, i)), want, f"{b} {i}")
+
+
 def test_padded_trees():
     """Trees of several sizes in one batch: what is no token sees nothing and is not seen, nor is what lies before it on a
     path, and its rows may hold anything."""
