@@ -333,19 +333,15 @@ __device__ __forceinline__ double key_score(uint64_t u) { return __builtin_bit_c
 
 // Largest of all lanes.
 template <int CTRL>
-__device__ __forceinline__ uint64_t dpp_max(uint64_t v) {
-  const uint64_t far = __builtin_bit_cast(uint64_t, dpp_mov_d<CTRL>(__builtin_bit_cast(double, v)));
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  const uint32_t far = (uint32_t)dpp_mov_i<CTRL>((int)v);
   return far > v ? far : v;
 }
-__device__ __forceinline__ uint64_t wave_largest(uint64_t v) {
-  v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
-  uint64_t most = 0;
-#pragma unroll
-  for (int row = 0; row < 64; row += 16) {
-    const uint64_t x = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), row) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, row);
-    most = x > most ? x : most;
-  }
-  return most;
+__device__ __forceinline__ uint32_t wave_largest(uint32_t v) {
+  const int x = (int)dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
+  const uint32_t a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16), c = __builtin_amdgcn_readlane(x, 32),
+                 d = __builtin_amdgcn_readlane(x, 48), ab = a > b ? a : b, cd = c > d ? c : d;
+  return ab > cd ? ab : cd;
 }
 
 // Bits that any lane has.
@@ -375,13 +371,14 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t v, int lane) {
 // leading bits are its exponent, which nearly all scores share.  Where more scores than wanted share a fraction, or the
 // range is not finite, those scores' keys are gone through in the same way, from the highest bit in which two differ.
 // Then the blocks above, and the first of those that are equal, are written in order.  Bound by latency: a chain of
-// barriers for short lists (32 lists of 2048 blocks 6 us, 2048 lists of 512 12 us), one compute unit's instructions for
+// barriers for short lists (32 lists of 2048 blocks 6 us, 2048 lists of 512 10 us), one compute unit's instructions for
 // long ones (8192 blocks 16 us; in digits of the keys alone 18).  E keys a thread in registers; E = 0: read again in every pass.
 constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
 template <int E>
 __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const SelectArgs a) {
   __shared__ uint32_t sh_hist[2][256];
-  __shared__ uint64_t sh_wave[4][kSelectWaves];
+  __shared__ uint64_t sh_wave[2][kSelectWaves];
+  __shared__ uint32_t sh_ends[2][kSelectWaves];
   __shared__ uint32_t sh_digit, sh_need, sh_in;
   __shared__ uint32_t sh_count[2][kSelectWaves];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -428,25 +425,25 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
       lies[e] = 0;
     }
   }
-  // the two ends of the keys
-  uint64_t top = 0, low_end = 0;  // (the least as its complement)
+  // the two ends of the keys' leading halves (the least as its complement)
+  uint32_t top = 0, bottom = 0;
   each([&](int, uint64_t u, uint32_t) {
-    top = u > top ? u : top;
-    const uint64_t c = u ? ~u : 0;
-    low_end = c > low_end ? c : low_end;
+    const uint32_t half = (uint32_t)(u >> 32), c = u ? ~half : 0;
+    top = half > top ? half : top;
+    bottom = c > bottom ? c : bottom;
   });
   top = wave_largest(top);
-  low_end = wave_largest(low_end);
+  bottom = wave_largest(bottom);
   if (lane == 0) {
-    sh_wave[0][wave] = top;
-    sh_wave[1][wave] = low_end;
+    sh_ends[0][wave] = top;
+    sh_ends[1][wave] = bottom;
   }
   (&sh_hist[0][0])[tid] = 0;  // (kSelectThreads bins)
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < kSelectWaves; ++x) {
-    top = sh_wave[0][x] > top ? sh_wave[0][x] : top;
-    low_end = sh_wave[1][x] > low_end ? sh_wave[1][x] : low_end;
+    top = sh_ends[0][x] > top ? sh_ends[0][x] : top;
+    bottom = sh_ends[1][x] > bottom ? sh_ends[1][x] : bottom;
   }
   uint32_t need = (uint32_t)(a.k - a.first - a.last);
   int turn = 0;
@@ -483,9 +480,9 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
   };
   // Taken: scores whose fraction is above `at`; of those at it, keys above `edge` or (if set) at or above `above_edge`, and the
   // first `need` of the keys at `edge`.
-  first_key = ~low_end;
+  first_key = (uint64_t)~bottom << 32;
   least = key_score(first_key);
-  const double range = key_score(top) - least;
+  const double range = key_score((uint64_t)top << 32 | 0xffffffffu) - least;
   linear = range >= 1e-290 && range <= 1.7e308;  // (and a number)
   scale = linear ? 4294967295.0 / range : 0;
   if constexpr (E > 0) {
@@ -520,14 +517,14 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
       some = wave_or(some);
       all = ~wave_or(~all);
       if (lane == 0) {
-        sh_wave[2][wave] = some;
-        sh_wave[3][wave] = all;
+        sh_wave[0][wave] = some;
+        sh_wave[1][wave] = all;
       }
       __syncthreads();
 #pragma unroll
       for (int x = 0; x < kSelectWaves; ++x) {
-        some |= sh_wave[2][x];
-        all &= sh_wave[3][x];
+        some |= sh_wave[0][x];
+        all &= sh_wave[1][x];
       }
       const uint64_t differ = some & ~all;
       edge = some & all;
