@@ -257,8 +257,8 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
 
 // Scores of more tokens: sixteen blocks times sixteen tokens at a time on the matrix cores (64-bit), whose operand of
 // the blocks is the bounds as they lie in memory (lane l: block l % 16, a slice of its channels), and that of the tokens is
-// P and M, in LDS for the workgroup's sixteen tokens and `sets` of 64 blocks; the next set is on its way while one is
-// multiplied.  Workgroups of other tokens and the same blocks follow on the same XCD, whose L2 has the bounds.  A product
+// P and M, in LDS for the workgroup's sixteen tokens and `sets` of 64 blocks (the next set comes while other wavefronts
+// multiply).  Workgroups of other tokens and the same blocks follow on the same XCD, whose L2 has the bounds.  A product
 // takes what 64-bit vector arithmetic takes, but nothing has to be summed across lanes.  Bound by the products: 16 tokens of
 // 32 streams x 2048 blocks 20 us, 9 at the rate of a large 64-bit product (the rest are P and M, 64-bit conversions and
 // the launch).
