@@ -1,7 +1,7 @@
 // Joins the pieces that a unit's cache rows were cut into (see attend_pass.hpp for how two states join): a workgroup
 // or a wavefront takes one query row, a lane four channels of every so many pieces.  Few rows: bound by the launch
-// and the latency of two dependent reads (2.5 to 4 us, at most 256 pieces of a row).  Many: by memory (8192 rows in 8 pieces,
-// 33 MB, 9.6 us).  The workgroups of the first kernel cannot do it, the last one to end say: a count of those that have ended
+// and the latency of two dependent reads (2.5 to 3 us, at most 256 pieces of a row).  Many: by memory (8192 rows in 8 pieces,
+// 33 MB, 8.6 us).  The workgroups of the first kernel cannot do it, the last one to end say: a count of those that have ended
 // would have to be cleared before, which is a launch as well.
 #include "attend_pass.hpp"
 
@@ -26,21 +26,36 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
   // lanes: four channels each, of one piece or of two or four
   const int per = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, quad = lane % per, sub = lane / per, pieces = 64 / per;
   const bool have = quad * 4 < a.D;
+  // the first of a lane's pieces are asked for before the largest maximum is known
+  constexpr int AHEAD = 4;
+  const int turn = (WAVES == 1 ? 0 : wave * pieces) + sub, stride = WAVES * pieces;
+  f32x4 x[AHEAD];
+  float mx[AHEAD], lx[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int s = turn + i * stride;
+    const int64_t at = first + (int64_t)(s < a.splits ? s : 0) * a.rows;
+    x[i] = *(const f32x4*)(a.part_o + at * a.part_ld + (have ? quad * 4 : 0));
+    mx[i] = a.part_ml[at * 2];
+    lx[i] = s < a.splits ? a.part_ml[at * 2 + 1] : 0.f;
+  }
   float top = -INFINITY;
   for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.part_ml[(first + (int64_t)s * a.rows) * 2]);
   top = wave_max(top);
   float sum = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  const int turn = (WAVES == 1 ? 0 : wave * pieces) + sub;
-#pragma unroll 4
-  for (int s = turn; s < a.splits; s += WAVES * pieces) {
-    const int64_t at = first + (int64_t)s * a.rows;
-    const f32x4 x = *(const f32x4*)(a.part_o + at * a.part_ld + (have ? quad * 4 : 0));
-    const float mx = a.part_ml[at * 2], lx = a.part_ml[at * 2 + 1];
+  auto add = [&](f32x4 x, float mx, float lx) {
     // (a piece that saw nothing has zeros)
     const float f = lx == 0.f ? 0.f : __builtin_amdgcn_exp2f((mx - top) * E::UNIT);
     sum += f * lx;
-    v += f * x;
+    v += lx == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f * x;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) add(x[i], mx[i], lx[i]);
+#pragma unroll 4
+  for (int s = turn + AHEAD * stride; s < a.splits; s += stride) {
+    const int64_t at = first + (int64_t)s * a.rows;
+    add(*(const f32x4*)(a.part_o + at * a.part_ld + (have ? quad * 4 : 0)), a.part_ml[at * 2], a.part_ml[at * 2 + 1]);
   }
   for (int far = per; far < 64; far <<= 1) {
     sum += __shfl_xor(sum, far);

@@ -6,8 +6,8 @@
 // rows (32 beyond 128 channels) at a time, which lie in LDS for all of them (the next ones are on their way through
 // registers meanwhile); each wavefront keeps 32 query rows to itself, so that nothing is exchanged between wavefronts.  32x32
 // products: a lane holds one query row (of S^T, P^T and O^T), so that maxima and sums need one exchange between the lane's
-// halves only.  Measured: 256 rows of 32 streams x 33536 (bf16, 128 channels) 147 us, 0.96 Pflop/s, and 9.6 for joining the
-// pieces; 2048 rows of 8 streams x 8640 89 us, 0.83 Pflop/s, and 11 (a large product of the library: 1.09).  The matrix cores are
+// halves only.  Measured: 256 rows of 32 streams x 33536 (bf16, 128 channels) 147 us, 0.96 Pflop/s, and 8.6 for joining the
+// pieces; 2048 rows of 8 streams x 8640 89 us, 0.83 Pflop/s, and 9 (a large product of the library: 1.09).  The matrix cores are
 // busy in 55 % of the cycles, at a clock of 1.7 GHz; there are no conflicts of LDS banks to speak of.
 //
 // P is put in rounded to the type: two numbers, as in the narrow kernel, would cost half as many products again.  The
