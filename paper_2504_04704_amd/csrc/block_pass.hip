@@ -58,6 +58,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void block_bounds_kernel(const BoundsArgs a, int lpr) {
   using ET = typename Of<DT>::T;
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC;
+  fetch_arguments<BoundsArgs>();
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t per = a.nb - a.first, id = (int64_t)blockIdx.x * 4 + wave;
   const int64_t stream = id / per, j = a.first + id % per;
@@ -202,6 +203,7 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
   using ET = typename Of<DT>::T;
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC, AHEAD = 4;
   __shared__ double sh_p[kFewTokens][kMaxHead], sh_m[kFewTokens][kMaxHead];  // of a token: [channel of a slice][slice]
+  fetch_arguments<SelectArgs>();
   const uint32_t tiles = (uint32_t)((a.nb + kScoreBlocks - 1) / kScoreBlocks), st = blockIdx.x / tiles;
   const int64_t stream = st, j0 = (int64_t)(blockIdx.x % tiles) * kScoreBlocks, b = st / (uint32_t)a.H, h = st % (uint32_t)a.H;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -269,6 +271,7 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC, NC = DP / VEC / 4;
   constexpr int LD = DP + 1;  // doubles between tokens: sixteen lanes' reads on different banks
   extern __shared__ __attribute__((aligned(16))) double sh_pm[];  // [16][LD] of P, then of M
+  fetch_arguments<SelectArgs>();
   const uint32_t tiles = (uint32_t)((a.nb + kScoreBlocks * sets - 1) / (kScoreBlocks * sets)), token_groups = (uint32_t)(a.N + 15) / 16;
   const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, of = rest / token_groups, id = of * 8 + slot, st = id / tiles;
   if (st >= (uint32_t)a.B * (uint32_t)a.H) return;
@@ -382,7 +385,8 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const Sele
   __shared__ uint32_t sh_digit, sh_need, sh_in;
   __shared__ uint32_t sh_count[2][kSelectWaves];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int64_t unit = blockIdx.x, b = unit / a.N / a.H;
+  fetch_arguments<SelectArgs>();
+  const int64_t unit = blockIdx.x, b = (uint32_t)blockIdx.x / (uint32_t)a.N / (uint32_t)a.H;
   const int64_t len = rows_held(a.lengths, b, a.T), nb = (len + a.block - 1) / a.block;
   const double* score = a.score + unit * a.nb;
   int32_t* to = a.blocks + unit * a.k;
