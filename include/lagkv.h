@@ -328,6 +328,17 @@ typedef struct {
 size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p);
 
 /*
+ * The launch shape of that call, as lagkv_path_for and lagkv_kernel_for give it of a lagkv_compress call: which kernel runs
+ * (many_rows: the one that many query rows share, of 16-bit types), how many query rows a workgroup takes, with how many
+ * wavefronts, and into how many pieces the cache is cut (from two on a second kernel joins them).  It depends on the same
+ * parameters as the workspace.  Host only; the lagkv_status that the call itself would return for parameters it rejects.
+ */
+typedef struct {
+  int32_t many_rows, row_tile, wavefronts, pieces;
+} lagkv_attend_plan_t;
+int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out);
+
+/*
  * out = softmax(scale Q K^T) V over what each new token sees, and the logarithm of the softmax's denominator:
  *   - rows 0 .. lengths[b]-1 of the cache (lengths: [B] device int32, values below 0 or above T count as 0 and T; NULL: all T);
  *   - of the new tokens' rows K_new, V_new (NULL: none), with parents NULL those of tokens 0 .. n: a single token, or

@@ -269,6 +269,22 @@ size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p) {
   return pl.ws_bytes;
 }
 
+int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out) {
+  if (!p || !out) return LAGKV_EINVAL;
+  const bool pick = p->n_blocks > 0;
+  const int rc = check_attend(p, pick);
+  if (rc != LAGKV_OK) return rc;
+  std::memset(out, 0, sizeof(*out));
+  if (p->N == 0) return LAGKV_OK;
+  AttendPlan pl;
+  if (!plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
+  out->many_rows = pl.wide;
+  out->row_tile = pl.row_tile;
+  out->wavefronts = pl.wide ? pl.row_tile / 32 : pl.waves;
+  out->pieces = pl.splits;
+  return LAGKV_OK;
+}
+
 int lagkv_attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
                  const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse, void* ws, size_t ws_bytes,
                  void* hip_stream) {

@@ -37,7 +37,7 @@ EXPORTS = ("lagkv_plan", "lagkv_keep_for_compression", "lagkv_workspace_bytes", 
            "lagkv_append_and_compress", "lagkv_prefill", "lagkv_launch_hint", "lagkv_launch_hint_ex", "lagkv_path_for",
            "lagkv_kernel_for", "lagkv_strerror",
            "lagkv_version",
-           "lagkv_attend_workspace_bytes", "lagkv_attend", "lagkv_attend_blocks", "lagkv_block_bounds",
+           "lagkv_attend_workspace_bytes", "lagkv_attend_plan", "lagkv_attend", "lagkv_attend_blocks", "lagkv_block_bounds",
            "lagkv_select_blocks")
 
 
@@ -73,6 +73,10 @@ class AttendParams(C.Structure):
                 ("T", C.c_int64), ("scale", C.c_double),
                 ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3), ("new_stride", C.c_int64 * 3),
                 ("out_stride", C.c_int64 * 3), ("parents_stride_b", C.c_int64)]
+
+
+class AttendPlanT(C.Structure):
+    _fields_ = [("many_rows", C.c_int32), ("row_tile", C.c_int32), ("wavefronts", C.c_int32), ("pieces", C.c_int32)]
 
 
 def lib_path() -> str:
@@ -128,6 +132,8 @@ def load():
     ap = C.POINTER(AttendParams)
     lib.lagkv_attend_workspace_bytes.argtypes = [ap]
     lib.lagkv_attend_workspace_bytes.restype = sz
+    lib.lagkv_attend_plan.argtypes = [ap, C.POINTER(AttendPlanT)]
+    lib.lagkv_attend_plan.restype = C.c_int
     lib.lagkv_attend.argtypes = [ap] + [vp] * 10 + [sz, vp]
     lib.lagkv_attend.restype = C.c_int
     lib.lagkv_attend_blocks.argtypes = [ap] + [vp] * 11 + [sz, vp]
@@ -391,6 +397,13 @@ def compress_static(K: torch.Tensor, V: torch.Tensor, S: int, L: int, r: float, 
 # ---- operators that read a cache (include/lagkv.h, "Operators that read a cache") ----
 
 TREE_MAX = 256
+
+
+def attend_plan(p: AttendParams) -> AttendPlanT:
+    """lagkv_attend_plan: the launch shape of an attend (with n_blocks an attend_blocks) call with these parameters."""
+    out = AttendPlanT()
+    _check(load().lagkv_attend_plan(C.byref(p), C.byref(out)), "lagkv_attend_plan")
+    return out
 
 
 @dataclass
