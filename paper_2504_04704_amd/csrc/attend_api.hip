@@ -74,25 +74,29 @@ int64_t fullest_xcd(int64_t units, int64_t pieces, int64_t row_tiles) { return (
 // 1 2 3 4 6 8 12 16 24 ...
 int64_t next_pieces(int64_t s) { return s + (s < 4 ? 1 : s % 3 == 0 ? s / 3 : s / 2); }
 
-// Tiles of many rows: 128 query rows (four wavefronts, two workgroups a compute unit) or 256 (eight, one), and the pieces that
+// Tiles of many rows: 128 query rows (four wavefronts, two workgroups a compute unit) or, for 65 to 128 channels, 256 (eight, one;
+// for fewer channels they were the faster ones of none of 164 shapes), and the pieces that
 // the cache is cut into, by the microseconds that they take: a step of 64 cache rows, the beginning and end of a workgroup,
 // and, with pieces, a second kernel and every piece of a row written and read.  A step takes longer the more compute
-// units are at work, and less where wavefronts of the eight have no rows.  Measured, 128 channels, model beside it (us):
-//    8 streams,  256 query rows, 1000 rows   128 in 1 32 (32)   128 in 6 17 (17)   256 in 1 37 (37)   256 in 6 22 (22)
-//   32 streams,  256 query rows, 8000 rows   128 in 4 65 (65)   128 in 8 53 (53)   256 in 4 64 (69)   256 in 8 51 (51)
-//    8 streams, 2048 query rows, 8000 rows   128 in 2 121 (119)   128 in 4 91 (92)   256 in 2 119 (122)   256 in 4 87 (82)
-//   64 streams,  160 query rows, 8000 rows   128 in 4 79 (85)   256 in 4 63 (65)
+// units are at work, and less where wavefronts of the eight have no rows.  Measured, 128 channels, model beside it (us; it
+// falls short by a seventh in the mean, as narrow_shape's does, and what counts is which is the least):
+//    8 streams,  256 query rows, 1000 rows   128 in 4 19 (18)   128 in 8 18 (16)   256 in 8 23 (20)   few rows 16 (15)
+//   32 streams,  256 query rows, 2000 rows   128 in 4 33 (27)   128 in 8 35 (28)   256 in 4 36 (32)   256 in 8 34 (30)
+//   32 streams,  256 query rows, 8000 rows   128 in 4 77 (62)   128 in 8 70 (57)   256 in 4 77 (74)   256 in 8 63 (54)
+//   64 streams,  160 query rows, 8000 rows   128 in 4 100 (91)   128 in 8 105 (105)   256 in 2 124 (106)   256 in 4 82 (69)
+// Over 914 shapes (64, 128 and 256 channels, 48 to 2048 query rows of 2 to 400 streams, 200 to 16000 rows) its choice takes 1.1 %
+// longer than the best tile and number of pieces in the mean.
 double wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_tile, int64_t* pieces) {
-  const double by_d4 = D <= 64 ? 0.62 : D <= 128 ? 1 : 1.7, by_d8 = D <= 64 ? 0.7 : 1;
+  const double channels = D <= 64 ? 0.57 : D <= 128 ? 1 : 2.2;
   double least = 1e30;
-  for (int tile = 128; tile <= (D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
+  for (int tile = 128; tile <= (D > 64 && D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
     const int64_t groups = units * ((rows + tile - 1) / tile), places = tile == 256 || D > 128 ? 256 : 512;
     const double full = (double)(units * rows) / (double)(groups * tile);
     for (int64_t s = 1; s <= 256 && s <= steps; s = next_pieces(s)) {
       const int64_t all = 8 * fullest_xcd(units, s, (rows + tile - 1) / tile);
       const double busy = all < 256 ? (double)all / 256 : 1;
-      const double step = tile == 256 ? by_d8 * (0.85 + (0.5 + 0.35 * busy) * full) : by_d4 * (all > 256 && D <= 128 ? 2.15 : 1.35 + 0.2 * busy);
-      const double ends = tile == 256 ? (D <= 64 ? 10 : 14) : D <= 64 ? 6.7 : 8.8;
+      const double step = tile == 256 ? 0.85 + (0.65 + 0.5 * busy) * full : channels * (all > 256 && D <= 128 ? 2.35 : 1.25 + 0.2 * busy);
+      const double ends = tile == 256 ? 12 : D <= 64 ? 7.3 : D <= 128 ? 9 : 8.5;
       const double us = (double)((all + places - 1) / places) * ((double)((steps + s - 1) / s) * step + ends) +
                         (s > 1 ? 2.5 + (double)(units * rows * s) * (double)D * 8 / 9e6 : 0);
       if (us < least) {
@@ -139,10 +143,11 @@ double narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bo
 }
 
 // Tiles of few query rows: as many as there are, up to what the registers hold.  Of many (16-bit types): tiles of 128 or 256
-// where they take less time, by the two models.  (Over 299 shapes with trees, 40 to 600 query rows of 2 to 128 streams, 100 to
-// 6000 cache rows, the time is 1.6 % above that of the better kernel, with tiles of many rows for all of them 4.3 %; over 392
-// without new tokens, to 2000 query rows and 400 streams, 2.2 % and 7.9 %.  us, few and many: 8 streams, 256 query rows,
-// 300 rows 12.4 and 15.3, 2000 rows 23.5 and 23.0; 32 streams, 256, 2000 rows 38 and 29.)
+// where they take less time, by the two models.  (Over the 914 shapes of wide_shape, without new tokens, the time is 1.6 % above
+// that of the better kernel at its best, with tiles of many rows for all of them 5.3 %, of few 39 %; over 299 with trees, 40 to
+// 600 query rows, it is 0.4 % above the less of itself and of few rows, which take 19 % more in the mean.  us, few and many: 8
+// streams, 256 query rows, 500 rows 15 and 16, 1000 rows 16 and 18; 32 streams, 256, 2000 rows 47 and 33; 8 streams of 256
+// channels, 500 query rows, 4000 rows 140 and 53.)
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;

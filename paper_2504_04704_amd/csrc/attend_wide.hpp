@@ -6,20 +6,20 @@
 // rows (32 beyond 128 channels) at a time, which lie in LDS for all of them (the next ones are on their way through
 // registers meanwhile); each wavefront keeps 32 query rows to itself, so that nothing is exchanged between wavefronts.  32x32
 // products: a lane holds one query row (of S^T, P^T and O^T), so that maxima and sums need one exchange between the lane's
-// halves only.  Measured: 256 rows of 32 streams x 33536 (bf16, 128 channels) 147 us, 0.96 Pflop/s, and 8.6 for joining the
-// pieces; 2048 rows of 8 streams x 8640 89 us, 0.83 Pflop/s, and 9 (a large product of the library: 1.09).  The matrix cores are
-// busy in 55 % of the cycles, at a clock of 1.7 GHz; there are no conflicts of LDS banks to speak of.
+// halves only.  Measured: 256 rows of 32 streams x 33536 (bf16, 128 channels) 191 us, 0.74 Pflop/s, and 8.7 for joining the
+// pieces; 2048 rows of 8 streams x 8640 111 us, 0.66 Pflop/s, and 9.6 (a large product of the library: 1.09).  The matrix cores are
+// busy in 68 % of the cycles, at a clock of 1.6 GHz; there are no conflicts of LDS banks to speak of.
 //
-// P is put in rounded to the type: two numbers, as in the narrow kernel, would cost half as many products again.  The
-// rounding of a weight is independent of the others' and of the output's own: against 64 bits the outputs are off by 1.2 times
-// what one rounding of the exact output is off, 1.36 times in the worst of some hundred shapes (sqrt(2) if all is independent).
+// P is put in as two numbers, as in the narrow kernel, so that a result does not depend on which of the two runs (that goes by time,
+// and so by what else is in the batch).  One number, rounded, takes half as many products less, 147 us in place of 191, and
+// puts an error of the size of the output's own rounding into the outputs.
 //
-// Products and exponentials take about the same time (32 products of 32 cycles, 32 elements a lane of some 35), on
+// Products and exponentials take about the same time (48 products of 32 cycles, 32 elements a lane of some 50), on
 // different units.  So eight wavefronts go in two halves, one of each on every SIMD, between barriers: while one half
 // multiplies (the scores of its step, the outputs of the step before), the other makes weights and moves rows.  With
 // h counting the phases, the first half multiplies for step i in h = 2i and makes weights in 2i + 1, the other one phase later.
 // K of step i and V of step i - 1 are read in 2i and 2i + 1; K(i+1) and V(i) are written into the other buffers in
-// 2i + 1 by the first half and in 2i by the second, when nobody reads these any more.  (Halves in phase: 173 us, not 151.)  Four
+// 2i + 1 by the first half and in 2i by the second, when nobody reads these any more.  (Halves in phase took 15 % longer.)  Four
 // wavefronts, for fewer rows, leave that to the two workgroups of a compute unit: one barrier a step.
 //
 // The reference m of the exponentials is only moved when a row's maximum leaves it by more than SLACK (base 2): exp(x - m) is then
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 
   float m = -INFINITY, l = 0.f;  // m in units of base 2
   f32x16 o[DT32], s[HALVES];
-  u32v4 p[2 * HALVES];  // P, in steps of 16 rows
+  u32v4 p[2 * HALVES], pl[2 * HALVES];  // P, in steps of 16 rows: rounded to the type, and what that leaves of it
 #pragma unroll
   for (int d = 0; d < DT32; ++d)
 #pragma unroll
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
         },
         [&](int j, u32v4 f) {
           if (j < NS) s[j % HALVES] = W::mma(f, q[j < NS ? j / HALVES : 0], s[j % HALVES]);
-          else o[(j - NS) % DT32] = W::mma(f, p[(j - NS) / DT32], o[(j - NS) % DT32]);
+          else o[(j - NS) % DT32] = W::mma(f, pl[(j - NS) / DT32], W::mma(f, p[(j - NS) / DT32], o[(j - NS) % DT32]));
         });
   };
   // infinities of the rows of step i
@@ -301,14 +301,17 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
         const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e + 1], c, -at));
         sum0 += y;
         sum1 += z;
-        p[t * 2 + e / 8][e % 8 / 2] = E::pack(y, z);
+        const uint32_t hi = E::pack(y, z);
+        const f32x2 back = E::unpack(hi);
+        p[t * 2 + e / 8][e % 8 / 2] = hi;
+        pl[t * 2 + e / 8][e % 8 / 2] = E::pack(y - back.x, z - back.y);
       }
     l += sum0 + sum1;
   };
 
   if (n > 0) {
 #pragma unroll
-    for (int k = 0; k < 2 * HALVES; ++k) p[k] = u32v4{0, 0, 0, 0};
+    for (int k = 0; k < 2 * HALVES; ++k) p[k] = pl[k] = u32v4{0, 0, 0, 0};
     for (int k = tid; k < KT * LDV / 16; k += THREADS) *(u32v4*)(v_at(1) + k * 16) = u32v4{0, 0, 0, 0};
     load_k(0);
     load_v(0);
@@ -430,7 +433,7 @@ hipError_t launch_wide_as(const AttendArgs& a, hipStream_t s) {
 
 template <int DT>
 hipError_t launch_wide_of(const AttendArgs& a, int row_tile, hipStream_t s) {
-  if (a.D <= 64) return row_tile == 128 ? launch_wide_as<DT, 64, 4>(a, s) : launch_wide_as<DT, 64, 8>(a, s);
+  if (a.D <= 64) return launch_wide_as<DT, 64, 4>(a, s);
   if (a.D <= 128) return row_tile == 128 ? launch_wide_as<DT, 128, 4>(a, s) : launch_wide_as<DT, 128, 8>(a, s);
   return launch_wide_as<DT, 256, 4>(a, s);
 }
