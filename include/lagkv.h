@@ -348,7 +348,8 @@ int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out);
  *   out  dtype of Q; a row that sees nothing is 0.  May be Q itself (with Q's strides), and overlap no other input.
  *   lse  [B, H*G, N] device fp32, dense, or NULL: log sum exp of the logits, natural; -inf where nothing is seen
  * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold;
- * one that it sees does: an output with a logit that is no number is none.
+ * one that it sees does: an output with a logit that is no number is none, and one with an infinite value is infinite (NaN with
+ * two of either sign, or where the row's weight is too small to be held: below 2^-34 of the largest in fp16, 2^-126 else).
  * Logits, sums and products are held in fp32, and weights go into the products with V as fp32 or as two numbers of the type (16
  * bits of them in bf16, 22 in fp16), whichever kernel runs; results do not depend on anything but the arguments (no atomics).
  * N = 0: LAGKV_OK, nothing is done.  T = 0 is allowed (K, V may be NULL then).

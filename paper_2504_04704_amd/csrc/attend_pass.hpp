@@ -15,7 +15,7 @@
 // V^T needs four cache rows of one channel in a lane: V goes through LDS, into memory private to the wavefront, and
 // comes back through the transposing read (16-bit types) or element by element (fp32).
 //
-// P is put in as the sum of two 16-bit numbers (the value rounded, and what the rounding left): one alone would add as
+// P is put in as the sum of two 16-bit numbers (the value's leading bits, and the rest): one alone would add as
 // much error to the output as its own rounding, and the pass is bound by memory where tiles are small.
 //
 // Bound by memory where the rows of K and V are many (four query rows of 256 streams of up to 8384 rows, bf16: 151 to 155 us,
@@ -60,6 +60,11 @@ __device__ __forceinline__ float sum_across_32(float x) {
   return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
+// What is left of a weight x >= 0 beside its leading bits: at least the type's smallest number, if x is not 0.  Both parts of
+// a weight are then of one sign, and their products with an infinity add up to it: a rest of 0 or below would make them NaN.
+// (x - lead <= x, so that the middle one of the three is this.)
+__device__ __forceinline__ float rest_of(float x, float lead, float smallest) { return __builtin_amdgcn_fmed3f(x - lead, smallest, x); }
+
 template <int DT>
 struct AElem;
 template <>
@@ -79,7 +84,12 @@ struct AElem<LAGKV_BF16> {
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
   }
-  static __device__ __forceinline__ f32x2 unpack(uint32_t v) { return f32x2{__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)}; }
+  // x and y >= 0 as pairs of numbers of the type: the leading bits, and the rest rounded
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+    hi = __builtin_amdgcn_perm(b, a, 0x07060302);
+    lo = pack(rest_of(x, __uint_as_float(a & 0xffff0000u), 0x1p-126f), rest_of(y, __uint_as_float(b & 0xffff0000u), 0x1p-126f));
+  }
   static __device__ __forceinline__ float one(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 };
 template <>
@@ -95,7 +105,11 @@ struct AElem<LAGKV_F16> {
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, f16x2));
   }
-  static __device__ __forceinline__ f32x2 unpack(uint32_t v) { return __builtin_convertvector(__builtin_bit_cast(f16x2, v), f32x2); }
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+    const f32x2 back = __builtin_convertvector(__builtin_bit_cast(f16x2, hi), f32x2);
+    lo = pack(rest_of(x, back.x, 0x1p-24f), rest_of(y, back.y, 0x1p-24f));
+  }
   static __device__ __forceinline__ float one(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
 };
 
@@ -533,11 +547,10 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
         for (int s = 0; s < SUBS; ++s)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float x = p[rt][s][2 * i], y = p[rt][s][2 * i + 1];
-            const uint32_t hi = E::pack(x, y);
-            const f32x2 back = E::unpack(hi);
+            uint32_t hi, lo;
+            E::split(p[rt][s][2 * i], p[rt][s][2 * i + 1], hi, lo);
             ph[rt][s * 2 + i] = hi;
-            pl[rt][s * 2 + i] = E::pack(x - back.x, y - back.y);
+            pl[rt][s * 2 + i] = lo;
           }
 #pragma unroll
       for (int d = 0; d < DT16; ++d) {

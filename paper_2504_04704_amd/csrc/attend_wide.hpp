@@ -216,7 +216,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 
   float m = -INFINITY, l = 0.f;  // m in units of base 2
   f32x16 o[DT32], s[HALVES];
-  u32v4 p[2 * HALVES], pl[2 * HALVES];  // P, in steps of 16 rows: rounded to the type, and what that leaves of it
+  u32v4 p[2 * HALVES], pl[2 * HALVES];  // P, in steps of 16 rows: its leading bits, and the rest
 #pragma unroll
   for (int d = 0; d < DT32; ++d)
 #pragma unroll
@@ -301,10 +301,10 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
         const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e + 1], c, -at));
         sum0 += y;
         sum1 += z;
-        const uint32_t hi = E::pack(y, z);
-        const f32x2 back = E::unpack(hi);
+        uint32_t hi, lo;
+        E::split(y, z, hi, lo);
         p[t * 2 + e / 8][e % 8 / 2] = hi;
-        pl[t * 2 + e / 8][e % 8 / 2] = E::pack(y - back.x, z - back.y);
+        pl[t * 2 + e / 8][e % 8 / 2] = lo;
       }
     l += sum0 + sum1;
   };

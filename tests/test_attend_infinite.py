@@ -1,0 +1,78 @@
+"""Infinite numbers in rows of a cache that are seen: what the formulas give for them is what comes out, of every kernel."""
+import math
+
+import pytest
+import torch
+
+import attend_util as A
+from paper_2504_04704_amd import lagkv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, HF, FL = torch.bfloat16, torch.float16, torch.float32
+CODE = {BF: lagkv.BF16, HF: lagkv.F16, FL: lagkv.F32}
+
+
+def rand(*shape, dtype, seed, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * scale).to(dtype).to(DEV)
+
+
+def problem(dtype, H, G, N, D, T, seed):
+    return (rand(1, H * G, N, D, dtype=dtype, seed=seed), rand(1, H, T, D, dtype=dtype, seed=seed + 1),
+            rand(1, H, T, D, dtype=dtype, seed=seed + 2), rand(1, H, N, D, dtype=dtype, seed=seed + 3), rand(1, H, N, D, dtype=dtype, seed=seed + 4))
+
+
+def same(got, want, where):
+    """got.out and got.lse against a form in 64 bits that holds infinities and NaN."""
+    out, lse, tol, tol_lse = want
+    for g, w, t in ((got.out, out, tol), (got.lse, lse, tol_lse)):
+        g = g.cpu().double()
+        odd = ~torch.isfinite(w)
+        assert bool(((g == w) | (torch.isnan(g) & torch.isnan(w)))[odd].all()), where
+        assert bool((abs(g - w)[~odd] <= t[~odd]).all()), where
+
+
+SIZES = [  # copies, H, G, N, D, T, kernel of many rows
+    (1, 2, 3, 1, 64, 90, False), (1, 1, 4, 3, 128, 70, False), (2, 1, 4, 7, 100, 700, False), (1, 1, 4, 1, 128, 5000, False),
+    (1, 2, 2, 2, 256, 100, False), (1200, 1, 4, 20, 64, 90, True), (1200, 1, 2, 40, 128, 300, True), (1200, 1, 4, 10, 256, 90, True),
+    (1200, 1, 4, 65, 100, 300, True), (4, 2, 4, 64, 128, 2000, True), (1200, 2, 4, 40, 128, 700, True),
+]
+
+
+def call(size, dtype, args):
+    copies, H, G, N, D, T, many = size
+    x = lagkv.attend_plan(lagkv.AttendParams(copies, H, G, N, D, CODE[dtype], 0, 0, T, 0.1))
+    assert bool(x.many_rows) == (many and dtype != FL)
+    got = lagkv.attend(*(t.expand(copies, *t.shape[1:]) for t in args), want_lse=True)
+    assert bool((got.out.nan_to_num(7.0) == got.out[:1].nan_to_num(7.0)).all())
+    return lagkv.Attended(got.out[:1], got.lse[:1])
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_infinite_values(size, dtype):
+    copies, H, G, N, D, T, _ = size
+    print("[gpu-test] infinite values", size, dtype, flush=True)
+    args = q, K, V, Kn, Vn = problem(dtype, H, G, N, D, T, D + T)
+    V[0, 0, T // 2, 3] = math.inf
+    V[0, 0, T - 1, D - 1] = -math.inf
+    V[0, 0, 0, 5], V[0, 0, T // 3, 5] = math.inf, -math.inf
+    V[0, 0, 7, 6] = math.nan
+    want = A.attend(q, K, V, Kn, Vn)
+    assert bool((want[0][0, :G, :, 3] == math.inf).all()) and bool((want[0][0, :G, :, D - 1] == -math.inf).all())
+    assert bool(torch.isnan(want[0][0, :G, :, 5:7]).all())
+    same(call(size, dtype, args), want, "in the cache")
+    if N == 1 and copies == 1:                       # the same row, not appended yet
+        Vn[0, 0, 0, 9], V[0, 0, 11, 9] = math.inf, math.inf
+        same(call(size, dtype, args), A.attend(q, K, V, Kn, Vn), "in both")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("k", [4, 100])
+def test_infinite_values_in_listed_blocks(dtype, k):
+    q, K, V, Kn, Vn = problem(dtype, 2, 4, 3, 128, 3000, 5)
+    blocks = torch.stack([torch.randperm(188, generator=torch.Generator().manual_seed(i))[:k] for i in range(6)]).view(1, 2, 3, k).to(torch.int32)
+    for n in range(3):
+        V[0, 1, int(blocks[0, 1, n, k // 2]) * 16 % 2990, 3 + n] = math.inf
+    got = lagkv.attend_blocks(q, K, V, blocks.to(DEV), 16, Kn, Vn, want_lse=True)
+    same(got, A.attend(q, K, V, Kn, Vn, blocks=blocks, block=16), str(k))
