@@ -347,6 +347,7 @@ int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out);
  *     value says that n is no token (padding): it sees nothing, nothing sees it, and a path up the tree ends before it.
  *   out  dtype of Q; a row that sees nothing is 0.  May be Q itself (with Q's strides), and overlap no other input.
  *   lse  [B, H*G, N] device fp32, dense, or NULL: log sum exp of the logits, natural; -inf where nothing is seen
+ * A row whose logits are all -inf is taken for one that sees nothing.
  * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold;
  * one that it sees does: an output with a logit that is no number is none, and one with an infinite value is infinite (NaN with
  * two of either sign, or where the row's weight is too small to be held: below 2^-34 of the largest in fp16, 2^-126 else).

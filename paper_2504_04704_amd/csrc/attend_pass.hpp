@@ -123,10 +123,28 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 
 // Channel at which the c-th 16-byte slice of a row of D begins: the last one of a row that is no whole number of slices
 // is taken from the row's end, so that nothing behind the row is read.  The channels it shares with the slice before it
-// are zeroed in q (they count once) and not stored (they come out twice).
+// are zeroed in q and in k (they count once, and 0 alone in one of them would make an infinity there NaN) and not stored (they
+// come out twice).
 __device__ __forceinline__ int slice_at(int c, int D, int per) {
   const int at = c * per;
   return at + per <= D ? at : D - per;
+}
+// The slice v that begins at channel `begin` of a row of D, in place of which slice_at's was loaded: 0 where it has no channels of
+// its own.  (Worked out where it is used: kept, the conditions take more scalar registers than there are.)
+template <int PER>
+__device__ __forceinline__ u32v4 own_channels(u32v4 v, int begin, int D) {
+  asm volatile("" : "+v"(begin));
+  if (begin >= D) v = u32v4{0, 0, 0, 0};
+  if (D % PER != 0) {
+    const bool part = begin < D && begin + PER > D;
+    const int dup = PER - D % PER;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t own = PER == 4 ? (i < dup ? 0u : ~0u) : (2 * i < dup ? 0u : 0x0000ffffu) | (2 * i + 1 < dup ? 0u : 0xffff0000u);
+      v[i] &= part ? own : ~0u;
+    }
+  }
+  return v;
 }
 
 // Asks for every line of the kernel's arguments at once.  They lie in host memory, and the compiler loads them where they
@@ -303,13 +321,14 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
     return x;
   };
   // K: lane (col, grp) has row col of each sixteen, slices grp, 4 + grp, ...: what its operand takes.  V: whole rows, a slice
-  // a lane.  Slices behind a row's last repeat another: q is 0 there, and what V gives for them is not stored.
+  // a lane.  Slices behind a row's last repeat another: q and K are made 0 there, and what V gives for them is not stored.
   u32v4 kf[SUBS][NC], vf[NV];
   const int vslice = lane % CPR, vrow = lane / CPR;
   auto offset = [&](int slice) { return (slice * PER < a.D ? slice_at(slice, a.D, PER) : 0) * E::SIZE; };
   int koff[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) koff[c] = offset(c * 4 + grp);
+  auto own = [&](int c, u32v4 v) { return own_channels<PER>(v, (c * 4 + grp) * PER, a.D); };
   const int64_t klane = (int64_t)col * a.kst, vlane = (int64_t)vrow * a.kst + offset(vslice), vpass = a.kst * VROWS;
   auto load_k = [&](const Step& x) {
     if (x.whole) {
@@ -390,17 +409,8 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int begin = (c * 4 + grp) * PER, dup = begin - koff[c] / E::SIZE;
-      u32v4 v = q[rt][c];
-      if (row0 + rt * 16 + col >= row1 || begin >= a.D) v = u32v4{0, 0, 0, 0};
-      if (a.D % PER != 0) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (i < dup) {
-            if constexpr (E::SIZE == 4) v[i] = 0;
-            else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
-          }
-      }
+      u32v4 v = own(c, q[rt][c]);
+      if (row0 + rt * 16 + col >= row1) v = u32v4{0, 0, 0, 0};
       asm volatile("" : "+v"(v));
       q[rt][c] = v;
     }
@@ -453,6 +463,12 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
     if (more) load_v(next);
     __builtin_amdgcn_sched_barrier(0);
 
+    if (a.D != DP) {
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int c = DP > 64 ? NC / 2 : 0; c < NC; ++c) kf[s][c] = own(c, kf[s][c]);
+    }
     f32x4 p[RT][SUBS];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)

@@ -123,7 +123,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   const char* knb = a.K_new + b * a.nsb + h * a.nsh;
   const char* vnb = a.V_new + b * a.nsb + h * a.nsh;
   // This thread's slice of each row it loads, and where it is in the next step's first row.  (Slices behind a row's last
-  // repeat its last: q is 0 there, and what V gives for them is not stored.)
+  // repeat its first: q and K are made 0 there, and what V gives for them is not stored.)
   const int lslice = tid % CPR, lrow = tid / CPR;
   const int loff = (lslice * 8 < a.D ? slice_at(lslice, a.D, 8) : 0) * 2;
   constexpr int LROWS = THREADS / CPR;
@@ -174,6 +174,13 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     to += lrow * ld + lslice * 16;
 #pragma unroll
     for (int k = 0; k < PASSES; ++k) *(u32v4*)(to + k * LROWS * ld) = from[k];
+  };
+  auto store_k = [&](int i) {
+    if (a.D != DP) {
+#pragma unroll
+      for (int k = 0; k < PASSES; ++k) kr[k] = own_channels<8>(kr[k], lslice * 8, a.D);
+    }
+    store(kr, k_at(i), LDK);
   };
   auto store_v = [&](int i) {
     if (i >= n_whole && i < n) {
@@ -321,21 +328,15 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     // first rows' loads, and not with what else is on its way in every step.)
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      const int begin = (2 * k + half) * 8, dup = begin < a.D ? begin - slice_at(2 * k + half, a.D, 8) : 0;
-      u32v4 v = mine && begin < a.D ? q[k] ^ flip : u32v4{0, 0, 0, 0};
-      if (a.D % 8 != 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < dup) v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
-      }
+      u32v4 v = mine ? own_channels<8>(q[k] ^ flip, (2 * k + half) * 8, a.D) : u32v4{0, 0, 0, 0};
       asm volatile("" : "+v"(v));
       q[k] = v;
     }
-    store(kr, k_at(0), LDK);
+    store_k(0);
     load_k(1);
     __syncthreads();
     if (late) {
-      store(kr, k_at(1), LDK);
+      store_k(1);
       store_v(0);
       load_k(2);
       load_v(1);
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
       if (WAVES == 8) __syncthreads();  // (four wavefronts write buffers that nobody reads in this step)
       if (i < n) {
         if (!idle) weights(i);
-        store(kr, k_at(i + late + 1), LDK);  // (behind the last step: what was there)
+        store_k(i + late + 1);  // (behind the last step: what was there)
         store_v(i + late);
         load_k(i + late + 2);
         load_v(i + late + 1);

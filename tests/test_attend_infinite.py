@@ -76,3 +76,50 @@ def test_infinite_values_in_listed_blocks(dtype, k):
         V[0, 1, int(blocks[0, 1, n, k // 2]) * 16 % 2990, 3 + n] = math.inf
     got = lagkv.attend_blocks(q, K, V, blocks.to(DEV), 16, Kn, Vn, want_lse=True)
     same(got, A.attend(q, K, V, Kn, Vn, blocks=blocks, block=16), str(k))
+
+
+KEYS = [  # copies, H, G, N, D, T, kernel of many rows
+    (1, 2, 3, 1, 64, 90, False), (1, 1, 4, 1, 72, 90, False), (1, 1, 2, 1, 41, 300, False), (1, 1, 4, 3, 100, 70, False),
+    (2, 1, 4, 7, 80, 700, False), (1, 1, 4, 1, 128, 5000, False), (1, 2, 2, 2, 250, 100, False), (1, 1, 8, 1, 8, 50, False),
+    (1, 1, 3, 2, 13, 50, False), (1, 1, 4, 1, 200, 3000, False),
+    (1200, 1, 4, 20, 64, 90, True), (1200, 1, 2, 40, 96, 300, True), (1200, 1, 4, 10, 200, 90, True), (1200, 1, 4, 20, 41, 90, True),
+    (1200, 1, 4, 65, 100, 300, True), (4, 2, 4, 64, 120, 2000, True), (1200, 2, 4, 40, 84, 700, True),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", KEYS, ids=lambda s: "x".join(map(str, s)))
+def test_keys_that_make_a_logit_infinite(size, dtype):
+    """A logit of -inf is a weight of 0, whichever channel has the infinity; one of inf leaves no number."""
+    copies, H, G, N, D, T, _ = size
+    print("[gpu-test] infinite keys", size, dtype, flush=True)
+    args = q, K, V, Kn, Vn = problem(dtype, H, G, N, D, T, D + T)
+    channels = sorted({0, 3, D // 2, D - 7, D - 1})
+    rows = [T // 2 + i for i in range(len(channels))]
+    for t, c in zip(rows, channels):
+        q[..., c] = q[..., c].abs() + 0.25
+        K[:, :, t, c] = -math.inf
+    keep = [t for t in range(T) if t not in rows]
+    want = A.attend(q, K[:, :, keep], V[:, :, keep], Kn, Vn)
+    same(call(size, dtype, args), want, "-inf")
+    if N == 1:
+        Kn[:, :, 0, channels[1]] = -math.inf
+        same(call(size, dtype, args), A.attend(q, K[:, :, keep], V[:, :, keep]), "-inf of the token")
+        blocks = torch.arange(-(-T // 16), dtype=torch.int32).expand(1, H, 1, -1).contiguous()
+        got = lagkv.attend_blocks(q, K, V, blocks.to(DEV), 16, Kn, Vn, want_lse=True)
+        same(got, A.attend(q, K[:, :, keep], V[:, :, keep]), "-inf, listed")
+    K[:, 0, T // 3, channels[0]] = math.inf
+    got = call(size, dtype, args)
+    assert bool(torch.isnan(got.out[:, :G]).all()) and bool(torch.isfinite(got.out[:, G:]).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", [(1, 1, 4, 1, 100, 70, False), (1, 1, 4, 1, 64, 5000, False), (1200, 1, 2, 40, 96, 300, True)], ids=lambda s: "x".join(map(str, s)))
+def test_no_logit_above_minus_infinity(size, dtype):
+    """As if nothing were seen: 0, and -inf as the logarithm of the denominator."""
+    copies, H, G, N, D, T, _ = size
+    args = q, K, V, Kn, Vn = problem(dtype, H, G, N, D, T, D + T)
+    q[..., 1] = 1.0
+    K[..., 1], Kn[..., 1] = -math.inf, -math.inf
+    got = call(size, dtype, args)
+    assert bool((got.out == 0).all()) and bool((got.lse == -math.inf).all())
