@@ -382,7 +382,8 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
  *     sum over the head's G query rows and the channels of max(q lo, q hi),
  * which no row of the block exceeds with its sum of q.k; of equal ones the lower.  The first `n_first` and the last `n_last`
  * of the blocks that lengths[b] leaves are always among them (n_first + n_last <= n_blocks).  Scores are summed in 64 bits.
- * A block whose score is no number, as one with an infinite bound may be, comes behind all others.
+ * A block whose score is not finite comes behind all others.  (An infinite bound alone does not make it so: with q < 0 and hi =
+ * inf it is q lo that counts.)
  *   lo, hi [B, H, ceil(T / block), D] device, type of Q, both with kv_stride_* (b, h, block)
  *   blocks [B, H, N, n_blocks] device int32, dense: ascending; -1 behind the last where there are fewer blocks
  * Of p the fields B, H, G, N, D, dtype, T, block, n_blocks, q_stride_* and kv_stride_* are read.  Workspace: 8 * B * H * N *

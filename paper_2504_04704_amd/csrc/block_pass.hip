@@ -7,6 +7,11 @@
 // and q lo for q < 0, so the heads' sum is P.hi + M.lo with P = sum_g max(q_g, 0) and M = sum_g min(q_g, 0): one pass over
 // the bounds, whatever G.  Scores are summed in 64 bits: products of two 16-bit numbers are exact there and their sums
 // nearly always, so that which of two blocks is taken does not hang on the order in which a kernel adds.
+//
+// With an infinite bound P.hi + M.lo is infinite or no number, while max(q lo, q hi) may be finite (q < 0, hi = inf), and where a
+// P or M is 0 only because a lane has no channel there it says nothing at all.  Finite numbers never add up to such a score: a
+// score that is not finite is worked out again, head by head and channel by channel (score_again).  What is infinite or none
+// even so comes behind all others: a bound of infinity is that of a logit which leaves attention without a number.
 #include "attend_pass.hpp"
 #include "row_ops.hpp"
 
@@ -191,6 +196,38 @@ __device__ __forceinline__ void query_slices(const SelectArgs& a, int64_t b, int
   }
 }
 
+__device__ __forceinline__ bool is_finite(double s) { return __builtin_fabs(s) < (double)INFINITY; }
+
+// s[j] of token n as it is defined, NaN where that is not finite.  One lane's work, in the order of the channels.  (Blocks without
+// rows, whose bounds are infinite, are nobody's choice: they are left.)
+template <int DT>
+__device__ __forceinline__ void score_again(const SelectArgs& a, int64_t stream, int n, int64_t j) {
+  using ET = typename Of<DT>::T;
+  constexpr int VEC = ET::VEC, SIZE = 16 / VEC;
+  const int64_t b = (uint32_t)stream / (uint32_t)a.H, h = (uint32_t)stream % (uint32_t)a.H;
+  if (j * a.block >= rows_held(a.lengths, b, a.T)) return;
+  const int64_t bound = b * a.bsb + h * a.bsh + j * a.bst;
+  const char* q = a.Q + b * a.qsb + h * a.G * a.qsh + (int64_t)n * a.qsn;
+  double s = 0;
+#pragma unroll 1
+  for (int c = 0; c * VEC < a.D && is_finite(s); ++c) {
+    const int at = slice_at(c, a.D, VEC), dup = c * VEC - at;
+    float lo[VEC], hi[VEC], x[VEC];
+    unpack<ET>(ld16_any(a.lo + bound + at * SIZE), lo);
+    unpack<ET>(ld16_any(a.hi + bound + at * SIZE), hi);
+#pragma unroll 1
+    for (int g = 0; g < a.G; ++g) {
+      unpack<ET>(ld16_any(q + g * a.qsh + at * SIZE), x);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const double l = (double)x[i] * lo[i], u = (double)x[i] * hi[i];
+        if (i >= dup) s += l > u ? l : l == l ? u : l;  // (NaN if either is)
+      }
+    }
+  }
+  a.score[(stream * a.N + n) * a.nb + j] = is_finite(s) ? s : __builtin_nan("");
+}
+
 // Scores of one, two or three tokens: a wavefront takes 16 blocks, LPR lanes a block; the bounds are on their way while P
 // and M are made.  Bound by reading the bounds (34 MB, 32 streams x 2048 blocks: 9 us traced, 6.6 at a copy's rate) and the
 // latency of q, of the sums and of the launch; 64-bit products of two tokens take as long as that (beyond three tokens the
@@ -211,6 +248,7 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
   const int at = slice * VEC < a.D ? slice_at(slice, a.D, VEC) : 0;
   const int64_t jw = j0 + wave * 16;
   const int passes = (16 + step - 1) / step;  // of `step` blocks
+  uint64_t again = 0;  // scores that are not finite: bit 16 n + block
   for (int p0 = 0; p0 < passes; p0 += AHEAD) {
     uint4 lo4[AHEAD], hi4[AHEAD];
 #pragma unroll
@@ -251,9 +289,16 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
           s1 = __builtin_fma(m[c], (double)lo[c], s1);
         }
         const double s = lanes_sum(s0 + s1, lpr);
-        if (slice == 0 && of < 16 && j < a.nb) a.score[(stream * a.N + n) * a.nb + j] = s;
+        if (slice == 0 && of < 16 && j < a.nb) {
+          a.score[(stream * a.N + n) * a.nb + j] = s;
+          if (!is_finite(s)) again |= 1ull << (n * 16 + of);
+        }
       }
     }
+  }
+  for (; again; again &= again - 1) {
+    const int bit = __builtin_ctzll(again);
+    score_again<DT>(a, stream, bit / 16, jw + bit % 16);
   }
 }
 
@@ -279,6 +324,7 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
   const int64_t stream = st, b = st / (uint32_t)a.H, h = st % (uint32_t)a.H;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int64_t j0 = (int64_t)(id - st * tiles) * kScoreBlocks * sets + wave * 16;
+  uint32_t again = 0;  // scores that are not finite: bit 4 set + i (eight sets at most)
   int here = 0;  // sets that are there
   while (here < sets && j0 - wave * 16 + here * kScoreBlocks < a.nb) ++here;
   uint4 lo4[NC], hi4[NC];
@@ -320,12 +366,19 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t to = j0 + set * kScoreBlocks + grp + 4 * i;
-      if (n < a.N && to < a.nb) a.score[(stream * a.N + n) * a.nb + to] = s[i];
+      if (n < a.N && to < a.nb) {
+        a.score[(stream * a.N + n) * a.nb + to] = s[i];
+        if (!is_finite(s[i])) again |= 1u << (4 * set + i);
+      }
     }
+  }
+  for (; again; again &= again - 1) {
+    const int bit = __builtin_ctz(again);
+    score_again<DT>(a, stream, n0 + col, j0 + bit / 4 * kScoreBlocks + grp + 4 * (bit % 4));
   }
 }
 
-// 64-bit key in the order of the scores (-0 like 0, what is no number below all); 0 is no key.
+// 64-bit key in the order of the scores (-0 like 0, what is no number below all; none is infinite); 0 is no key.
 __device__ __forceinline__ uint64_t score_key(double s) {
   if (s != s) return 1;
   const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
