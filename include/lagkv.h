@@ -354,6 +354,8 @@ int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out);
  * Logits, sums and products are held in fp32, and weights go into the products with V as fp32 or as two numbers of the type (16
  * bits of them in bf16, 22 in fp16), whichever kernel runs; results do not depend on anything but the arguments (no atomics).
  * N = 0: LAGKV_OK, nothing is done.  T = 0 is allowed (K, V may be NULL then).
+ * LAGKV_ESHAPE beyond 2^31 - 2^16 query rows (B*H*G*N) and beyond the workgroups of a grid: B*H, rounded up to a multiple of 8,
+ * times ceil(G*N / 16) below 2^23 always fits.
  */
 int lagkv_attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
                  const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse, void* ws,
@@ -363,6 +365,7 @@ int lagkv_attend(const lagkv_attend_params* p, const void* Q, const void* K, con
  * The same over listed blocks of the cache: `blocks` [B, H, N, n_blocks] device int32, dense, names for every token and KV
  * head the blocks (rows j*block .. j*block+block-1) that its G query heads read, as lagkv_select_blocks writes them.  An
  * entry outside the blocks that lengths[b] leaves (-1, say) stands for no rows; one that is listed twice counts twice.
+ * Here B*H*N, rounded up to a multiple of 8, times ceil(G / 16) below 2^23 always fits.
  */
 int lagkv_attend_blocks(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
                         const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out,
@@ -387,7 +390,8 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
  *   lo, hi [B, H, ceil(T / block), D] device, type of Q, both with kv_stride_* (b, h, block)
  *   blocks [B, H, N, n_blocks] device int32, dense: ascending; -1 behind the last where there are fewer blocks
  * Of p the fields B, H, G, N, D, dtype, T, block, n_blocks, q_stride_* and kv_stride_* are read.  Workspace: 8 * B * H * N *
- * ceil(T / block) bytes, 16-byte aligned.
+ * ceil(T / block) bytes, 16-byte aligned.  LAGKV_ESHAPE from B*H*N = 2^23 lists on, and from
+ * (B*H * ceil(ceil(T / block) / 64) + 7) * ceil(N / 16) = 2^24 on.
  */
 int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void* lo, const void* hi, const int32_t* lengths,
                         int32_t n_first, int32_t n_last, int32_t* blocks, void* ws, size_t ws_bytes, void* hip_stream);

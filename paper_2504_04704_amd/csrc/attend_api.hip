@@ -151,7 +151,8 @@ double narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bo
 bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
-  if (pl->units > kMost || !grid_fits(pl->units * pl->rows, 256)) return false;  // (the second kernel's grid)
+  const int64_t all_rows = pl->units * pl->rows;
+  if (pl->units > kMost || all_rows > kMostRows) return false;  // (they are numbered in 31 bits)
   const bool f32 = p->dtype == LAGKV_F32;
   const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
   auto steps_of = [&](int64_t kt) { return (seen + kt - 1) / kt + (p->N + kt - 1) / kt; };
@@ -179,11 +180,17 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
     splits = 1;
     pl->waves = 8;
   }
+  // one piece where the grids do not hold more
+  auto fits = [&](int64_t s) {
+    const int64_t join = all_rows >= kJoinByWave ? (all_rows + 3) / 4 : all_rows;
+    return grid_fits((pl->units * s + 7) / 8 * 8 * pl->row_tiles, pl->wide ? pl->row_tile * 2 : pl->waves * 64) && (s == 1 || grid_fits(join, 256));
+  };
+  if (!fits(splits)) splits = 1;
   pl->splits = (int)splits;
-  const int64_t parts = pl->units * splits * pl->rows, ld = (p->D + 3) & ~3;
+  const int64_t parts = all_rows * splits, ld = (p->D + 3) & ~3;
   pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
   pl->ws_bytes = splits > 1 ? pl->off_ml + ws_align_up((size_t)parts * 8) : 0;
-  return grid_fits((pl->units * splits + 7) / 8 * 8 * pl->row_tiles, 512);
+  return fits(splits);
 }
 
 int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
@@ -379,8 +386,7 @@ int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void*
   a.last = n_last;
   a.dtype = p->dtype;
   const int64_t units = (int64_t)p->B * p->H * p->N;
-  if (!grid_fits(units, 512) || !grid_fits((int64_t)p->B * p->H * (a.nb + 1), 256) ||
-      !grid_fits(((int64_t)p->B * p->H * ((a.nb + 63) / 64) + 7) * (((int64_t)p->N + 15) / 16), 256))
+  if (!grid_fits(units, 512) || !grid_fits(((int64_t)p->B * p->H * ((a.nb + 63) / 64) + 7) * (((int64_t)p->N + 15) / 16), 256))
     return LAGKV_ESHAPE;
   if (a.nb > 0 && (!ws || ws_bytes < 8 * (size_t)(units * a.nb) || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
   hipStream_t s = (hipStream_t)hip_stream;

@@ -83,6 +83,7 @@ struct SelectArgs {
 hipError_t launch_block_scores(const SelectArgs& a, hipStream_t s);
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t s);
 
+constexpr int kJoinByWave = 2048;  // rows from which a wavefront joins the pieces of one, else a workgroup
 constexpr int kMaxTree = 256;  // tokens of a drafted tree
 constexpr int kMinHead = 8, kMaxHead = 256;
 

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a) {
 template <int DT>
 static hipError_t launch_join_of(const AttendArgs& a, hipStream_t s) {
   const int64_t rows = a.units * a.rows;
-  if (rows >= 2048) attend_join_kernel<DT, 1><<<dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
+  if (rows >= kJoinByWave) attend_join_kernel<DT, 1><<<dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
   else attend_join_kernel<DT, 4><<<dim3((uint32_t)rows), dim3(256), 0, s>>>(a);
   return hipGetLastError();
 }

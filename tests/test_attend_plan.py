@@ -43,3 +43,45 @@ def test_shapes_are_ones_that_there_are_kernels_for(lib, dtype):
                         assert (x.pieces > 1) == (lagkv.load().lagkv_attend_workspace_bytes(C.byref(p)) > 0)
                         seen.add(kind)
     assert len(seen) == (3 if dtype == lagkv.F32 else 5)
+
+
+def status(lib, **kw):
+    return lib.lagkv_attend_plan(C.byref(params(**kw)), C.byref(lagkv.AttendPlanT()))
+
+
+def test_prompts_of_many_query_rows_are_taken(lib):
+    """What a call cannot do is what the grids and 31-bit numbers of rows do not hold, not less."""
+    whole = dict(B=4, H=8, G=4, T=0, D=128)
+    for N in (131071, 131072, 1 << 19):
+        assert status(lib, N=N, **whole) == lagkv.OK, N
+        assert status(lib, N=N, dtype=lagkv.F32, **whole) == lagkv.OK, N
+    # 2^31 - 2^16 query rows
+    assert status(lib, B=8, H=1, G=1, N=(1 << 28) - (1 << 13) - 1, D=64, T=0) == lagkv.OK
+    assert status(lib, B=8, H=1, G=1, N=(1 << 28) - (1 << 13), D=64, T=0) == lagkv.ESHAPE
+    # 2^23 tiles always fit, 2^24 workgroups of four wavefronts never
+    assert status(lib, B=1 << 23, H=1, G=16, N=1, T=0) == lagkv.OK
+    assert status(lib, B=(1 << 24) - 8, H=1, G=4, N=1, T=4000) == lagkv.OK
+    assert status(lib, B=1 << 24, H=1, G=4, N=1, T=4000) == lagkv.ESHAPE
+    for k in (0, 4):
+        assert status(lib, B=4, H=8, G=4, N=131072, T=4096, n_blocks=k) == lagkv.OK
+
+
+def test_no_pieces_where_the_second_grid_does_not_hold_them(lib):
+    for B, T in ((1, 1 << 20), (4, 1 << 20), (1 << 12, 1 << 16)):
+        for N in (1 << 10, 1 << 16, 1 << 18):
+            for dtype in (lagkv.BF16, lagkv.F32):
+                p = params(B=B, H=1, G=4, N=N, T=T, dtype=dtype)
+                x = lagkv.AttendPlanT()
+                if lib.lagkv_attend_plan(C.byref(p), C.byref(x)) == lagkv.OK and x.pieces > 1:
+                    assert B * 4 * N < 1 << 26
+                    assert lib.lagkv_attend_workspace_bytes(C.byref(p)) >= B * 4 * N * x.pieces * 4 * 64
+
+
+def test_selection_among_all_streams_of_a_folded_cache(lib):
+    """32 layers of 32 requests, 8 KV heads: 8192 streams of 2048 blocks; refused for a workspace too short, and nothing else."""
+    P = 0x10000
+    p = params(B=1024, H=8, G=4, N=1, T=131072, block=64, n_blocks=64)
+    need = 8 * 1024 * 8 * 2048
+    assert lib.lagkv_select_blocks(C.byref(p), P, P, P, None, 0, 0, P, P, need - 1, None) == lagkv.EWORKSPACE
+    p = params(B=1 << 23, H=1, G=4, N=1, T=131072, block=64, n_blocks=64)
+    assert lib.lagkv_select_blocks(C.byref(p), P, P, P, None, 0, 0, P, P, 1 << 60, None) == lagkv.ESHAPE
