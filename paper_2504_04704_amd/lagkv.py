@@ -811,9 +811,14 @@ class Cache:
 
     def select_blocks(self, q: torch.Tensor, block: int, k: int, first: int = 0, last: int = 0,
                       batch: slice = slice(None)) -> torch.Tensor:
-        """select_blocks() among the blocks of the rows held."""
-        lo, hi = self.block_bounds(block)
-        return select_blocks(q, lo[batch], hi[batch], self.length, block, k, first, last)
+        """select_blocks() among the blocks of the rows held, by the bounds that block_bounds() keeps.  In a captured graph, by
+        bounds of the rows of `batch` alone: a step that goes layer by layer reads every layer's keys once."""
+        n = self.length
+        if self.K.is_cuda and torch.cuda.is_current_stream_capturing():
+            lo, hi = block_bounds(self.K[batch, :, :n], block)
+        else:
+            lo, hi = (t[batch] for t in self.block_bounds(block))
+        return select_blocks(q, lo, hi, n, block, k, first, last)
 
     def attend_blocks(self, q: torch.Tensor, blocks: torch.Tensor, block: int, K_new: Optional[torch.Tensor] = None,
                       V_new: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
