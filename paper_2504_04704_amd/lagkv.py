@@ -449,6 +449,14 @@ class _on:
             self.guard.__exit__(*a)
 
 
+def _capturing(device) -> bool:
+    """Whether the device's current stream (not that of the current device) is being captured into a graph."""
+    if device.type != "cuda":
+        return False
+    with _on(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _bytes(ws: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tensor]:
     if ws is None:
         return torch.empty(need, dtype=torch.uint8, device=device) if need else None
@@ -789,7 +797,7 @@ class Cache:
         if kept is None:
             if block < 1:
                 raise LagKVError(EINVAL, "lagkv_block_bounds")
-        if self.K.is_cuda and torch.cuda.is_current_stream_capturing():
+        if _capturing(self.K.device):
             return block_bounds(self.K[:, :, :n], block)
         device = self.K.device
         stream = _stream_ptr(device)
@@ -814,7 +822,7 @@ class Cache:
         """select_blocks() among the blocks of the rows held, by the bounds that block_bounds() keeps.  In a captured graph, by
         bounds of the rows of `batch` alone: a step that goes layer by layer reads every layer's keys once."""
         n = self.length
-        if self.K.is_cuda and torch.cuda.is_current_stream_capturing():
+        if _capturing(self.K.device):
             lo, hi = block_bounds(self.K[batch, :, :n], block)
         else:
             lo, hi = (t[batch] for t in self.block_bounds(block))

@@ -12,6 +12,37 @@ def rand(*shape, dtype, seed):
     return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype).to(DEV)
 
 
+def test_whose_stream_is_captured(monkeypatch):
+    """A cache on a device that is not the current one: it is its own device's stream that counts."""
+    now = [0]
+
+    class Guard:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.device.index
+
+        def __exit__(self, *a):
+            now[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: now[0] == 1)
+    seen = []
+
+    class Keys:
+        device, is_cuda, shape = torch.device("cuda", 1), True, (1, 1, 64, 8)
+
+        def __getitem__(self, at):
+            return self
+
+    cache = lagkv.Cache(1, 1, 8, 64, 2, 16, 0.5, device="cpu")
+    cache.K, cache.c.n_static = Keys(), 40
+    monkeypatch.setattr(lagkv, "block_bounds", lambda K, block: seen.append(K) or ("lo", "hi"))
+    assert cache.block_bounds(16) == ("lo", "hi") and len(seen) == 1 and cache._bounds == {} and now == [0]
+
+
 @pytest.mark.gpu
 def test_a_captured_step_reads_every_layer_once(monkeypatch):
     layers, B, H, G, D, T, block, k = 4, 2, 2, 4, 64, 600, 16, 5
