@@ -705,8 +705,16 @@ class Cache:
         return self._ws
 
     def append_and_compress(self, K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]) -> None:
-        if self._bounds:
-            return self._append_tracked(K_new, V_new)
+        if not self._bounds:
+            return self._append(K_new, V_new)
+        # (a round rewrites the rows behind the static part; a call that makes none, those behind the tail)
+        static, held = self.c.n_static, self.length
+        try:
+            self._append(K_new, V_new)
+        finally:
+            self.changed_from(held if self.c.n_static == static else static)
+
+    def _append(self, K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]) -> None:
         K = self.K
         if _native is not None:
             rc = _native.append(self.c, K, self.S, self.L, self.r, self.variant, self.std_ddof, self.launch, self._ws, K_new, V_new)
@@ -772,16 +780,6 @@ class Cache:
         of the accepted ones are what append_and_compress takes afterwards."""
         n = self.length
         return attend(q, self.K[batch, :, :n], self.V[batch, :, :n], K_new, V_new, parents, **kw)
-
-    def _append_tracked(self, K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]) -> None:
-        # (a round rewrites the rows behind the static part; a call that makes none, those behind the tail)
-        kept, static, held = self._bounds, self.c.n_static, self.length
-        self._bounds = {}
-        try:
-            self.append_and_compress(K_new, V_new)
-        finally:
-            self._bounds = kept
-            self.changed_from(held if self.c.n_static == static else static)
 
     def changed_from(self, row: int) -> None:
         """Says that rows from `row` on were written past this object's calls: block_bounds() works them out again."""
