@@ -208,9 +208,10 @@ bool small(const at::Tensor& t) {
     if (n > INT32_MAX) return false;
   return true;
 }
+// A backward pass or, of a dual tensor, a tangent that the operators do not give.
 template <typename... Ts>
 bool needs_grad(const Ts*... t) {
-  return c10::GradMode::is_enabled() && ((t && t->requires_grad()) || ...);
+  return (c10::GradMode::is_enabled() && ((t && t->requires_grad()) || ...)) || ((t && t->_fw_grad(0).defined()) || ...);
 }
 bool device_is_current(const at::Tensor& t) {
   return c10::impl::VirtualGuardImpl(at::DeviceType::CUDA).getDevice() == t.device();

@@ -19,6 +19,7 @@ from operator import index
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblagkv.so")
 _lib = None
@@ -430,6 +431,8 @@ def _ints(name: str, t: torch.Tensor, shape, device):
 
 
 def _no_grad(*tensors):
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise RuntimeError("the operators that read a cache have no forward-mode derivatives: call them on the primal tensors")
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         raise RuntimeError("the operators that read a cache have no backward pass: call them under torch.no_grad()")
 
