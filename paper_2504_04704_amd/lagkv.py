@@ -809,6 +809,8 @@ class Cache:
         elif kept[3] != stream:
             now = torch.cuda.current_stream(device)
             now.wait_stream(kept[4])
+            for t in kept[:2]:
+                t.record_stream(now)  # (not anyone else's memory before this stream is done with it, should the cache be dropped)
             kept[3:] = stream, now
         nb = -(-n // block)
         lo, hi = kept[0][:, :, :nb], kept[1][:, :, :nb]
