@@ -413,8 +413,15 @@ class Attended:
     lse: Optional[torch.Tensor]     # [B,H*G,N] fp32
 
 
+def _int32(where: str, *values: int):
+    """Refuses what a 32-bit field does not hold (ctypes would drop its upper bits without a word)."""
+    if any(not -1 << 31 <= v < 1 << 31 for v in values):
+        raise LagKVError(EINVAL, where)
+
+
 def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
     """A [.., .., rows, D] device tensor with contiguous channels, of the type and on the device of `like`."""
+    _int32(name, *t.shape)
     if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
         raise ValueError(f"{name} must be a 4-dimensional tensor with contiguous channels")
     if t.dtype not in _DTYPES:
@@ -475,6 +482,7 @@ def _attend(where, q, K, V, blocks, block, K_new, V_new, parents, lengths, scale
             raise LagKVError(got, where)
         if got is not None:
             return Attended(*got)
+    _int32(where, block, 0 if blocks is None else blocks.shape[-1])
     _rows("q", q)
     _rows("K", K, q)
     _same_layout(K, V)
@@ -565,10 +573,11 @@ def block_bounds(K: torch.Tensor, block: int, lengths: Optional[torch.Tensor] = 
             raise LagKVError(got, "lagkv_block_bounds")
         if got is not None:
             return got
+    block, start = index(block), index(start)
+    _int32("lagkv_block_bounds", block)
     _rows("K", K)
     _no_grad(K)
     B, H, T, D = K.shape
-    block, start = index(block), index(start)
     if block < 1:
         raise LagKVError(EINVAL, "lagkv_block_bounds")
     shape = (B, H, -(-T // block), D)
@@ -603,12 +612,13 @@ def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, b
             raise LagKVError(got, "lagkv_select_blocks")
         if got is not None:
             return got
+    T, block, k, first, last = index(T), index(block), index(k), index(first), index(last)
+    _int32("lagkv_select_blocks", block, k, first, last, *lo.shape)
     _rows("q", q)
     _rows("lo", lo, q)
     _no_grad(q, lo, hi)
     B, H, nb, D = lo.shape
     heads, N = q.shape[1], q.shape[2]
-    T, block, k = index(T), index(block), index(k)
     if block < 1 or k < 1 or T < 0:
         raise LagKVError(EINVAL, "lagkv_select_blocks")
     if q.shape[0] != B or q.shape[3] != D or H == 0 or heads % H or nb != -(-T // block):
@@ -625,8 +635,8 @@ def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, b
     p.kv_stride[:] = lo.stride()[:3]
     with _on(q.device):
         ws = _bytes(ws, 8 * B * H * N * nb, q.device)
-        _check(load().lagkv_select_blocks(C.byref(p), q.data_ptr(), lo.data_ptr(), hi.data_ptr(), _ptr(lengths), index(first),
-                                          index(last), out.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
+        _check(load().lagkv_select_blocks(C.byref(p), q.data_ptr(), lo.data_ptr(), hi.data_ptr(), _ptr(lengths), first,
+                                          last, out.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
                                           _stream_ptr(q.device)), "lagkv_select_blocks")
     return out
 
