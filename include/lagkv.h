@@ -350,7 +350,8 @@ int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out);
  * A row whose logits are all -inf is taken for one that sees nothing.
  * Rows behind lengths[b] and rows of the new tokens that a token does not see do not reach its output, whatever they hold;
  * one that it sees does: an output with a logit that is no number is none, and one with an infinite value is infinite (NaN with
- * two of either sign, or where the row's weight is too small to be held: below 2^-34 of the largest in fp16, 2^-126 else).
+ * two of either sign; the one or the other where the row's weight is too small to be held, below 2^-34 of the largest in fp16 and
+ * 2^-126 else).
  * Logits, sums and products are held in fp32, and weights go into the products with V as fp32 or as two numbers of the type (16
  * bits of them in bf16, 22 in fp16), whichever kernel runs; results do not depend on anything but the arguments (no atomics).
  * N = 0: LAGKV_OK, nothing is done.  T = 0 is allowed (K, V may be NULL then).

@@ -60,11 +60,6 @@ __device__ __forceinline__ float sum_across_32(float x) {
   return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
-// What is left of a weight x >= 0 beside its leading bits: at least the type's smallest number, if x is not 0.  Both parts of
-// a weight are then of one sign, and their products with an infinity add up to it: a rest of 0 or below would make them NaN.
-// (x - lead <= x, so that the middle one of the three is this.)
-__device__ __forceinline__ float rest_of(float x, float lead, float smallest) { return __builtin_amdgcn_fmed3f(x - lead, smallest, x); }
-
 template <int DT>
 struct AElem;
 template <>
@@ -84,11 +79,13 @@ struct AElem<LAGKV_BF16> {
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
   }
-  // x and y >= 0 as pairs of numbers of the type: the leading bits, and the rest rounded
+  // Weights x and y >= 0 as pairs of numbers of the type: their leading bits, and the rest rounded.  The rest is above 0 if the
+  // weight is: both parts' products with an infinity then add up to it, and are NaN with a rest of 0 or below.  It has
+  // 2^-22 of the weight too much for that (the rounding of the rest leaves 2^-15).
   static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
     const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
     hi = __builtin_amdgcn_perm(b, a, 0x07060302);
-    lo = pack(rest_of(x, __uint_as_float(a & 0xffff0000u), 0x1p-126f), rest_of(y, __uint_as_float(b & 0xffff0000u), 0x1p-126f));
+    lo = pack(__builtin_fmaf(x, 1 + 0x1p-22f, -__uint_as_float(a & 0xffff0000u)), __builtin_fmaf(y, 1 + 0x1p-22f, -__uint_as_float(b & 0xffff0000u)));
   }
   static __device__ __forceinline__ float one(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 };
@@ -105,10 +102,11 @@ struct AElem<LAGKV_F16> {
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, f16x2));
   }
+  // (here the rest has to be of the smallest number at least; x - lead <= x, so that the middle one of the three is that)
   static __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
     hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
     const f32x2 back = __builtin_convertvector(__builtin_bit_cast(f16x2, hi), f32x2);
-    lo = pack(rest_of(x, back.x, 0x1p-24f), rest_of(y, back.y, 0x1p-24f));
+    lo = pack(__builtin_amdgcn_fmed3f(x - back.x, 0x1p-24f, x), __builtin_amdgcn_fmed3f(y - back.y, 0x1p-24f, y));
   }
   static __device__ __forceinline__ float one(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
 };
