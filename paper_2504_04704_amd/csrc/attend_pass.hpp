@@ -18,9 +18,9 @@
 // P is put in as the sum of two 16-bit numbers (the value's leading bits, and the rest): one alone would add as
 // much error to the output as its own rounding, and the pass is bound by memory where tiles are small.
 //
-// Bound by memory where the rows of K and V are many (four query rows of 256 streams of up to 8384 rows, bf16: 151 to 155 us,
-// 5.4 to 5.5 TB/s, where a copy reaches 5.07; 32 streams x 8192 rows 28 us; fp32 55 us), by latency where they are few (one token,
-// 8 streams x 4288 rows: 8.8 us and 2.5 for joining the pieces, at the copy's rate 3.5), by the products for 32 fp32 rows and more
+// Bound by memory where the rows of K and V are many (four query rows of 256 streams of up to 8384 rows, bf16: 155 us,
+// 5.4 TB/s, where a copy reaches 5.07; 32 streams x 8192 rows 28 us; fp32 55 us), by latency where they are few (one token,
+// 8 streams x 4288 rows: 9.4 us and 2.5 for joining the pieces, at the copy's rate 3.5), by the products for 32 fp32 rows and more
 // (256 rows of 32 streams x 8192, 326 us: 105 Tflop/s of the 151 of a large product).  The next step's K and V
 // are on their way, in registers, while one is worked on.
 #pragma once

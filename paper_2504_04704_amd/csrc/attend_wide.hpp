@@ -6,13 +6,13 @@
 // rows (32 beyond 128 channels) at a time, which lie in LDS for all of them (the next ones are on their way through
 // registers meanwhile); each wavefront keeps 32 query rows to itself, so that nothing is exchanged between wavefronts.  32x32
 // products: a lane holds one query row (of S^T, P^T and O^T), so that maxima and sums need one exchange between the lane's
-// halves only.  Measured: 256 rows of 32 streams x 33536 (bf16, 128 channels) 191 us, 0.74 Pflop/s, and 8.7 for joining the
-// pieces; 2048 rows of 8 streams x 8640 111 us, 0.66 Pflop/s, and 9.6 (a large product of the library: 1.09).  The matrix cores are
-// busy in 68 % of the cycles, at a clock of 1.6 GHz; there are no conflicts of LDS banks to speak of.
+// halves only.  Measured: 256 rows of 32 streams x 33536 (bf16, 128 channels) 191 to 196 us, 0.73 Pflop/s, and 8.7 for joining the
+// pieces; 2048 rows of 8 streams x 8640 111 us, 0.66 Pflop/s, and 9.5 (a large product of the library: 1.09).  The matrix cores are
+// busy in 65 % of the cycles, at a clock of 1.6 GHz; there are no conflicts of LDS banks to speak of.
 //
-// P is put in as two numbers, as in the narrow kernel, so that a result does not depend on which of the two runs (that goes by time,
-// and so by what else is in the batch).  One number, rounded, takes half as many products less, 147 us in place of 191, and
-// puts an error of the size of the output's own rounding into the outputs.
+// P is put in as two numbers, as in the narrow kernel: which of the two runs goes by time, and so by what else is in the batch, and
+// the precision of a request's result must not.  One number, rounded, takes a third of the products less, 147 us in place of
+// 191, and puts an error of the size of the output's own rounding into the outputs.
 //
 // Products and exponentials take about the same time (48 products of 32 cycles, 32 elements a lane of some 50), on
 // different units.  So eight wavefronts go in two halves, one of each on every SIMD, between barriers: while one half
