@@ -161,6 +161,16 @@ __device__ __forceinline__ void fetch_arguments() {
   asm volatile("" ::"s"(any));
 }
 
+// The kernel's arguments, loaded where they are used next: for a part that hardly ever runs, so that the others' registers do not hold
+// what it needs.
+template <typename T>
+__device__ __forceinline__ const T& arguments_again() {
+  typedef const __attribute__((address_space(4))) T* args_t;
+  args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const T*)p;
+}
+
 // The workgroup's unit, row tile and piece.  Tiles of one unit and piece read the same cache rows: they are dealt to
 // workgroups whose numbers differ by multiples of eight, which share an L2.
 struct WorkItem {

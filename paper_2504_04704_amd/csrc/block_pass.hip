@@ -10,8 +10,10 @@
 //
 // With an infinite bound P.hi + M.lo is infinite or no number, while max(q lo, q hi) may be finite (q < 0, hi = inf), and where a
 // P or M is 0 only because a lane has no channel there it says nothing at all.  Finite numbers never add up to such a score: a
-// score that is not finite is worked out again, head by head and channel by channel (score_again).  What is infinite or none
-// even so comes behind all others: a bound of infinity is that of a logit which leaves attention without a number.
+// score that is not finite is worked out again, without the infinite bounds, and stays if none of them counts: if P is 0 where hi
+// is infinite and M where lo is, and no query head has a 0 there.  What is infinite or none even so comes behind all
+// others: a bound of infinity is that of a logit which leaves attention without a number.  (us, 2048 blocks of 32 streams: one
+// token 13.7, with one block of each stream so 15.5, with all 24; sixteen 28, 37 and 62.)
 #include "attend_pass.hpp"
 #include "row_ops.hpp"
 
@@ -198,34 +200,39 @@ __device__ __forceinline__ void query_slices(const SelectArgs& a, int64_t b, int
 
 __device__ __forceinline__ bool is_finite(double s) { return __builtin_fabs(s) < (double)INFINITY; }
 
-// s[j] of token n as it is defined, NaN where that is not finite.  One lane's work, in the order of the channels.  (Blocks without
-// rows, whose bounds are infinite, are nobody's choice: they are left.)
+// A channel's bounds for a score that is not finite: in their order, and what of them is infinite put aside as 0.  NaN stays.
+struct Edge {
+  double lo, hi;
+  bool far_lo, far_hi;
+};
+__device__ __forceinline__ Edge edge_of(float lo, float hi) {
+  const bool none = lo != lo || hi != hi;
+  const float low = none ? NAN : fminf(lo, hi), top = none ? NAN : fmaxf(lo, hi);
+  Edge e;
+  e.far_lo = __builtin_fabsf(low) == INFINITY;
+  e.far_hi = __builtin_fabsf(top) == INFINITY;
+  e.lo = e.far_lo ? 0.0 : (double)low;
+  e.hi = e.far_hi ? 0.0 : (double)top;
+  return e;
+}
+// Channels of a token's slice, as bits, in which a query head has 0: an infinite bound counts there (0 * inf is no number), as it
+// does where its P or M is not 0.
 template <int DT>
-__device__ __forceinline__ void score_again(const SelectArgs& a, int64_t stream, int n, int64_t j) {
+__device__ __forceinline__ uint32_t zeros_of(const SelectArgs& a, int64_t b, int64_t h, int n, int slice) {
   using ET = typename Of<DT>::T;
   constexpr int VEC = ET::VEC, SIZE = 16 / VEC;
-  const int64_t b = (uint32_t)stream / (uint32_t)a.H, h = (uint32_t)stream % (uint32_t)a.H;
-  if (j * a.block >= rows_held(a.lengths, b, a.T)) return;
-  const int64_t bound = b * a.bsb + h * a.bsh + j * a.bst;
-  const char* q = a.Q + b * a.qsb + h * a.G * a.qsh + (int64_t)n * a.qsn;
-  double s = 0;
+  if (n >= a.N || slice * VEC >= a.D) return 0;
+  const int at = slice_at(slice, a.D, VEC);
+  const char* q = a.Q + b * a.qsb + h * a.G * a.qsh + (int64_t)n * a.qsn + at * SIZE;
+  uint32_t bits = 0;
 #pragma unroll 1
-  for (int c = 0; c * VEC < a.D && is_finite(s); ++c) {
-    const int at = slice_at(c, a.D, VEC), dup = c * VEC - at;
-    float lo[VEC], hi[VEC], x[VEC];
-    unpack<ET>(ld16_any(a.lo + bound + at * SIZE), lo);
-    unpack<ET>(ld16_any(a.hi + bound + at * SIZE), hi);
-#pragma unroll 1
-    for (int g = 0; g < a.G; ++g) {
-      unpack<ET>(ld16_any(q + g * a.qsh + at * SIZE), x);
+  for (int g = 0; g < a.G; ++g) {
+    float x[VEC];
+    unpack<ET>(ld16_any(q + g * a.qsh), x);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const double l = (double)x[i] * lo[i], u = (double)x[i] * hi[i];
-        if (i >= dup) s += l > u ? l : l == l ? u : l;  // (NaN if either is)
-      }
-    }
+    for (int i = 0; i < VEC; ++i) bits |= (x[i] == 0.f ? 1u : 0u) << i;
   }
-  a.score[(stream * a.N + n) * a.nb + j] = is_finite(s) ? s : __builtin_nan("");
+  return bits >> (slice * VEC - at) << (slice * VEC - at);  // (without those of the slice before)
 }
 
 // Scores of one, two or three tokens: a wavefront takes 16 blocks, LPR lanes a block; the bounds are on their way while P
@@ -291,14 +298,39 @@ __global__ __launch_bounds__(256, 4) void block_scores_kernel(const SelectArgs a
         const double s = lanes_sum(s0 + s1, lpr);
         if (slice == 0 && of < 16 && j < a.nb) {
           a.score[(stream * a.N + n) * a.nb + j] = s;
-          if (!is_finite(s)) again |= 1ull << (n * 16 + of);
+          again |= is_finite(s) ? 0 : 1ull << (n * 16 + of);
         }
       }
     }
   }
-  for (; again; again &= again - 1) {
-    const int bit = __builtin_ctzll(again);
-    score_again<DT>(a, stream, bit / 16, jw + bit % 16);
+  if (!__any(again != 0)) return;
+  const SelectArgs& r = arguments_again<SelectArgs>();
+  const int64_t held = (rows_held(r.lengths, b, r.T) + r.block - 1) / r.block;  // (blocks without rows are nobody's choice)
+#pragma unroll 1
+  for (int n = 0; n < r.N; ++n) {
+    if (!__any((again >> (16 * n) & 0xffff) != 0)) continue;
+    const uint32_t zeros = zeros_of<DT>(r, b, h, n, slice);
+#pragma unroll 1
+    for (int pass = 0; pass < passes; ++pass) {
+      const int of = pass * step + sub;
+      const int64_t j = jw + of, jj = j < r.nb ? j : r.nb - 1;
+      const bool mine = of < 16 && j < held && (again >> (16 * n + of) & 1);
+      if (!__any(mine)) continue;
+      const int64_t from = b * r.bsb + h * r.bsh + jj * r.bst + at * SIZE;
+      float lo[VEC], hi[VEC];
+      unpack<ET>(ld16_any(r.lo + from), lo);
+      unpack<ET>(ld16_any(r.hi + from), hi);
+      double s = 0;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) {
+        const double p = sh_p[n][c * lpr + slice], m = sh_m[n][c * lpr + slice];
+        const Edge e = edge_of(lo[c], hi[c]);
+        const bool zero = zeros >> c & 1;
+        s += (e.far_hi && (p != 0 || zero)) || (e.far_lo && (m != 0 || zero)) ? (double)NAN : p * e.hi + m * e.lo;
+      }
+      s = lanes_sum(s, lpr);
+      if (mine) r.score[(stream * r.N + n) * r.nb + j] = is_finite(s) ? s : (double)NAN;
+    }
   }
 }
 
@@ -368,13 +400,46 @@ __global__ __launch_bounds__(256) void block_scores_many_kernel(const SelectArgs
       const int64_t to = j0 + set * kScoreBlocks + grp + 4 * i;
       if (n < a.N && to < a.nb) {
         a.score[(stream * a.N + n) * a.nb + to] = s[i];
-        if (!is_finite(s[i])) again |= 1u << (4 * set + i);
+        again |= is_finite(s[i]) ? 0 : 1u << (4 * set + i);
       }
     }
   }
-  for (; again; again &= again - 1) {
-    const int bit = __builtin_ctz(again);
-    score_again<DT>(a, stream, n0 + col, j0 + bit / 4 * kScoreBlocks + grp + 4 * (bit % 4));
+  if (!__any(again != 0)) return;
+  const SelectArgs& r = arguments_again<SelectArgs>();
+  const int64_t held = (rows_held(r.lengths, b, r.T) + r.block - 1) / r.block;  // (blocks without rows are nobody's choice)
+#pragma unroll 1
+  for (int set = 0; set < here; ++set) {
+    uint32_t mine = again >> (4 * set) & 15;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (j0 + set * kScoreBlocks + grp + 4 * i >= held) mine &= ~(1u << i);
+    if (!__any(mine != 0)) continue;
+    const int64_t j = j0 + set * kScoreBlocks + col, row = b * r.bsb + h * r.bsh + (j < r.nb ? j : r.nb - 1) * r.bst;
+    f64x4 s = {0, 0, 0, 0};  // (with 1e300 for each infinite bound that counts; finite ones add up to less than 1e90)
+#pragma unroll 1
+    for (int c = 0; c < NC; ++c) {
+      const int slice = c * 4 + grp;
+      const bool have = slice * VEC < r.D;
+      const uint32_t zeros = zeros_of<DT>(r, b, h, n0 + col, slice);
+      const int64_t from = row + (have ? slice_at(slice, r.D, VEC) : 0) * SIZE;
+      float lo[VEC], hi[VEC];
+      unpack<ET>(ld16_any(r.lo + from), lo);
+      unpack<ET>(ld16_any(r.hi + from), hi);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const double p = sh_pm[col * LD + slice * VEC + i], m = sh_pm[(16 + col) * LD + slice * VEC + i];
+        const Edge e = edge_of(have ? lo[i] : 0.f, have ? hi[i] : 0.f);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(e.hi, p, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(e.lo, m, s, 0, 0, 0);
+        const bool zero = zeros >> i & 1;
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(e.far_hi ? 1e300 : 0.0, p != 0 || zero ? 1.0 : 0.0, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(e.far_lo ? 1e300 : 0.0, m != 0 || zero ? 1.0 : 0.0, s, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (mine >> i & 1)
+        r.score[(stream * r.N + n0 + col) * r.nb + j0 + set * kScoreBlocks + grp + 4 * i] = __builtin_fabs(s[i]) < 1e200 ? s[i] : (double)NAN;
   }
 }
 

@@ -45,6 +45,7 @@ def test_infinite_bounds(dtype, D, N):
     q[:, :, :, 0] = -q[:, :, :, 0].abs() - 0.25            # below 0 in every head: hi = inf leaves the score finite
     q[:, :, :, D - 1] = q[:, :, :, D - 1].abs() + 0.25     # above 0: lo = -inf does
     q[:, ::4, :, 5] = 0.0                                  # 0 in some heads
+    q[:, :, :, 6] = 0.0                                    # and in all
     for j in range(nb):
         kind = j % 12
         if kind == 0:
@@ -63,6 +64,12 @@ def test_infinite_bounds(dtype, D, N):
             lo[:, :, j, 3], hi[:, :, j, 3] = math.inf, -math.inf
         elif kind == 7 and j % 24 == 7:
             hi[:, :, j, 2] = math.nan
+        elif kind == 8:
+            lo[:, :, j, 5] = -math.inf
+        elif kind == 9 and j % 24 == 9:
+            hi[:, :, j, 6] = math.inf
+        elif kind == 10:
+            hi[:, :, j, 0], lo[:, :, j, 0] = -0.5, math.inf  # (out of order)
     T = nb * block - 5
     lengths = torch.tensor([T, 100 * block + 1], dtype=torch.int32)
     held = [nb, 101]
