@@ -795,7 +795,8 @@ class Cache:
         return attend(q, self.K[batch, :, :n], self.V[batch, :, :n], K_new, V_new, parents, **kw)
 
     def changed_from(self, row: int) -> None:
-        """Says that rows from `row` on were written past this object's calls: block_bounds() works them out again."""
+        """Says that rows from `row` on were written past this object's calls (by a graph that is replayed, say): block_bounds()
+        works them out again."""
         for kept in self._bounds.values():
             kept[2] = min(kept[2], max(int(row), 0))
 
