@@ -331,7 +331,7 @@ size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p);
  * The launch shape of that call, as lagkv_path_for and lagkv_kernel_for give it of a lagkv_compress call: which kernel runs
  * (many_rows: the one that many query rows share, of 16-bit types), how many query rows a workgroup takes, with how many
  * wavefronts, and into how many pieces the cache is cut (from two on a second kernel joins them).  It depends on the same
- * parameters as the workspace.  Host only; the lagkv_status that the call itself would return for parameters it rejects.
+ * parameters as the workspace.  Host only; LAGKV_OK, or the lagkv_status of a call of such sizes, types or scale.
  */
 typedef struct {
   int32_t many_rows, row_tile, wavefronts, pieces;

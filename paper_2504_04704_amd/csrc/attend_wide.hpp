@@ -20,7 +20,8 @@
 // h counting the phases, the first half multiplies for step i in h = 2i and makes weights in 2i + 1, the other one phase later.
 // K of step i and V of step i - 1 are read in 2i and 2i + 1; K(i+1) and V(i) are written into the other buffers in
 // 2i + 1 by the first half and in 2i by the second, when nobody reads these any more.  (Halves in phase took 15 % longer.)  Four
-// wavefronts, for fewer rows, leave that to the two workgroups of a compute unit: one barrier a step.
+// wavefronts, for fewer rows or 64 channels, leave that to the two workgroups of a compute unit (for 256 it holds one): one barrier
+// a step.
 //
 // The reference m of the exponentials is only moved when a row's maximum leaves it by more than SLACK (base 2): exp(x - m) is then
 // up to 2^SLACK, which costs nothing in a floating-point number, and the outputs are rescaled in a few steps, not most.
