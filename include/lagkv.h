@@ -397,6 +397,88 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
 int lagkv_select_blocks(const lagkv_attend_params* p, const void* Q, const void* lo, const void* hi, const int32_t* lengths,
                         int32_t n_first, int32_t n_last, int32_t* blocks, void* ws, size_t ws_bytes, void* hip_stream);
 
+/*
+ * ---- A cache in 8 bits --------------------------------------------------------------------
+ *
+ * Rows as codes of 8 bits with one fp32 scale for every block of rows and head: a row's value is code * scale.  Rows that
+ * the compression pass has kept do not change any more (lagkv_cache.n_static): they are written once and read in every
+ * step, at half the bytes.  Conventions are those of the operators that read a cache: strides in elements, taken as they are (0
+ * repeats what is read), contiguous channels, 16 to 256 of them, addresses aligned to an element; the stream's device current; nothing
+ * allocated or kept, so that calls can be captured; `lengths` read on the device, any value safe.
+ */
+typedef enum {
+  LAGKV_CODE_INT8 = 0, /* -127 .. 127 (-128 stands for itself where it is given)                                */
+  LAGKV_CODE_E4M3 = 1  /* sign, 4 exponent and 3 mantissa bits, bias 7, no infinities, 0x7f and 0xff no number   */
+} lagkv_code;
+
+typedef struct {
+  int32_t B, H, G, N, D;    /* as in lagkv_attend_params; G and N of lagkv_attend_quantized alone                   */
+  int32_t dtype;            /* lagkv_dtype of rows that are not codes (K, V, Q, K_tail, V_tail, K_new, V_new, out)  */
+  int32_t code;             /* lagkv_code of Kq and Vq                                                              */
+  int32_t block;            /* rows of a scale: a power of two, 16 .. 1024                                          */
+  int64_t T;                /* rows of Kq and Vq                                                                    */
+  int64_t R;                /* rows of K_tail and V_tail (lagkv_attend_quantized)                                   */
+  double scale;             /* of the logits                                                                        */
+  int64_t code_stride_b, code_stride_h, code_stride_t; /* Kq, Vq [B, H, T, D]                                       */
+  int64_t scale_stride_b, scale_stride_h;              /* K_scale, V_scale [B, H, ceil(T / block)], blocks contiguous */
+  int64_t row_stride_b, row_stride_h, row_stride_t;    /* K, V [B, H, T, D]; K_tail, V_tail [B, H, R, D]            */
+  int64_t q_stride_b, q_stride_h, q_stride_n;          /* Q    [B, H*G, N, D]                                       */
+  int64_t new_stride_b, new_stride_h, new_stride_n;    /* K_new, V_new [B, H, N, D]                                 */
+  int64_t out_stride_b, out_stride_h, out_stride_n;    /* out  [B, H*G, N, D]                                       */
+  int64_t parents_stride_b;                            /* parents [B, N]; 0: one tree for all                       */
+} lagkv_quant_params;
+
+/*
+ * Rows K, V into codes Kq, Vq and scales.  With a the largest absolute value of a block (its rows before lengths[b], all
+ * channels; K and V apart):
+ *   int8   scale = a / 127 rounded to fp32, code = 127 x / a rounded to the nearest whole number
+ *   e4m3   scale = 2^e with the smallest e >= -126 for which a <= 448 * 2^e, code = x / scale rounded to the nearest
+ * of two nearest the even one; neither depends on how a kernel divides.  a = 0: scale 0.  A block with a value that is no finite
+ * number: scale NaN, codes 0 (all of it reads back as NaN).
+ * Only blocks from that of row `start` on are written (an update behind appended rows; 0: all; from T on: none), and of the last one of
+ * lengths[b] (NULL: T) rows the rows before it: what lies behind, blocks without a row among it, is left as it was.
+ * Of p the fields B, H, D, dtype, code, block, T, row_stride_*, code_stride_* and scale_stride_* are read.  Inputs and outputs
+ * must not overlap.  LAGKV_ESHAPE beyond 2^31 - 2^16 blocks of K and V.
+ */
+int lagkv_quantize(const lagkv_quant_params* p, const void* K, const void* V, const int32_t* lengths, int64_t start, void* Kq,
+                   void* Vq, float* K_scale, float* V_scale, void* hip_stream);
+
+/*
+ * The rows back: code * scale in fp32, rounded once to the type of K and V.  Rows from `start` on and before lengths[b] (NULL: T)
+ * are written.  Fields and limits as of lagkv_quantize.
+ */
+int lagkv_dequantize(const lagkv_quant_params* p, const void* Kq, const void* Vq, const float* K_scale, const float* V_scale,
+                     const int32_t* lengths, int64_t start, void* K, void* V, void* hip_stream);
+
+/*
+ * Device workspace, in bytes, of a lagkv_attend_quantized call with these parameters; 0 on invalid ones.  It depends on B, H, G, N, D, dtype, code, T
+ * and R alone.  16-byte aligned; nothing in it has to be cleared, and nothing in it outlives the call.
+ */
+size_t lagkv_attend_quantized_workspace_bytes(const lagkv_quant_params* p);
+
+/*
+ * The launch shape of that call: of the rows in 8 bits (pieces 0: there are none) and of the tail and the new tokens, where a call
+ * has any.  As lagkv_attend_plan; host only.
+ */
+int lagkv_attend_quantized_plan(const lagkv_quant_params* p, lagkv_attend_plan_t* codes, lagkv_attend_plan_t* rows);
+
+/*
+ * lagkv_attend over the rows 0 .. lengths[b]-1 of a cache in 8 bits, as their codes and scales give them, over rows 0 ..
+ * tail_lengths[b]-1 of K_tail, V_tail (NULL: none; those that are not quantised yet, which every token sees), and over the new
+ * tokens' own rows (K_new, V_new, parents, as there).  Lengths below 0 or above T and R count as 0, T and R; NULL: all.
+ * out, lse, and what is no number: as of lagkv_attend.  (A row of the cache is none with a scale or, in e4m3, a code that is none; scales
+ * are neither negative nor infinite.)
+ * Codes go into the products as they are, which binary16 holds, and scales into logits and weights in fp32.  A query row goes in
+ * as binary16 times a power of two: in bf16 and fp16 as it is (bf16: what is below 2^-14 of the row's largest off by up to 2^-25 of
+ * it), in fp32 as two such numbers (off by up to 2^-23 of the largest).  Weights, times their rows' scales, go in as two (22 bits).
+ * The rest as of lagkv_attend: logits, sums and products in fp32, no atomics, its limits on sizes; LAGKV_ESHAPE from 2^26 query
+ * rows on too (all of them are joined from pieces).
+ */
+int lagkv_attend_quantized(const lagkv_quant_params* p, const void* Q, const void* Kq, const void* Vq, const float* K_scale,
+                           const float* V_scale, const int32_t* lengths, const void* K_tail, const void* V_tail,
+                           const int32_t* tail_lengths, const void* K_new, const void* V_new, const int32_t* parents, void* out,
+                           float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* Static, human readable text for a lagkv_status. */
 const char* lagkv_strerror(int status);
 

@@ -35,39 +35,6 @@ int check_tokens(const lagkv_attend_params* p) {
   return LAGKV_OK;
 }
 
-// Rows [B, heads, N] of D channels that lie apart: with the axes of more than one entry from the smallest stride up, each
-// steps over all of what the ones before it span.
-bool apart(int64_t D, const int64_t (&n)[3], const int64_t (&stride)[3]) {
-  int order[3] = {0, 1, 2};
-  for (int i = 0; i < 3; ++i)
-    for (int j = i + 1; j < 3; ++j)
-      if (stride[order[j]] < stride[order[i]]) {
-        const int t = order[i];
-        order[i] = order[j];
-        order[j] = t;
-      }
-  int64_t span = D;
-  for (int i : order) {
-    if (n[i] <= 1) continue;
-    if (stride[i] < span) return false;
-    span += stride[i] * (n[i] - 1);
-  }
-  return true;
-}
-
-int check_attend(const lagkv_attend_params* p, bool pick) {
-  int rc = check_heads(p);
-  if (rc != LAGKV_OK) return rc;
-  rc = check_tokens(p);
-  if (rc != LAGKV_OK) return rc;
-  if (!std::isfinite((float)(p->scale * 1.4426950408889634))) return LAGKV_EINVAL;
-  if (pick && (!block_ok(p->block) || p->n_blocks < 1 || (int64_t)p->n_blocks * p->block > kMostRows)) return LAGKV_EINVAL;
-  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0 || p->new_stride_b < 0 || p->new_stride_h < 0 ||
-      p->new_stride_n < 0 || p->out_stride_b < 0 || p->out_stride_h < 0 || p->out_stride_n < 0 || p->parents_stride_b < 0)
-    return LAGKV_ESHAPE;
-  return LAGKV_OK;
-}
-
 // Workgroups of the fullest of the eight XCDs (work_item deals units and pieces to them in turn, with all their tiles).
 int64_t fullest_xcd(int64_t units, int64_t pieces, int64_t row_tiles) { return (units * pieces + 7) / 8 * row_tiles; }
 
@@ -79,7 +46,7 @@ int64_t next_pieces(int64_t s) { return s + (s < 4 ? 1 : s % 3 == 0 ? s / 3 : s 
 // the cache is cut into, by the microseconds that they take: a step of 64 cache rows, the beginning and end of a workgroup,
 // and, with pieces, a second kernel and every piece of a row written and read.  A step takes longer the more compute
 // units are at work, and less where wavefronts of the eight have no rows.  Measured, 128 channels, model beside it (us; it
-// falls short by a seventh in the mean, as narrow_shape's does, and what counts is which is the least):
+// falls short by a seventh in the mean, as attend_narrow_shape's does, and what counts is which is the least):
 //    8 streams,  256 query rows, 1000 rows   128 in 4 19 (18)   128 in 8 18 (16)   256 in 8 23 (20)   few rows 16 (15)
 //   32 streams,  256 query rows, 2000 rows   128 in 4 33 (27)   128 in 8 35 (28)   256 in 4 36 (32)   256 in 8 34 (30)
 //   32 streams,  256 query rows, 8000 rows   128 in 4 77 (62)   128 in 8 70 (57)   256 in 4 77 (74)   256 in 8 63 (54)
@@ -109,6 +76,43 @@ double wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* ro
   return least;
 }
 
+}  // namespace
+
+namespace lagkv {
+
+// Rows [B, heads, N] of D channels that lie apart: with the axes of more than one entry from the smallest stride up, each
+// steps over all of what the ones before it span.
+bool rows_apart(int64_t D, const int64_t (&n)[3], const int64_t (&stride)[3]) {
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[order[j]] < stride[order[i]]) {
+        const int t = order[i];
+        order[i] = order[j];
+        order[j] = t;
+      }
+  int64_t span = D;
+  for (int i : order) {
+    if (n[i] <= 1) continue;
+    if (stride[i] < span) return false;
+    span += stride[i] * (n[i] - 1);
+  }
+  return true;
+}
+
+int attend_check(const lagkv_attend_params* p, bool pick) {
+  int rc = check_heads(p);
+  if (rc != LAGKV_OK) return rc;
+  rc = check_tokens(p);
+  if (rc != LAGKV_OK) return rc;
+  if (!std::isfinite((float)(p->scale * 1.4426950408889634))) return LAGKV_EINVAL;
+  if (pick && (!block_ok(p->block) || p->n_blocks < 1 || (int64_t)p->n_blocks * p->block > kMostRows)) return LAGKV_EINVAL;
+  if (p->kv_stride_b < 0 || p->kv_stride_h < 0 || p->kv_stride_t < 0 || p->new_stride_b < 0 || p->new_stride_h < 0 ||
+      p->new_stride_n < 0 || p->out_stride_b < 0 || p->out_stride_h < 0 || p->out_stride_n < 0 || p->parents_stride_b < 0)
+    return LAGKV_ESHAPE;
+  return LAGKV_OK;
+}
+
 // Tiles of 16 or 32 query rows: the pieces of the cache by the microseconds that they take, none below a step a wavefront.
 // A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them, at
 // no cost to each other but memory's with 16 query rows (32: 0.75 us beside another, in fp32 0.75 alone and 1.4), and one where
@@ -118,7 +122,7 @@ double wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* ro
 // time is 1 % above that of the best number of pieces in the mean; with as many pieces as make 512 workgroups, 11.9 %.  Where
 // lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4
 // 115; 192 streams in 1 70, in 2 79.)
-double narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces) {
+double attend_narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces) {
   const bool heavy = f32 && row_tile == 32;  // (bound by the products)
   const int64_t tiles = (rows + row_tile - 1) / row_tile, places = D > 128 ? 32 : 64;  // of an XCD
   const double channels = D <= 64 ? 0.5 : D <= 128 ? 1 : 2, alone = (heavy ? 0.75 : 0.45) * channels;
@@ -148,7 +152,7 @@ double narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bo
 // 600 query rows, it is 0.4 % above the less of itself and of few rows, which take 19 % more in the mean.  us, few and many: 8
 // streams, 256 query rows, 500 rows 15 and 16, 1000 rows 16 and 18; 32 streams, 256, 2000 rows 47 and 33; 8 streams of 256
 // channels, 500 query rows, 4000 rows 140 and 53.)
-bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
+bool attend_plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
   pl->rows = pick ? p->G : p->G * p->N;
   const int64_t all_rows = pl->units * pl->rows;
@@ -159,7 +163,7 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   const int64_t steps = steps_of(f32 ? 16 : 32);
   int64_t splits = 1;
   pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
-  const double us = narrow_shape(pl->units, pl->rows, pl->row_tile, p->D, f32, steps, &splits);
+  const double us = attend_narrow_shape(pl->units, pl->rows, pl->row_tile, p->D, f32, steps, &splits);
   pl->wide = false;
   if (!pick && !f32 && pl->rows > 32) {
     int row_tile;
@@ -193,26 +197,12 @@ bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
   return fits(splits);
 }
 
-int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
-           const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse,
-           void* ws, size_t ws_bytes, void* hip_stream, bool pick) {
-  int rc = check_attend(p, pick);
-  if (rc != LAGKV_OK) return rc;
-  if (p->N == 0) return LAGKV_OK;
-  if (!Q || !out || (p->T > 0 && (!K || !V)) || (pick && !blocks) || !K_new != !V_new || (parents && !K_new)) return LAGKV_EINVAL;
-  if (parents && p->N > kMaxTree) return LAGKV_ESHAPE;
-  const int64_t n[3] = {p->B, (int64_t)p->H * p->G, p->N};
-  const int64_t st[3] = {p->out_stride_b, p->out_stride_h, p->out_stride_n};
-  if (!apart(p->D, n, st)) return LAGKV_ESHAPE;
-  const int es = esize_of(p);
-  if (!aligned(Q, es) || !aligned(K, es) || !aligned(V, es) || !aligned(K_new, es) || !aligned(V_new, es) || !aligned(out, es) ||
-      !aligned(lengths, 4) || !aligned(parents, 4) || !aligned(blocks, 4) || !aligned(lse, 4))
-    return LAGKV_EINVAL;
-  AttendPlan pl;
-  if (!plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
-  if (pl.ws_bytes > 0 && (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
+AttendArgs attend_args(const lagkv_attend_params* p, const AttendPlan& pl, bool pick, const void* Q, const void* K, const void* V,
+                       const int32_t* lengths, const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents,
+                       void* out, float* lse, void* ws) {
   AttendArgs a;
   std::memset(&a, 0, sizeof(a));
+  const int es = esize_of(p);
   a.Q = (const char*)Q;
   a.K = (const char*)K;
   a.V = (const char*)V;
@@ -253,6 +243,7 @@ int attend(const lagkv_attend_params* p, const void* Q, const void* K, const voi
   a.rows = pl.rows;
   a.row_tiles = pl.row_tiles;
   a.splits = pl.splits;
+  a.part_splits = pl.splits;
   a.by_tiles = Divide::by(pl.row_tiles);
   a.by_splits = Divide::by(pl.splits);
   a.by_n = Divide::by(p->N);
@@ -260,11 +251,41 @@ int attend(const lagkv_attend_params* p, const void* Q, const void* K, const voi
   a.by_g = Divide::by(p->G);
   a.by_rows = Divide::by(pl.rows);
   a.scale = (float)(p->dtype == LAGKV_F32 ? p->scale : p->scale * 1.4426950408889634);
+  return a;
+}
+
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& pl, int dtype, hipStream_t s) {
+  return pl.wide ? (dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))
+         : dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, pl.waves, s)
+         : dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, pl.waves, s)
+                                  : launch_attend_f16(a, pl.row_tile, pl.waves, s);
+}
+
+}  // namespace lagkv
+
+namespace {
+
+int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
+           const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse,
+           void* ws, size_t ws_bytes, void* hip_stream, bool pick) {
+  int rc = attend_check(p, pick);
+  if (rc != LAGKV_OK) return rc;
+  if (p->N == 0) return LAGKV_OK;
+  if (!Q || !out || (p->T > 0 && (!K || !V)) || (pick && !blocks) || !K_new != !V_new || (parents && !K_new)) return LAGKV_EINVAL;
+  if (parents && p->N > kMaxTree) return LAGKV_ESHAPE;
+  const int64_t n[3] = {p->B, (int64_t)p->H * p->G, p->N};
+  const int64_t st[3] = {p->out_stride_b, p->out_stride_h, p->out_stride_n};
+  if (!rows_apart(p->D, n, st)) return LAGKV_ESHAPE;
+  const int es = esize_of(p);
+  if (!aligned(Q, es) || !aligned(K, es) || !aligned(V, es) || !aligned(K_new, es) || !aligned(V_new, es) || !aligned(out, es) ||
+      !aligned(lengths, 4) || !aligned(parents, 4) || !aligned(blocks, 4) || !aligned(lse, 4))
+    return LAGKV_EINVAL;
+  AttendPlan pl;
+  if (!attend_plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
+  if (pl.ws_bytes > 0 && (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
+  const AttendArgs a = attend_args(p, pl, pick, Q, K, V, lengths, blocks, K_new, V_new, parents, out, lse, ws);
   hipStream_t s = (hipStream_t)hip_stream;
-  hipError_t e = pl.wide ? (p->dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))
-                 : p->dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, pl.waves, s)
-                 : p->dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, pl.waves, s)
-                                          : launch_attend_f16(a, pl.row_tile, pl.waves, s);
+  hipError_t e = launch_attend(a, pl, p->dtype, s);
   if (e == hipSuccess && pl.splits > 1) e = launch_attend_join(a, p->dtype, s);
   return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
 }
@@ -277,19 +298,19 @@ size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p) {
   if (!p) return 0;
   const bool pick = p->n_blocks > 0;
   AttendPlan pl;
-  if (check_attend(p, pick) != LAGKV_OK || p->N == 0 || !plan_of(p, pick, &pl)) return 0;
+  if (attend_check(p, pick) != LAGKV_OK || p->N == 0 || !attend_plan_of(p, pick, &pl)) return 0;
   return pl.ws_bytes;
 }
 
 int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out) {
   if (!p || !out) return LAGKV_EINVAL;
   const bool pick = p->n_blocks > 0;
-  const int rc = check_attend(p, pick);
+  const int rc = attend_check(p, pick);
   if (rc != LAGKV_OK) return rc;
   std::memset(out, 0, sizeof(*out));
   if (p->N == 0) return LAGKV_OK;
   AttendPlan pl;
-  if (!plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
+  if (!attend_plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
   out->many_rows = pl.wide;
   out->row_tile = pl.row_tile;
   out->wavefronts = pl.wide ? pl.row_tile / 32 : pl.waves;
@@ -323,7 +344,7 @@ int lagkv_block_bounds(const lagkv_attend_params* p, const void* K, const int32_
   if (!aligned(K, es) || !aligned(lo, es) || !aligned(hi, es) || !aligned(lengths, 4)) return LAGKV_EINVAL;
   const int64_t nb = (p->T + p->block - 1) / p->block;
   const int64_t n[3] = {p->B, p->H, nb}, st[3] = {p->out_stride_b, p->out_stride_h, p->out_stride_n};
-  if (!apart(p->D, n, st)) return LAGKV_ESHAPE;
+  if (!rows_apart(p->D, n, st)) return LAGKV_ESHAPE;
   BoundsArgs a;
   a.osb = p->out_stride_b * es;
   a.osh = p->out_stride_h * es;

@@ -31,8 +31,8 @@ struct AttendArgs {
   const int32_t* blocks;   // [B,H,N,n_blocks] or nullptr
   char* out;
   float* lse;      // [B,H*G,N] or nullptr
-  float* part_o;   // [units, splits, rows, part_ld], where splits > 1
-  float* part_ml;  // [units, splits, rows, 2]: maximum (base 2), sum
+  float* part_o;   // [units, part_splits, rows, part_ld], where part_splits > 1
+  float* part_ml;  // [units, part_splits, rows, 2]: maximum (base 2), sum
   int64_t qsb, qsh, qsn, ksb, ksh, kst, nsb, nsh, nst, osb, osh, osn, psb;
   int64_t T, units;
   int32_t B, H, G, N, D;
@@ -41,6 +41,7 @@ struct AttendArgs {
   int32_t part_ld;  // D, rounded up to 4
   int32_t rows;    // of a unit
   int32_t row_tiles, splits;
+  int32_t part_splits, part_first;  // pieces of a unit, and the first of them that is this kernel's: `splits` and 0 but for rows behind ones in 8 bits
   Divide by_tiles, by_splits, by_n, by_h, by_g, by_rows;  // row_tiles, splits, N, H, G, rows
   float scale;  // times log2 e for the 16-bit types
 };
@@ -53,6 +54,16 @@ struct AttendPlan {
   int32_t rows;
   size_t off_ml, ws_bytes;
 };
+
+// What the host layer of attend_api.hip has for that of quant_api.hip as well.
+bool rows_apart(int64_t D, const int64_t (&n)[3], const int64_t (&stride)[3]);
+int attend_check(const lagkv_attend_params* p, bool pick);
+double attend_narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces);
+bool attend_plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl);
+AttendArgs attend_args(const lagkv_attend_params* p, const AttendPlan& pl, bool pick, const void* Q, const void* K, const void* V,
+                       const int32_t* lengths, const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents,
+                       void* out, float* lse, void* ws);
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& pl, int dtype, hipStream_t s);
 
 hipError_t launch_attend_f32(const AttendArgs& a, int row_tile, int waves, hipStream_t s);
 hipError_t launch_attend_bf16(const AttendArgs& a, int row_tile, int waves, hipStream_t s);

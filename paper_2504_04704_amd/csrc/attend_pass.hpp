@@ -178,7 +178,8 @@ struct WorkItem {
   int tile, split;
   bool any;
 };
-__device__ __forceinline__ WorkItem work_item(const AttendArgs& a) {
+template <typename Args>
+__device__ __forceinline__ WorkItem work_item(const Args& a) {
   const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, many = a.by_tiles.of(rest), us = many * 8 + slot;
   const uint32_t unit = a.by_splits.of(us);
   WorkItem w;
@@ -661,8 +662,8 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
     // the slots' channels: `dup` leading ones of a slice are the slice before's
     const int slot = quad * 4, begin = slot / PER * PER;
     const int base = begin < a.D ? slice_at(slot / PER, a.D, PER) : 0, dup = begin - base, within = slot - begin;
-    if (a.splits > 1) {
-      const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
+    if (a.part_splits > 1) {
+      const int64_t at = (w.unit * a.part_splits + a.part_first + w.split) * a.rows + r;
       if (slices && begin < a.D) {
         *(f32x4*)(a.part_o + at * a.part_ld + slot) = v;
       } else if (begin < a.D) {

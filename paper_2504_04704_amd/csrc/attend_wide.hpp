@@ -1,5 +1,5 @@
 // Attention of many query rows over all rows of a cache (lagkv_attend, 16-bit types; the mathematics is attend_pass.hpp's; when
-// it is taken, plan_of says).
+// it is taken, attend_plan_of says).
 //
 // Where a stream has tens of query rows (a drafted tree under grouped heads, a chunk of a prompt) the matrix cores are the
 // bound, not memory: 256 rows make 256 flop of a cache byte.  A workgroup of four or eight wavefronts goes over 64 cache
@@ -364,8 +364,8 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   if (!mine) return;
   l = sum_across_32(l);
   const bool whole = a.D % 8 == 0;
-  if (a.splits > 1) {
-    const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
+  if (a.part_splits > 1) {
+    const int64_t at = (w.unit * a.part_splits + a.part_first + w.split) * a.rows + r;
     float* po = a.part_o + at * a.part_ld;
 #pragma unroll
     for (int d = 0; d < DT32; ++d)

@@ -1,0 +1,41 @@
+// 8-bit codes in registers: to and from floating point.
+#pragma once
+#include "attend_pass.hpp"
+
+namespace lagkv {
+
+typedef uint32_t u32v2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32v4_bytes __attribute__((ext_vector_type(4), aligned(1)));
+
+template <int CODE>
+struct Code;
+template <>
+struct Code<LAGKV_CODE_INT8> {
+  // Four codes as binary16: with 128 added, a code is the low byte of a number between 1024 and 1279.
+  static __device__ __forceinline__ void to_half(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    const uint32_t u = w ^ 0x80808080u;
+    const f16x2 k = {(_Float16)1152.f, (_Float16)1152.f};
+    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - k);
+    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - k);
+  }
+  static __device__ __forceinline__ void to_float(uint32_t w, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  }
+};
+template <>
+struct Code<LAGKV_CODE_E4M3> {
+  static __device__ __forceinline__ void to_half(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true));
+  }
+  static __device__ __forceinline__ void to_float(uint32_t w, float* x) {
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    x[0] = a[0];
+    x[1] = a[1];
+    x[2] = b[0];
+    x[3] = b[1];
+  }
+};
+
+}  // namespace lagkv

@@ -1,0 +1,408 @@
+// Attention of few query rows over rows in 8 bits (lagkv_attend_quantized; the mathematics is attend_pass.hpp's).
+//
+// With codes k_t, v_t and their blocks' scales s_t, r_t the logits are x_t = scale s_t q.k_t and the outputs sum (p_t r_t) v_t: a
+// scale is a factor of a logit and of a weight, and the products take the codes as they are.  Binary16 holds them (whole numbers up to 128,
+// and numbers of 4 mantissa bits from 2^-9 to 448), so both products go to the matrix cores in that type, whatever that of Q.
+//
+// A wavefront takes every fourth step of 64 cache rows (32 where 64 do not fit the registers) for all query rows of its workgroup; K's codes become
+// numbers in the registers that they are loaded into, V's on their way into LDS.  Scales are those of sixteen rows that
+// lie in one block.  Weights times scales go in as two numbers of binary16, relative to the largest scale's power of two that
+// the wavefront has met, as exponentials are relative to the largest logit: scales of 1e-30 are as good as those of 1.
+//
+// Each piece of a cache leaves its maximum, sum and outputs; launch_attend_join joins them with those of the tail and the new tokens.
+#pragma once
+#include "code_ops.hpp"
+#include "quant_internal.hpp"
+
+namespace lagkv {
+
+constexpr float kQuantLift = 14.f;  // weights are held times 2^14, as in AElem<LAGKV_F16>
+
+template <int DP, int RT>
+struct QuantShape {
+  static constexpr int SUBS = DP * RT > 128 ? 2 : 4, KT = 16 * SUBS;  // sixteens of a step
+  static constexpr int CPR = DP / 16, NC = CPR / 4;              // slices of 16 codes in a row; a lane's of K
+  static constexpr int VROWS = 64 / CPR, NV = KT / VROWS;        // rows that a wavefront loads at a time
+  static constexpr int ROWS = 16 * RT;
+  static constexpr int LDV = DP * 2 + 32;  // bytes between rows of V in LDS
+  static constexpr int LDO = DP + 4;       // floats between rows of the outputs in LDS
+  static constexpr int V_BYTES = 4 * KT * LDV, O_BYTES = 4 * ROWS * LDO * 4;
+  static constexpr int MAIN = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
+};
+
+// A lane's part of a query row as binary16: eight channels of each of 2 * NC slices, times a power of two (of fp32 the rest as
+// well).  What a slice behind the row's end repeats is 0.
+template <int DT, int NC>
+struct Query {
+  static constexpr int PARTS = DT == LAGKV_F32 ? 2 : 1;
+  u32v4 part[PARTS][2 * NC];
+  float unit;  // that power's inverse
+  __device__ __forceinline__ void load(const char* p, int grp, int D, bool there) {
+    constexpr int ES = AElem<DT>::SIZE;
+    uint32_t raw[2 * NC][2 * ES];
+#pragma unroll
+    for (int j = 0; j < 2 * NC; ++j) {
+      const int slice = j / 2 * 4 + grp, base = (slice * 16 < D ? slice_at(slice, D, 16) : 0) + j % 2 * 8;
+#pragma unroll
+      for (int i = 0; i < 2 * ES; i += 4) {
+        const u32v4 v = *(const u32v4_any*)(p + base * ES + i * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[j][i + e] = v[e];
+      }
+    }
+    // channels that are this slice's own
+#pragma unroll
+    for (int j = 0; j < 2 * NC; ++j) {
+      const int begin = (j / 2 * 4 + grp) * 16, dup = begin + 16 <= D ? 0 : begin < D ? begin + 16 - D : 16;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool own = there && j % 2 * 8 + e >= dup;
+        if constexpr (DT == LAGKV_F32) raw[j][e] = own ? raw[j][e] : 0u;
+        else raw[j][e / 2] &= own ? ~0u : e % 2 ? 0x0000ffffu : 0xffff0000u;
+      }
+    }
+    if constexpr (DT == LAGKV_F16) {
+      unit = 1.f;
+#pragma unroll
+      for (int j = 0; j < 2 * NC; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[0][j][i] = raw[j][i];
+    } else {
+      auto at = [&](int j, int e) {
+        if constexpr (DT == LAGKV_F32) return __uint_as_float(raw[j][e]);
+        else return AElem<LAGKV_BF16>::one((uint16_t)(raw[j][e / 2] >> (16 * (e % 2))));
+      };
+      float most = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2 * NC; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = fabsf(at(j, e));
+          most = fmaxf(most, x < INFINITY ? x : 0.f);
+        }
+      most = max_across_32(max_across_16(most));
+      const uint32_t exponent = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+      const float by = __uint_as_float((254u - exponent) << 23);
+      unit = __uint_as_float(exponent << 23);
+#pragma unroll
+      for (int j = 0; j < 2 * NC; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = at(j, 2 * i) * by, y = at(j, 2 * i + 1) * by;
+          const uint32_t hi = AElem<LAGKV_F16>::pack(x, y);
+          part[0][j][i] = hi;
+          if constexpr (PARTS == 2) {
+            const f32x2 back = __builtin_convertvector(__builtin_bit_cast(f16x2, hi), f32x2);
+            // (nothing is left of an infinity, and not NaN)
+            part[1][j][i] = AElem<LAGKV_F16>::pack(fabsf(x) < INFINITY ? x - back.x : 0.f, fabsf(y) < INFINITY ? y - back.y : 0.f);
+          }
+        }
+    }
+  }
+};
+
+template <int CODE>
+__device__ __forceinline__ void half_of(u32v4 w, u32v4& lo, u32v4& hi) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t a, b;
+    Code<CODE>::to_half(w[i], a, b);
+    lo[2 * i] = a;
+    lo[2 * i + 1] = b;
+    Code<CODE>::to_half(w[2 + i], a, b);
+    hi[2 * i] = a;
+    hi[2 * i + 1] = b;
+  }
+}
+
+template <int DT, int CODE, int DP, int RT>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(const QuantArgs a) {
+  using E = AElem<DT>;
+  using F = AElem<LAGKV_F16>;
+  using Sh = QuantShape<DP, RT>;
+  constexpr int SUBS = Sh::SUBS, KT = Sh::KT, CPR = Sh::CPR, NC = Sh::NC, VROWS = Sh::VROWS, NV = Sh::NV, ROWS = Sh::ROWS;
+  constexpr int LDV = Sh::LDV, LDO = Sh::LDO, DT16 = DP / 16, WAVES = 4, THREADS = 256;
+  extern __shared__ __attribute__((aligned(16))) char quant_lds[];
+  __shared__ float sh_ml[WAVES][ROWS][2];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
+
+  fetch_arguments<QuantArgs>();
+  const WorkItem w = work_item(a);
+  if (!w.any) return;
+  const uint32_t bu = a.by_h.of((uint32_t)w.unit);
+  const int64_t b = bu, h = (uint32_t)w.unit - bu * (uint32_t)a.H;
+  const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
+  const int64_t held = a.lengths ? a.lengths[b] : a.T;
+  const int len = (int)(held < 0 ? 0 : held > a.T ? a.T : held);
+  const int steps = (int)(((int64_t)len + KT - 1) / KT);
+  const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
+  const char* kb = a.Kq + b * a.csb + h * a.csh;
+  const char* vb = a.Vq + b * a.csb + h * a.csh;
+  const float* ksb = a.ks + b * a.ssb + h * a.ssh;
+  const float* vsb = a.vs + b * a.ssb + h * a.ssh;
+  char* vl = quant_lds + wave * (KT * LDV);
+
+  auto offset = [&](int slice) { return slice * 16 < a.D ? slice_at(slice, a.D, 16) : 0; };
+  const int vslice = lane % CPR, vrow = lane / CPR, voff = offset(vslice);
+  int koff[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) koff[c] = offset(c * 4 + grp);
+  u32v4 kf[SUBS][NC], vf[NV];
+  float ks[SUBS], vs[SUBS];  // of the rows in kf and vf, as the step's scales are loaded with them
+  auto load_k = [&](int step) {
+    const int first = step * KT;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      const int row = first + s * 16 + col;
+      const char* at = kb + (int64_t)(row < len ? row : len - 1) * a.cst;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) kf[s][c] = *(const u32v4_bytes*)(at + koff[c]);
+      ks[s] = ksb[min(first + s * 16, len - 1) >> a.block_shift];
+    }
+  };
+  auto load_v = [&](int step) {
+    const int first = step * KT;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int row = first + i * VROWS + vrow;
+      vf[i] = *(const u32v4_bytes*)(vb + (int64_t)(row < len ? row : len - 1) * a.cst + voff);
+    }
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) vs[s] = vsb[min(first + s * 16, len - 1) >> a.block_shift];
+  };
+
+  int step = step0 + wave;
+  if (step < step1) {
+    load_k(step);
+    load_v(step);
+  }
+  Query<DT, NC> q[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + rt * 16 + col, rr = r < row1 ? r : row0, n = (int)a.by_g.of(rr);
+    q[rt].load(a.Q + b * a.qsb + (h * a.G + rr - n * a.G) * a.qsh + (int64_t)n * a.qsn, grp, a.D, r < row1);
+  }
+  float m[RT], l[RT];
+  f32x4 o[RT][DT16];
+  int top_scale = 0;  // exponent (biased) of the largest scale of V so far: o is relative to it
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = -INFINITY;
+    l[rt] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT16; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (; step < step1; step += WAVES) {
+    const bool more = step + WAVES < step1, whole = (step + 1) * KT <= len;
+    const int first = step * KT;
+    wave_order();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      // (a row that is not there: its codes may be no numbers)
+      if (!whole && first + i * VROWS + vrow >= len) vf[i] = u32v4{0, 0, 0, 0};
+      u32v4 lo, hi;
+      half_of<CODE>(vf[i], lo, hi);
+      char* at = vl + (i * VROWS + vrow) * LDV + vslice * 32;
+      *(u32v4*)at = lo;
+      *(u32v4*)(at + 16) = hi;
+    }
+    wave_order();
+    float r[SUBS];
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) r[s] = whole || first + s * 16 < len ? vs[s] : 0.f;
+    if (more) load_v(step + WAVES);
+    __builtin_amdgcn_sched_barrier(0);
+
+    f32x4 p[RT][SUBS];
+    float x_scale[SUBS];
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) p[rt][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        u32v4 k[2];
+        half_of<CODE>(kf[s][c], k[0], k[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int part = 0; part < Query<DT, NC>::PARTS; ++part) p[rt][s] = F::mma(k[i], q[rt].part[part][c * 2 + i], p[rt][s]);
+      }
+      x_scale[s] = ks[s] * a.scale;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load_k(step + WAVES);
+    __builtin_amdgcn_sched_barrier(0);
+
+    // scales of V, as parts of the largest's power of two
+    {
+      uint32_t most = 0;
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s) most = max(most, __float_as_uint(r[s]) & 0x7fffffffu);
+      const int now = (int)(most >> 23);
+      if (now > top_scale) {
+        const float f = __builtin_ldexpf(1.f, top_scale - now);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int d = 0; d < DT16; ++d) o[rt][d] *= f;
+        top_scale = now;
+      }
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s) r[s] = __builtin_ldexpf(r[s], 126 - top_scale);
+    }
+    u32v4 ph[RT][SUBS / 2], pl[RT][SUBS / 2];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s) p[rt][s] *= x_scale[s] * q[rt].unit;
+      if (!whole) {
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (first + s * 16 + grp * 4 + i >= len) p[rt][s][i] = -INFINITY;
+      }
+      float top = p[rt][0][0];
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, p[rt][s][i]);
+      top = max_across_32(max_across_16(top));
+      const float before = m[rt];
+      m[rt] = fmaxf(before, top);
+      const float at = m[rt] == -INFINITY ? 0.f : m[rt];
+      const float keep = __builtin_amdgcn_exp2f((before - at) * E::UNIT);
+      float sum = 0.f;
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // (the difference first: its rounding is that of a number near zero)
+          const float e = __builtin_amdgcn_exp2f((p[rt][s][i] - at) * E::UNIT + kQuantLift);
+          p[rt][s][i] = e * r[s];
+          sum += e;
+        }
+      l[rt] = l[rt] * keep + sum;
+      if (__any(keep != 1.f)) {
+#pragma unroll
+        for (int d = 0; d < DT16; ++d) o[rt][d] *= keep;
+      }
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t hi, lo;
+          F::split(p[rt][s][2 * i], p[rt][s][2 * i + 1], hi, lo);
+          ph[rt][s / 2][s % 2 * 2 + i] = hi;
+          pl[rt][s / 2][s % 2 * 2 + i] = lo;
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DT16; ++d)
+#pragma unroll
+      for (int t = 0; t < SUBS / 2; ++t) {
+        u32v4 v;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_s16x4)(vl + ((t * 2 + s) * 16 + grp * 4 + (col >> 2)) * LDV + (d * 16 + (col & 3) * 4) * 2));
+          const u32v2 y = __builtin_bit_cast(u32v2, x);
+          v[s * 2] = y.x;
+          v[s * 2 + 1] = y.y;
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          o[rt][d] = F::mma(v, ph[rt][t], o[rt][d]);
+          o[rt][d] = F::mma(v, pl[rt][t], o[rt][d]);
+        }
+      }
+  }
+
+  // the wavefronts' states join, with the scales put in
+  constexpr float LIFT = E::LIFT - kQuantLift;  // what launch_attend_join counts on, over what there is
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float sum = l[rt];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (grp == 0) {
+      sh_ml[wave][rt * 16 + col][0] = m[rt];
+      sh_ml[wave][rt * 16 + col][1] = sum;
+    }
+  }
+  __syncthreads();  // (V of all wavefronts is done with as well)
+  float* ol = (float*)quant_lds;
+  const float lift = __builtin_ldexpf(1.f, (int)LIFT), unit = __builtin_ldexpf(lift, top_scale - 126);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
+    const bool none = sh_ml[wave][rt * 16 + col][1] == 0.f;  // (what is no number has a maximum of -inf too, and is not dropped)
+    const float f = none ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT) * unit;
+#pragma unroll
+    for (int d = 0; d < DT16; ++d)
+      *(f32x4*)(ol + (wave * ROWS + rt * 16 + col) * LDO + d * 16 + grp * 4) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][d] * f;
+  }
+  __syncthreads();
+  constexpr int QUADS = DP / 4;
+  for (int i = tid; i < ROWS * QUADS; i += THREADS) {
+    const int rl = i / QUADS, quad = i % QUADS, r = row0 + rl;
+    if (r >= row1) continue;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rl][0]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) {
+      const float lx = sh_ml[x][rl][1];
+      if (lx != 0.f) sum += lx * __builtin_amdgcn_exp2f((sh_ml[x][rl][0] - top) * E::UNIT);
+      v += *(const f32x4*)(ol + (x * ROWS + rl) * LDO + quad * 4);
+    }
+    // the slots' channels: `dup` leading ones of a slice are the slice before's
+    const int slot = quad * 4, begin = slot / 16 * 16;
+    const int base = begin < a.D ? slice_at(slot / 16, a.D, 16) : 0, dup = begin - base, within = slot - begin;
+    const int64_t at = (w.unit * a.part_splits + w.split) * a.rows + r;
+    if (begin < a.D && dup == 0) {
+      *(f32x4*)(a.part_o + at * a.part_ld + slot) = v;
+    } else if (begin < a.D) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (within + e >= dup) a.part_o[at * a.part_ld + base + within + e] = v[e];
+    }
+    if (quad == 0) {
+      a.part_ml[at * 2] = top;
+      a.part_ml[at * 2 + 1] = sum * lift;
+    }
+  }
+}
+
+template <int DT, int CODE, int DP, int RT>
+hipError_t launch_quant_as(const QuantArgs& a, hipStream_t s) {
+  const int64_t groups = (a.units * a.splits + 7) / 8 * 8 * a.row_tiles;
+  constexpr size_t lds = QuantShape<DP, RT>::MAIN;
+  auto kernel = attend_quant_kernel<DT, CODE, DP, RT>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((uint32_t)groups), dim3(256), lds, s>>>(a);
+  return hipGetLastError();
+}
+template <int DT, int CODE>
+hipError_t launch_quant_code(const QuantArgs& a, int row_tile, hipStream_t s) {
+  const bool one = row_tile == 16;
+  if (a.D <= 64) return one ? launch_quant_as<DT, CODE, 64, 1>(a, s) : launch_quant_as<DT, CODE, 64, 2>(a, s);
+  if (a.D <= 128) return one ? launch_quant_as<DT, CODE, 128, 1>(a, s) : launch_quant_as<DT, CODE, 128, 2>(a, s);
+  return launch_quant_as<DT, CODE, 256, 1>(a, s);
+}
+template <int DT>
+hipError_t launch_quant_of(const QuantArgs& a, int code, int row_tile, hipStream_t s) {
+  return code == LAGKV_CODE_INT8 ? launch_quant_code<DT, LAGKV_CODE_INT8>(a, row_tile, s) : launch_quant_code<DT, LAGKV_CODE_E4M3>(a, row_tile, s);
+}
+
+}  // namespace lagkv

@@ -1,0 +1,9 @@
+#include "quant_attend.hpp"
+
+namespace lagkv {
+
+hipError_t launch_quant_f16(const QuantArgs& a, int code, int row_tile, hipStream_t s) {
+  return launch_quant_of<LAGKV_F16>(a, code, row_tile, s);
+}
+
+}  // namespace lagkv

@@ -39,7 +39,9 @@ EXPORTS = ("lagkv_plan", "lagkv_keep_for_compression", "lagkv_workspace_bytes", 
            "lagkv_kernel_for", "lagkv_strerror",
            "lagkv_version",
            "lagkv_attend_workspace_bytes", "lagkv_attend_plan", "lagkv_attend", "lagkv_attend_blocks", "lagkv_block_bounds",
-           "lagkv_select_blocks")
+           "lagkv_select_blocks",
+           "lagkv_quantize", "lagkv_dequantize", "lagkv_attend_quantized_workspace_bytes", "lagkv_attend_quantized_plan",
+           "lagkv_attend_quantized")
 
 
 class LagKVError(RuntimeError):
@@ -78,6 +80,15 @@ class AttendParams(C.Structure):
 
 class AttendPlanT(C.Structure):
     _fields_ = [("many_rows", C.c_int32), ("row_tile", C.c_int32), ("wavefronts", C.c_int32), ("pieces", C.c_int32)]
+
+
+class QuantParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("G", C.c_int32), ("N", C.c_int32), ("D", C.c_int32),
+                ("dtype", C.c_int32), ("code", C.c_int32), ("block", C.c_int32),
+                ("T", C.c_int64), ("R", C.c_int64), ("scale", C.c_double),
+                ("code_stride", C.c_int64 * 3), ("scale_stride", C.c_int64 * 2), ("row_stride", C.c_int64 * 3),
+                ("q_stride", C.c_int64 * 3), ("new_stride", C.c_int64 * 3), ("out_stride", C.c_int64 * 3),
+                ("parents_stride_b", C.c_int64)]
 
 
 def lib_path() -> str:
@@ -143,6 +154,17 @@ def load():
     lib.lagkv_block_bounds.restype = C.c_int
     lib.lagkv_select_blocks.argtypes = [ap, vp, vp, vp, vp, C.c_int32, C.c_int32, vp, vp, sz, vp]
     lib.lagkv_select_blocks.restype = C.c_int
+    qp = C.POINTER(QuantParams)
+    lib.lagkv_quantize.argtypes = [qp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.lagkv_quantize.restype = C.c_int
+    lib.lagkv_dequantize.argtypes = [qp, vp, vp, vp, vp, vp, i64, vp, vp, vp]
+    lib.lagkv_dequantize.restype = C.c_int
+    lib.lagkv_attend_quantized_workspace_bytes.argtypes = [qp]
+    lib.lagkv_attend_quantized_workspace_bytes.restype = sz
+    lib.lagkv_attend_quantized_plan.argtypes = [qp, C.POINTER(AttendPlanT), C.POINTER(AttendPlanT)]
+    lib.lagkv_attend_quantized_plan.restype = C.c_int
+    lib.lagkv_attend_quantized.argtypes = [qp] + [vp] * 15 + [sz, vp]
+    lib.lagkv_attend_quantized.restype = C.c_int
     _lib = lib
     _native = _load_native(lib)
     return lib
@@ -639,6 +661,189 @@ def select_blocks(q: torch.Tensor, lo: torch.Tensor, hi: torch.Tensor, T: int, b
                                           last, out.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
                                           _stream_ptr(q.device)), "lagkv_select_blocks")
     return out
+
+
+# ---- a cache in 8 bits (include/lagkv.h, "A cache in 8 bits") ----
+
+CODE_INT8, CODE_E4M3 = 0, 1
+_CODES = {torch.int8: CODE_INT8, torch.float8_e4m3fn: CODE_E4M3}
+
+
+@dataclass
+class Quantized:
+    """Rows in 8 bits: a row's value is its code times the scale of its block of rows."""
+    K: torch.Tensor                 # [B,H,T,D] int8 or float8_e4m3fn
+    V: torch.Tensor
+    K_scale: torch.Tensor           # [B,H,ceil(T/block)] fp32
+    V_scale: torch.Tensor
+    block: int
+
+    @classmethod
+    def empty(cls, B: int, H: int, T: int, D: int, block: int, code: torch.dtype = torch.int8, device="cuda") -> "Quantized":
+        """Room for T rows."""
+        K, V = (torch.empty((B, H, T, D), dtype=torch.int8, device=device).view(code) for _ in range(2))
+        nb = -(-T // index(block))
+        return cls(K, V, *(torch.empty((B, H, nb), dtype=torch.float32, device=device) for _ in range(2)), index(block))
+
+    def view(self, n: int, batch: slice = slice(None)) -> "Quantized":
+        """The first n rows (of a slice of the batch)."""
+        nb = -(-n // self.block)
+        return Quantized(self.K[batch, :, :n], self.V[batch, :, :n], self.K_scale[batch, :, :nb], self.V_scale[batch, :, :nb], self.block)
+
+
+def _quant_params(x: Quantized, dtype) -> QuantParams:
+    """The parameters that are those of the codes, which it looks over."""
+    K, V, ks, vs = x.K, x.V, x.K_scale, x.V_scale
+    block = index(x.block)
+    _int32("Quantized", block, *K.shape)
+    if K.dim() != 4 or (K.stride(3) != 1 and K.shape[3] > 1):
+        raise ValueError("codes must be a 4-dimensional tensor with contiguous channels")
+    if K.dtype not in _CODES:
+        raise TypeError(f"codes: unsupported dtype {K.dtype}")
+    if not K.is_cuda:
+        raise RuntimeError("codes must be a device tensor; there is no CPU path")
+    _same_layout(K, V)
+    if block < 1:
+        raise LagKVError(EINVAL, "Quantized")
+    B, H, T, D = K.shape
+    nb = -(-T // block)
+    for t in (ks, vs):
+        if t.dtype != torch.float32 or tuple(t.shape) != (B, H, nb) or t.device != K.device or (t.stride(2) != 1 and nb > 1) or t.stride() != ks.stride():
+            raise ValueError("scales must be two fp32 [B,H,ceil(T/block)] tensors with the same strides, contiguous blocks, on the device of the codes")
+    p = QuantParams(B=B, H=H, D=D, dtype=_DTYPES[dtype], code=_CODES[K.dtype], block=block, T=T)
+    p.code_stride[:] = K.stride()[:3]
+    p.scale_stride[:] = ks.stride()[:2]
+    return p
+
+
+def quantize(K: torch.Tensor, V: torch.Tensor, block: int, code: torch.dtype = torch.int8, lengths: Optional[torch.Tensor] = None,
+             start: int = 0, out: Optional[Quantized] = None) -> Quantized:
+    """lagkv_quantize: rows K, V [B,H,T,D] as codes (torch.int8 or torch.float8_e4m3fn) with a scale for each block of `block`
+    rows and head.  With `start` and `out` only the blocks from that of row `start` on are written; rows behind lengths[b] are left
+    as they are."""
+    block, start = index(block), index(start)
+    _int32("lagkv_quantize", block)
+    _rows("K", K)
+    _same_layout(K, V)
+    _no_grad(K, V)
+    if block < 1 or start < 0:
+        raise LagKVError(EINVAL, "lagkv_quantize")
+    B, H, T, D = K.shape
+    if out is None:
+        if code not in _CODES:
+            raise TypeError(f"codes: unsupported dtype {code}")
+        if start > 0:
+            raise ValueError("start needs out: the blocks before it are left as they are")
+        out = Quantized.empty(B, H, T, D, block, code, K.device)
+    elif out.block != block or out.K.shape != K.shape or out.K.device != K.device:
+        raise ValueError("out must hold codes of the shape of K, in blocks of `block` rows, on its device")
+    p = _quant_params(out, K.dtype)
+    _no_grad(out.K, out.V, out.K_scale, out.V_scale)
+    p.row_stride[:] = K.stride()[:3]
+    if lengths is not None:
+        _ints("lengths", lengths, (B,), K.device)
+    with _on(K.device):
+        _check(load().lagkv_quantize(C.byref(p), K.data_ptr(), V.data_ptr(), _ptr(lengths), start, out.K.data_ptr(), out.V.data_ptr(),
+                                     out.K_scale.data_ptr(), out.V_scale.data_ptr(), _stream_ptr(K.device)), "lagkv_quantize")
+    return out
+
+
+def dequantize(x: Quantized, dtype: torch.dtype = torch.bfloat16, lengths: Optional[torch.Tensor] = None, start: int = 0,
+               out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """lagkv_dequantize: the rows K, V [B,H,T,D] that the codes stand for, in `dtype` (that of `out` where it is given).  Rows before
+    `start` and behind lengths[b] are left as they are (not written, in new tensors)."""
+    start = index(start)
+    if start < 0:
+        raise LagKVError(EINVAL, "lagkv_dequantize")
+    if out is None:
+        if dtype not in _DTYPES:
+            raise TypeError(f"unsupported dtype {dtype}")
+        out = tuple(torch.empty(x.K.shape, dtype=dtype, device=x.K.device) for _ in range(2))
+    K, V = out
+    _rows("out", K)
+    _same_layout(K, V)
+    _no_grad(K, V, x.K, x.V, x.K_scale, x.V_scale)
+    if K.shape != x.K.shape or K.device != x.K.device:
+        raise ValueError("output buffers must be [B,H,T,D] as the codes, on their device")
+    p = _quant_params(x, K.dtype)
+    p.row_stride[:] = K.stride()[:3]
+    if lengths is not None:
+        _ints("lengths", lengths, (p.B,), K.device)
+    with _on(K.device):
+        _check(load().lagkv_dequantize(C.byref(p), x.K.data_ptr(), x.V.data_ptr(), x.K_scale.data_ptr(), x.V_scale.data_ptr(),
+                                       _ptr(lengths), start, K.data_ptr(), V.data_ptr(), _stream_ptr(K.device)), "lagkv_dequantize")
+    return K, V
+
+
+def attend_quantized_plan(p: QuantParams) -> Tuple[AttendPlanT, AttendPlanT]:
+    """lagkv_attend_quantized_plan: the launch shape of an attend_quantized call, of the rows in 8 bits and of those behind them."""
+    codes, rows = AttendPlanT(), AttendPlanT()
+    _check(load().lagkv_attend_quantized_plan(C.byref(p), C.byref(codes), C.byref(rows)), "lagkv_attend_quantized_plan")
+    return codes, rows
+
+
+def attend_quantized(q: torch.Tensor, x: Quantized, K_tail: Optional[torch.Tensor] = None, V_tail: Optional[torch.Tensor] = None,
+                     K_new: Optional[torch.Tensor] = None, V_new: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
+                     lengths: Optional[torch.Tensor] = None, tail_lengths: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None, want_lse: bool = False, ws: Optional[torch.Tensor] = None) -> Attended:
+    """lagkv_attend_quantized: `attend` over the rows that x holds in 8 bits (its first lengths[b]), over rows K_tail, V_tail
+    [B,H,R,D] behind them that are not quantised (their first tail_lengths[b]) and, with K_new, V_new [B,H,N,D], over the new tokens
+    themselves.  There is no backward pass."""
+    _rows("q", q)
+    p = _quant_params(x, q.dtype)
+    _no_grad(q, K_tail, V_tail, K_new, V_new, x.K, x.V, x.K_scale, x.V_scale)
+    B, H, D = p.B, p.H, p.D
+    heads, N = q.shape[1], q.shape[2]
+    if q.device != x.K.device or q.shape[0] != B or q.shape[3] != D or H == 0 or heads % H:
+        raise ValueError("q must be [B,H*G,N,D] for codes [B,H,T,D], on their device")
+    p.G, p.N, p.scale = heads // H, N, 1.0 / math.sqrt(D) if scale is None else float(scale)
+    p.q_stride[:] = q.stride()[:3]
+    device = q.device
+    if (K_tail is None) != (V_tail is None) or (K_new is None) != (V_new is None) or (parents is not None and K_new is None):
+        raise ValueError("K_tail and V_tail go together, K_new and V_new, and parents with these")
+    if K_tail is not None:
+        _rows("K_tail", K_tail, q)
+        _same_layout(K_tail, V_tail)
+        if K_tail.shape[:2] != (B, H) or K_tail.shape[3] != D:
+            raise ValueError("K_tail, V_tail must be [B,H,R,D]")
+        p.R = K_tail.shape[2]
+        p.row_stride[:] = K_tail.stride()[:3]
+    elif tail_lengths is not None:
+        raise ValueError("tail_lengths go with K_tail and V_tail")
+    if K_new is not None:
+        _rows("K_new", K_new, q)
+        _same_layout(K_new, V_new)
+        if tuple(K_new.shape) != (B, H, N, D):
+            raise ValueError("K_new, V_new must be [B,H,N,D]")
+        p.new_stride[:] = K_new.stride()[:3]
+    if parents is not None:
+        if parents.dim() == 2:
+            _ints("parents", parents, (B, N), device)
+            p.parents_stride_b = N
+        else:
+            _ints("parents", parents, (N,), device)
+    for name, t in (("lengths", lengths), ("tail_lengths", tail_lengths)):
+        if t is not None:
+            _ints(name, t, (B,), device)
+    if out is None:
+        out = torch.empty_like(q)
+        if out.stride(3) != 1 and D > 1:
+            out = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        _rows("out", out, q)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    p.out_stride[:] = out.stride()[:3]
+    lse = torch.empty((B, heads, N), dtype=torch.float32, device=device) if want_lse else None
+    lib = load()
+    ref = C.byref(p)
+    with _on(device):
+        ws = _bytes(ws, lib.lagkv_attend_quantized_workspace_bytes(ref), device)
+        _check(lib.lagkv_attend_quantized(
+            ref, q.data_ptr(), x.K.data_ptr(), x.V.data_ptr(), x.K_scale.data_ptr(), x.V_scale.data_ptr(), _ptr(lengths), _ptr(K_tail),
+            _ptr(V_tail), _ptr(tail_lengths), _ptr(K_new), _ptr(V_new), _ptr(parents), out.data_ptr(), _ptr(lse), _ptr(ws),
+            0 if ws is None else ws.numel(), _stream_ptr(device)), "lagkv_attend_quantized")
+    return Attended(out, lse)
 
 
 class Cache:
