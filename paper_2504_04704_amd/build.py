@@ -18,7 +18,8 @@ SOURCES = ["lagkv_api.hip", "split_pass.hip", "hold_pass.hip", "append_pass.hip"
            "ring_f32.hip", "ring_bf16.hip", "ring_f16.hip",
            "round_f32.hip", "round_bf16.hip", "round_f16.hip", "static_scratch.hip",
            "attend_api.hip", "attend_f32.hip", "attend_bf16.hip", "attend_f16.hip", "attend_wide_bf16.hip", "attend_wide_f16.hip",
-           "attend_join.hip", "block_pass.hip", "quant_api.hip", "quant_rows.hip", "quant_f32.hip", "quant_bf16.hip", "quant_f16.hip"]
+           "attend_join.hip", "block_pass.hip", "quant_api.hip", "quant_rows.hip", "quant_f32.hip", "quant_bf16.hip", "quant_f16.hip",
+           "quant_wide_bf16.hip", "quant_wide_f16.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

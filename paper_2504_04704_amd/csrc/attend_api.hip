@@ -35,47 +35,6 @@ int check_tokens(const lagkv_attend_params* p) {
   return LAGKV_OK;
 }
 
-// Workgroups of the fullest of the eight XCDs (work_item deals units and pieces to them in turn, with all their tiles).
-int64_t fullest_xcd(int64_t units, int64_t pieces, int64_t row_tiles) { return (units * pieces + 7) / 8 * row_tiles; }
-
-// 1 2 3 4 6 8 12 16 24 ...
-int64_t next_pieces(int64_t s) { return s + (s < 4 ? 1 : s % 3 == 0 ? s / 3 : s / 2); }
-
-// Tiles of many rows: 128 query rows (four wavefronts, two workgroups a compute unit) or, for 65 to 128 channels, 256 (eight, one;
-// for fewer channels they were the faster ones of none of 164 shapes), and the pieces that
-// the cache is cut into, by the microseconds that they take: a step of 64 cache rows, the beginning and end of a workgroup,
-// and, with pieces, a second kernel and every piece of a row written and read.  A step takes longer the more compute
-// units are at work, and less where wavefronts of the eight have no rows.  Measured, 128 channels, model beside it (us; it
-// falls short by a seventh in the mean, as attend_narrow_shape's does, and what counts is which is the least):
-//    8 streams,  256 query rows, 1000 rows   128 in 4 19 (18)   128 in 8 18 (16)   256 in 8 23 (20)   few rows 16 (15)
-//   32 streams,  256 query rows, 2000 rows   128 in 4 33 (27)   128 in 8 35 (28)   256 in 4 36 (32)   256 in 8 34 (30)
-//   32 streams,  256 query rows, 8000 rows   128 in 4 77 (62)   128 in 8 70 (57)   256 in 4 77 (74)   256 in 8 63 (54)
-//   64 streams,  160 query rows, 8000 rows   128 in 4 100 (91)   128 in 8 105 (105)   256 in 2 124 (106)   256 in 4 82 (69)
-// Over 914 shapes (64, 128 and 256 channels, 48 to 2048 query rows of 2 to 400 streams, 200 to 16000 rows) its choice takes 1.1 %
-// longer than the best tile and number of pieces in the mean.
-double wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_tile, int64_t* pieces) {
-  const double channels = D <= 64 ? 0.57 : D <= 128 ? 1 : 2.2;
-  double least = 1e30;
-  for (int tile = 128; tile <= (D > 64 && D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
-    const int64_t groups = units * ((rows + tile - 1) / tile), places = tile == 256 || D > 128 ? 256 : 512;
-    const double full = (double)(units * rows) / (double)(groups * tile);
-    for (int64_t s = 1; s <= 256 && s <= steps; s = next_pieces(s)) {
-      const int64_t all = 8 * fullest_xcd(units, s, (rows + tile - 1) / tile);
-      const double busy = all < 256 ? (double)all / 256 : 1;
-      const double step = tile == 256 ? 0.85 + (0.65 + 0.5 * busy) * full : channels * (all > 256 && D <= 128 ? 2.35 : 1.25 + 0.2 * busy);
-      const double ends = tile == 256 ? 12 : D <= 64 ? 7.3 : D <= 128 ? 9 : 8.5;
-      const double us = (double)((all + places - 1) / places) * ((double)((steps + s - 1) / s) * step + ends) +
-                        (s > 1 ? 2.5 + (double)(units * rows * s) * (double)D * 8 / 9e6 : 0);
-      if (us < least) {
-        least = us;
-        *row_tile = tile;
-        *pieces = s;
-      }
-    }
-  }
-  return least;
-}
-
 }  // namespace
 
 namespace lagkv {
@@ -111,90 +70,6 @@ int attend_check(const lagkv_attend_params* p, bool pick) {
       p->new_stride_n < 0 || p->out_stride_b < 0 || p->out_stride_h < 0 || p->out_stride_n < 0 || p->parents_stride_b < 0)
     return LAGKV_ESHAPE;
   return LAGKV_OK;
-}
-
-// Tiles of 16 or 32 query rows: the pieces of the cache by the microseconds that they take, none below a step a wavefront.
-// A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them, at
-// no cost to each other but memory's with 16 query rows (32: 0.75 us beside another, in fp32 0.75 alone and 1.4), and one where
-// the outputs fill its registers.  All rows together pass memory at 6 TB/s, less where some compute
-// units have a workgroup more than others.  With pieces, a second kernel and every piece of a row written and read.
-// Over 205 shapes (16-bit and fp32, 64 to 256 channels, 4 to 600 query rows, 1 to 1000 workgroups, 200 to 50000 rows) the
-// time is 1 % above that of the best number of pieces in the mean; with as many pieces as make 512 workgroups, 11.9 %.  Where
-// lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4
-// 115; 192 streams in 1 70, in 2 79.)
-double attend_narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces) {
-  const bool heavy = f32 && row_tile == 32;  // (bound by the products)
-  const int64_t tiles = (rows + row_tile - 1) / row_tile, places = D > 128 ? 32 : 64;  // of an XCD
-  const double channels = D <= 64 ? 0.5 : D <= 128 ? 1 : 2, alone = (heavy ? 0.75 : 0.45) * channels;
-  const double both = (heavy ? 1.4 : row_tile == 32 ? 0.75 : 0.45) * channels;  // (beside another workgroup)
-  const double ends = 5.5;
-  const double memory = (double)units * (double)steps * (double)D * 128 / 6e6;
-  double least = 1e30;
-  for (int64_t s = 1; s <= 256 && (s == 1 || s <= steps / 4); s = next_pieces(s)) {
-    const int64_t load = fullest_xcd(units, s, tiles);
-    const double uneven = load > 32 ? (double)((load + 31) / 32 * 32) / (double)load - 1 : 0;
-    const int64_t full = load / places, rest = load - full * places;
-    const double each = (double)((steps + s - 1) / s);
-    const double go = (double)full * (each * both + ends) + (rest > 32 ? each * both + ends : rest > 0 ? each * alone + ends : 0);
-    const double pass = memory * (1 + 0.35 * uneven) + ends;
-    const double us = (go > pass ? go : pass) + (s > 1 ? 3.5 + (double)(units * rows * s) * (double)D * 8 / 3e6 : 0);
-    if (us < least) {
-      least = us;
-      *pieces = s;
-    }
-  }
-  return least;
-}
-
-// Tiles of few query rows: as many as there are, up to what the registers hold.  Of many (16-bit types): tiles of 128 or 256
-// where they take less time, by the two models.  (Over the 914 shapes of wide_shape, without new tokens, the time is 1.6 % above
-// that of the better kernel at its best, with tiles of many rows for all of them 5.3 %, of few 39 %; over 299 with trees, 40 to
-// 600 query rows, it is 0.4 % above the less of itself and of few rows, which take 19 % more in the mean.  us, few and many: 8
-// streams, 256 query rows, 500 rows 15 and 16, 1000 rows 16 and 18; 32 streams, 256, 2000 rows 47 and 33; 8 streams of 256
-// channels, 500 query rows, 4000 rows 140 and 53.)
-bool attend_plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
-  pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
-  pl->rows = pick ? p->G : p->G * p->N;
-  const int64_t all_rows = pl->units * pl->rows;
-  if (pl->units > kMost || all_rows > kMostRows) return false;  // (they are numbered in 31 bits)
-  const bool f32 = p->dtype == LAGKV_F32;
-  const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
-  auto steps_of = [&](int64_t kt) { return (seen + kt - 1) / kt + (p->N + kt - 1) / kt; };
-  const int64_t steps = steps_of(f32 ? 16 : 32);
-  int64_t splits = 1;
-  pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
-  const double us = attend_narrow_shape(pl->units, pl->rows, pl->row_tile, p->D, f32, steps, &splits);
-  pl->wide = false;
-  if (!pick && !f32 && pl->rows > 32) {
-    int row_tile;
-    int64_t pieces;
-    pl->wide = wide_shape(pl->units, pl->rows, p->D, steps_of(64), &row_tile, &pieces) < us;
-    if (pl->wide) {
-      pl->row_tile = row_tile;
-      splits = pieces;
-    }
-  }
-  pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
-  const int64_t groups = pl->units * pl->row_tiles;
-  // Short caches whole, by twice the wavefronts in one kernel: up to two steps a wavefront.  (One token over 300 rows of 128
-  // 16-bit channels 7.1 us, in pieces about 8; over 640 rows, three steps, 9.5 us, over 1000 12.9 us and in pieces 8.4 us.
-  // Rows of 64 fp32 channels: 300 rows 7.6 us, 640 rows 11.2 us and in pieces 7.6 us.)
-  pl->waves = 4;
-  if (!pl->wide && steps <= 16 && groups <= 256 && pl->row_tile == 16 && p->D <= 128) {
-    splits = 1;
-    pl->waves = 8;
-  }
-  // one piece where the grids do not hold more
-  auto fits = [&](int64_t s) {
-    const int64_t join = all_rows >= kJoinByWave ? (all_rows + 3) / 4 : all_rows;
-    return grid_fits((pl->units * s + 7) / 8 * 8 * pl->row_tiles, pl->wide ? pl->row_tile * 2 : pl->waves * 64) && (s == 1 || grid_fits(join, 256));
-  };
-  if (!fits(splits)) splits = 1;
-  pl->splits = (int)splits;
-  const int64_t parts = all_rows * splits, ld = (p->D + 3) & ~3;
-  pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
-  pl->ws_bytes = splits > 1 ? pl->off_ml + ws_align_up((size_t)parts * 8) : 0;
-  return fits(splits);
 }
 
 AttendArgs attend_args(const lagkv_attend_params* p, const AttendPlan& pl, bool pick, const void* Q, const void* K, const void* V,
@@ -254,16 +129,134 @@ AttendArgs attend_args(const lagkv_attend_params* p, const AttendPlan& pl, bool 
   return a;
 }
 
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& pl, int dtype, hipStream_t s) {
-  return pl.wide ? (dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))
-         : dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, pl.waves, s)
-         : dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, pl.waves, s)
-                                  : launch_attend_f16(a, pl.row_tile, pl.waves, s);
-}
-
 }  // namespace lagkv
 
 namespace {
+
+// Workgroups of the fullest of the eight XCDs (work_item deals units and pieces to them in turn, with all their tiles).
+int64_t fullest_xcd(int64_t units, int64_t pieces, int64_t row_tiles) { return (units * pieces + 7) / 8 * row_tiles; }
+
+// 1 2 3 4 6 8 12 16 24 ...
+int64_t next_pieces(int64_t s) { return s + (s < 4 ? 1 : s % 3 == 0 ? s / 3 : s / 2); }
+
+// Tiles of many rows: 128 query rows (four wavefronts, two workgroups a compute unit) or, for 65 to 128 channels, 256 (eight, one;
+// for fewer channels they were the faster ones of none of 164 shapes), and the pieces that
+// the cache is cut into, by the microseconds that they take: a step of 64 cache rows, the beginning and end of a workgroup,
+// and, with pieces, a second kernel and every piece of a row written and read.  A step takes longer the more compute
+// units are at work, and less where wavefronts of the eight have no rows.  Measured, 128 channels, model beside it (us; it
+// falls short by a seventh in the mean, as narrow_shape's does, and what counts is which is the least):
+//    8 streams,  256 query rows, 1000 rows   128 in 4 19 (18)   128 in 8 18 (16)   256 in 8 23 (20)   few rows 16 (15)
+//   32 streams,  256 query rows, 2000 rows   128 in 4 33 (27)   128 in 8 35 (28)   256 in 4 36 (32)   256 in 8 34 (30)
+//   32 streams,  256 query rows, 8000 rows   128 in 4 77 (62)   128 in 8 70 (57)   256 in 4 77 (74)   256 in 8 63 (54)
+//   64 streams,  160 query rows, 8000 rows   128 in 4 100 (91)   128 in 8 105 (105)   256 in 2 124 (106)   256 in 4 82 (69)
+// Over 914 shapes (64, 128 and 256 channels, 48 to 2048 query rows of 2 to 400 streams, 200 to 16000 rows) its choice takes 1.1 %
+// longer than the best tile and number of pieces in the mean.
+double wide_shape(int64_t units, int64_t rows, int64_t D, int64_t steps, int* row_tile, int64_t* pieces) {
+  const double channels = D <= 64 ? 0.57 : D <= 128 ? 1 : 2.2;
+  double least = 1e30;
+  for (int tile = 128; tile <= (D > 64 && D <= 128 && rows > 128 ? 256 : 128); tile += 128) {
+    const int64_t groups = units * ((rows + tile - 1) / tile), places = tile == 256 || D > 128 ? 256 : 512;
+    const double full = (double)(units * rows) / (double)(groups * tile);
+    for (int64_t s = 1; s <= 256 && s <= steps; s = next_pieces(s)) {
+      const int64_t all = 8 * fullest_xcd(units, s, (rows + tile - 1) / tile);
+      const double busy = all < 256 ? (double)all / 256 : 1;
+      const double step = tile == 256 ? 0.85 + (0.65 + 0.5 * busy) * full : channels * (all > 256 && D <= 128 ? 2.35 : 1.25 + 0.2 * busy);
+      const double ends = tile == 256 ? 12 : D <= 64 ? 7.3 : D <= 128 ? 9 : 8.5;
+      const double us = (double)((all + places - 1) / places) * ((double)((steps + s - 1) / s) * step + ends) +
+                        (s > 1 ? 2.5 + (double)(units * rows * s) * (double)D * 8 / 9e6 : 0);
+      if (us < least) {
+        least = us;
+        *row_tile = tile;
+        *pieces = s;
+      }
+    }
+  }
+  return least;
+}
+
+// Tiles of 16 or 32 query rows: the pieces of the cache by the microseconds that they take, none below a step a wavefront.
+// A workgroup's steps take 0.45 us for 128 channels and it has beginning and end (5.5 us); a compute unit holds two of them, at
+// no cost to each other but memory's with 16 query rows (32: 0.75 us beside another, in fp32 0.75 alone and 1.4), and one where
+// the outputs fill its registers.  All rows together pass memory at 6 TB/s, less where some compute
+// units have a workgroup more than others.  With pieces, a second kernel and every piece of a row written and read.
+// Over 205 shapes (16-bit and fp32, 64 to 256 channels, 4 to 600 query rows, 1 to 1000 workgroups, 200 to 50000 rows) the
+// time is 1 % above that of the best number of pieces in the mean; with as many pieces as make 512 workgroups, 11.9 %.  Where
+// lengths differ within a batch (a quarter of T to T; 57 shapes) 3.9 % and 7.1 %.  (us: 40 streams of 4000 rows in 1 136, in 4
+// 115; 192 streams in 1 70, in 2 79.)
+double narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces) {
+  const bool heavy = f32 && row_tile == 32;  // (bound by the products)
+  const int64_t tiles = (rows + row_tile - 1) / row_tile, places = D > 128 ? 32 : 64;  // of an XCD
+  const double channels = D <= 64 ? 0.5 : D <= 128 ? 1 : 2, alone = (heavy ? 0.75 : 0.45) * channels;
+  const double both = (heavy ? 1.4 : row_tile == 32 ? 0.75 : 0.45) * channels;  // (beside another workgroup)
+  const double ends = 5.5;
+  const double memory = (double)units * (double)steps * (double)D * 128 / 6e6;
+  double least = 1e30;
+  for (int64_t s = 1; s <= 256 && (s == 1 || s <= steps / 4); s = next_pieces(s)) {
+    const int64_t load = fullest_xcd(units, s, tiles);
+    const double uneven = load > 32 ? (double)((load + 31) / 32 * 32) / (double)load - 1 : 0;
+    const int64_t full = load / places, rest = load - full * places;
+    const double each = (double)((steps + s - 1) / s);
+    const double go = (double)full * (each * both + ends) + (rest > 32 ? each * both + ends : rest > 0 ? each * alone + ends : 0);
+    const double pass = memory * (1 + 0.35 * uneven) + ends;
+    const double us = (go > pass ? go : pass) + (s > 1 ? 3.5 + (double)(units * rows * s) * (double)D * 8 / 3e6 : 0);
+    if (us < least) {
+      least = us;
+      *pieces = s;
+    }
+  }
+  return least;
+}
+
+// Tiles of few query rows: as many as there are, up to what the registers hold.  Of many (16-bit types): tiles of 128 or 256
+// where they take less time, by the two models.  (Over the 914 shapes of wide_shape, without new tokens, the time is 1.6 % above
+// that of the better kernel at its best, with tiles of many rows for all of them 5.3 %, of few 39 %; over 299 with trees, 40 to
+// 600 query rows, it is 0.4 % above the less of itself and of few rows, which take 19 % more in the mean.  us, few and many: 8
+// streams, 256 query rows, 500 rows 15 and 16, 1000 rows 16 and 18; 32 streams, 256, 2000 rows 47 and 33; 8 streams of 256
+// channels, 500 query rows, 4000 rows 140 and 53.)
+bool plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl) {
+  pl->units = (int64_t)p->B * p->H * (pick ? p->N : 1);
+  pl->rows = pick ? p->G : p->G * p->N;
+  const int64_t all_rows = pl->units * pl->rows;
+  if (pl->units > kMost || all_rows > kMostRows) return false;  // (they are numbered in 31 bits)
+  const bool f32 = p->dtype == LAGKV_F32;
+  const int64_t seen = pick ? (int64_t)p->n_blocks * p->block : p->T;
+  auto steps_of = [&](int64_t kt) { return (seen + kt - 1) / kt + (p->N + kt - 1) / kt; };
+  const int64_t steps = steps_of(f32 ? 16 : 32);
+  int64_t splits = 1;
+  pl->row_tile = pl->rows <= 16 || p->D > 128 ? 16 : 32;
+  const double us = narrow_shape(pl->units, pl->rows, pl->row_tile, p->D, f32, steps, &splits);
+  pl->wide = false;
+  if (!pick && !f32 && pl->rows > 32) {
+    int row_tile;
+    int64_t pieces;
+    pl->wide = wide_shape(pl->units, pl->rows, p->D, steps_of(64), &row_tile, &pieces) < us;
+    if (pl->wide) {
+      pl->row_tile = row_tile;
+      splits = pieces;
+    }
+  }
+  pl->row_tiles = (int)(((int64_t)pl->rows + pl->row_tile - 1) / pl->row_tile);
+  const int64_t groups = pl->units * pl->row_tiles;
+  // Short caches whole, by twice the wavefronts in one kernel: up to two steps a wavefront.  (One token over 300 rows of 128
+  // 16-bit channels 7.1 us, in pieces about 8; over 640 rows, three steps, 9.5 us, over 1000 12.9 us and in pieces 8.4 us.
+  // Rows of 64 fp32 channels: 300 rows 7.6 us, 640 rows 11.2 us and in pieces 7.6 us.)
+  pl->waves = 4;
+  if (!pl->wide && steps <= 16 && groups <= 256 && pl->row_tile == 16 && p->D <= 128) {
+    splits = 1;
+    pl->waves = 8;
+  }
+  // one piece where the grids do not hold more
+  auto fits = [&](int64_t s) {
+    const int64_t join = all_rows >= kJoinByWave ? (all_rows + 3) / 4 : all_rows;
+    return grid_fits((pl->units * s + 7) / 8 * 8 * pl->row_tiles, pl->wide ? pl->row_tile * 2 : pl->waves * 64) && (s == 1 || grid_fits(join, 256));
+  };
+  if (!fits(splits)) splits = 1;
+  pl->splits = (int)splits;
+  const int64_t parts = all_rows * splits, ld = (p->D + 3) & ~3;
+  pl->off_ml = splits > 1 ? ws_align_up((size_t)parts * ld * 4) : 0;
+  pl->ws_bytes = splits > 1 ? pl->off_ml + ws_align_up((size_t)parts * 8) : 0;
+  return fits(splits);
+}
 
 int attend(const lagkv_attend_params* p, const void* Q, const void* K, const void* V, const int32_t* lengths,
            const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents, void* out, float* lse,
@@ -281,11 +274,14 @@ int attend(const lagkv_attend_params* p, const void* Q, const void* K, const voi
       !aligned(lengths, 4) || !aligned(parents, 4) || !aligned(blocks, 4) || !aligned(lse, 4))
     return LAGKV_EINVAL;
   AttendPlan pl;
-  if (!attend_plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
+  if (!plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
   if (pl.ws_bytes > 0 && (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
   const AttendArgs a = attend_args(p, pl, pick, Q, K, V, lengths, blocks, K_new, V_new, parents, out, lse, ws);
   hipStream_t s = (hipStream_t)hip_stream;
-  hipError_t e = launch_attend(a, pl, p->dtype, s);
+  hipError_t e = pl.wide ? (p->dtype == LAGKV_BF16 ? launch_wide_bf16(a, pl.row_tile, s) : launch_wide_f16(a, pl.row_tile, s))
+                 : p->dtype == LAGKV_F32  ? launch_attend_f32(a, pl.row_tile, pl.waves, s)
+                 : p->dtype == LAGKV_BF16 ? launch_attend_bf16(a, pl.row_tile, pl.waves, s)
+                                          : launch_attend_f16(a, pl.row_tile, pl.waves, s);
   if (e == hipSuccess && pl.splits > 1) e = launch_attend_join(a, p->dtype, s);
   return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
 }
@@ -298,7 +294,7 @@ size_t lagkv_attend_workspace_bytes(const lagkv_attend_params* p) {
   if (!p) return 0;
   const bool pick = p->n_blocks > 0;
   AttendPlan pl;
-  if (attend_check(p, pick) != LAGKV_OK || p->N == 0 || !attend_plan_of(p, pick, &pl)) return 0;
+  if (attend_check(p, pick) != LAGKV_OK || p->N == 0 || !plan_of(p, pick, &pl)) return 0;
   return pl.ws_bytes;
 }
 
@@ -310,7 +306,7 @@ int lagkv_attend_plan(const lagkv_attend_params* p, lagkv_attend_plan_t* out) {
   std::memset(out, 0, sizeof(*out));
   if (p->N == 0) return LAGKV_OK;
   AttendPlan pl;
-  if (!attend_plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
+  if (!plan_of(p, pick, &pl)) return LAGKV_ESHAPE;
   out->many_rows = pl.wide;
   out->row_tile = pl.row_tile;
   out->wavefronts = pl.wide ? pl.row_tile / 32 : pl.waves;

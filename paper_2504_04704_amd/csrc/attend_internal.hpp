@@ -58,12 +58,9 @@ struct AttendPlan {
 // What the host layer of attend_api.hip has for that of quant_api.hip as well.
 bool rows_apart(int64_t D, const int64_t (&n)[3], const int64_t (&stride)[3]);
 int attend_check(const lagkv_attend_params* p, bool pick);
-double attend_narrow_shape(int64_t units, int64_t rows, int64_t row_tile, int64_t D, bool f32, int64_t steps, int64_t* pieces);
-bool attend_plan_of(const lagkv_attend_params* p, bool pick, AttendPlan* pl);
 AttendArgs attend_args(const lagkv_attend_params* p, const AttendPlan& pl, bool pick, const void* Q, const void* K, const void* V,
                        const int32_t* lengths, const int32_t* blocks, const void* K_new, const void* V_new, const int32_t* parents,
                        void* out, float* lse, void* ws);
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& pl, int dtype, hipStream_t s);
 
 hipError_t launch_attend_f32(const AttendArgs& a, int row_tile, int waves, hipStream_t s);
 hipError_t launch_attend_bf16(const AttendArgs& a, int row_tile, int waves, hipStream_t s);

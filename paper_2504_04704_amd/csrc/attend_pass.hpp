@@ -179,8 +179,8 @@ struct WorkItem {
   bool any;
 };
 template <typename Args>
-__device__ __forceinline__ WorkItem work_item(const Args& a) {
-  const uint32_t slot = blockIdx.x % 8, rest = blockIdx.x / 8, many = a.by_tiles.of(rest), us = many * 8 + slot;
+__device__ __forceinline__ WorkItem work_item(const Args& a, uint32_t group = blockIdx.x) {
+  const uint32_t slot = group % 8, rest = group / 8, many = a.by_tiles.of(rest), us = many * 8 + slot;
   const uint32_t unit = a.by_splits.of(us);
   WorkItem w;
   w.tile = (int)(rest - many * a.row_tiles);
@@ -249,21 +249,18 @@ constexpr int kAttendWaves = DP > 128 ? 1 : 2;
 template <int DT, int DP, int RT>
 constexpr bool kQueryInLds = DT == LAGKV_F32 && DP == 128 && RT == 2;
 
+// What a workgroup does, with AttendShape's MAIN bytes of LDS.
 template <int DT, int DP, int RT, int WAVES, bool PICK>
-__global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend_kernel(const AttendArgs a) {
+__device__ __forceinline__ void attend_body(const AttendArgs& a, const WorkItem& w, char* lds) {
   using E = AElem<DT>;
   using Sh = AttendShape<DT, DP, RT, WAVES>;
   constexpr int PER = Sh::PER, NC = Sh::NC, CPR = Sh::CPR, SUBS = E::SUBS, KT = Sh::KT, ROWS = Sh::ROWS, THREADS = WAVES * 64;
   constexpr int LDV = Sh::LDV, LDO = Sh::LDO, DT16 = DP / 16, NV = SUBS * NC, VROWS = 64 / CPR;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float sh_ml[WAVES][ROWS][2];
   __shared__ int32_t sh_parent[kMaxTree];
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
-  fetch_arguments<AttendArgs>();
-  const WorkItem w = work_item(a);
-  if (!w.any) return;
   const uint32_t stream = PICK ? a.by_n.of((uint32_t)w.unit) : (uint32_t)w.unit, bu = a.by_h.of(stream);
   const int n_fixed = PICK ? (int)((uint32_t)w.unit - stream * a.N) : 0;
   const int64_t b = bu, h = stream - bu * a.H;
@@ -703,6 +700,14 @@ __global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend
     }
     if (quad == 0 && a.lse) a.lse[(b * a.H * a.G + head) * a.N + n] = blind ? -INFINITY : lse_of<DT>(top, sum);
   }
+}
+
+template <int DT, int DP, int RT, int WAVES, bool PICK>
+__global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend_kernel(const AttendArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  fetch_arguments<AttendArgs>();
+  const WorkItem w = work_item(a);
+  if (w.any) attend_body<DT, DP, RT, WAVES, PICK>(a, w, lds);
 }
 
 template <int DT, int DP, int RT, int WAVES, bool PICK>

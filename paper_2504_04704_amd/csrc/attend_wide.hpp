@@ -1,5 +1,5 @@
 // Attention of many query rows over all rows of a cache (lagkv_attend, 16-bit types; the mathematics is attend_pass.hpp's; when
-// it is taken, attend_plan_of says).
+// it is taken, plan_of says).
 //
 // Where a stream has tens of query rows (a drafted tree under grouped heads, a chunk of a prompt) the matrix cores are the
 // bound, not memory: 256 rows make 256 flop of a cache byte.  A workgroup of four or eight wavefronts goes over 64 cache
@@ -73,24 +73,21 @@ struct WideShape {
   static constexpr int BUF = KT * (LDK + LDV);
 };
 
+// What a workgroup does, with two buffers of [K rows][V rows] in LDS.
 template <int DT, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_kernel(const AttendArgs a) {
+__device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const WorkItem& w, char* wide_lds) {
   using E = AElem<DT>;
   using W = Wide<DT>;
   using Sh = WideShape<DP>;
   constexpr int KT = Sh::KT, CPR = Sh::CPR, LDK = Sh::LDK, LDV = Sh::LDV, THREADS = WAVES * 64, ROWS = WAVES * 32;
   constexpr int HALVES = KT / 32, KS = DP / 16, DT32 = DP / 32, PASSES = KT * CPR / THREADS;
   static_assert(KT * CPR % THREADS == 0, "");
-  extern __shared__ __attribute__((aligned(16))) char wide_lds[];  // two buffers of [K rows][V rows]
   __shared__ int32_t sh_parent[kMaxTree];
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   __shared__ int sh_odd[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int late = wave >> 2;  // (of the half of eight wavefronts that is a phase behind)
 
-  fetch_arguments<AttendArgs>();
-  const WorkItem w = work_item(a);
-  if (!w.any) return;
   const uint32_t bu = a.by_h.of((uint32_t)w.unit);
   const int64_t b = bu, h = (uint32_t)w.unit - bu * a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
@@ -418,6 +415,14 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
     }
   if (half == 0 && a.lse)
     a.lse[(b * a.H * a.G + head) * a.N + token] = blind ? -INFINITY : (m + __builtin_amdgcn_logf(l) - W::LIFT) * 0.693147180559945f;
+}
+
+template <int DT, int DP, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_kernel(const AttendArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char wide_lds[];
+  fetch_arguments<AttendArgs>();
+  const WorkItem w = work_item(a);
+  if (w.any) attend_wide_body<DT, DP, WAVES>(a, w, wide_lds);
 }
 
 template <int DT, int DP, int WAVES>

@@ -31,6 +31,10 @@ decltype(&lagkv_attend) attend_fn;
 decltype(&lagkv_attend_blocks) attend_blocks_fn;
 decltype(&lagkv_block_bounds) bounds_fn;
 decltype(&lagkv_select_blocks) select_fn;
+decltype(&lagkv_quantize) quantize_fn;
+decltype(&lagkv_dequantize) dequantize_fn;
+decltype(&lagkv_attend_quantized_workspace_bytes) attend_quant_ws_fn;
+decltype(&lagkv_attend_quantized) attend_quant_fn;
 PyObject* raw_stream_fn;  // device index -> handle of the current stream
 
 bool to_int(PyObject* o, int32_t* v) {
@@ -420,6 +424,189 @@ PyObject* block_bounds(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   }
 }
 
+// ---- a cache in 8 bits ----
+
+// Codes, scales and block from args[0 .. 5): the parameters that are theirs.
+struct CodesOf {
+  const at::Tensor *K, *V, *ks, *vs;
+};
+bool codes_of(PyObject* const* args, lagkv_quant_params* p, CodesOf* c) {
+  for (int i = 0; i < 4; ++i)
+    if (!THPVariable_CheckExact(args[i])) return false;
+  c->K = &THPVariable_Unpack(args[0]);
+  c->V = &THPVariable_Unpack(args[1]);
+  c->ks = &THPVariable_Unpack(args[2]);
+  c->vs = &THPVariable_Unpack(args[3]);
+  const at::Tensor& K = *c->K;
+  if (!K.is_cuda() || K.layout() != at::kStrided || K.dim() != 4 || K.stride(3) != 1 || !small(K) || c->V->layout() != at::kStrided ||
+      c->V->scalar_type() != K.scalar_type() || !alike(K, *c->V) || !to_int(args[4], &p->block) || p->block < 1)
+    return false;
+  if (K.scalar_type() == at::kChar) p->code = LAGKV_CODE_INT8;
+  else if (K.scalar_type() == at::kFloat8_e4m3fn) p->code = LAGKV_CODE_E4M3;
+  else return false;
+  p->B = (int32_t)K.size(0);
+  p->H = (int32_t)K.size(1);
+  p->T = K.size(2);
+  p->D = (int32_t)K.size(3);
+  const int64_t nb = (p->T + p->block - 1) / p->block;
+  for (const at::Tensor* t : {c->ks, c->vs})
+    if (t->scalar_type() != at::kFloat || t->layout() != at::kStrided || t->device() != K.device() || t->dim() != 3 || t->size(0) != p->B ||
+        t->size(1) != p->H || t->size(2) != nb || t->stride(2) != 1 || t->strides() != c->ks->strides())
+      return false;
+  p->code_stride_b = K.stride(0);
+  p->code_stride_h = K.stride(1);
+  p->code_stride_t = K.stride(2);
+  p->scale_stride_b = c->ks->stride(0);
+  p->scale_stride_h = c->ks->stride(1);
+  return true;
+}
+
+// go_over(back, Kq, Vq, K_scale, V_scale, block, K, V, lengths or None, start) -> the status of lagkv_quantize or (back) lagkv_dequantize, or
+// -1: not called
+PyObject* go_over(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  auto status = [](long v) {
+    PyErr_Clear();
+    return PyLong_FromLong(v);
+  };
+  if (nargs != 10 || !PyBool_Check(args[0])) return status(-1);
+  try {
+    int32_t dk, dv, start;
+    lagkv_quant_params p = {};
+    CodesOf c;
+    const at::Tensor *K = rows_of(args[6], &dk), *V = rows_of(args[7], &dv), *lengths;
+    void* stream;
+    if (!K || !V || dk != dv || !alike(*K, *V) || !small(*K) || !codes_of(args + 1, &p, &c) || K->device() != c.K->device() || K->sizes() != c.K->sizes() ||
+        !ints_of(args[8], *K, &lengths) || (lengths && (lengths->dim() != 1 || lengths->size(0) != p.B)) || !to_int(args[9], &start) || start < 0 ||
+        needs_grad(K, V, c.K, c.V, c.ks, c.vs) || !device_is_current(*K) || !stream_of(*K, &stream))
+      return status(-1);
+    p.dtype = dk;
+    p.row_stride_b = K->stride(0);
+    p.row_stride_h = K->stride(1);
+    p.row_stride_t = K->stride(2);
+    void *k = K->data_ptr(), *v = V->data_ptr(), *kq = c.K->data_ptr(), *vq = c.V->data_ptr();
+    float *ks = (float*)c.ks->data_ptr(), *vs = (float*)c.vs->data_ptr();
+    const int32_t* lp = (const int32_t*)at_of(lengths);
+    const bool back = args[0] == Py_True;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = back ? dequantize_fn(&p, kq, vq, ks, vs, lp, start, k, v, stream) : quantize_fn(&p, k, v, lp, start, kq, vq, ks, vs, stream);
+    Py_END_ALLOW_THREADS
+    return status(rc);
+  } catch (...) {
+    return status(-1);
+  }
+}
+
+// attend_quantized(q, Kq, Vq, K_scale, V_scale, block, K_tail, V_tail, K_new, V_new, parents, lengths, tail_lengths, scale or None,
+//                  out or None, want_lse, ws or None)
+//   -> (out, lse or None), the status that the C function refused with, or None: not called
+PyObject* attend_quantized(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs != 17 || !PyBool_Check(args[15])) return none();
+  try {
+    int32_t dq, dk, dv;
+    lagkv_quant_params p = {};
+    CodesOf c;
+    const at::Tensor* q = rows_of(args[0], &dq);
+    if (!q || !small(*q) || !codes_of(args + 1, &p, &c) || q->device() != c.K->device()) return none();
+    p.dtype = dq;
+    p.N = (int32_t)q->size(2);
+    if (q->size(0) != p.B || q->size(3) != p.D || p.H == 0 || q->size(1) % p.H != 0) return none();
+    p.G = (int32_t)(q->size(1) / p.H);
+    const at::Tensor *Kt = nullptr, *Vt = nullptr, *Kn = nullptr, *Vn = nullptr, *parents, *lengths, *tails;
+    if (args[6] != Py_None || args[7] != Py_None) {
+      Kt = rows_of(args[6], &dk);
+      Vt = rows_of(args[7], &dv);
+      if (!Kt || !Vt || dk != dq || dv != dq || !alike(*Kt, *Vt) || !small(*Kt) || Kt->device() != q->device() || Kt->size(0) != p.B || Kt->size(1) != p.H ||
+          Kt->size(3) != p.D)
+        return none();
+      p.R = Kt->size(2);
+      p.row_stride_b = Kt->stride(0);
+      p.row_stride_h = Kt->stride(1);
+      p.row_stride_t = Kt->stride(2);
+    }
+    if (args[8] != Py_None || args[9] != Py_None) {
+      Kn = rows_of(args[8], &dk);
+      Vn = rows_of(args[9], &dv);
+      if (!Kn || !Vn || dk != dq || dv != dq || !alike(*Kn, *Vn) || Kn->device() != q->device() || Kn->size(0) != p.B || Kn->size(1) != p.H ||
+          Kn->size(2) != p.N || Kn->size(3) != p.D)
+        return none();
+      p.new_stride_b = Kn->stride(0);
+      p.new_stride_h = Kn->stride(1);
+      p.new_stride_n = Kn->stride(2);
+    }
+    if (!ints_of(args[10], *q, &parents) || !ints_of(args[11], *q, &lengths) || !ints_of(args[12], *q, &tails)) return none();
+    if (parents) {
+      if (!Kn || parents->dim() < 1 || parents->dim() > 2 || parents->size(-1) != p.N || (parents->dim() == 2 && parents->size(0) != p.B))
+        return none();
+      p.parents_stride_b = parents->dim() == 2 ? p.N : 0;
+    }
+    for (const at::Tensor* t : {lengths, tails})
+      if (t && (t->dim() != 1 || t->size(0) != p.B)) return none();
+    if (tails && !Kt) return none();
+    if (args[13] == Py_None) p.scale = 1.0 / std::sqrt((double)p.D);
+    else if (!to_double(args[13], &p.scale)) return none();
+    if (needs_grad(q, Kt, Vt, Kn, Vn, c.K, c.V, c.ks, c.vs) || !device_is_current(*q)) return none();
+    p.q_stride_b = q->stride(0);
+    p.q_stride_h = q->stride(1);
+    p.q_stride_n = q->stride(2);
+    void* stream;
+    if (!stream_of(*q, &stream)) return none();
+    const auto opt = q->options().requires_grad(false);
+    at::Tensor out, lse, ws;
+    if (args[14] == Py_None) {
+      out = at::empty_like(*q, opt);
+      if (out.stride(3) != 1) return none();
+    } else {
+      int32_t d;
+      const at::Tensor* given = rows_of(args[14], &d);
+      if (!given || d != dq || given->device() != q->device() || given->sizes() != q->sizes()) return none();
+      out = *given;
+    }
+    p.out_stride_b = out.stride(0);
+    p.out_stride_h = out.stride(1);
+    p.out_stride_n = out.stride(2);
+    if (args[15] == Py_True) lse = at::empty({q->size(0), q->size(1), q->size(2)}, opt.dtype(at::kFloat));
+    size_t need = attend_quant_ws_fn(&p);
+    if (args[16] != Py_None) {
+      if (!THPVariable_CheckExact(args[16])) return none();
+      ws = THPVariable_Unpack(args[16]);
+      if (ws.scalar_type() != at::kByte || !ws.is_contiguous() || ws.device() != q->device()) return none();
+      need = (size_t)ws.numel();
+    } else if (need) {
+      ws = at::empty({(int64_t)need}, opt.dtype(at::kByte));
+    }
+    const void *qp = q->data_ptr(), *kq = c.K->data_ptr(), *vq = c.V->data_ptr(), *ktp = at_of(Kt), *vtp = at_of(Vt), *knp = at_of(Kn), *vnp = at_of(Vn);
+    const float *ks = (const float*)c.ks->data_ptr(), *vs = (const float*)c.vs->data_ptr();
+    const int32_t *pp = (const int32_t*)at_of(parents), *lp = (const int32_t*)at_of(lengths), *tp = (const int32_t*)at_of(tails);
+    void *op = out.data_ptr(), *wp = ws.defined() ? ws.data_ptr() : nullptr;
+    float* ep = lse.defined() ? (float*)lse.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = attend_quant_fn(&p, qp, kq, vq, ks, vs, lp, ktp, vtp, tp, knp, vnp, pp, op, ep, wp, need, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != LAGKV_OK) return PyLong_FromLong(rc);
+    PyObject* o = args[14] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(args[14]);
+    PyObject* e = o ? (lse.defined() ? THPVariable_Wrap(lse) : Py_NewRef(Py_None)) : nullptr;
+    PyObject* both = e ? PyTuple_Pack(2, o, e) : nullptr;
+    Py_XDECREF(o);
+    Py_XDECREF(e);
+    return both;
+  } catch (...) {
+    return none();
+  }
+}
+
+// init_codes(quantize, dequantize, attend_quantized_workspace_bytes, attend_quantized: addresses)
+PyObject* init_codes(PyObject*, PyObject* args) {
+  size_t a[4];
+  if (!PyArg_ParseTuple(args, "kkkk", &a[0], &a[1], &a[2], &a[3])) return nullptr;
+  quantize_fn = (decltype(quantize_fn))a[0];
+  dequantize_fn = (decltype(dequantize_fn))a[1];
+  attend_quant_ws_fn = (decltype(attend_quant_ws_fn))a[2];
+  attend_quant_fn = (decltype(attend_quant_fn))a[3];
+  Py_RETURN_NONE;
+}
+
 // init(plan, workspace_bytes, compress, append_and_compress, attend_workspace_bytes, attend, attend_blocks, block_bounds,
 //      select_blocks: addresses; raw stream function)
 PyObject* init(PyObject*, PyObject* args) {
@@ -448,6 +635,9 @@ PyMethodDef methods[] = {
     {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, nullptr},
     {"select_blocks", (PyCFunction)(void (*)(void))select_blocks, METH_FASTCALL, nullptr},
     {"block_bounds", (PyCFunction)(void (*)(void))block_bounds, METH_FASTCALL, nullptr},
+    {"init_codes", init_codes, METH_VARARGS, nullptr},
+    {"go_over", (PyCFunction)(void (*)(void))go_over, METH_FASTCALL, nullptr},
+    {"attend_quantized", (PyCFunction)(void (*)(void))attend_quantized, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lagkv_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -117,28 +117,102 @@ int check_quant(const lagkv_quant_params* p) {
   return attend_check(&r, false);
 }
 
-// Rows in 8 bits: tiles of 16 or 32 query rows and the pieces that attend_narrow_shape gives for as many bytes; then the tail and the
-// new tokens, as they would be alone.
+// A form of the kernels: rows of a tile, the cache rows of a step in 8 bits and in the type, and the microseconds of a step with
+// one workgroup on a compute unit, of one with others beside it, and of a workgroup's beginning and end; a step of the tail and the new tokens takes
+// `of_rows` of one in 8 bits.
+struct QuantForm {
+  bool wide;
+  int row_tile, step, step_of_rows;
+  double alone, beside, ends, of_rows;
+};
+// Few rows: 16, or 32 where the registers hold them; many (16-bit types): 128.
+int quant_forms(const lagkv_quant_params* p, int64_t rows, QuantForm (&f)[2]) {
+  const bool f32 = p->dtype == LAGKV_F32;
+  const int kr = f32 ? 16 : 32;
+  int n = 0;
+  if (p->D <= 64) f[n++] = rows <= 16 ? QuantForm{false, 16, 64, kr, 0.39, 0.58, 4.4, f32 ? 0.64 : 0.73} : QuantForm{false, 32, 64, kr, 0.41, f32 ? 0.75 : 0.63, f32 ? 7.6 : 6.2, 0.8};
+  else if (p->D > 128) f[n++] = {false, 16, 32, kr, f32 ? 0.55 : 0.48, f32 ? 0.67 : 0.52, f32 ? 10.2 : 8.6, f32 ? 1.3 : 1.8};
+  else if (rows <= 16) f[n++] = {false, 16, 64, kr, 0.54, 1.0, f32 ? 6.6 : 5.4, f32 ? 0.72 : 0.81};
+  else f[n++] = {false, 32, 32, kr, f32 ? 0.34 : 0.29, f32 ? 0.59 : 0.51, f32 ? 10.4 : 8.4, f32 ? 2.1 : 1.4};
+  if (f32 || rows <= 32) return n;
+  if (p->D <= 64) f[n++] = {true, 128, 64, 64, 1.0, 1.6, 6.1, 1.7};
+  else if (p->D > 128) f[n++] = {true, 128, 32, 32, 2.8 / 2, 3.6 / 2, 12.8, 1.0};
+  else f[n++] = {true, 128, 64, 64, 1.26, 2.17, 8.3, 1.6};
+  return n;
+}
+
+// The pieces of the rows in 8 bits and of the others by the microseconds that they take: rounds of workgroups on the fullest of the eight
+// XCDs (two a compute unit; one beyond 128 channels), or all rows past memory at 5.5 TB/s; and the kernel that joins the
+// pieces.  Over 3486 shapes (64 to 256 channels, 1 to 4000 query rows of 1 to 256 streams, 64 to 65536 rows in 8 bits and up to 2048 behind
+// them, a quarter with lengths that differ) its choice takes 3.4 % longer than the best form and numbers of pieces of up to 60 that were
+// measured in the mean (half of them at most 0.2 %, nine in ten 12 %), where pieces as for a cache in 16 bits alone, with the others' share of them, take 9.8 %.
+double quant_shape(const lagkv_quant_params* p, const QuantForm& f, int64_t units, int64_t rows, int* pieces, int* pieces_of_rows) {
+  const int64_t steps = (p->T + f.step - 1) / f.step, others = (p->R + f.step_of_rows - 1) / f.step_of_rows + (p->N + f.step_of_rows - 1) / f.step_of_rows;
+  const int64_t tiles = (rows + f.row_tile - 1) / f.row_tile, places = p->D > 128 ? 32 : 64;
+  const double memory = (double)units * (double)p->D * ((double)p->T * 2 + (double)(p->R + p->N) * 2 * esize_of(p)) / 5.5e6;
+  double least = 1e30;
+  for (int64_t sq = 1; sq <= 128 && (sq == 1 || sq * (f.wide ? 1 : 4) <= steps); sq += sq < 4 ? 1 : sq % 3 == 0 ? sq / 3 : sq / 2) {
+    const int64_t share = others * sq / steps;
+    const int64_t choices[] = {1, 2, 3, share / 2, share};
+    int64_t before = 0;
+    for (int64_t st : choices) {
+      if (st <= before || st > 3 * sq + 2 || (st > 1 && st > others)) continue;
+      before = st;
+      const double nq = (double)((units * sq + 7) / 8 * tiles), nt = (double)((units * st + 7) / 8 * tiles);
+      const double step = nq + nt > 32 ? f.beside : f.alone;
+      const double tq = (double)((steps + sq - 1) / sq) * step + f.ends, tt = (double)((others + st - 1) / st) * step * f.of_rows + f.ends;
+      double us = (double)(((int64_t)nq + places - 1) / places) * tq;
+      us = us > tt ? us : tt;
+      const double all = (nq * tq + nt * tt) / (double)places;
+      us = us > all ? us : all;
+      us = us > memory + f.ends ? us : memory + f.ends;
+      us += 4 + (double)(units * rows * (sq + st)) * (double)p->D * 2e-6;
+      if (us < least) {
+        least = us;
+        *pieces = (int)sq;
+        *pieces_of_rows = (int)st;
+      }
+    }
+  }
+  return least;
+}
+
 struct QuantPlan {
-  AttendPlan rows;  // (its units and rows are of both)
-  int row_tile, row_tiles, splits;
-  int total;  // pieces of both
+  AttendPlan rows;  // of the tail and the new tokens; units, rows and tiles are those of both
+  int splits;       // pieces of the rows in 8 bits
+  int64_t groups, groups_of_rows;
   size_t off_ml, ws_bytes;
 };
 bool quant_plan_of(const lagkv_quant_params* p, QuantPlan* pl) {
-  const lagkv_attend_params r = rows_of(p);
-  if (!attend_plan_of(&r, false, &pl->rows)) return false;
-  const int64_t units = pl->rows.units, rows = pl->rows.rows, all = units * rows;
-  pl->row_tile = rows <= 16 || p->D > 128 ? 16 : 32;
-  pl->row_tiles = (int)((rows + pl->row_tile - 1) / pl->row_tile);
-  int64_t splits = 1;
-  attend_narrow_shape(units, rows, pl->row_tile, p->D, p->dtype == LAGKV_F32, (p->T + 63) / 64, &splits);
-  auto fits = [&](int64_t s) { return grid_fits((units * s + 7) / 8 * 8 * pl->row_tiles, 256); };
-  if (!fits(splits)) splits = 1;
-  if (!fits(splits) || !grid_fits((all + 3) / 4, 256)) return false;
-  pl->splits = (int)splits;
-  pl->total = pl->splits + pl->rows.splits;
-  const int64_t parts = all * pl->total, ld = (p->D + 3) & ~3;
+  AttendPlan& t = pl->rows;
+  std::memset(&t, 0, sizeof(t));
+  t.units = (int64_t)p->B * p->H;
+  t.rows = p->G * p->N;
+  const int64_t all = t.units * t.rows;
+  if (all > kMostRows || !grid_fits((all + 3) / 4, 256)) return false;
+  QuantForm forms[2];
+  const int n = quant_forms(p, t.rows, forms);
+  double least = 1e30;
+  for (int i = 0; i < n; ++i) {
+    int pieces = 1, others = 1;
+    const double us = quant_shape(p, forms[i], t.units, t.rows, &pieces, &others);
+    if (i > 0 && us >= least) continue;
+    least = us;
+    t.wide = forms[i].wide;
+    t.row_tile = forms[i].row_tile;
+    t.splits = others;
+    pl->splits = pieces;
+  }
+  t.row_tiles = (int)((t.rows + t.row_tile - 1) / t.row_tile);
+  t.waves = 4;
+  for (;;) {
+    pl->groups = (t.units * pl->splits + 7) / 8 * 8 * t.row_tiles;
+    pl->groups_of_rows = (t.units * t.splits + 7) / 8 * 8 * t.row_tiles;
+    if (grid_fits(pl->groups + pl->groups_of_rows, t.waves * 64)) break;
+    if (pl->splits == 1 && t.splits == 1) return false;
+    pl->splits = t.splits = 1;  // (one piece where the grids do not hold more)
+  }
+  const int64_t parts = all * (pl->splits + t.splits), ld = (p->D + 3) & ~3;
   pl->off_ml = ws_align_up((size_t)parts * ld * 4);
   pl->ws_bytes = pl->off_ml + ws_align_up((size_t)parts * 8);
   return true;
@@ -179,9 +253,11 @@ int lagkv_attend_quantized_plan(const lagkv_quant_params* p, lagkv_attend_plan_t
   if (p->T == 0) return lagkv_attend_plan(&r, rows);
   QuantPlan pl;
   if (!quant_plan_of(p, &pl)) return LAGKV_ESHAPE;
-  lagkv_attend_plan(&r, rows);
-  codes->row_tile = pl.row_tile;
-  codes->wavefronts = 4;
+  rows->many_rows = pl.rows.wide;
+  rows->row_tile = pl.rows.row_tile;
+  rows->wavefronts = pl.rows.waves;
+  rows->pieces = pl.rows.splits;
+  *codes = *rows;
   codes->pieces = pl.splits;
   return LAGKV_OK;
 }
@@ -209,13 +285,15 @@ int lagkv_attend_quantized(const lagkv_quant_params* p, const void* Q, const voi
   QuantPlan pl;
   if (!quant_plan_of(p, &pl)) return LAGKV_ESHAPE;
   if (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16)) return LAGKV_EWORKSPACE;
-  AttendArgs t = attend_args(&r, pl.rows, false, Q, K_tail, V_tail, tail_lengths, nullptr, K_new, V_new, parents, out, lse, ws);
-  const bool tail = p->R > 0 || K_new;
+  const bool rows = p->R > 0 || K_new;
+  QuantBoth both;
+  std::memset(&both, 0, sizeof(both));
+  AttendArgs& t = both.rows;
+  t = attend_args(&r, pl.rows, false, Q, K_tail, V_tail, tail_lengths, nullptr, K_new, V_new, parents, out, lse, ws);
   t.part_ml = (float*)((char*)ws + pl.off_ml);
-  t.part_splits = tail ? pl.total : pl.splits;
+  t.part_splits = pl.splits + (rows ? pl.rows.splits : 0);
   t.part_first = pl.splits;
-  QuantArgs a;
-  std::memset(&a, 0, sizeof(a));
+  QuantArgs& a = both.codes;
   a.Q = (const char*)Q;
   a.Kq = (const char*)Kq;
   a.Vq = (const char*)Vq;
@@ -242,19 +320,23 @@ int lagkv_attend_quantized(const lagkv_quant_params* p, const void* Q, const voi
   a.block_shift = __builtin_ctz((unsigned)p->block);
   a.part_ld = t.part_ld;
   a.rows = t.rows;
-  a.row_tiles = pl.row_tiles;
+  a.row_tiles = t.row_tiles;
   a.splits = pl.splits;
   a.part_splits = t.part_splits;
-  a.by_tiles = Divide::by(pl.row_tiles);
+  a.by_tiles = t.by_tiles;
   a.by_splits = Divide::by(pl.splits);
   a.by_h = t.by_h;
   a.by_g = t.by_g;
   a.scale = t.scale;
+  both.groups = (uint32_t)pl.groups;
+  const int64_t groups = pl.groups + (rows ? pl.groups_of_rows : 0);
+  const int tile = pl.rows.row_tile;
   hipStream_t s = (hipStream_t)hip_stream;
-  hipError_t e = p->dtype == LAGKV_F32  ? launch_quant_f32(a, p->code, pl.row_tile, s)
-                 : p->dtype == LAGKV_BF16 ? launch_quant_bf16(a, p->code, pl.row_tile, s)
-                                          : launch_quant_f16(a, p->code, pl.row_tile, s);
-  if (e == hipSuccess && tail) e = launch_attend(t, pl.rows, p->dtype, s);
+  hipError_t e = pl.rows.wide ? (p->dtype == LAGKV_BF16 ? launch_quant_wide_bf16(both, groups, p->code, s)
+                                                        : launch_quant_wide_f16(both, groups, p->code, s))
+                 : p->dtype == LAGKV_F32  ? launch_quant_f32(both, groups, p->code, tile, s)
+                 : p->dtype == LAGKV_BF16 ? launch_quant_bf16(both, groups, p->code, tile, s)
+                                          : launch_quant_f16(both, groups, p->code, tile, s);
   t.splits = t.part_splits;  // (all of the pieces are joined)
   if (e == hipSuccess) e = launch_attend_join(t, p->dtype, s);
   return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;

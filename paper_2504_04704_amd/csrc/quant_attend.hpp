@@ -6,10 +6,11 @@
 //
 // A wavefront takes every fourth step of 64 cache rows (32 where 64 do not fit the registers) for all query rows of its workgroup; K's codes become
 // numbers in the registers that they are loaded into, V's on their way into LDS.  Scales are those of sixteen rows that
-// lie in one block.  Weights times scales go in as two numbers of binary16, relative to the largest scale's power of two that
+// lie in one block.  Weights times scales go in as one or two numbers of binary16 (kWeightParts), relative to the largest scale's power of two that
 // the wavefront has met, as exponentials are relative to the largest logit: scales of 1e-30 are as good as those of 1.
 //
-// Each piece of a cache leaves its maximum, sum and outputs; launch_attend_join joins them with those of the tail and the new tokens.
+// Each piece of a cache leaves its maximum, sum and outputs; launch_attend_join joins them with those of the tail and the new tokens, which
+// other workgroups of the same launch have gone over.
 #pragma once
 #include "code_ops.hpp"
 #include "quant_internal.hpp"
@@ -30,65 +31,82 @@ struct QuantShape {
   static constexpr int MAIN = V_BYTES > O_BYTES ? V_BYTES : O_BYTES;
 };
 
-// A lane's part of a query row as binary16: eight channels of each of 2 * NC slices, times a power of two (of fp32 the rest as
-// well).  What a slice behind the row's end repeats is 0.
+// Eight slots of a query row: those of codes come in slices of sixteen, of which slice_at gives the channels.  What a slice behind the
+// row's end repeats is 0.
+template <int DT>
+struct QuerySlots {
+  static constexpr int ES = AElem<DT>::SIZE;
+  uint32_t w[2 * ES];
+  __device__ __forceinline__ void load(const char* p, int eight, int D) {
+    const int slice = eight >> 1, base = (slice * 16 < D ? slice_at(slice, D, 16) : 0) + (eight & 1) * 8;
+#pragma unroll
+    for (int i = 0; i < 2 * ES; i += 4) {
+      const u32v4 v = *(const u32v4_any*)(p + base * ES + i * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[i + e] = v[e];
+    }
+  }
+  __device__ __forceinline__ void own(int eight, int D, bool there) {
+    const int begin = (eight >> 1) * 16, dup = begin + 16 <= D ? 0 : begin < D ? begin + 16 - D : 16;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool mine = there && (eight & 1) * 8 + e >= dup;
+      if constexpr (DT == LAGKV_F32) w[e] = mine ? w[e] : 0u;
+      else w[e / 2] &= mine ? ~0u : e % 2 ? 0x0000ffffu : 0xffff0000u;
+    }
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (DT == LAGKV_F32) return __uint_as_float(w[e]);
+    else return AElem<DT>::one((uint16_t)(w[e / 2] >> (16 * (e % 2))));
+  }
+  // the largest finite magnitude
+  __device__ __forceinline__ float most(float m) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = fabsf(at(e));
+      m = fmaxf(m, x < INFINITY ? x : 0.f);
+    }
+    return m;
+  }
+};
+// The power of two, near a row's largest magnitude, that is taken out of the row where it is put into binary16; and its inverse.
+struct QueryUnit {
+  float unit, by;
+  __device__ __forceinline__ explicit QueryUnit(float most) {
+    const uint32_t exponent = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+    unit = __uint_as_float(exponent << 23);
+    by = __uint_as_float((254u - exponent) << 23);
+  }
+};
+
+// A lane's part of a query row as binary16: eight slots of each of 2 * NC, times a power of two (of fp32 the rest as well).
 template <int DT, int NC>
 struct Query {
   static constexpr int PARTS = DT == LAGKV_F32 ? 2 : 1;
   u32v4 part[PARTS][2 * NC];
   float unit;  // that power's inverse
   __device__ __forceinline__ void load(const char* p, int grp, int D, bool there) {
-    constexpr int ES = AElem<DT>::SIZE;
-    uint32_t raw[2 * NC][2 * ES];
+    QuerySlots<DT> raw[2 * NC];
+    auto eight = [&](int j) { return (j / 2 * 4 + grp) * 2 + j % 2; };
 #pragma unroll
-    for (int j = 0; j < 2 * NC; ++j) {
-      const int slice = j / 2 * 4 + grp, base = (slice * 16 < D ? slice_at(slice, D, 16) : 0) + j % 2 * 8;
+    for (int j = 0; j < 2 * NC; ++j) raw[j].load(p, eight(j), D);
 #pragma unroll
-      for (int i = 0; i < 2 * ES; i += 4) {
-        const u32v4 v = *(const u32v4_any*)(p + base * ES + i * 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) raw[j][i + e] = v[e];
-      }
-    }
-    // channels that are this slice's own
-#pragma unroll
-    for (int j = 0; j < 2 * NC; ++j) {
-      const int begin = (j / 2 * 4 + grp) * 16, dup = begin + 16 <= D ? 0 : begin < D ? begin + 16 - D : 16;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool own = there && j % 2 * 8 + e >= dup;
-        if constexpr (DT == LAGKV_F32) raw[j][e] = own ? raw[j][e] : 0u;
-        else raw[j][e / 2] &= own ? ~0u : e % 2 ? 0x0000ffffu : 0xffff0000u;
-      }
-    }
+    for (int j = 0; j < 2 * NC; ++j) raw[j].own(eight(j), D, there);
     if constexpr (DT == LAGKV_F16) {
       unit = 1.f;
 #pragma unroll
-      for (int j = 0; j < 2 * NC; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) part[0][j][i] = raw[j][i];
+      for (int j = 0; j < 2 * NC; ++j) part[0][j] = u32v4{raw[j].w[0], raw[j].w[1], raw[j].w[2], raw[j].w[3]};
     } else {
-      auto at = [&](int j, int e) {
-        if constexpr (DT == LAGKV_F32) return __uint_as_float(raw[j][e]);
-        else return AElem<LAGKV_BF16>::one((uint16_t)(raw[j][e / 2] >> (16 * (e % 2))));
-      };
       float most = 0.f;
 #pragma unroll
-      for (int j = 0; j < 2 * NC; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = fabsf(at(j, e));
-          most = fmaxf(most, x < INFINITY ? x : 0.f);
-        }
-      most = max_across_32(max_across_16(most));
-      const uint32_t exponent = min(max(__float_as_uint(most) >> 23, 1u), 253u);
-      const float by = __uint_as_float((254u - exponent) << 23);
-      unit = __uint_as_float(exponent << 23);
+      for (int j = 0; j < 2 * NC; ++j) most = raw[j].most(most);
+      const QueryUnit u(max_across_32(max_across_16(most)));
+      unit = u.unit;
 #pragma unroll
       for (int j = 0; j < 2 * NC; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float x = at(j, 2 * i) * by, y = at(j, 2 * i + 1) * by;
+          const float x = raw[j].at(2 * i) * u.by, y = raw[j].at(2 * i + 1) * u.by;
           const uint32_t hi = AElem<LAGKV_F16>::pack(x, y);
           part[0][j][i] = hi;
           if constexpr (PARTS == 2) {
@@ -115,20 +133,17 @@ __device__ __forceinline__ void half_of(u32v4 w, u32v4& lo, u32v4& hi) {
   }
 }
 
+// What a workgroup does with a piece of the rows in 8 bits.
 template <int DT, int CODE, int DP, int RT>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(const QuantArgs a) {
+__device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const WorkItem& w, char* quant_lds) {
   using E = AElem<DT>;
   using F = AElem<LAGKV_F16>;
   using Sh = QuantShape<DP, RT>;
   constexpr int SUBS = Sh::SUBS, KT = Sh::KT, CPR = Sh::CPR, NC = Sh::NC, VROWS = Sh::VROWS, NV = Sh::NV, ROWS = Sh::ROWS;
   constexpr int LDV = Sh::LDV, LDO = Sh::LDO, DT16 = DP / 16, WAVES = 4, THREADS = 256;
-  extern __shared__ __attribute__((aligned(16))) char quant_lds[];
   __shared__ float sh_ml[WAVES][ROWS][2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
-  fetch_arguments<QuantArgs>();
-  const WorkItem w = work_item(a);
-  if (!w.any) return;
   const uint32_t bu = a.by_h.of((uint32_t)w.unit);
   const int64_t b = bu, h = (uint32_t)w.unit - bu * (uint32_t)a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
@@ -254,7 +269,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(con
 #pragma unroll
       for (int s = 0; s < SUBS; ++s) r[s] = __builtin_ldexpf(r[s], 126 - top_scale);
     }
-    u32v4 ph[RT][SUBS / 2], pl[RT][SUBS / 2];
+    constexpr int PP = kWeightParts<DT>;
+    u32v4 weight[RT][SUBS / 2][PP];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
@@ -295,10 +311,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(con
       for (int s = 0; s < SUBS; ++s)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          uint32_t hi, lo;
-          F::split(p[rt][s][2 * i], p[rt][s][2 * i + 1], hi, lo);
-          ph[rt][s / 2][s % 2 * 2 + i] = hi;
-          pl[rt][s / 2][s % 2 * 2 + i] = lo;
+          uint32_t part[PP];
+          weights_of(p[rt][s][2 * i], p[rt][s][2 * i + 1], part);
+#pragma unroll
+          for (int k = 0; k < PP; ++k) weight[rt][s / 2][k][s % 2 * 2 + i] = part[k];
         }
     }
 #pragma unroll
@@ -315,10 +331,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(con
           v[s * 2 + 1] = y.y;
         }
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          o[rt][d] = F::mma(v, ph[rt][t], o[rt][d]);
-          o[rt][d] = F::mma(v, pl[rt][t], o[rt][d]);
-        }
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int k = 0; k < PP; ++k) o[rt][d] = F::mma(v, weight[rt][t][k], o[rt][d]);
       }
   }
 
@@ -381,28 +396,42 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(con
   }
 }
 
+// The pieces of rows in 8 bits and, by attend_pass.hpp's way, those of the tail and the new tokens: workgroups of one launch.
 template <int DT, int CODE, int DP, int RT>
-hipError_t launch_quant_as(const QuantArgs& a, hipStream_t s) {
-  const int64_t groups = (a.units * a.splits + 7) / 8 * 8 * a.row_tiles;
-  constexpr size_t lds = QuantShape<DP, RT>::MAIN;
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(const QuantBoth a) {
+  extern __shared__ __attribute__((aligned(16))) char quant_lds[];
+  fetch_arguments<QuantBoth>();
+  if (blockIdx.x < a.groups) {
+    const WorkItem w = work_item(a.codes);
+    if (w.any) attend_quant_body<DT, CODE, DP, RT>(a.codes, w, quant_lds);
+  } else {
+    const WorkItem w = work_item(a.rows, blockIdx.x - a.groups);
+    if (w.any) attend_body<DT, DP, RT, 4, false>(a.rows, w, quant_lds);
+  }
+}
+
+template <int DT, int CODE, int DP, int RT>
+hipError_t launch_quant_as(const QuantBoth& a, int64_t groups, hipStream_t s) {
+  constexpr int of_codes = QuantShape<DP, RT>::MAIN, of_rows = AttendShape<DT, DP, RT, 4>::MAIN, lds = of_codes > of_rows ? of_codes : of_rows;
   auto kernel = attend_quant_kernel<DT, CODE, DP, RT>;
   if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
   kernel<<<dim3((uint32_t)groups), dim3(256), lds, s>>>(a);
   return hipGetLastError();
 }
 template <int DT, int CODE>
-hipError_t launch_quant_code(const QuantArgs& a, int row_tile, hipStream_t s) {
+hipError_t launch_quant_code(const QuantBoth& a, int64_t groups, int row_tile, hipStream_t s) {
   const bool one = row_tile == 16;
-  if (a.D <= 64) return one ? launch_quant_as<DT, CODE, 64, 1>(a, s) : launch_quant_as<DT, CODE, 64, 2>(a, s);
-  if (a.D <= 128) return one ? launch_quant_as<DT, CODE, 128, 1>(a, s) : launch_quant_as<DT, CODE, 128, 2>(a, s);
-  return launch_quant_as<DT, CODE, 256, 1>(a, s);
+  if (a.codes.D <= 64) return one ? launch_quant_as<DT, CODE, 64, 1>(a, groups, s) : launch_quant_as<DT, CODE, 64, 2>(a, groups, s);
+  if (a.codes.D <= 128) return one ? launch_quant_as<DT, CODE, 128, 1>(a, groups, s) : launch_quant_as<DT, CODE, 128, 2>(a, groups, s);
+  return launch_quant_as<DT, CODE, 256, 1>(a, groups, s);
 }
 template <int DT>
-hipError_t launch_quant_of(const QuantArgs& a, int code, int row_tile, hipStream_t s) {
-  return code == LAGKV_CODE_INT8 ? launch_quant_code<DT, LAGKV_CODE_INT8>(a, row_tile, s) : launch_quant_code<DT, LAGKV_CODE_E4M3>(a, row_tile, s);
+hipError_t launch_quant_of(const QuantBoth& a, int64_t groups, int code, int row_tile, hipStream_t s) {
+  return code == LAGKV_CODE_INT8 ? launch_quant_code<DT, LAGKV_CODE_INT8>(a, groups, row_tile, s)
+                                 : launch_quant_code<DT, LAGKV_CODE_E4M3>(a, groups, row_tile, s);
 }
 
 }  // namespace lagkv

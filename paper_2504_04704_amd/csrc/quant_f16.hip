@@ -2,8 +2,8 @@
 
 namespace lagkv {
 
-hipError_t launch_quant_f16(const QuantArgs& a, int code, int row_tile, hipStream_t s) {
-  return launch_quant_of<LAGKV_F16>(a, code, row_tile, s);
+hipError_t launch_quant_f16(const QuantBoth& a, int64_t groups, int code, int row_tile, hipStream_t s) {
+  return launch_quant_of<LAGKV_F16>(a, groups, code, row_tile, s);
 }
 
 }  // namespace lagkv

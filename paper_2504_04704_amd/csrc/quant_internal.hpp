@@ -34,9 +34,17 @@ struct QuantArgs {
   Divide by_tiles, by_splits, by_h, by_g;
   float scale;  // times log2 e for the 16-bit types
 };
-hipError_t launch_quant_f32(const QuantArgs& a, int code, int row_tile, hipStream_t s);
-hipError_t launch_quant_bf16(const QuantArgs& a, int code, int row_tile, hipStream_t s);
-hipError_t launch_quant_f16(const QuantArgs& a, int code, int row_tile, hipStream_t s);
+// Both parts of a call; the tail and the new tokens are the pieces behind those of the rows in 8 bits.
+struct QuantBoth {
+  QuantArgs codes;
+  AttendArgs rows;
+  uint32_t groups;  // workgroups of the first
+};
+hipError_t launch_quant_f32(const QuantBoth& a, int64_t groups, int code, int row_tile, hipStream_t s);
+hipError_t launch_quant_bf16(const QuantBoth& a, int64_t groups, int code, int row_tile, hipStream_t s);
+hipError_t launch_quant_f16(const QuantBoth& a, int64_t groups, int code, int row_tile, hipStream_t s);
+hipError_t launch_quant_wide_bf16(const QuantBoth& a, int64_t groups, int code, hipStream_t s);
+hipError_t launch_quant_wide_f16(const QuantBoth& a, int64_t groups, int code, hipStream_t s);
 
 constexpr int kMinCodes = 16;  // channels: a slice of codes has sixteen
 

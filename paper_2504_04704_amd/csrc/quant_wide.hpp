@@ -1,0 +1,351 @@
+// Attention of many query rows over rows in 8 bits (lagkv_attend_quantized of 16-bit types; when it is taken, quant_plan_of says).
+// attend_wide.hpp's way, by workgroups of four wavefronts with 32 query rows each, with quant_attend.hpp's numbers: the rows in LDS are binary16,
+// made of codes on the way from the registers that they are loaded into, and the scales of a step lie beside them.  (Eight wavefronts, 256 query rows, in
+// two phases as there were the better ones of 14 in 100 of 528 shapes, by 4 % in the mean.)
+//
+// A lane has one query row and, of 32 cache rows, eight of the first sixteen and eight of the others in its registers, and scales are those of
+// sixteen rows: a logit's goes into the factor that it is multiplied by anyway, and a weight's into what is taken from the logit, as its logarithm.
+//
+// Bound by the matrix cores, the vector instructions and the reads of LDS together: 256 query rows of 32 streams x 33280 rows, 128 channels, bf16
+// 187 us, with the pieces joined, 0.75 Pflop/s.
+#pragma once
+#include "attend_wide.hpp"
+#include "quant_attend.hpp"
+
+namespace lagkv {
+
+template <int DP>
+struct QuantWideShape {
+  static constexpr int KT = DP > 128 ? 32 : 64, SUBS = KT / 16, CPR = DP / 16;
+  static constexpr int LDK = DP * 2 + 16, LDV = DP * 2 + 64;  // bytes between rows, as in WideShape
+  static constexpr int BUF = KT * (LDK + LDV);
+};
+
+template <int DT, int CODE, int DP>
+__device__ __forceinline__ void attend_quant_wide_body(const QuantArgs& a, const WorkItem& w, char* wide_lds) {
+  using E = AElem<DT>;
+  using F = AElem<LAGKV_F16>;
+  using W = Wide<LAGKV_F16>;
+  using Sh = QuantWideShape<DP>;
+  constexpr int KT = Sh::KT, SUBS = Sh::SUBS, CPR = Sh::CPR, LDK = Sh::LDK, LDV = Sh::LDV, THREADS = 256, ROWS = 128;
+  constexpr int HALVES = KT / 32, KS = DP / 16, DT32 = DP / 32, PASSES = KT * CPR / THREADS;
+  static_assert(KT * CPR % THREADS == 0, "");
+  __shared__ __attribute__((aligned(16))) float sh_scale[2][2][4];  // of a step's sixteens of K, of V
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+
+  const uint32_t bu = a.by_h.of((uint32_t)w.unit);
+  const int64_t b = bu, h = (uint32_t)w.unit - bu * (uint32_t)a.H;
+  const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
+  int64_t held = a.lengths ? a.lengths[b] : a.T;
+  const int len = (int)(held < 0 ? 0 : held > a.T ? a.T : held);
+  const int steps = (int)(((int64_t)len + KT - 1) / KT);
+  const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
+  const int n = step1 - step0, n_whole = min(n, len / KT - step0);  // steps, and those whose rows are all there
+
+  const int r = row0 + wave * 32 + col;
+  const bool mine = r < row1, idle = row0 + wave * 32 >= row1;  // (a wavefront without rows loads for the others)
+  const int rr = mine ? r : row0, token = (int)a.by_g.of(rr), head = (int)h * a.G + rr - token * a.G;
+  // In LDS a row has the first halves of its slices and then the second ones: what a lane writes at a time lies beside what its neighbours
+  // write.  `eight` gives the eight channels that the i-th eight there are.
+  auto eight = [](int i) { return i < CPR ? 2 * i : 2 * (i - CPR) + 1; };
+  QuerySlots<DT> raw[KS];
+  {
+    const char* p = a.Q + b * a.qsb + head * a.qsh + (int64_t)token * a.qsn;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) raw[k].load(p, eight(2 * k + half), a.D);
+  }
+
+  // This thread's slice of each row it loads, and where it is in the next step's first row.
+  const int lslice = tid % CPR, lrow = tid / CPR;
+  const int loff = lslice * 16 < a.D ? slice_at(lslice, a.D, 16) : 0;
+  constexpr int LROWS = THREADS / CPR;
+  const char* kb = a.Kq + b * a.csb + h * a.csh + loff;
+  const char* vb = a.Vq + b * a.csb + h * a.csh + loff;
+  const float* sb = ((tid & 4) ? a.vs : a.ks) + b * a.ssb + h * a.ssh;
+  const char* kp = kb + ((int64_t)step0 * KT + lrow) * a.cst;
+  const char* vp = vb + ((int64_t)step0 * KT + lrow) * a.cst;
+  const int64_t pass = a.cst * LROWS, stride = a.cst * KT;
+  u32v4 kr[PASSES], vr[PASSES];
+  float scale_in = 0.f;  // of threads 0 to 7: a step's scales of K, of V
+  auto load_rows = [&](int i, const char*& p, const char* base, u32v4 (&to)[PASSES]) {
+    if (i < n_whole) {
+#pragma unroll
+      for (int k = 0; k < PASSES; ++k) to[k] = *(const u32v4_bytes*)(p + k * pass);
+      p += stride;
+    } else if (i < n) {
+#pragma unroll
+      for (int k = 0; k < PASSES; ++k) {
+        const int row = (step0 + i) * KT + lrow + k * LROWS;
+        to[k] = *(const u32v4_bytes*)(base + (int64_t)(row < len ? row : len - 1) * a.cst);
+      }
+    }
+  };
+  // (called for one step after another)
+  auto load_k = [&](int i) {
+    load_rows(i, kp, kb, kr);
+    if (i < n) scale_in = sb[min((step0 + i) * KT + (tid & 3) * 16, len - 1) >> a.block_shift];
+  };
+  auto load_v = [&](int i) { load_rows(i, vp, vb, vr); };
+  auto k_at = [&](int i) { return wide_lds + (i & 1) * (KT * LDK); };
+  auto v_at = [&](int i) { return wide_lds + 2 * KT * LDK + (i & 1) * (KT * LDV); };
+  auto store = [&](const u32v4 (&from)[PASSES], char* to, int ld) {
+    to += lrow * ld + lslice * 16;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      u32v4 lo, hi;
+      half_of<CODE>(from[k], lo, hi);
+      *(u32v4*)(to + k * LROWS * ld) = lo;
+      *(u32v4*)(to + k * LROWS * ld + CPR * 16) = hi;
+    }
+  };
+  auto store_k = [&](int i) {
+    store(kr, k_at(i), LDK);
+    if (tid < 8) sh_scale[i & 1][tid >> 2][tid & 3] = scale_in;
+  };
+  auto store_v = [&](int i) {
+    if (i >= n_whole && i < n) {
+      // (a row that is not there: its codes may be no numbers)
+#pragma unroll
+      for (int k = 0; k < PASSES; ++k)
+        if ((step0 + i) * KT + lrow + k * LROWS >= len) vr[k] = u32v4{0, 0, 0, 0};
+    }
+    store(vr, v_at(i), LDV);
+  };
+
+  float c = 0.f;                 // what a query row's products are multiplied by, without the cache rows' scales
+  float m = -INFINITY, l = 0.f;  // m in units of base 2
+  int top_scale = 0;             // exponent (biased) of the largest scale of V so far: o is relative to it
+  f32x16 o[DT32];
+  constexpr int PP = kWeightParts<DT>;
+  u32v4 q[KS], p[2 * HALVES][PP];  // P, in steps of 16 rows
+#pragma unroll
+  for (int d = 0; d < DT32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  // Scores of step i and outputs of step i - 1, in one stream of products.  (Before the first step P and V are 0; behind the
+  // last the scores are not used.)
+  constexpr int NS = KS * HALVES, NO = 2 * HALVES * DT32;
+  auto multiply = [&](int i, f32x16 (&s)[HALVES]) {
+    const char* kl = k_at(i) + col * LDK + half * 16;
+    const char* vl = v_at(i - 1) + (half * 4 + (lane & 15) / 4) * LDV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+    for (int t = 0; t < HALVES; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+    products<NS + NO, 4>(
+        [&](int j) {
+          if (j < NS) return *(const u32v4*)(kl + j % HALVES * 32 * LDK + j / HALVES * 32);
+          const char* at = vl + (j - NS) / DT32 * 16 * LDV + (j - NS) % DT32 * 64;
+          const u32v2 y = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at));
+          const u32v2 z = __builtin_bit_cast(u32v2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 8 * LDV)));
+          return u32v4{y.x, y.y, z.x, z.y};
+        },
+        [&](int j, u32v4 f) {
+          if (j < NS) s[j % HALVES] = W::mma(f, q[j < NS ? j / HALVES : 0], s[j % HALVES]);
+          else {
+#pragma unroll
+            for (int k = 0; k < PP; ++k) o[(j - NS) % DT32] = W::mma(f, p[(j - NS) / DT32][k], o[(j - NS) % DT32]);
+          }
+        });
+  };
+  auto weights = [&](int i, f32x16 (&s)[HALVES]) {
+    const f32x4 ks = *(const f32x4*)sh_scale[i & 1][0], vs = *(const f32x4*)sh_scale[i & 1][1];
+    float by[SUBS], of[SUBS];
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) {
+      by[u] = ks[u] * c;
+      of[u] = vs[u];
+    }
+    if (i >= n_whole) {
+      const int left = len - (step0 + i) * KT;
+      // Rows that are not there get -inf by a product of a column that has it for them with ones, and the scores of both ways here come
+      // together as whole vectors: one by one they would be copied in every step.
+#pragma unroll
+      for (int t = 0; t < HALVES; ++t)
+        s[t] = W::mma(u32v4{half == 0 && t * 32 + col >= left ? 0xfc00u : 0u, 0, 0, 0}, u32v4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}, s[t]);
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) {
+        by[u] = by[u] < 1e-30f ? 1e-30f : by[u];  // (times -inf; what is no number stays that)
+        of[u] = u * 16 < left ? of[u] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < HALVES; ++t) asm volatile("" : "+v"(s[t]));
+    // scales of V, as parts of the largest's power of two: a weight's is put into its exponent, and taken out of the sums
+    uint32_t largest = 0;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) largest = max(largest, __float_as_uint(of[u]) & 0x7fffffffu);
+    const int now_scale = __builtin_amdgcn_readfirstlane((int)(largest >> 23));
+    if (now_scale > top_scale) {
+      // (one that is no number: neither are the outputs, and the sums do not change)
+      const float f = now_scale == 255 ? __uint_as_float(0x7fc00000u) : __builtin_ldexpf(1.f, top_scale - now_scale);
+#pragma unroll
+      for (int d = 0; d < DT32; ++d) o[d] *= f;
+      top_scale = now_scale;
+    }
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) of[u] = __builtin_amdgcn_logf(fmaxf(__builtin_ldexpf(of[u], 126 - top_scale), 0x1p-60f));
+
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) {
+      float x = s[u / 2][u % 2 * 8];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e]);
+      top = fmaxf(top, x * by[u]);
+    }
+    top = max_across_32(top);
+    if (__any(top > m + W::SLACK)) {
+      const float now = fmaxf(m, top);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DT32; ++d) o[d] *= keep;
+    }
+    const float at = m == -INFINITY ? 0.f : m - W::LIFT;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) {
+      const float less = at - of[u];
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][u % 2 * 8 + e], by[u], -less));
+        const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][u % 2 * 8 + e + 1], by[u], -less));
+        sum0 += y;
+        sum1 += z;
+        uint32_t part[PP];
+        weights_of(y, z, part);
+#pragma unroll
+        for (int k = 0; k < PP; ++k) p[u][k][e / 2] = part[k];
+      }
+      l = __builtin_fmaf(sum0 + sum1, __builtin_amdgcn_exp2f(-of[u]), l);
+    }
+  };
+
+  if (n > 0) {
+#pragma unroll
+    for (int k = 0; k < 2 * HALVES; ++k)
+#pragma unroll
+      for (int i = 0; i < PP; ++i) p[k][i] = u32v4{0, 0, 0, 0};
+    for (int k = tid; k < KT * LDV / 16; k += THREADS) *(u32v4*)(v_at(1) + k * 16) = u32v4{0, 0, 0, 0};
+    load_k(0);
+    load_v(0);
+    // q, with the scale's sign: what is left of it is not negative, and the largest logit that of the largest product.  (It is waited for
+    // here, behind the first rows' loads.)
+    {
+      const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+      float most = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        raw[k].own(eight(2 * k + half), a.D, mine);
+        if constexpr (DT != LAGKV_F16) most = raw[k].most(most);
+      }
+      const QueryUnit u(max_across_32(most));
+      c = fabsf(a.scale) * (DT == LAGKV_F16 ? 1.f : u.unit);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        u32v4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[i] = (DT == LAGKV_F16 ? raw[k].w[i] : F::pack(raw[k].at(2 * i) * u.by, raw[k].at(2 * i + 1) * u.by)) ^ flip;
+        asm volatile("" : "+v"(v));
+        q[k] = v;
+      }
+    }
+    store_k(0);
+    load_k(1);
+    __syncthreads();
+    // (one barrier a step: what is written in one are the buffers that nobody reads in it)
+    auto move = [&](int i) {
+      store_k(i + 1);  // (behind the last step: what was there)
+      store_v(i);
+      load_k(i + 2);
+      load_v(i + 1);
+    };
+    // (Two loops: the scores of one have a beginning and an end in every step, and no copies.)
+    if (idle) {
+      for (int i = 0; i <= n; ++i) {
+        if (i < n) move(i);
+        __syncthreads();
+      }
+    } else {
+      for (int i = 0; i <= n; ++i) {
+        f32x16 s[HALVES];
+        multiply(i, s);
+        if (i < n) {
+          weights(i, s);
+          move(i);
+        }
+        __syncthreads();
+      }
+    }
+  }
+
+  if (!mine) return;
+  l = sum_across_32(l);
+  // as launch_attend_join counts on it: the type's factor in place of this kernel's, and the scales put in
+  const float unit = __builtin_ldexpf(1.f, top_scale - 126);
+  const int64_t at = (w.unit * a.part_splits + w.split) * a.rows + r;
+  float* po = a.part_o + at * a.part_ld;
+#pragma unroll
+  for (int d = 0; d < DT32; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // (slots of a row of codes, in slices of sixteen)
+      const int slot = eight(d * 4 + e) * 8 + 4 * half, begin = slot & ~15;
+      if (begin >= a.D) continue;
+      const f32x4 v = {o[d][4 * e] * unit, o[d][4 * e + 1] * unit, o[d][4 * e + 2] * unit, o[d][4 * e + 3] * unit};
+      const int base = slice_at(begin / 16, a.D, 16), dup = begin - base;
+      if (dup == 0) {
+        *(f32x4*)(po + slot) = v;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((slot & 15) + i >= dup) po[base + (slot & 15) + i] = v[i];
+      }
+    }
+  if (half == 0) {
+    a.part_ml[at * 2] = m - W::LIFT + E::LIFT;
+    a.part_ml[at * 2 + 1] = l;
+  }
+}
+
+// The pieces of rows in 8 bits and those of the tail and the new tokens, as in attend_quant_kernel.
+template <int DT, int CODE, int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_quant_wide_kernel(const QuantBoth a) {
+  extern __shared__ __attribute__((aligned(16))) char wide_lds[];
+  fetch_arguments<QuantBoth>();
+  if (blockIdx.x < a.groups) {
+    const WorkItem w = work_item(a.codes);
+    if (w.any) attend_quant_wide_body<DT, CODE, DP>(a.codes, w, wide_lds);
+  } else {
+    const WorkItem w = work_item(a.rows, blockIdx.x - a.groups);
+    if (w.any) attend_wide_body<DT, DP, 4>(a.rows, w, wide_lds);
+  }
+}
+
+template <int DT, int CODE, int DP>
+hipError_t launch_quant_wide_as(const QuantBoth& a, int64_t groups, hipStream_t s) {
+  static_assert(QuantWideShape<DP>::BUF == WideShape<DP>::BUF, "");
+  constexpr int lds = 2 * QuantWideShape<DP>::BUF;
+  auto kernel = attend_quant_wide_kernel<DT, CODE, DP>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((uint32_t)groups), dim3(256), lds, s>>>(a);
+  return hipGetLastError();
+}
+template <int DT, int CODE>
+hipError_t launch_quant_wide_code(const QuantBoth& a, int64_t groups, hipStream_t s) {
+  if (a.codes.D <= 64) return launch_quant_wide_as<DT, CODE, 64>(a, groups, s);
+  return a.codes.D <= 128 ? launch_quant_wide_as<DT, CODE, 128>(a, groups, s) : launch_quant_wide_as<DT, CODE, 256>(a, groups, s);
+}
+template <int DT>
+hipError_t launch_quant_wide_of(const QuantBoth& a, int64_t groups, int code, hipStream_t s) {
+  return code == LAGKV_CODE_INT8 ? launch_quant_wide_code<DT, LAGKV_CODE_INT8>(a, groups, s) : launch_quant_wide_code<DT, LAGKV_CODE_E4M3>(a, groups, s);
+}
+
+}  // namespace lagkv

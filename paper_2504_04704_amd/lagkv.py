@@ -186,6 +186,8 @@ def _load_native(lib):
         lib.lagkv_plan, lib.lagkv_workspace_bytes, lib.lagkv_compress, lib.lagkv_append_and_compress,
         lib.lagkv_attend_workspace_bytes, lib.lagkv_attend, lib.lagkv_attend_blocks, lib.lagkv_block_bounds,
         lib.lagkv_select_blocks)), raw_stream)
+    native.init_codes(*(C.cast(f, C.c_void_p).value for f in (
+        lib.lagkv_quantize, lib.lagkv_dequantize, lib.lagkv_attend_quantized_workspace_bytes, lib.lagkv_attend_quantized)))
     return native
 
 
@@ -721,6 +723,11 @@ def quantize(K: torch.Tensor, V: torch.Tensor, block: int, code: torch.dtype = t
     """lagkv_quantize: rows K, V [B,H,T,D] as codes (torch.int8 or torch.float8_e4m3fn) with a scale for each block of `block`
     rows and head.  With `start` and `out` only the blocks from that of row `start` on are written; rows behind lengths[b] are left
     as they are."""
+    if _native is not None and out is not None and out.block == block:
+        rc = _native.go_over(False, out.K, out.V, out.K_scale, out.V_scale, block, K, V, lengths, start)
+        if rc >= 0:
+            _check(rc, "lagkv_quantize")
+            return out
     block, start = index(block), index(start)
     _int32("lagkv_quantize", block)
     _rows("K", K)
@@ -729,6 +736,7 @@ def quantize(K: torch.Tensor, V: torch.Tensor, block: int, code: torch.dtype = t
     if block < 1 or start < 0:
         raise LagKVError(EINVAL, "lagkv_quantize")
     B, H, T, D = K.shape
+    start = min(start, T)
     if out is None:
         if code not in _CODES:
             raise TypeError(f"codes: unsupported dtype {code}")
@@ -752,6 +760,11 @@ def dequantize(x: Quantized, dtype: torch.dtype = torch.bfloat16, lengths: Optio
                out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """lagkv_dequantize: the rows K, V [B,H,T,D] that the codes stand for, in `dtype` (that of `out` where it is given).  Rows before
     `start` and behind lengths[b] are left as they are (not written, in new tensors)."""
+    if _native is not None and out is not None:
+        rc = _native.go_over(True, x.K, x.V, x.K_scale, x.V_scale, x.block, *out, lengths, start)
+        if rc >= 0:
+            _check(rc, "lagkv_dequantize")
+            return out
     start = index(start)
     if start < 0:
         raise LagKVError(EINVAL, "lagkv_dequantize")
@@ -767,6 +780,7 @@ def dequantize(x: Quantized, dtype: torch.dtype = torch.bfloat16, lengths: Optio
         raise ValueError("output buffers must be [B,H,T,D] as the codes, on their device")
     p = _quant_params(x, K.dtype)
     p.row_stride[:] = K.stride()[:3]
+    start = min(start, p.T)
     if lengths is not None:
         _ints("lengths", lengths, (p.B,), K.device)
     with _on(K.device):
@@ -789,6 +803,13 @@ def attend_quantized(q: torch.Tensor, x: Quantized, K_tail: Optional[torch.Tenso
     """lagkv_attend_quantized: `attend` over the rows that x holds in 8 bits (its first lengths[b]), over rows K_tail, V_tail
     [B,H,R,D] behind them that are not quantised (their first tail_lengths[b]) and, with K_new, V_new [B,H,N,D], over the new tokens
     themselves.  There is no backward pass."""
+    if _native is not None:
+        got = _native.attend_quantized(q, x.K, x.V, x.K_scale, x.V_scale, x.block, K_tail, V_tail, K_new, V_new, parents, lengths,
+                                       tail_lengths, scale, out, want_lse, ws)
+        if isinstance(got, int):
+            raise LagKVError(got, "lagkv_attend_quantized")
+        if got is not None:
+            return Attended(*got)
     _rows("q", q)
     p = _quant_params(x, q.dtype)
     _no_grad(q, K_tail, V_tail, K_new, V_new, x.K, x.V, x.K_scale, x.V_scale)
