@@ -687,10 +687,12 @@ class Quantized:
         nb = -(-T // index(block))
         return cls(K, V, *(torch.empty((B, H, nb), dtype=torch.float32, device=device) for _ in range(2)), index(block))
 
-    def view(self, n: int, batch: slice = slice(None)) -> "Quantized":
-        """The first n rows (of a slice of the batch)."""
-        nb = -(-n // self.block)
-        return Quantized(self.K[batch, :, :n], self.V[batch, :, :n], self.K_scale[batch, :, :nb], self.V_scale[batch, :, :nb], self.block)
+    def view(self, n: int, batch: slice = slice(None), first: int = 0) -> "Quantized":
+        """Rows first .. n-1, from the beginning of a block on (of a slice of the batch)."""
+        if first % self.block:
+            raise ValueError("first must be a multiple of block")
+        rows, blocks = slice(first, n), slice(first // self.block, -(-n // self.block))
+        return Quantized(self.K[batch, :, rows], self.V[batch, :, rows], self.K_scale[batch, :, blocks], self.V_scale[batch, :, blocks], self.block)
 
 
 def _quant_params(x: Quantized, dtype) -> QuantParams:
@@ -1074,3 +1076,110 @@ class Cache:
         """attend_blocks() over listed blocks of the rows held, as select_blocks() gives them."""
         n = self.length
         return attend_blocks(q, self.K[batch, :, :n], self.V[batch, :, :n], blocks, block, K_new, V_new, parents, **kw)
+
+
+class QuantizedCache:
+    """A decode-time cache whose final rows are in 8 bits.  Rows that the compression still goes over, and final ones that do not make a
+    whole block yet, lie in a small Cache of the type (`window`); those that append_and_compress makes final are quantised from
+    there, block by block, and leave it.  The same rows are kept, in the same order, as a Cache keeps."""
+
+    def __init__(self, B: int, H: int, D: int, capacity: int, S: int, L: int, r: float, block: int = 64, code: torch.dtype = torch.int8,
+                 window: Optional[int] = None, dtype=torch.bfloat16, device="cuda", variant=SCORE_LAG, std_ddof: int = 1,
+                 track_positions: bool = True, launch: int = 0):
+        """`capacity`: rows in 8 bits; `window`: rows of the others (a call needs room for what is held there, fewer than block +
+        2 L rows, and for its new ones; S + 4 L + block where it is not given)."""
+        self.rows = Quantized.empty(B, H, capacity, D, block, code, device)
+        self.n = 0  # rows held in 8 bits
+        self.pos = torch.empty((B, H, capacity), dtype=torch.int32, device=device) if track_positions else None
+        self.window = Cache(B, H, D, S + 4 * L + index(block) if window is None else window, S, L, r, dtype, device, variant, std_ddof,
+                            track_positions, launch)
+
+    @classmethod
+    def from_compressed(cls, comp: Compressed, T: int, capacity: int, S: int, L: int, r: float, block: int = 64,
+                        code: torch.dtype = torch.int8, window: Optional[int] = None, variant=SCORE_LAG, std_ddof: int = 1,
+                        launch: int = 0) -> "QuantizedCache":
+        """A cache that holds the output of compress() on T rows, its final rows in 8 bits."""
+        B, H, T_out, D = comp.K.shape
+        x = cls(B, H, D, capacity, S, L, r, block, code, window, comp.K.dtype, comp.K.device, variant, std_ddof, comp.idx is not None, launch)
+        c = CacheT(capacity=T_out)
+        _check(load().lagkv_cache_after_compress(C.byref(x.window._params()), T, C.byref(c)), "lagkv_cache_after_compress")
+        m = x._settle(comp.K, comp.V, comp.idx, c.n_static if T >= S else 0)
+        if T_out - m > x.window.K.shape[2]:
+            raise LagKVError(ECAPACITY, "QuantizedCache.from_compressed")
+        w = x.window
+        for to, rows in ((w.K, comp.K), (w.V, comp.V), (w.pos, comp.idx)):
+            if rows is not None:
+                to[:, :, :T_out - m].copy_(rows[:, :, m:])
+        w.c.n_static, w.c.n_tail, w.c.n_seen = c.n_static - m, c.n_tail, c.n_seen
+        return x
+
+    def _settle(self, K, V, pos, n_static: int) -> int:
+        """Whole blocks of the first n_static rows of K and V into 8 bits, as many as there is room for; returns how many rows."""
+        block = self.rows.block
+        m = min(n_static, self.rows.K.shape[2] - self.n) // block * block
+        if m > 0:
+            quantize(K[:, :, :m], V[:, :, :m], block, out=self.rows.view(self.n + m, first=self.n))
+            if pos is not None:
+                self.pos[:, :, self.n:self.n + m].copy_(pos[:, :, :m])
+            self.n += m
+        return m
+
+    @property
+    def n_static(self) -> int:
+        return self.n + self.window.n_static
+
+    @property
+    def n_tail(self) -> int:
+        return self.window.n_tail
+
+    @property
+    def n_seen(self) -> int:
+        return self.window.n_seen
+
+    @property
+    def length(self) -> int:
+        return self.n + self.window.length
+
+    def append_and_compress(self, K_new: Optional[torch.Tensor], V_new: Optional[torch.Tensor]) -> None:
+        """Cache.append_and_compress; rows that it makes final go into 8 bits (where `capacity` has room: else they stay in the window)."""
+        w = self.window
+        w.append_and_compress(K_new, V_new)
+        if w.n_seen < w.S or w.n_static < self.rows.block:
+            return
+        end = w.length
+        m = self._settle(w.K, w.V, w.pos, w.n_static)
+        if m > 0:
+            for t in (w.K, w.V, w.pos):
+                if t is not None:
+                    rest = t[:, :, m:end]
+                    t[:, :, :end - m].copy_(rest.clone() if end > 2 * m else rest)
+            w.c.n_static -= m
+            w.changed_from(0)
+
+    def prefill_chunked(self, K: torch.Tensor, V: torch.Tensor) -> int:
+        """A prompt by calls of append_and_compress with the rows that lagkv_prefill_rows says; returns their number.  (A prompt whose
+        rows are all there: compress() and from_compressed() are two calls.)"""
+        w, T, t, calls = self.window, K.shape[2], 0, 0
+        p = w._params()
+        while t < T:
+            n = load().lagkv_prefill_rows(C.byref(p), C.byref(w.c), T - t)
+            if n <= 0:
+                raise LagKVError(EINVAL, "lagkv_prefill_rows")
+            self.append_and_compress(K[:, :, t:t + n], V[:, :, t:t + n])
+            t += n
+            calls += 1
+        return calls
+
+    def view(self) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+        """The rows held, those in 8 bits read back, and their positions."""
+        K, V, pos = self.window.view()
+        back = dequantize(self.rows.view(self.n), K.dtype)
+        return torch.cat([back[0], K], 2), torch.cat([back[1], V], 2), None if pos is None else torch.cat([self.pos[:, :, :self.n], pos], 2)
+
+    def attend(self, q: torch.Tensor, K_new: Optional[torch.Tensor] = None, V_new: Optional[torch.Tensor] = None,
+               parents: Optional[torch.Tensor] = None, batch: slice = slice(None), **kw) -> Attended:
+        """attend_quantized() of new tokens over the rows held; `batch`: a slice of the batch (one layer of those folded into it).  The tokens'
+        own rows are not in the cache yet, as of Cache.attend."""
+        w = self.window
+        n = w.length
+        return attend_quantized(q, self.rows.view(self.n, batch), w.K[batch, :, :n], w.V[batch, :, :n], K_new, V_new, parents, **kw)
