@@ -73,9 +73,41 @@ struct WideShape {
   static constexpr int BUF = KT * (LDK + LDV);
 };
 
-// What a workgroup does, with two buffers of [K rows][V rows] in LDS.
+// What a lane has of its query row's state: outputs (32x32 products' layout; slot d * 32 + 8 e + 4 half + i in o[d][4 e + i]), maximum in
+// base 2 and its half's sum.
+template <int DP>
+struct WideState {
+  f32x16 o[DP / 32];
+  float m, l;
+};
+template <int DP>
+__device__ __forceinline__ WideState<DP> no_rows_yet() {
+  WideState<DP> x;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x.o[d][i] = 0.f;
+  x.m = -INFINITY;
+  x.l = 0.f;
+  return x;
+}
+
+// Steps of a unit's rows, up to what a tile of ROWS query rows sees of the new tokens.
+template <int DP, int ROWS>
+__device__ __forceinline__ int attend_wide_steps(const AttendArgs& a, const WorkItem& w) {
+  constexpr int KT = WideShape<DP>::KT;
+  const uint32_t b = a.by_h.of((uint32_t)w.unit);
+  int64_t len = a.lengths ? a.lengths[b] : a.T;
+  len = len < 0 ? 0 : len > a.T ? a.T : len;
+  const int last_token = (int)a.by_g.of(min(w.tile * ROWS + ROWS, a.rows) - 1);
+  const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
+  return (int)((len + KT - 1) / KT) + (seen_new + KT - 1) / KT;
+}
+
+// What a workgroup does, with two buffers of [K rows][V rows] in LDS: from a state on that `before` steps of its unit's rows, those of the piece
+// among them, have left.
 template <int DT, int DP, int WAVES>
-__device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const WorkItem& w, char* wide_lds) {
+__device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const WorkItem& w, char* wide_lds, int before, const WideState<DP>& from) {
   using E = AElem<DT>;
   using W = Wide<DT>;
   using Sh = WideShape<DP>;
@@ -97,7 +129,8 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const Work
   const int token0 = (int)a.by_g.of(row0), last_token = (int)a.by_g.of(row1 - 1), tokens = last_token - token0 + 1;
   const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
-  const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
+  const int all = before + steps, step0 = max((int)((int64_t)all * w.split / a.splits) - before, 0);
+  const int step1 = max((int)((int64_t)all * (w.split + 1) / a.splits) - before, 0);
   const int n = step1 - step0;
 
   const int words = (seen_new + 31) / 32;
@@ -219,13 +252,11 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const Work
     return bits;
   };
 
-  float m = -INFINITY, l = 0.f;  // m in units of base 2
+  float m = from.m, l = from.l;  // m in units of base 2
   f32x16 o[DT32], s[HALVES];
   u32v4 p[2 * HALVES], pl[2 * HALVES];  // P, in steps of 16 rows: its leading bits, and the rest
 #pragma unroll
-  for (int d = 0; d < DT32; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  for (int d = 0; d < DT32; ++d) o[d] = from.o[d];
 
   // Scores of step i and outputs of step i - 1, in one stream of products.  (Before the first step P and V are 0; behind the
   // last the scores are not used.)
@@ -422,7 +453,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
   extern __shared__ __attribute__((aligned(16))) char wide_lds[];
   fetch_arguments<AttendArgs>();
   const WorkItem w = work_item(a);
-  if (w.any) attend_wide_body<DT, DP, WAVES>(a, w, wide_lds);
+  if (w.any) attend_wide_body<DT, DP, WAVES>(a, w, wide_lds, 0, no_rows_yet<DP>());
 }
 
 template <int DT, int DP, int WAVES>

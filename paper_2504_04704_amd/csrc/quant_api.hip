@@ -117,56 +117,52 @@ int check_quant(const lagkv_quant_params* p) {
   return attend_check(&r, false);
 }
 
-// A form of the kernels: rows of a tile, the cache rows of a step in 8 bits and in the type, and the microseconds of a step with
-// one workgroup on a compute unit, of one with others beside it, and of a workgroup's beginning and end; a step of the tail and the new tokens takes
-// `of_rows` of one in 8 bits.
+// The kernel of few rows: tiles of 16, or of 32 where the registers hold them, the cache rows of a step in 8 bits and in the type, and the
+// microseconds of a step with one workgroup on a compute unit, of one with others beside it, of a workgroup's beginning and end, and of the kernel that
+// joins the pieces; a step of the tail and the new tokens takes `of_rows` of one in 8 bits.
 struct QuantForm {
-  bool wide;
   int row_tile, step, step_of_rows;
-  double alone, beside, ends, of_rows;
+  double alone, beside, ends, join, of_rows;
 };
-// Few rows: 16, or 32 where the registers hold them; many (16-bit types): 128.
-int quant_forms(const lagkv_quant_params* p, int64_t rows, QuantForm (&f)[2]) {
-  const bool f32 = p->dtype == LAGKV_F32;
-  const int kr = f32 ? 16 : 32;
-  int n = 0;
-  if (p->D <= 64) f[n++] = rows <= 16 ? QuantForm{false, 16, 64, kr, 0.39, 0.58, 4.4, f32 ? 0.64 : 0.73} : QuantForm{false, 32, 64, kr, 0.41, f32 ? 0.75 : 0.63, f32 ? 7.6 : 6.2, 0.8};
-  else if (p->D > 128) f[n++] = {false, 16, 32, kr, f32 ? 0.55 : 0.48, f32 ? 0.67 : 0.52, f32 ? 10.2 : 8.6, f32 ? 1.3 : 1.8};
-  else if (rows <= 16) f[n++] = {false, 16, 64, kr, 0.54, 1.0, f32 ? 6.6 : 5.4, f32 ? 0.72 : 0.81};
-  else f[n++] = {false, 32, 32, kr, f32 ? 0.34 : 0.29, f32 ? 0.59 : 0.51, f32 ? 10.4 : 8.4, f32 ? 2.1 : 1.4};
-  if (f32 || rows <= 32) return n;
-  if (p->D <= 64) f[n++] = {true, 128, 64, 64, 1.0, 1.6, 6.1, 1.7};
-  else if (p->D > 128) f[n++] = {true, 128, 32, 32, 2.8 / 2, 3.6 / 2, 12.8, 1.0};
-  else f[n++] = {true, 128, 64, 64, 1.26, 2.17, 8.3, 1.6};
-  return n;
+QuantForm quant_form(const lagkv_quant_params* p, int64_t rows) {
+  if (p->dtype == LAGKV_F32) {
+    if (p->D > 128) return {16, 32, 16, 0.55, 0.62, 9.8, 4.4, 1.4};
+    if (p->D > 64) return rows <= 16 ? QuantForm{16, 64, 16, 0.61, 1.05, 5, 5, 0.71} : QuantForm{32, 32, 16, 0.4, 0.59, 5, 8.3, 1.6};
+    return rows <= 16 ? QuantForm{16, 64, 16, 0.44, 0.64, 3.8, 4.6, 0.64} : QuantForm{32, 64, 16, 0.41, 0.69, 5.2, 5.5, 0.92};
+  }
+  if (p->D > 128) return {16, 32, 32, 0.52, 0.52, 10.3, 2.4, 1.7};
+  if (p->D > 64) return rows <= 16 ? QuantForm{16, 64, 32, 0.58, 1.06, 6.8, 2.2, 0.74} : QuantForm{32, 32, 32, 0.3, 0.47, 5.9, 6.5, 1.5};
+  return rows <= 16 ? QuantForm{16, 64, 32, 0.43, 0.66, 5, 3.2, 0.75} : QuantForm{32, 64, 32, 0.38, 0.6, 5.4, 4.9, 0.75};
 }
+int64_t next_of(int64_t pieces) { return pieces + (pieces < 4 ? 1 : pieces % 3 == 0 ? pieces / 3 : pieces / 2); }  // 1 2 3 4 6 8 12 16 24 ...
 
-// The pieces of the rows in 8 bits and of the others by the microseconds that they take: rounds of workgroups on the fullest of the eight
-// XCDs (two a compute unit; one beyond 128 channels), or all rows past memory at 5.5 TB/s; and the kernel that joins the
-// pieces.  Over 3486 shapes (64 to 256 channels, 1 to 4000 query rows of 1 to 256 streams, 64 to 65536 rows in 8 bits and up to 2048 behind
-// them, a quarter with lengths that differ) its choice takes 3.4 % longer than the best form and numbers of pieces of up to 60 that were
-// measured in the mean (half of them at most 0.2 %, nine in ten 12 %), where pieces as for a cache in 16 bits alone, with the others' share of them, take 9.8 %.
-double quant_shape(const lagkv_quant_params* p, const QuantForm& f, int64_t units, int64_t rows, int* pieces, int* pieces_of_rows) {
+// Its pieces of the rows in 8 bits and of the others by the microseconds that they take: rounds of workgroups on the fullest of the eight
+// XCDs (two a compute unit; one beyond 128 channels), or all rows past memory at 5.5 TB/s; and the kernel that joins the pieces.
+double quant_narrow_shape(const lagkv_quant_params* p, const QuantForm& f, int64_t units, int64_t rows, int* pieces, int* pieces_of_rows) {
   const int64_t steps = (p->T + f.step - 1) / f.step, others = (p->R + f.step_of_rows - 1) / f.step_of_rows + (p->N + f.step_of_rows - 1) / f.step_of_rows;
   const int64_t tiles = (rows + f.row_tile - 1) / f.row_tile, places = p->D > 128 ? 32 : 64;
   const double memory = (double)units * (double)p->D * ((double)p->T * 2 + (double)(p->R + p->N) * 2 * esize_of(p)) / 5.5e6;
   double least = 1e30;
-  for (int64_t sq = 1; sq <= 128 && (sq == 1 || sq * (f.wide ? 1 : 4) <= steps); sq += sq < 4 ? 1 : sq % 3 == 0 ? sq / 3 : sq / 2) {
-    const int64_t share = others * sq / steps;
-    const int64_t choices[] = {1, 2, 3, share / 2, share};
-    int64_t before = 0;
-    for (int64_t st : choices) {
-      if (st <= before || st > 3 * sq + 2 || (st > 1 && st > others)) continue;
-      before = st;
+  for (int64_t sq = 1; sq <= 128 && (sq == 1 || sq * 4 <= steps); sq = next_of(sq)) {
+    // (their share of the pieces, some less and some more; with one piece of the rows in 8 bits any number)
+    const int64_t share = others * sq / steps, choices[] = {1, 2, 3, share / 2, share, 2 * share};
+    int64_t st = 0;
+    for (int i = 0; sq == 1 || i < 6; ++i) {
+      const int64_t now = sq == 1 ? next_of(st) : choices[i];
+      if (sq == 1 && (now > 128 || (now > 1 && now * 4 > others))) break;
+      if (now <= st || (now > 1 && now * 4 > others)) continue;
+      st = now;
       const double nq = (double)((units * sq + 7) / 8 * tiles), nt = (double)((units * st + 7) / 8 * tiles);
       const double step = nq + nt > 32 ? f.beside : f.alone;
       const double tq = (double)((steps + sq - 1) / sq) * step + f.ends, tt = (double)((others + st - 1) / st) * step * f.of_rows + f.ends;
-      double us = (double)(((int64_t)nq + places - 1) / places) * tq;
+      const int64_t rounds = ((int64_t)nq + places - 1) / places;
+      // (pieces of a kind end together: what does not fit beside them comes behind, where it is not dealt out to those that end sooner)
+      double us = (double)rounds * tq + (nq + nt > (double)(rounds * places) ? 0.4 * (tt < tq ? tt : tq) : 0);
       us = us > tt ? us : tt;
       const double all = (nq * tq + nt * tt) / (double)places;
       us = us > all ? us : all;
       us = us > memory + f.ends ? us : memory + f.ends;
-      us += 4 + (double)(units * rows * (sq + st)) * (double)p->D * 2e-6;
+      us += f.join + (double)(units * rows * (sq + st)) * (double)p->D * 2.5e-6;
       if (us < least) {
         least = us;
         *pieces = (int)sq;
@@ -177,9 +173,33 @@ double quant_shape(const lagkv_quant_params* p, const QuantForm& f, int64_t unit
   return least;
 }
 
+// The kernel of many rows: tiles of 128, and the pieces of all rows.
+// Of both: over 8781 shapes (1 to 4000 query rows of 1 to 256 streams, 64 to 256 channels, 64 to 65536 rows in 8 bits and up to 2048 behind them, some
+// with lengths that differ) the choice takes 2.4 % longer in the mean than the best form and pieces of up to 60 that were measured: half of them at most
+// 0.1 %, nine in ten 10 %.
+double quant_wide_shape(const lagkv_quant_params* p, int64_t units, int64_t rows, int* pieces) {
+  const int64_t kt = p->D > 128 ? 32 : 64, steps = (p->T + kt - 1) / kt + (p->R + kt - 1) / kt + (p->N + kt - 1) / kt;
+  const int64_t tiles = (rows + 127) / 128, places = p->D > 128 ? 32 : 64;
+  const bool f16 = p->dtype == LAGKV_F16;  // (half as many products again)
+  const double alone = p->D <= 64 ? (f16 ? 1.4 : 1.25) : p->D <= 128 ? (f16 ? 2.2 : 1.7) : f16 ? 2.2 : 1.75;
+  const double beside = p->D <= 64 ? (f16 ? 1.95 : 1.75) : p->D <= 128 ? (f16 ? 2.7 : 2.3) : f16 ? 2.1 : 1.75;
+  const double ends = p->D <= 64 ? 9.5 : p->D <= 128 ? 12.3 : 21, traffic = p->D <= 128 ? 1.8e-6 : 1e-6;
+  double least = 1e30;
+  for (int64_t s = 1; s <= 128 && s <= steps; s = next_of(s)) {
+    const int64_t groups = (units * s + 7) / 8 * tiles;
+    const double us = (double)((groups + places - 1) / places) * ((double)((steps + s - 1) / s) * (groups > 32 ? beside : alone) + ends) +
+                      (s > 1 ? 2.2 + (double)(units * rows * s) * (double)p->D * traffic : 0);
+    if (us < least) {
+      least = us;
+      *pieces = (int)s;
+    }
+  }
+  return least;
+}
+
 struct QuantPlan {
   AttendPlan rows;  // of the tail and the new tokens; units, rows and tiles are those of both
-  int splits;       // pieces of the rows in 8 bits
+  int splits;       // pieces of the rows in 8 bits; of many query rows, all pieces
   int64_t groups, groups_of_rows;
   size_t off_ml, ws_bytes;
 };
@@ -190,29 +210,28 @@ bool quant_plan_of(const lagkv_quant_params* p, QuantPlan* pl) {
   t.rows = p->G * p->N;
   const int64_t all = t.units * t.rows;
   if (all > kMostRows || !grid_fits((all + 3) / 4, 256)) return false;
-  QuantForm forms[2];
-  const int n = quant_forms(p, t.rows, forms);
-  double least = 1e30;
-  for (int i = 0; i < n; ++i) {
-    int pieces = 1, others = 1;
-    const double us = quant_shape(p, forms[i], t.units, t.rows, &pieces, &others);
-    if (i > 0 && us >= least) continue;
-    least = us;
-    t.wide = forms[i].wide;
-    t.row_tile = forms[i].row_tile;
-    t.splits = others;
-    pl->splits = pieces;
+  const QuantForm f = quant_form(p, t.rows);
+  t.row_tile = f.row_tile;
+  t.waves = 4;
+  const double us = quant_narrow_shape(p, f, t.units, t.rows, &pl->splits, &t.splits);
+  if (p->dtype != LAGKV_F32 && t.rows > 32 && p->D % 16 <= 8) {  // (a row's last channels: see attend_quant_wide_body)
+    int pieces = 1;
+    t.wide = quant_wide_shape(p, t.units, t.rows, &pieces) < us;
+    if (t.wide) {
+      t.row_tile = 128;
+      pl->splits = t.splits = pieces;
+    }
   }
   t.row_tiles = (int)((t.rows + t.row_tile - 1) / t.row_tile);
-  t.waves = 4;
   for (;;) {
     pl->groups = (t.units * pl->splits + 7) / 8 * 8 * t.row_tiles;
-    pl->groups_of_rows = (t.units * t.splits + 7) / 8 * 8 * t.row_tiles;
-    if (grid_fits(pl->groups + pl->groups_of_rows, t.waves * 64)) break;
+    pl->groups_of_rows = t.wide ? 0 : (t.units * t.splits + 7) / 8 * 8 * t.row_tiles;
+    if (grid_fits(pl->groups + pl->groups_of_rows, 256)) break;
     if (pl->splits == 1 && t.splits == 1) return false;
     pl->splits = t.splits = 1;  // (one piece where the grids do not hold more)
   }
-  const int64_t parts = all * (pl->splits + t.splits), ld = (p->D + 3) & ~3;
+  const int pieces = t.wide ? pl->splits : pl->splits + t.splits;
+  const int64_t parts = pieces > 1 ? all * pieces : 0, ld = (p->D + 3) & ~3;
   pl->off_ml = ws_align_up((size_t)parts * ld * 4);
   pl->ws_bytes = pl->off_ml + ws_align_up((size_t)parts * 8);
   return true;
@@ -284,15 +303,15 @@ int lagkv_attend_quantized(const lagkv_quant_params* p, const void* Q, const voi
     return LAGKV_EINVAL;
   QuantPlan pl;
   if (!quant_plan_of(p, &pl)) return LAGKV_ESHAPE;
-  if (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16)) return LAGKV_EWORKSPACE;
+  if (pl.ws_bytes > 0 && (!ws || ws_bytes < pl.ws_bytes || !aligned(ws, 16))) return LAGKV_EWORKSPACE;
   const bool rows = p->R > 0 || K_new;
   QuantBoth both;
   std::memset(&both, 0, sizeof(both));
   AttendArgs& t = both.rows;
   t = attend_args(&r, pl.rows, false, Q, K_tail, V_tail, tail_lengths, nullptr, K_new, V_new, parents, out, lse, ws);
   t.part_ml = (float*)((char*)ws + pl.off_ml);
-  t.part_splits = pl.splits + (rows ? pl.rows.splits : 0);
-  t.part_first = pl.splits;
+  t.part_splits = pl.splits + (rows && !pl.rows.wide ? pl.rows.splits : 0);
+  t.part_first = pl.rows.wide ? 0 : pl.splits;
   QuantArgs& a = both.codes;
   a.Q = (const char*)Q;
   a.Kq = (const char*)Kq;
@@ -337,8 +356,8 @@ int lagkv_attend_quantized(const lagkv_quant_params* p, const void* Q, const voi
                  : p->dtype == LAGKV_F32  ? launch_quant_f32(both, groups, p->code, tile, s)
                  : p->dtype == LAGKV_BF16 ? launch_quant_bf16(both, groups, p->code, tile, s)
                                           : launch_quant_f16(both, groups, p->code, tile, s);
-  t.splits = t.part_splits;  // (all of the pieces are joined)
-  if (e == hipSuccess) e = launch_attend_join(t, p->dtype, s);
+  t.splits = t.part_splits;  // (all of the pieces are joined; of few query rows there are always some)
+  if (e == hipSuccess && (t.splits > 1 || !pl.rows.wide)) e = launch_attend_join(t, p->dtype, s);
   return e == hipSuccess ? LAGKV_OK : LAGKV_EHIP;
 }
 

@@ -21,9 +21,10 @@ struct QuantWideShape {
   static constexpr int BUF = KT * (LDK + LDV);
 };
 
+// The part of a piece that is in 8 bits; returns the state that it leaves, as attend_wide_body goes on from it, and the steps that the unit's
+// rows in 8 bits are.  `others`: steps of the rows behind them.
 template <int DT, int CODE, int DP>
-__device__ __forceinline__ void attend_quant_wide_body(const QuantArgs& a, const WorkItem& w, char* wide_lds) {
-  using E = AElem<DT>;
+__device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs& a, const WorkItem& w, char* wide_lds, int others, int& steps) {
   using F = AElem<LAGKV_F16>;
   using W = Wide<LAGKV_F16>;
   using Sh = QuantWideShape<DP>;
@@ -38,8 +39,9 @@ __device__ __forceinline__ void attend_quant_wide_body(const QuantArgs& a, const
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
   int64_t held = a.lengths ? a.lengths[b] : a.T;
   const int len = (int)(held < 0 ? 0 : held > a.T ? a.T : held);
-  const int steps = (int)(((int64_t)len + KT - 1) / KT);
-  const int step0 = (int)((int64_t)steps * w.split / a.splits), step1 = (int)((int64_t)steps * (w.split + 1) / a.splits);
+  steps = (int)(((int64_t)len + KT - 1) / KT);
+  const int all = steps + others, step0 = min((int)((int64_t)all * w.split / a.splits), steps);
+  const int step1 = min((int)((int64_t)all * (w.split + 1) / a.splits), steps);
   const int n = step1 - step0, n_whole = min(n, len / KT - step0);  // steps, and those whose rows are all there
 
   const int r = row0 + wave * 32 + col;
@@ -283,47 +285,39 @@ __device__ __forceinline__ void attend_quant_wide_body(const QuantArgs& a, const
     }
   }
 
-  if (!mine) return;
-  l = sum_across_32(l);
-  // as launch_attend_join counts on it: the type's factor in place of this kernel's, and the scales put in
+  // The scales put in, the type's factor in place of this kernel's, and channels where attend_wide_body has them.  (A last slice of sixteen that
+  // is no whole one has the row's last eight channels, of which there are at most eight of its own, as its second half.)
   const float unit = __builtin_ldexpf(1.f, top_scale - 126);
-  const int64_t at = (w.unit * a.part_splits + w.split) * a.rows + r;
-  float* po = a.part_o + at * a.part_ld;
+  WideState<DP> x;
 #pragma unroll
-  for (int d = 0; d < DT32; ++d)
+  for (int i = 0; i < DP / 8; ++i) {
+    const int to = eight(i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // (slots of a row of codes, in slices of sixteen)
-      const int slot = eight(d * 4 + e) * 8 + 4 * half, begin = slot & ~15;
-      if (begin >= a.D) continue;
-      const f32x4 v = {o[d][4 * e] * unit, o[d][4 * e + 1] * unit, o[d][4 * e + 2] * unit, o[d][4 * e + 3] * unit};
-      const int base = slice_at(begin / 16, a.D, 16), dup = begin - base;
-      if (dup == 0) {
-        *(f32x4*)(po + slot) = v;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((slot & 15) + i >= dup) po[base + (slot & 15) + i] = v[i];
-      }
-    }
-  if (half == 0) {
-    a.part_ml[at * 2] = m - W::LIFT + E::LIFT;
-    a.part_ml[at * 2 + 1] = l;
+    for (int e = 0; e < 4; ++e) x.o[to / 4][to % 4 * 4 + e] = o[i / 4][i % 4 * 4 + e] * unit;
   }
+#pragma unroll
+  for (int slice = 0; slice < CPR; ++slice)
+    if (slice * 16 < a.D && a.D < slice * 16 + 16) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.o[slice / 2][slice % 2 * 8 + e] = x.o[slice / 2][slice % 2 * 8 + 4 + e];
+    }
+  x.m = m - W::LIFT + Wide<DT>::LIFT;
+  x.l = l;
+  return x;
 }
 
-// The pieces of rows in 8 bits and those of the tail and the new tokens, as in attend_quant_kernel.
+// A piece goes over the rows in 8 bits, the tail and the new tokens as one line of steps: its workgroup does what of it is in 8 bits, and goes
+// on with the rest.  (With workgroups apart, as in attend_quant_kernel, 290 query rows of 128 streams x 508 rows and 8 took 62 us in place of
+// 48: every piece of a query row is 4 bytes a channel, written and read.)
 template <int DT, int CODE, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_quant_wide_kernel(const QuantBoth a) {
   extern __shared__ __attribute__((aligned(16))) char wide_lds[];
   fetch_arguments<QuantBoth>();
-  if (blockIdx.x < a.groups) {
-    const WorkItem w = work_item(a.codes);
-    if (w.any) attend_quant_wide_body<DT, CODE, DP>(a.codes, w, wide_lds);
-  } else {
-    const WorkItem w = work_item(a.rows, blockIdx.x - a.groups);
-    if (w.any) attend_wide_body<DT, DP, 4>(a.rows, w, wide_lds);
-  }
+  const WorkItem w = work_item(a.rows);
+  if (!w.any) return;
+  int steps;
+  const WideState<DP> x = attend_quant_wide_body<DT, CODE, DP>(a.codes, w, wide_lds, attend_wide_steps<DP, 128>(a.rows, w), steps);
+  attend_wide_body<DT, DP, 4>(a.rows, w, wide_lds, steps, x);
 }
 
 template <int DT, int CODE, int DP>

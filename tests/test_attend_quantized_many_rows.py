@@ -44,10 +44,11 @@ def of_many(q, x, Kt, Vt, Kn, Vn, parents=None, **kw):
 
 SIZES = [  # H, G, N, D, T, R, new, block
     (1, 1, 70, 128, 20, 7, "tree", 16), (1, 3, 50, 128, 100, 31, "chain", 64), (2, 4, 40, 128, 700, 90, "tree", 64),
-    (1, 2, 130, 64, 129, 33, "chain", 16), (1, 3, 12, 41, 100, 12, "tree", 32), (1, 7, 21, 100, 230, 50, "chain", 32),
-    (1, 4, 20, 250, 150, 20, "tree", 16), (1, 2, 65, 256, 61, 60, "chain", 32), (1, 4, 30, 128, 300, 0, "none", 16),
+    (1, 2, 130, 64, 129, 33, "chain", 16), (1, 3, 30, 40, 100, 12, "tree", 32), (1, 7, 21, 100, 230, 50, "chain", 32),
+    (1, 4, 20, 200, 150, 20, "tree", 16), (1, 2, 65, 256, 61, 60, "chain", 32), (1, 4, 30, 128, 300, 0, "none", 16),
     (1, 5, 60, 128, 390, 10, "chain", 1024), (1, 2, 20, 17, 64, 0, "none", 64), (1, 8, 16, 96, 1, 0, "chain", 16),
-    (1, 2, 64, 128, 64, 5, "chain", 32), (1, 2, 100, 128, 64 * 6 + 1, 5, "chain", 32),
+    (1, 2, 64, 128, 64, 5, "chain", 32), (1, 2, 100, 128, 64 * 6 + 1, 5, "chain", 32), (1, 2, 90, 72, 130, 70, "chain", 32),
+    (1, 1, 150, 104, 64, 200, "tree", 16), (1, 2, 40, 245, 40, 3, "chain", 16), (1, 4, 50, 128, 3, 500, "chain", 16),
 ]
 
 
