@@ -38,7 +38,8 @@ struct Code<LAGKV_CODE_E4M3> {
   }
 };
 
-// x less the first or the second of two numbers of binary16, in one instruction.
+// x less the first or the second of two numbers of binary16, in one instruction.  (It reads registers alone, and x has been read by the conversion
+// that h comes from: the compiler, which does not look into it, has no wait to put before it.)
 __device__ __forceinline__ float less_first(float x, uint32_t h) {
   float y;
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(y) : "v"(h), "v"(x));

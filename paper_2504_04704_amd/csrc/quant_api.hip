@@ -143,7 +143,7 @@ double quant_narrow_shape(const lagkv_quant_params* p, const QuantForm& f, int64
   const int64_t tiles = (rows + f.row_tile - 1) / f.row_tile, places = p->D > 128 ? 32 : 64;
   const double memory = (double)units * (double)p->D * ((double)p->T * 2 + (double)(p->R + p->N) * 2 * esize_of(p)) / 5.5e6;
   double least = 1e30;
-  for (int64_t sq = 1; sq <= 128 && (sq == 1 || sq * 4 <= steps); sq = next_of(sq)) {
+  for (int64_t sq = 1; sq <= 512 && (sq == 1 || sq * 4 <= steps); sq = next_of(sq)) {
     // (their share of the pieces, some less and some more; with one piece of the rows in 8 bits any number)
     const int64_t share = others * sq / steps, choices[] = {1, 2, 3, share / 2, share, 2 * share};
     int64_t st = 0;
@@ -185,7 +185,7 @@ double quant_wide_shape(const lagkv_quant_params* p, int64_t units, int64_t rows
   const double beside = p->D <= 64 ? (f16 ? 1.95 : 1.75) : p->D <= 128 ? (f16 ? 2.7 : 2.3) : f16 ? 2.1 : 1.75;
   const double ends = p->D <= 64 ? 9.5 : p->D <= 128 ? 12.3 : 21, traffic = p->D <= 128 ? 1.8e-6 : 1e-6;
   double least = 1e30;
-  for (int64_t s = 1; s <= 128 && s <= steps; s = next_of(s)) {
+  for (int64_t s = 1; s <= 512 && s <= steps; s = next_of(s)) {
     const int64_t groups = (units * s + 7) / 8 * tiles;
     const double us = (double)((groups + places - 1) / places) * ((double)((steps + s - 1) / s) * (groups > 32 ? beside : alone) + ends) +
                       (s > 1 ? 2.2 + (double)(units * rows * s) * (double)p->D * traffic : 0);

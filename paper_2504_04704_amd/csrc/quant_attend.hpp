@@ -338,7 +338,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
   }
 
   // the wavefronts' states join, with the scales put in
-  constexpr float LIFT = E::LIFT - kQuantLift;  // what launch_attend_join counts on, over what there is
+  constexpr int LIFT = (int)(E::LIFT - kQuantLift);  // what launch_attend_join counts on, over what there is
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float sum = l[rt];
@@ -351,17 +351,20 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
   }
   __syncthreads();  // (V of all wavefronts is done with as well)
   float* ol = (float*)quant_lds;
-  const float lift = __builtin_ldexpf(1.f, (int)LIFT), unit = __builtin_ldexpf(lift, top_scale - 126);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
     const bool none = sh_ml[wave][rt * 16 + col][1] == 0.f;  // (what is no number has a maximum of -inf too, and is not dropped)
-    const float f = none ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT) * unit;
+    const float f = none ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
 #pragma unroll
-    for (int d = 0; d < DT16; ++d)
-      *(f32x4*)(ol + (wave * ROWS + rt * 16 + col) * LDO + d * 16 + grp * 4) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][d] * f;
+    for (int d = 0; d < DT16; ++d) {
+      f32x4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = none ? 0.f : __builtin_ldexpf(o[rt][d][i] * f, top_scale - 126 + LIFT);
+      *(f32x4*)(ol + (wave * ROWS + rt * 16 + col) * LDO + d * 16 + grp * 4) = y;
+    }
   }
   __syncthreads();
   constexpr int QUADS = DP / 4;
@@ -391,7 +394,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     }
     if (quad == 0) {
       a.part_ml[at * 2] = top;
-      a.part_ml[at * 2 + 1] = sum * lift;
+      a.part_ml[at * 2 + 1] = __builtin_ldexpf(sum, LIFT);
     }
   }
 }

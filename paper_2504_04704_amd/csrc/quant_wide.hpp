@@ -287,13 +287,13 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 
   // The scales put in, the type's factor in place of this kernel's, and channels where attend_wide_body has them.  (A last slice of sixteen that
   // is no whole one has the row's last eight channels, of which there are at most eight of its own, as its second half.)
-  const float unit = __builtin_ldexpf(1.f, top_scale - 126);
+  constexpr int LIFT = (int)(Wide<DT>::LIFT - W::LIFT);
   WideState<DP> x;
 #pragma unroll
   for (int i = 0; i < DP / 8; ++i) {
     const int to = eight(i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x.o[to / 4][to % 4 * 4 + e] = o[i / 4][i % 4 * 4 + e] * unit;
+    for (int e = 0; e < 4; ++e) x.o[to / 4][to % 4 * 4 + e] = __builtin_ldexpf(o[i / 4][i % 4 * 4 + e], top_scale - 126 + LIFT);
   }
 #pragma unroll
   for (int slice = 0; slice < CPR; ++slice)
@@ -301,8 +301,8 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.o[slice / 2][slice % 2 * 8 + e] = x.o[slice / 2][slice % 2 * 8 + 4 + e];
     }
-  x.m = m - W::LIFT + Wide<DT>::LIFT;
-  x.l = l;
+  x.m = m;
+  x.l = __builtin_ldexpf(l, LIFT);
   return x;
 }
 

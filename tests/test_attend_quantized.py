@@ -144,7 +144,7 @@ def test_scales_of_all_sizes(T, N, dtype, code):
     q, x, Kt, Vt, Kn, Vn = problem(dtype, code, 2, 1, 3, N, 64, T, 20, "chain", 16, seed=21)
     g = torch.Generator().manual_seed(4)
     nb = x.V_scale.shape[2]
-    for lo, hi in ((-30, 30), (-30, -28), (-2, 2), (25, 30)):
+    for lo, hi in ((-30, 30), (-30, -28), (-2, 2), (25, 30), (-44, -38), (35.5, 35.5)):
         if dtype == HF and hi > 2:
             continue  # (the outputs would not fit)
         powers = torch.linspace(lo, hi, nb)
