@@ -151,7 +151,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
           }
         });
   };
-  auto weights = [&](int i, f32x16 (&s)[HALVES]) {
+  auto weights = [&](int i, f32x16 (&s)[HALVES], auto part) {
     const f32x4 ks = *(const f32x4*)sh_scale[i & 1][0], vs = *(const f32x4*)sh_scale[i & 1][1];
     float by[SUBS], of[SUBS];
 #pragma unroll
@@ -159,21 +159,16 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
       by[u] = ks[u] * c;
       of[u] = vs[u];
     }
-    if (i >= n_whole) {
+    if constexpr (decltype(part)::value) {
+      // Rows that are not there get -inf, by a product of a column that has it for them with ones.  (-inf times a factor of 0 would be none; what is no
+      // number stays that.)
       const int left = len - (step0 + i) * KT;
-      // Rows that are not there get -inf by a product of a column that has it for them with ones, and the scores of both ways here come
-      // together as whole vectors: one by one they would be copied in every step.
 #pragma unroll
       for (int t = 0; t < HALVES; ++t)
         s[t] = W::mma(u32v4{half == 0 && t * 32 + col >= left ? 0xfc00u : 0u, 0, 0, 0}, u32v4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}, s[t]);
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) {
-        by[u] = by[u] < 1e-30f ? 1e-30f : by[u];  // (times -inf; what is no number stays that)
-        of[u] = u * 16 < left ? of[u] : 0.f;
-      }
+      for (int u = 0; u < SUBS; ++u) by[u] = by[u] < 1e-30f ? 1e-30f : by[u];
     }
-#pragma unroll
-    for (int t = 0; t < HALVES; ++t) asm volatile("" : "+v"(s[t]));
     // scales of V, as parts of the largest's power of two: a weight's is put into its exponent, and taken out of the sums
     uint32_t largest = 0;
 #pragma unroll
@@ -266,22 +261,26 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
       load_k(i + 2);
       load_v(i + 1);
     };
-    // (Two loops: the scores of one have a beginning and an end in every step, and no copies.)
+    // (A wavefront without rows has a loop of its own, and so have the steps whose rows are all there: where the scores of two ways come together they
+    // are copied in every step.  256 channels 164 us without, 145 with; 64 channels 94 and 90.)
     if (idle) {
       for (int i = 0; i <= n; ++i) {
         if (i < n) move(i);
         __syncthreads();
       }
     } else {
-      for (int i = 0; i <= n; ++i) {
+      auto step = [&](int i, auto part) {
         f32x16 s[HALVES];
         multiply(i, s);
         if (i < n) {
-          weights(i, s);
+          weights(i, s, part);
           move(i);
         }
         __syncthreads();
-      }
+      };
+      int i = 0;
+      for (; i < n_whole; ++i) step(i, std::false_type());
+      for (; i <= n; ++i) step(i, std::true_type());
     }
   }
 
