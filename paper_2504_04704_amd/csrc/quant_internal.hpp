@@ -15,6 +15,7 @@ struct CodeArgs {
   int64_t T, start, units;  // units: blocks of K and V, of all streams
   int32_t B, H, D, block, first, count;  // first block, and how many from it on
   int32_t slices;                        // of a row, eight channels each
+  int32_t walk_rows, walk_slices;        // whole rows that the slices of all threads are, and what is left
   Divide by_count, by_h, by_slices;
 };
 hipError_t launch_quantize(const CodeArgs& a, int dtype, int code, hipStream_t s);

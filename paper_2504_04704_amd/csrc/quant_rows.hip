@@ -2,7 +2,9 @@
 //
 // With a = max |x| over a block, code = 127 x / a rounded (int8) or x / 2^e rounded to 4 mantissa bits (e4m3).  The block is
 // read once and waits in registers for its maximum: a wavefront or a workgroup of four takes a block, eight channels of a row a
-// lane at a time.  Bound by memory: three bytes an element of 16 bits.
+// lane at a time.  Bound by memory, at three bytes an element of 16 bits: 32 x 8 streams of 33536 rows with 128 channels, bf16 to int8,
+// blocks of 64, 1057 us (6.2 TB/s; a large copy reaches 5.1); 4 x 8 streams back to bf16 138 us (5.8 TB/s).  The exact quotients of
+// int8 are then 83 % of what the vector units do in that time.
 #include "code_ops.hpp"
 #include "lagkv_internal.hpp"
 #include "quant_internal.hpp"
@@ -37,10 +39,12 @@ template <int DT>
 struct Eight {
   static constexpr int WORDS = DT == LAGKV_F32 ? 8 : 4;
   uint32_t w[WORDS];
+  // (FAR: past the caches, of rows that these do not hold)
+  template <bool FAR>
   __device__ __forceinline__ void load(const char* p) {
 #pragma unroll
     for (int i = 0; i < WORDS; i += 4) {
-      const u32v4 v = *(const u32v4_any*)(p + i * 4);
+      const u32v4 v = FAR ? __builtin_nontemporal_load((const u32v4_any*)(p + i * 4)) : *(const u32v4_any*)(p + i * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[i + e] = v[e];
     }
@@ -151,7 +155,7 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t m) {
 }
 
 // NV slices of eight channels a lane; AGAIN: of a block that has more, and is read a second time (from the L2 as a rule) for its codes.
-template <int DT, int CODE, int WAVES, int NV, bool AGAIN>
+template <int DT, int CODE, int WAVES, int NV, bool AGAIN, bool FAR>
 __global__ __launch_bounds__(256) void quantize_kernel(const CodeArgs a) {
   constexpr int ES = AElem<DT>::SIZE, THREADS = WAVES * 64, PER_GROUP = 4 / WAVES;
   __shared__ uint32_t sh_most[2][4];
@@ -178,7 +182,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const CodeArgs a) {
         int64_t row;
         int ch;
         place(i0 + k * THREADS + t, row, ch);
-        v[k].load(from + row * a.rst + ch * ES);
+        v[k].template load<FAR>(from + row * a.rst + ch * ES);
       }
     };
     uint32_t m = 0;
@@ -206,11 +210,37 @@ __global__ __launch_bounds__(256) void quantize_kernel(const CodeArgs a) {
         int64_t row;
         int ch;
         place(i, row, ch);
-        if (i < n) *(u32v2_any*)(to + row * a.cst + ch) = w;
+        if (i < n) __builtin_nontemporal_store(w, (u32v2_any*)(to + row * a.cst + ch));
       }
     }
   }
 }
+
+// A lane's slices of a block's rows, THREADS apart: where the next one is by additions.  (With a quotient for each, as in quantize_kernel, 141 us
+// in place of 138 on the way back of 4 x 8 streams x 33536 rows; that kernel, whose slices wait in registers, gains nothing: 1161 and 1172.)
+template <int THREADS>
+struct Walk {
+  const CodeArgs& a;
+  int64_t stride, skip;  // of a row, of the rows that THREADS slices are
+  char* p;               // the row's
+  int i, slice;
+  __device__ __forceinline__ Walk(const CodeArgs& a, char* base, int64_t stride, int t)
+      : a(a), stride(stride), skip(stride * a.walk_rows), i(t) {
+    const int row = (int)a.by_slices.of(t);
+    slice = t - row * a.slices;
+    p = base + row * stride;
+  }
+  __device__ __forceinline__ int channel() const { return slice_at(slice, a.D, 8); }
+  __device__ __forceinline__ void next() {
+    i += THREADS;
+    p += skip;
+    slice += a.walk_slices;
+    if (slice >= a.slices) {
+      slice -= a.slices;
+      p += stride;
+    }
+  }
+};
 
 template <int DT, int CODE, int WAVES, int NV>
 __global__ __launch_bounds__(256) void dequantize_kernel(const CodeArgs a) {
@@ -223,19 +253,16 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const CodeArgs a) {
     const int skip = a.start > x.row0 ? (int)(a.start - x.row0) : 0, n = (x.rows - skip) * a.slices;
     if (n <= 0) continue;
     const int64_t row0 = x.row0 + skip;
-    const char* from = (x.values ? a.Vq : a.Kq) + x.b * a.csb + x.h * a.csh + row0 * a.cst;
+    char* from = (char*)(x.values ? a.Vq : a.Kq) + x.b * a.csb + x.h * a.csh + row0 * a.cst;
     char* to = (char*)(x.values ? a.V : a.K) + x.b * a.rsb + x.h * a.rsh + row0 * a.rst;
     const float scale = ((x.values ? a.vs : a.ks) + x.b * a.ssb + x.h * a.ssh)[x.block];
-    for (int i0 = 0; i0 < n; i0 += NV * THREADS) {
+    Walk<THREADS> in(a, from, a.cst, t), at(a, to, a.rst, t);
+    do {
       u32v2 w[NV];
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int i = i0 + k * THREADS + t, at = i < n ? i : 0, r = (int)a.by_slices.of(at);
-        w[k] = *(const u32v2_any*)(from + (int64_t)r * a.cst + slice_at(at - r * a.slices, a.D, 8));
-      }
+      for (int k = 0; k < NV; ++k, in.next()) w[k] = *(const u32v2_any*)(in.i < n ? in.p + in.channel() : from);
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int i = i0 + k * THREADS + t, r = (int)a.by_slices.of(i < n ? i : 0);
+      for (int k = 0; k < NV; ++k, at.next()) {
         float y[8];
         Code<CODE>::to_float(w[k].x, y);
         Code<CODE>::to_float(w[k].y, y + 4);
@@ -249,9 +276,9 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const CodeArgs a) {
             v.w[e / 2] = AElem<DT>::pack(y[e] * scale, y[e + 1] * scale);
           }
         }
-        if (i < n) v.store(to + (int64_t)r * a.rst + slice_at(i - r * a.slices, a.D, 8) * ES);
+        if (at.i < n) v.store(at.p + at.channel() * ES);
       }
-    }
+    } while (at.i - t < n);
   }
 }
 
@@ -263,17 +290,36 @@ dim3 groups_of(const CodeArgs& a) {
   return dim3((uint32_t)(g < kMostGroups ? g : kMostGroups));
 }
 
+// (the steps of a Walk)
+inline CodeArgs walked(CodeArgs a, int threads) {
+  a.walk_rows = threads / a.slices;
+  a.walk_slices = threads % a.slices;
+  return a;
+}
+
+template <int DT, int CODE, bool FAR>
+void launch_quantize_as(const CodeArgs& a, hipStream_t s) {
+  const int n = a.block * a.slices;
+  if (n <= 64 * 8) quantize_kernel<DT, CODE, 1, 8, false, FAR><<<groups_of<4>(a), dim3(256), 0, s>>>(a);
+  else if (n <= 256 * 4) quantize_kernel<DT, CODE, 4, 4, false, FAR><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
+  else if (n <= 256 * 8) quantize_kernel<DT, CODE, 4, 8, false, FAR><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
+  else quantize_kernel<DT, CODE, 4, 4, true, false><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
+}
+// Codes are stored past the caches, and rows beyond what these hold (256 MB) are read past them: 8 x 32 streams x 33536 rows, 128 channels of bf16
+// to int8, 1057 us in place of 1161 (the stores alone: 1131).  32 streams x 8192 rows, 268 MB, 60 in place of 71; rows of 65 MB in
+// fp32, which the caches may still hold, would take 30 us in place of 24, and ones that are read again 117 in place of 107.  Rows on
+// their way back are stored as usual: past the caches the call itself takes 114 us in place of 135 at 512 MB, but with the one that
+// reads them 318 in place of 311.
 template <int DT, int CODE>
 hipError_t launch_quantize_of(const CodeArgs& a, hipStream_t s) {
-  const int n = a.block * a.slices;
-  if (n <= 64 * 8) quantize_kernel<DT, CODE, 1, 8, false><<<groups_of<4>(a), dim3(256), 0, s>>>(a);
-  else if (n <= 256 * 4) quantize_kernel<DT, CODE, 4, 4, false><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
-  else if (n <= 256 * 8) quantize_kernel<DT, CODE, 4, 8, false><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
-  else quantize_kernel<DT, CODE, 4, 4, true><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
+  const bool far = (double)a.units * a.block * a.D * AElem<DT>::SIZE > 268435456.0;
+  if (far) launch_quantize_as<DT, CODE, true>(a, s);
+  else launch_quantize_as<DT, CODE, false>(a, s);
   return hipGetLastError();
 }
 template <int DT, int CODE>
-hipError_t launch_dequantize_of(const CodeArgs& a, hipStream_t s) {
+hipError_t launch_dequantize_of(const CodeArgs& args, hipStream_t s) {
+  const CodeArgs a = walked(args, args.block * args.slices <= 64 * 8 ? 64 : 256);
   if (a.block * a.slices <= 64 * 8) dequantize_kernel<DT, CODE, 1, 4><<<groups_of<4>(a), dim3(256), 0, s>>>(a);
   else dequantize_kernel<DT, CODE, 4, 4><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
   return hipGetLastError();
