@@ -51,9 +51,9 @@ struct Wide<LAGKV_F16> {
 };
 
 // N products, of what the reads of LDS give that are made AHEAD products before.  (Left to itself the compiler reads, waits
-// and multiplies in turn, in one set of registers.)
-template <int N, int AHEAD, typename Read, typename Mul>
-__device__ __forceinline__ void products(Read read, Mul mul) {
+// and multiplies in turn, in one set of registers.)  `with`: what else is done behind each.
+template <int N, int AHEAD, typename Read, typename Mul, typename With>
+__device__ __forceinline__ void products(Read read, Mul mul, With with) {
   u32v4 f[AHEAD];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) f[i] = read(i);
@@ -62,8 +62,13 @@ __device__ __forceinline__ void products(Read read, Mul mul) {
     __builtin_amdgcn_sched_barrier(0);
     mul(i, f[i % AHEAD]);
     if (i + AHEAD < N) f[i % AHEAD] = read(i + AHEAD);
+    with(i);
   }
   __builtin_amdgcn_sched_barrier(0);
+}
+template <int N, int AHEAD, typename Read, typename Mul>
+__device__ __forceinline__ void products(Read read, Mul mul) {
+  products<N, AHEAD>(read, mul, [](int) {});
 }
 
 template <int DP>

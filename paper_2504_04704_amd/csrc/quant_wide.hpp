@@ -6,8 +6,12 @@
 // A lane has one query row and, of 32 cache rows, eight of the first sixteen and eight of the others in its registers, and scales are those of
 // sixteen rows: a logit's goes into the factor that it is multiplied by anyway, and a weight's into what is taken from the logit, as its logarithm.
 //
-// Bound by the matrix cores, the vector instructions and the reads of LDS together: 256 query rows of 32 streams x 33280 rows, 128 channels, bf16
-// 187 us, with the pieces joined, 0.75 Pflop/s.
+// Codes become numbers behind the products, one word at a time, and a wavefront that multiplies goes before the other workgroup's on its SIMD,
+// whose weights then fill the cycles between products: without either 212 us in place of 183, with one of them alone 209 and 205 (256
+// query rows of 32 streams x 33536 rows, 128 channels, bf16, int8).  Given to the wavefront that makes weights, priority gains 2 us.
+//
+// Bound by the vector instructions (some 260 a step and wavefront) and the matrix cores (32 products of 32 cycles) together, and by what two
+// wavefronts on a SIMD cannot overlap of them: 0.77 Pflop/s.
 #pragma once
 #include "attend_wide.hpp"
 #include "quant_attend.hpp"
@@ -100,18 +104,14 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
       *(u32v4*)(to + k * LROWS * ld + CPR * 16) = hi;
     }
   };
-  auto store_k = [&](int i) {
-    store(kr, k_at(i), LDK);
+  auto store_scales = [&](int i) {
     if (tid < 8) sh_scale[i & 1][tid >> 2][tid & 3] = scale_in;
   };
-  auto store_v = [&](int i) {
-    if (i >= n_whole && i < n) {
-      // (a row that is not there: its codes may be no numbers)
+  auto clear_v = [&](int i) {
+    // (a row that is not there: its codes may be no numbers)
 #pragma unroll
-      for (int k = 0; k < PASSES; ++k)
-        if ((step0 + i) * KT + lrow + k * LROWS >= len) vr[k] = u32v4{0, 0, 0, 0};
-    }
-    store(vr, v_at(i), LDV);
+    for (int k = 0; k < PASSES; ++k)
+      if ((step0 + i) * KT + lrow + k * LROWS >= len) vr[k] = u32v4{0, 0, 0, 0};
   };
 
   float c = 0.f;                 // what a query row's products are multiplied by, without the cache rows' scales
@@ -125,9 +125,11 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  // Scores of step i and outputs of step i - 1, in one stream of products.  (Before the first step P and V are 0; behind the
-  // last the scores are not used.)
+  // Scores of step i and outputs of step i - 1, in one stream of products; behind every second one four codes of V of step i, then of K of step
+  // i + 1, become numbers, and go to LDS when they are eight.  (Before the first step P and V are 0; behind the last the scores are not used, nor what
+  // is written.)
   constexpr int NS = KS * HALVES, NO = 2 * HALVES * DT32;
+  static_assert(NS + NO == 2 * (2 * PASSES * 4), "");
   auto multiply = [&](int i, f32x16 (&s)[HALVES]) {
     const char* kl = k_at(i) + col * LDK + half * 16;
     const char* vl = v_at(i - 1) + (half * 4 + (lane & 15) / 4) * LDV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
@@ -135,6 +137,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
     for (int t = 0; t < HALVES; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+    u32v4 eight_now;
     products<NS + NO, 4>(
         [&](int j) {
           if (j < NS) return *(const u32v4*)(kl + j % HALVES * 32 * LDK + j / HALVES * 32);
@@ -148,6 +151,19 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
           else {
 #pragma unroll
             for (int k = 0; k < PP; ++k) o[(j - NS) % DT32] = W::mma(f, p[(j - NS) / DT32][k], o[(j - NS) % DT32]);
+          }
+        },
+        [&](int j) {
+          if (j % 2 != 0) return;
+          const int word = j / 2 % 4, pass_now = j / 8 % PASSES;
+          const bool of_k = j / 8 >= PASSES;
+          uint32_t x, y;
+          Code<CODE>::to_half(of_k ? kr[pass_now][word] : vr[pass_now][word], x, y);
+          eight_now[word % 2 * 2] = x;
+          eight_now[word % 2 * 2 + 1] = y;
+          if (word % 2 == 1) {
+            char* to = (of_k ? k_at(i + 1) : v_at(i)) + (lrow + pass_now * LROWS) * (of_k ? LDK : LDV) + lslice * 16;
+            *(u32v4*)(to + word / 2 * CPR * 16) = eight_now;
           }
         });
   };
@@ -251,13 +267,13 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
         q[k] = v;
       }
     }
-    store_k(0);
+    store(kr, k_at(0), LDK);
+    store_scales(0);
     load_k(1);
     __syncthreads();
     // (one barrier a step: what is written in one are the buffers that nobody reads in it)
-    auto move = [&](int i) {
-      store_k(i + 1);  // (behind the last step: what was there)
-      store_v(i);
+    auto load_next = [&](int i) {
+      store_scales(i + 1);  // (behind the last step: what was there)
       load_k(i + 2);
       load_v(i + 1);
     };
@@ -265,16 +281,24 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
     // are copied in every step.  256 channels 164 us without, 145 with; 64 channels 94 and 90.)
     if (idle) {
       for (int i = 0; i <= n; ++i) {
-        if (i < n) move(i);
+        if (i < n) {
+          if (i >= n_whole) clear_v(i);
+          store(vr, v_at(i), LDV);
+          store(kr, k_at(i + 1), LDK);
+          load_next(i);
+        }
         __syncthreads();
       }
     } else {
       auto step = [&](int i, auto part) {
         f32x16 s[HALVES];
+        if (decltype(part)::value && i < n) clear_v(i);
+        __builtin_amdgcn_s_setprio(1);
         multiply(i, s);
+        __builtin_amdgcn_s_setprio(0);
         if (i < n) {
+          load_next(i);
           weights(i, s, part);
-          move(i);
         }
         __syncthreads();
       };
