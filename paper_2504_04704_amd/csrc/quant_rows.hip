@@ -3,8 +3,8 @@
 // With a = max |x| over a block, code = 127 x / a rounded (int8) or x / 2^e rounded to 4 mantissa bits (e4m3).  The block is
 // read once and waits in registers for its maximum: a wavefront or a workgroup of four takes a block, eight channels of a row a
 // lane at a time.  Bound by memory, at three bytes an element of 16 bits: 32 x 8 streams of 33536 rows with 128 channels, bf16 to int8,
-// blocks of 64, 1057 us (6.2 TB/s; a large copy reaches 5.1); 4 x 8 streams back to bf16 138 us (5.8 TB/s).  The exact quotients of
-// int8 are then 83 % of what the vector units do in that time.
+// blocks of 64, 1057 us (6.2 TB/s; a large copy reaches 5.1); 4 x 8 streams back to bf16 138 us (5.8 TB/s).  The vector
+// units are then busy too, with the exact quotients of int8, but e4m3, which has half as many instructions, takes no less.
 #include "code_ops.hpp"
 #include "lagkv_internal.hpp"
 #include "quant_internal.hpp"
