@@ -22,6 +22,11 @@ namespace lagkv {
 
 constexpr float kQuantLift = 14.f;  // weights are held times 2^14, as in AElem<LAGKV_F16>
 
+// A part of the largest scale of V below which a step's weights are held relative to their own largest.  From it on a weight of 1 keeps all bits
+// of what goes into the product: one number of binary16 down to 2^-28 of the largest, two down to 2^-17.
+template <int DT>
+constexpr float kFarScale = kWeightParts<DT> == 1 ? 0x1p-12f : 0x1p-6f;
+
 template <int DP, int RT>
 struct QuantShape {
   static constexpr int SUBS = DP * RT > 128 ? 2 : 4, KT = 16 * SUBS;  // sixteens of a step
@@ -189,6 +194,20 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     for (int s = 0; s < SUBS; ++s) vs[s] = vsb[min(first + s * 16, len - 1) >> a.block_shift];
   };
 
+  // sixteen channels of 32 rows, as the product with weights takes them
+  auto values_at = [&](int d, int t) {
+    u32v4 v;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4)(vl + ((t * 2 + s) * 16 + grp * 4 + (col >> 2)) * LDV + (d * 16 + (col & 3) * 4) * 2));
+      const u32v2 y = __builtin_bit_cast(u32v2, x);
+      v[s * 2] = y.x;
+      v[s * 2 + 1] = y.y;
+    }
+    return v;
+  };
+
   int step = step0 + wave;
   if (step < step1) {
     load_k(step);
@@ -256,6 +275,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     __builtin_amdgcn_sched_barrier(0);
 
     // scales of V, as parts of the largest's power of two
+    bool apart = false;
     {
       uint32_t most = 0;
 #pragma unroll
@@ -270,7 +290,10 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
         top_scale = now;
       }
 #pragma unroll
-      for (int s = 0; s < SUBS; ++s) r[s] = __builtin_ldexpf(r[s], 126 - top_scale);
+      for (int s = 0; s < SUBS; ++s) {
+        r[s] = __builtin_ldexpf(r[s], 126 - top_scale);
+        apart = apart || (r[s] < kFarScale<DT> && r[s] > 0.f);
+      }
     }
     constexpr int PP = kWeightParts<DT>;
     u32v4 weight[RT][SUBS / 2][PP];
@@ -310,6 +333,42 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
         for (int d = 0; d < DT16; ++d) o[rt][d] *= keep;
       }
+      if (apart) {
+        // Rows of a scale far below the largest may be those that a query row sees, and the largest's those that it does not: such a
+        // step's weights are held relative to their own largest, its products added by themselves, and nothing is left for those below.
+        for (int t = 0; t < SUBS / 2; ++t) {
+          float e[8], most = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            e[i] = p[rt][i / 4][i % 4];
+#pragma unroll
+            for (int x = 1; x < SUBS / 2; ++x)
+              if (t == x) e[i] = p[rt][2 * x + i / 4][i % 4];
+            most = fmaxf(most, e[i]);
+          }
+          most = max_across_32(max_across_16(most));
+          const int up = 127 + 14 - (int)max(__float_as_uint(most) >> 23, 1u);
+          u32v4 own[PP];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t part[PP];
+            weights_of(__builtin_ldexpf(e[2 * i], up), __builtin_ldexpf(e[2 * i + 1], up), part);
+#pragma unroll
+            for (int k = 0; k < PP; ++k) own[k][i] = part[k];
+          }
+#pragma unroll
+          for (int d = 0; d < DT16; ++d) {
+            const u32v4 v = values_at(d, t);
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < PP; ++k) y = F::mma(v, own[k], y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[rt][d][i] += __builtin_ldexpf(y[i], -up);
+          }
+        }
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) p[rt][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
 #pragma unroll
       for (int s = 0; s < SUBS; ++s)
 #pragma unroll
@@ -324,15 +383,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     for (int d = 0; d < DT16; ++d)
 #pragma unroll
       for (int t = 0; t < SUBS / 2; ++t) {
-        u32v4 v;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_s16x4)(vl + ((t * 2 + s) * 16 + grp * 4 + (col >> 2)) * LDV + (d * 16 + (col & 3) * 4) * 2));
-          const u32v2 y = __builtin_bit_cast(u32v2, x);
-          v[s * 2] = y.x;
-          v[s * 2 + 1] = y.y;
-        }
+        const u32v4 v = values_at(d, t);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll

@@ -185,20 +185,29 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
       for (int u = 0; u < SUBS; ++u) by[u] = by[u] < 1e-30f ? 1e-30f : by[u];
     }
-    // scales of V, as parts of the largest's power of two: a weight's is put into its exponent, and taken out of the sums
+    // scales of V, as parts of the largest's power of two (from 2^-80 of it on: sums stay in fp32's range): a weight's is put into its exponent,
+    // and taken out of the sums
     uint32_t largest = 0;
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) largest = max(largest, __float_as_uint(of[u]) & 0x7fffffffu);
     const int now_scale = __builtin_amdgcn_readfirstlane((int)(largest >> 23));
     if (now_scale > top_scale) {
-      // (one that is no number: neither are the outputs, and the sums do not change)
-      const float f = now_scale == 255 ? __uint_as_float(0x7fc00000u) : __builtin_ldexpf(1.f, top_scale - now_scale);
+      // m, which is of logits with their scale's logarithm, goes down; or the outputs, if the sums would leave the range.  (A scale that is no number:
+      // neither are the outputs, and the sums do not change.)
+      const int up = now_scale - top_scale;
+      const float more = __builtin_ldexpf(l, up);
+      if (now_scale == 255 || __any(more > 0x1p100f)) {
+        const float f = now_scale == 255 ? __uint_as_float(0x7fc00000u) : __builtin_ldexpf(1.f, -up);
 #pragma unroll
-      for (int d = 0; d < DT32; ++d) o[d] *= f;
+        for (int d = 0; d < DT32; ++d) o[d] *= f;
+      } else {
+        m -= (float)up;
+        l = more;
+      }
       top_scale = now_scale;
     }
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u) of[u] = __builtin_amdgcn_logf(fmaxf(__builtin_ldexpf(of[u], 126 - top_scale), 0x1p-60f));
+    for (int u = 0; u < SUBS; ++u) of[u] = __builtin_amdgcn_logf(fmaxf(__builtin_ldexpf(of[u], 126 - top_scale), 0x1p-80f));
 
     float top = -INFINITY;
 #pragma unroll
@@ -206,7 +215,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
       float x = s[u / 2][u % 2 * 8];
 #pragma unroll
       for (int e = 1; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e]);
-      top = fmaxf(top, x * by[u]);
+      top = fmaxf(top, __builtin_fmaf(x, by[u], of[u]));
     }
     top = max_across_32(top);
     if (__any(top > m + W::SLACK)) {
