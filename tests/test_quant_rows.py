@@ -194,3 +194,26 @@ def test_no_rows():
     x = lagkv.quantize(*(torch.empty(1, 2, 0, 64, dtype=BF, device=DEV) for _ in range(2)), 16)
     assert x.K.shape == (1, 2, 0, 64) and x.K_scale.shape == (1, 2, 0)
     assert lagkv.dequantize(x)[0].shape == (1, 2, 0, 64)
+
+
+@pytest.mark.parametrize("code", [I8, E4], ids=["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,D,block", [(BF, 128, 64), (HF, 100, 32), (FL, 96, 128), (BF, 256, 256), (FL, 17, 16)], ids=lambda v: str(v).split(".")[-1])
+def test_more_rows_than_the_caches_hold(dtype, D, block, code):
+    """Copies of a cache (a batch stride of 0), together more than 256 MB: the codes of each are those of one, and rows behind a length are left."""
+    T, B = 5000 + block // 2, 1 + 280_000_000 // (2 * 5000 * D * (4 if dtype == FL else 2))
+    g = torch.Generator().manual_seed(D)
+    K, V = (torch.randn((1, 1, T, D), generator=g).to(dtype).to(DEV) for _ in range(2))
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    lengths[1::2] = 777
+    out = lagkv.Quantized.empty(B, 1, T, D, block, code)
+    for t in (out.K, out.V):
+        t.view(torch.int8).fill_(85)
+    got = lagkv.quantize(K.expand(B, 1, T, D), V.expand(B, 1, T, D), block, code, lengths, out=out)
+    for b in range(2):
+        n = int(lengths[b])
+        one = lagkv.quantize(K[:, :, :n], V[:, :, :n], block, code)
+        for big, small in ((got.K, one.K), (got.V, one.V)):
+            big, small = big.view(torch.int8)[b::2], small.view(torch.int8)
+            assert bool((big[:, :, :n] == small).all()) and bool((big[:, :, n:] == 85).all())
+        for big, small in ((got.K_scale, one.K_scale), (got.V_scale, one.V_scale)):
+            assert bool((big[b::2, :, :-(-n // block)] == small).all())
