@@ -471,7 +471,7 @@ int lagkv_attend_quantized_plan(const lagkv_quant_params* p, lagkv_attend_plan_t
  * Codes go into the products as they are, which binary16 holds, and scales into logits and weights in fp32.  A query row goes in
  * as binary16 times a power of two: in bf16 and fp16 as it is (bf16: what is below 2^-14 of the row's largest off by up to 2^-25 of
  * it), in fp32 as two such numbers (off by up to 2^-23 of the largest).  Weights, times their rows' scales, go in as
- * one number of binary16 in bf16 (11 bits: an eighth of what the output's own rounding leaves), else as two (22 bits).
+ * two numbers of binary16 (22 bits).
  * They are relative to what a query row's largest weight times its scale is, also where others' scales are far larger; with more than 32
  * query rows, scales of V below 2^-80 of the largest count as 2^-80 of it.
  * The rest as of lagkv_attend: logits, sums and products in fp32, no atomics, its limits on sizes; LAGKV_ESHAPE from 2^26 query

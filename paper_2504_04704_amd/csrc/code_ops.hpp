@@ -50,22 +50,13 @@ __device__ __forceinline__ float less_second(float x, uint32_t h) {
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(h), "v"(x));
   return y;
 }
-// Numbers of binary16 that a weight goes into the product with V as.  Of outputs in bf16 one: its rounding, 2^-11 of a weight, is an eighth of
-// theirs, and a third of the products is saved (with two, 64 drafted tokens of four streams x 33280 rows took 243 us in place of 189).  Of the others two,
-// whose rounding is 2^-22: one would add as much to outputs in fp16 as their own.
-template <int DT>
-constexpr int kWeightParts = DT == LAGKV_BF16 ? 1 : 2;
-// Two weights as pairs of numbers of binary16: their leading bits, and the rest rounded (half of what AElem<LAGKV_F16>::split takes: codes are
-// never infinite, and the rest may be 0).
-__device__ __forceinline__ void split_weights(float x, float y, uint32_t& hi, uint32_t& lo) {
-  hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
-  lo = AElem<LAGKV_F16>::pack(less_first(x, hi), less_second(y, hi));
-}
-// The same, or as one number each (rounded).
-template <int PARTS>
-__device__ __forceinline__ void weights_of(float x, float y, uint32_t (&part)[PARTS]) {
-  if constexpr (PARTS == 1) part[0] = AElem<LAGKV_F16>::pack(x, y);
-  else split_weights(x, y, part[0], part[1]);
+// A weight goes into the product with V as two numbers of binary16, its leading bits and the rest rounded, 22 bits in all, whatever the type of the outputs.  (As
+// one number, 2^-12 of the sum of the weighted values' sizes may be lost: where these cancel that is more than the rounding of an output in bf16, and
+// more than attend of the same rows loses.)  Half of what AElem<LAGKV_F16>::split takes: codes are never infinite, and the rest may be 0.
+constexpr int kWeightParts = 2;
+__device__ __forceinline__ void split_weights(float x, float y, uint32_t (&part)[kWeightParts]) {
+  part[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+  part[1] = AElem<LAGKV_F16>::pack(less_first(x, part[0]), less_second(y, part[0]));
 }
 
 }  // namespace lagkv

@@ -174,15 +174,13 @@ double quant_narrow_shape(const lagkv_quant_params* p, const QuantForm& f, int64
 }
 
 // The kernel of many rows: tiles of 128, and the pieces of all rows.
-// Of both: over 8502 shapes (1 to 4000 query rows of 1 to 256 streams, 64 to 256 channels, 64 to 65536 rows in 8 bits and up to 2048 behind them, some
-// with lengths that differ) the choice takes 2.3 % longer in the mean than the best form and pieces of up to 60 that were measured: half of them at most
-// 0.1 %, nine in ten 10 %.
+// Of both: over 3268 shapes (17 to 4000 query rows of 1 to 256 streams, 64 to 256 channels, 64 to 65536 rows in 8 bits and up to 2048 behind them, some
+// with lengths that differ; bf16 and fp16) the choice takes 2.1 % longer in the mean than the best form and pieces of up to 128 that were measured: half of them
+// at most 0.1 %, nine in ten 8 %.
 double quant_wide_shape(const lagkv_quant_params* p, int64_t units, int64_t rows, int* pieces) {
   const int64_t kt = p->D > 128 ? 32 : 64, steps = (p->T + kt - 1) / kt + (p->R + kt - 1) / kt + (p->N + kt - 1) / kt;
   const int64_t tiles = (rows + 127) / 128, places = p->D > 128 ? 32 : 64;
-  const bool f16 = p->dtype == LAGKV_F16;  // (half as many products again)
-  const double alone = p->D <= 64 ? (f16 ? 1.35 : 1.1) : p->D <= 128 ? (f16 ? 1.85 : 1.4) : f16 ? 1.6 : 1.4;
-  const double beside = p->D <= 64 ? (f16 ? 1.6 : 1.45) : p->D <= 128 ? (f16 ? 2.3 : 1.85) : f16 ? 1.6 : 1.3;
+  const double alone = p->D <= 64 ? 1.35 : 1.6, beside = p->D <= 64 ? 1.6 : p->D <= 128 ? 2.15 : 1.6;
   const double ends = p->D <= 64 ? 9 : p->D <= 128 ? 12.5 : 24, traffic = p->D <= 128 ? 2.2e-6 : 1.2e-6;
   double least = 1e30;
   for (int64_t s = 1; s <= 512 && s <= steps; s = next_of(s)) {

@@ -6,7 +6,7 @@
 //
 // A wavefront takes every fourth step of 64 cache rows (32 where 64 do not fit the registers) for all query rows of its workgroup; K's codes become
 // numbers in the registers that they are loaded into, V's on their way into LDS.  Scales are those of sixteen rows that
-// lie in one block.  Weights times scales go in as one or two numbers of binary16 (kWeightParts), relative to the largest scale's power of two that
+// lie in one block.  Weights times scales go in as two numbers of binary16 (split_weights), relative to the largest scale's power of two that
 // the wavefront has met, as exponentials are relative to the largest logit: scales of 1e-30 are as good as those of 1.
 //
 // Each piece of a cache leaves its maximum, sum and outputs; launch_attend_join joins them with those of the tail and the new tokens, which
@@ -23,9 +23,8 @@ namespace lagkv {
 constexpr float kQuantLift = 14.f;  // weights are held times 2^14, as in AElem<LAGKV_F16>
 
 // A part of the largest scale of V below which a step's weights are held relative to their own largest.  From it on a weight of 1 keeps all bits
-// of what goes into the product: one number of binary16 down to 2^-28 of the largest, two down to 2^-17.
-template <int DT>
-constexpr float kFarScale = kWeightParts<DT> == 1 ? 0x1p-12f : 0x1p-6f;
+// of what goes into the product, down to 2^-17 of the largest.
+constexpr float kFarScale = 0x1p-6f;
 
 template <int DP, int RT>
 struct QuantShape {
@@ -292,10 +291,10 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
       for (int s = 0; s < SUBS; ++s) {
         r[s] = __builtin_ldexpf(r[s], 126 - top_scale);
-        apart = apart || (r[s] < kFarScale<DT> && r[s] > 0.f);
+        apart = apart || (r[s] < kFarScale && r[s] > 0.f);
       }
     }
-    constexpr int PP = kWeightParts<DT>;
+    constexpr int PP = kWeightParts;
     u32v4 weight[RT][SUBS / 2][PP];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -352,7 +351,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t part[PP];
-            weights_of(__builtin_ldexpf(e[2 * i], up), __builtin_ldexpf(e[2 * i + 1], up), part);
+            split_weights(__builtin_ldexpf(e[2 * i], up), __builtin_ldexpf(e[2 * i + 1], up), part);
 #pragma unroll
             for (int k = 0; k < PP; ++k) own[k][i] = part[k];
           }
@@ -374,7 +373,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           uint32_t part[PP];
-          weights_of(p[rt][s][2 * i], p[rt][s][2 * i + 1], part);
+          split_weights(p[rt][s][2 * i], p[rt][s][2 * i + 1], part);
 #pragma unroll
           for (int k = 0; k < PP; ++k) weight[rt][s / 2][k][s % 2 * 2 + i] = part[k];
         }

@@ -118,7 +118,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
   float m = -INFINITY, l = 0.f;  // m in units of base 2
   int top_scale = 0;             // exponent (biased) of the largest scale of V so far: o is relative to it
   f32x16 o[DT32];
-  constexpr int PP = kWeightParts<DT>;
+  constexpr int PP = kWeightParts;
   u32v4 q[KS], p[2 * HALVES][PP];  // P, in steps of 16 rows
 #pragma unroll
   for (int d = 0; d < DT32; ++d)
@@ -238,7 +238,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
         sum0 += y;
         sum1 += z;
         uint32_t part[PP];
-        weights_of(y, z, part);
+        split_weights(y, z, part);
 #pragma unroll
         for (int k = 0; k < PP; ++k) p[u][k][e / 2] = part[k];
       }
