@@ -6,8 +6,9 @@
 //
 // A wavefront takes every fourth step of 64 cache rows (32 where 64 do not fit the registers) for all query rows of its workgroup; K's codes become
 // numbers in the registers that they are loaded into, V's on their way into LDS.  Scales are those of sixteen rows that
-// lie in one block.  Weights times scales go in as two numbers of binary16 (split_weights), relative to the largest scale's power of two that
-// the wavefront has met, as exponentials are relative to the largest logit: scales of 1e-30 are as good as those of 1.
+// lie in one block.  Weights times scales go in as two numbers of binary16 (split_weights).  They are exponentials of logits with their scale's
+// logarithm, relative to the largest of these (m), so that it does not matter how far apart scales are, nor which of them comes first; the weights' sum,
+// without the scales, is relative to a reference of its own (R, WeightSum).
 //
 // Each piece of a cache leaves its maximum, sum and outputs; launch_attend_join joins them with those of the tail and the new tokens, which
 // other workgroups of the same launch have gone over.
@@ -22,9 +23,39 @@ namespace lagkv {
 
 constexpr float kQuantLift = 14.f;  // weights are held times 2^14, as in AElem<LAGKV_F16>
 
-// A part of the largest scale of V below which a step's weights are held relative to their own largest.  From it on a weight of 1 keeps all bits
-// of what goes into the product, down to 2^-17 of the largest.
-constexpr float kFarScale = 0x1p-6f;
+// Logarithms of scales of V are those of base 2 less `base`, an exponent near the largest of those met so far: they are small numbers then, and so are their roundings.
+// (-inf of 0, of what is below 2^-126 of 2^base, and of what is no number, with which the outputs are none anyway.)
+constexpr int kNoBase = -1000;  // (any scale is inf beside it)
+constexpr float kNearBase = 16.f;
+__device__ __forceinline__ float log_scale(float s, int base) { return fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(s, -base)), -INFINITY); }
+
+// The sum of a query row's weights, relative to exp(R), R a logit near the largest.  The weights that go into the products have their scales in them: sum(exp(x + s - m)) over
+// sixteen rows of a scale exp(s) is brought back by exp(m - R - s).  That is done up to 2^kFar; beyond, those products may have left the range of fp32 while their weights
+// are a large part of the sum, and these are worked out by themselves.  (m is that of a row whose logit R is not below and whose s is kNearBase + 1 at most: from
+// s = -kFarBelow on the factor is no larger.)
+constexpr float kFar = 64.f, kFarBelow = kFar - kNearBase - 1.f;
+struct WeightSum {
+  float R, l, from_m;  // (the last: m - R in base 2, or something below all numbers that matter where there are no rows of m, or none at all)
+  __device__ __forceinline__ void raise(float to, float unit) {
+    if (to > R) {
+      l *= __builtin_amdgcn_exp2f((R - to) * unit);
+      R = to;
+    }
+  }
+  __device__ __forceinline__ void with(float m, float unit) { from_m = fmaxf((m - R) * unit, -1e30f); }
+};
+
+// 2^(x + more) as a factor of what may be as far from 1 as it is.
+struct Power {
+  float f;
+  int e;
+  __device__ __forceinline__ Power(float x, int more) {
+    const float whole = fmaxf(floorf(x), -2000.f);
+    f = __builtin_amdgcn_exp2f(x - whole);
+    e = (int)whole + more;
+  }
+  __device__ __forceinline__ float times(float y) const { return __builtin_ldexpf(y * f, e); }
+};
 
 template <int DP, int RT>
 struct QuantShape {
@@ -218,13 +249,14 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     const int r = row0 + rt * 16 + col, rr = r < row1 ? r : row0, n = (int)a.by_g.of(rr);
     q[rt].load(a.Q + b * a.qsb + (h * a.G + rr - n * a.G) * a.qsh + (int64_t)n * a.qsn, grp, a.D, r < row1);
   }
-  float m[RT], l[RT];
+  float m[RT];        // of logits with their scale's logarithm: what o is relative to
+  WeightSum sum[RT];  // (of this lane's cache rows)
   f32x4 o[RT][DT16];
-  int top_scale = 0;  // exponent (biased) of the largest scale of V so far: o is relative to it
+  int base = kNoBase;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     m[rt] = -INFINITY;
-    l[rt] = 0.f;
+    sum[rt] = WeightSum{-INFINITY, 0.f, -1e30f};
 #pragma unroll
     for (int d = 0; d < DT16; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -244,9 +276,9 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
       *(u32v4*)(at + 16) = hi;
     }
     wave_order();
-    float r[SUBS];
+    float scale[SUBS], of[SUBS];  // of V, and their logarithms
 #pragma unroll
-    for (int s = 0; s < SUBS; ++s) r[s] = whole || first + s * 16 < len ? vs[s] : 0.f;
+    for (int s = 0; s < SUBS; ++s) scale[s] = whole || first + s * 16 < len ? vs[s] : 0.f;
     if (more) load_v(step + WAVES);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -273,27 +305,32 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     if (more) load_k(step + WAVES);
     __builtin_amdgcn_sched_barrier(0);
 
-    // scales of V, as parts of the largest's power of two
-    bool apart = false;
-    {
-      uint32_t most = 0;
-#pragma unroll
-      for (int s = 0; s < SUBS; ++s) most = max(most, __float_as_uint(r[s]) & 0x7fffffffu);
-      const int now = (int)(most >> 23);
-      if (now > top_scale) {
-        const float f = __builtin_ldexpf(1.f, top_scale - now);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int d = 0; d < DT16; ++d) o[rt][d] *= f;
-        top_scale = now;
-      }
+    constexpr float LOG2 = E::UNIT == 1.f ? 1.f : 0.693147180559945f;  // 1 in base 2, in units of the logits
+    float most_of, least_of;
+    auto logs = [&] {
 #pragma unroll
       for (int s = 0; s < SUBS; ++s) {
-        r[s] = __builtin_ldexpf(r[s], 126 - top_scale);
-        apart = apart || (r[s] < kFarScale && r[s] > 0.f);
+        // (rows that are not there have logits of -inf, whatever their scale)
+        of[s] = whole || first + s * 16 < len ? log_scale(scale[s], base) : 0.f;
+        most_of = s == 0 ? of[0] : fmaxf(most_of, of[s]);
+        least_of = s == 0 ? of[0] : fminf(least_of, of[s]);
       }
+    };
+    logs();
+    if (__any(most_of > kNearBase)) {
+      float most = 0.f;
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s) most = fmaxf(most, scale[s]);
+      const int now = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        m[rt] -= (float)(now - base) * LOG2;
+        sum[rt].with(m[rt], E::UNIT);
+      }
+      base = now;
+      logs();
     }
+    const bool far_scales = __any(least_of < -kFarBelow);
     constexpr int PP = kWeightParts;
     u32v4 weight[RT][SUBS / 2][PP];
 #pragma unroll
@@ -307,66 +344,77 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
           for (int i = 0; i < 4; ++i)
             if (first + s * 16 + grp * 4 + i >= len) p[rt][s][i] = -INFINITY;
       }
-      float top = p[rt][0][0];
+      float top = -INFINITY;
 #pragma unroll
-      for (int s = 0; s < SUBS; ++s)
+      for (int s = 0; s < SUBS; ++s) {
+        float x = p[rt][s][0];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, p[rt][s][i]);
+        for (int i = 1; i < 4; ++i) x = fmaxf(x, p[rt][s][i]);
+        top = fmaxf(top, __builtin_fmaf(of[s], LOG2, x));
+      }
       top = max_across_32(max_across_16(top));
-      const float before = m[rt];
-      m[rt] = fmaxf(before, top);
-      const float at = m[rt] == -INFINITY ? 0.f : m[rt];
-      const float keep = __builtin_amdgcn_exp2f((before - at) * E::UNIT);
-      float sum = 0.f;
+      if (__any(top > m[rt])) {
+        float x = -INFINITY;
 #pragma unroll
-      for (int s = 0; s < SUBS; ++s)
+        for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x = fmaxf(x, p[rt][s][i]);
+        x = max_across_32(max_across_16(x));
+        if (top > m[rt]) {
+          const float keep = __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
+#pragma unroll
+          for (int d = 0; d < DT16; ++d) o[rt][d] *= keep;
+          m[rt] = top;
+          sum[rt].raise(x, E::UNIT);
+          sum[rt].with(m[rt], E::UNIT);
+        }
+      }
+      const float at = m[rt] == -INFINITY ? 0.f : m[rt];
+      uint32_t apart = 0;  // sixteens whose weights are summed by themselves
+      if (__builtin_expect(far_scales, 0)) {
+        float x = -INFINITY, none = 0.f;
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+          none += scale[s];
+          if (sum[rt].from_m - of[s] > kFar) {
+            apart |= 1u << s;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x = fmaxf(x, p[rt][s][i]);
+          }
+        }
+        sum[rt].raise(max_across_32(max_across_16(x)), E::UNIT);
+        sum[rt].with(m[rt], E::UNIT);
+        const float R = sum[rt].R == -INFINITY ? 0.f : sum[rt].R;
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s)
+          if (apart >> s & 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[rt].l += __builtin_amdgcn_exp2f(__builtin_fmaf(p[rt][s][i] - R, E::UNIT, kQuantLift));
+          }
+        // (a scale that is no number: neither are the outputs)
+        if (none != none) {
+#pragma unroll
+          for (int d = 0; d < DT16; ++d) o[rt][d] *= none;
+        }
+      }
+      float y[SUBS];
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s) {
+        y[s] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // (the difference first: its rounding is that of a number near zero)
-          const float e = __builtin_amdgcn_exp2f((p[rt][s][i] - at) * E::UNIT + kQuantLift);
-          p[rt][s][i] = e * r[s];
-          sum += e;
+          p[rt][s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[rt][s][i] - at, E::UNIT, of[s] + kQuantLift));
+          y[s] += p[rt][s][i];
         }
-      l[rt] = l[rt] * keep + sum;
-      if (__any(keep != 1.f)) {
-#pragma unroll
-        for (int d = 0; d < DT16; ++d) o[rt][d] *= keep;
       }
-      if (apart) {
-        // Rows of a scale far below the largest may be those that a query row sees, and the largest's those that it does not: such a
-        // step's weights are held relative to their own largest, its products added by themselves, and nothing is left for those below.
-        for (int t = 0; t < SUBS / 2; ++t) {
-          float e[8], most = 0.f;
+      if (__builtin_expect(far_scales, 0)) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            e[i] = p[rt][i / 4][i % 4];
+        for (int s = 0; s < SUBS; ++s)
+          if (!(apart >> s & 1)) sum[rt].l = __builtin_fmaf(y[s], __builtin_amdgcn_exp2f(sum[rt].from_m - of[s]), sum[rt].l);
+      } else {
 #pragma unroll
-            for (int x = 1; x < SUBS / 2; ++x)
-              if (t == x) e[i] = p[rt][2 * x + i / 4][i % 4];
-            most = fmaxf(most, e[i]);
-          }
-          most = max_across_32(max_across_16(most));
-          const int up = 127 + 14 - (int)max(__float_as_uint(most) >> 23, 1u);
-          u32v4 own[PP];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t part[PP];
-            split_weights(__builtin_ldexpf(e[2 * i], up), __builtin_ldexpf(e[2 * i + 1], up), part);
-#pragma unroll
-            for (int k = 0; k < PP; ++k) own[k][i] = part[k];
-          }
-#pragma unroll
-          for (int d = 0; d < DT16; ++d) {
-            const u32v4 v = values_at(d, t);
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < PP; ++k) y = F::mma(v, own[k], y);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[rt][d][i] += __builtin_ldexpf(y[i], -up);
-          }
-        }
-#pragma unroll
-        for (int s = 0; s < SUBS; ++s) p[rt][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < SUBS; ++s) sum[rt].l = __builtin_fmaf(y[s], __builtin_amdgcn_exp2f(sum[rt].from_m - of[s]), sum[rt].l);
       }
 #pragma unroll
       for (int s = 0; s < SUBS; ++s)
@@ -390,16 +438,16 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
       }
   }
 
-  // the wavefronts' states join, with the scales put in
+  // the wavefronts' states join, relative to the sums' reference
   constexpr int LIFT = (int)(E::LIFT - kQuantLift);  // what launch_attend_join counts on, over what there is
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float sum = l[rt];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
+    float l = sum[rt].l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
     if (grp == 0) {
-      sh_ml[wave][rt * 16 + col][0] = m[rt];
-      sh_ml[wave][rt * 16 + col][1] = sum;
+      sh_ml[wave][rt * 16 + col][0] = sum[rt].R;
+      sh_ml[wave][rt * 16 + col][1] = l;
     }
   }
   __syncthreads();  // (V of all wavefronts is done with as well)
@@ -409,13 +457,13 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
-    const bool none = sh_ml[wave][rt * 16 + col][1] == 0.f;  // (what is no number has a maximum of -inf too, and is not dropped)
-    const float f = none ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
+    const bool none = sh_ml[wave][rt * 16 + col][1] == 0.f;  // (what is no number has a reference of -inf too, and is not dropped)
+    const Power of(fmaxf((m[rt] - top) * E::UNIT, -1e30f), base + LIFT);
 #pragma unroll
     for (int d = 0; d < DT16; ++d) {
       f32x4 y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = none ? 0.f : __builtin_ldexpf(o[rt][d][i] * f, top_scale - 126 + LIFT);
+      for (int i = 0; i < 4; ++i) y[i] = none ? 0.f : of.times(o[rt][d][i]);
       *(f32x4*)(ol + (wave * ROWS + rt * 16 + col) * LDO + d * 16 + grp * 4) = y;
     }
   }
