@@ -472,8 +472,8 @@ int lagkv_attend_quantized_plan(const lagkv_quant_params* p, lagkv_attend_plan_t
  * as binary16 times a power of two: in bf16 and fp16 as it is (bf16: what is below 2^-14 of the row's largest off by up to 2^-25 of
  * it), in fp32 as two such numbers (off by up to 2^-23 of the largest).  Weights, times their rows' scales, go in as
  * two numbers of binary16 (22 bits).
- * They are relative to a query row's largest product of a weight and its scale, in whatever order scales come.  With up to 32 query rows, scales of V count as 0 below
- * 2^-125 of the largest before them; with more, they count as 2^-80 of it below that, and where scales rise by 2^84 and more weights lose bits against it.
+ * They are relative to a query row's largest product of a weight and its scale, in whatever order and however far apart scales come; a scale of V
+ * counts as 0 below 2^-125 of the largest before it.
  * The rest as of lagkv_attend: logits, sums and products in fp32, no atomics, its limits on sizes; LAGKV_ESHAPE from 2^26 query
  * rows on too (all of them are joined from pieces).
  */

@@ -114,9 +114,10 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
       if ((step0 + i) * KT + lrow + k * LROWS >= len) vr[k] = u32v4{0, 0, 0, 0};
   };
 
-  float c = 0.f;                 // what a query row's products are multiplied by, without the cache rows' scales
-  float m = -INFINITY, l = 0.f;  // m in units of base 2
-  int top_scale = 0;             // exponent (biased) of the largest scale of V so far: o is relative to it
+  float c = 0.f;                   // what a query row's products are multiplied by, without the cache rows' scales
+  float m = -INFINITY;             // of logits in base 2 with their scale's logarithm: what o is relative to
+  WeightSum sum = {-INFINITY, 0.f, -1e30f};
+  int base = kNoBase;
   f32x16 o[DT32];
   constexpr int PP = kWeightParts;
   u32v4 q[KS], p[2 * HALVES][PP];  // P, in steps of 16 rows
@@ -169,46 +170,43 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
   };
   auto weights = [&](int i, f32x16 (&s)[HALVES], auto part) {
     const f32x4 ks = *(const f32x4*)sh_scale[i & 1][0], vs = *(const f32x4*)sh_scale[i & 1][1];
+    const int left = decltype(part)::value ? len - (step0 + i) * KT : KT;
     float by[SUBS], of[SUBS];
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u) {
-      by[u] = ks[u] * c;
-      of[u] = vs[u];
-    }
+    for (int u = 0; u < SUBS; ++u) by[u] = ks[u] * c;
+    float most_of, least_of;
+    auto logs = [&] {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) {
+        of[u] = u * 16 < left ? log_scale(vs[u], base) : 0.f;  // (rows that are not there have logits of -inf, whatever their scale)
+        most_of = u == 0 ? of[0] : fmaxf(most_of, of[u]);
+        least_of = u == 0 ? of[0] : fminf(least_of, of[u]);
+      }
+    };
+    logs();
     if constexpr (decltype(part)::value) {
       // Rows that are not there get -inf, by a product of a column that has it for them with ones.  (-inf times a factor of 0 would be none; what is no
       // number stays that.)
-      const int left = len - (step0 + i) * KT;
 #pragma unroll
       for (int t = 0; t < HALVES; ++t)
         s[t] = W::mma(u32v4{half == 0 && t * 32 + col >= left ? 0xfc00u : 0u, 0, 0, 0}, u32v4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}, s[t]);
 #pragma unroll
       for (int u = 0; u < SUBS; ++u) by[u] = by[u] < 1e-30f ? 1e-30f : by[u];
     }
-    // scales of V, as parts of the largest's power of two (from 2^-80 of it on: sums stay in fp32's range): a weight's is put into its exponent,
-    // and taken out of the sums
-    uint32_t largest = 0;
+    bool far_scales = false;
+    if (__builtin_expect(__any(fmaxf(most_of - kNearBase, -kFarBelow - least_of) > 0.f), 0)) {
+      if (__any(most_of > kNearBase)) {
+        float most = 0.f;
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u) largest = max(largest, __float_as_uint(of[u]) & 0x7fffffffu);
-    const int now_scale = __builtin_amdgcn_readfirstlane((int)(largest >> 23));
-    if (now_scale > top_scale) {
-      // m, which is of logits with their scale's logarithm, goes down; or the outputs, if the sums would leave the range.  (A scale that is no number:
-      // neither are the outputs, and the sums do not change.)
-      const int up = now_scale - top_scale;
-      const float more = __builtin_ldexpf(l, up);
-      if (now_scale == 255 || __any(more > 0x1p100f)) {
-        const float f = now_scale == 255 ? __uint_as_float(0x7fc00000u) : __builtin_ldexpf(1.f, -up);
-#pragma unroll
-        for (int d = 0; d < DT32; ++d) o[d] *= f;
-      } else {
-        m -= (float)up;
-        l = more;
+        for (int u = 0; u < SUBS; ++u) most = fmaxf(most, u * 16 < left ? vs[u] : 0.f);
+        const int now = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
+        m -= (float)(now - base);
+        sum.with(m, 1.f);
+        base = now;
+        logs();
       }
-      top_scale = now_scale;
+      far_scales = __any(least_of < -kFarBelow);
     }
-#pragma unroll
-    for (int u = 0; u < SUBS; ++u) of[u] = __builtin_amdgcn_logf(fmaxf(__builtin_ldexpf(of[u], 126 - top_scale), 0x1p-80f));
-
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
@@ -219,14 +217,50 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
     }
     top = max_across_32(top);
     if (__any(top > m + W::SLACK)) {
-      const float now = fmaxf(m, top);
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      l *= keep;
+      float x = -INFINITY;
 #pragma unroll
-      for (int d = 0; d < DT32; ++d) o[d] *= keep;
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e] * by[u]);
+      x = max_across_32(x);
+      if (top > m) {
+        const float keep = __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+        for (int d = 0; d < DT32; ++d) o[d] *= keep;
+        m = top;
+        sum.raise(x, 1.f);
+        sum.with(m, 1.f);
+      }
+    }
+    uint32_t apart = 0;  // sixteens whose weights are summed by themselves
+    if (__builtin_expect(far_scales, 0)) {
+      float x = -INFINITY, none = 0.f;
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) {
+        none += u * 16 < left ? vs[u] : 0.f;
+        if (sum.from_m - of[u] > kFar) {
+          apart |= 1u << u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e] * by[u]);
+        }
+      }
+      sum.raise(max_across_32(x), 1.f);
+      sum.with(m, 1.f);
+      const float R = (sum.R == -INFINITY ? 0.f : sum.R) - W::LIFT;
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+        if (apart >> u & 1) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum.l += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][u % 2 * 8 + e], by[u], -R));
+        }
+      // (a scale that is no number: neither are the outputs)
+      if (none != none) {
+#pragma unroll
+        for (int d = 0; d < DT32; ++d) o[d] *= none;
+      }
     }
     const float at = m == -INFINITY ? 0.f : m - W::LIFT;
+    float total[SUBS];
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
       const float less = at - of[u];
@@ -242,7 +276,15 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
         for (int k = 0; k < PP; ++k) p[u][k][e / 2] = part[k];
       }
-      l = __builtin_fmaf(sum0 + sum1, __builtin_amdgcn_exp2f(-of[u]), l);
+      total[u] = sum0 + sum1;
+    }
+    if (__builtin_expect(far_scales, 0)) {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+        if (!(apart >> u & 1)) sum.l = __builtin_fmaf(total[u], __builtin_amdgcn_exp2f(sum.from_m - of[u]), sum.l);
+    } else {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) sum.l = __builtin_fmaf(total[u], __builtin_amdgcn_exp2f(sum.from_m - of[u]), sum.l);
     }
   };
 
@@ -317,15 +359,16 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
     }
   }
 
-  // The scales put in, the type's factor in place of this kernel's, and channels where attend_wide_body has them.  (A last slice of sixteen that
+  // Relative to the sum's reference, with the type's factor in place of this kernel's, and channels where attend_wide_body has them.  (A last slice of sixteen that
   // is no whole one has the row's last eight channels, of which there are at most eight of its own, as its second half.)
   constexpr int LIFT = (int)(Wide<DT>::LIFT - W::LIFT);
+  const Power of(fmaxf(m - sum.R, -1e30f), base + LIFT);
   WideState<DP> x;
 #pragma unroll
   for (int i = 0; i < DP / 8; ++i) {
     const int to = eight(i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x.o[to / 4][to % 4 * 4 + e] = __builtin_ldexpf(o[i / 4][i % 4 * 4 + e], top_scale - 126 + LIFT);
+    for (int e = 0; e < 4; ++e) x.o[to / 4][to % 4 * 4 + e] = of.times(o[i / 4][i % 4 * 4 + e]);
   }
 #pragma unroll
   for (int slice = 0; slice < CPR; ++slice)
@@ -333,8 +376,8 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.o[slice / 2][slice % 2 * 8 + e] = x.o[slice / 2][slice % 2 * 8 + 4 + e];
     }
-  x.m = m;
-  x.l = __builtin_ldexpf(l, LIFT);
+  x.m = sum.R;
+  x.l = __builtin_ldexpf(sum.l, LIFT);
   return x;
 }
 

@@ -92,6 +92,15 @@ def test_few_rows(order, ratio, less, code, dtype):
         check(code, dtype, G, N, False, problem(code, G, N, D, order, ratio, abs(less), seed=D) if ratio > 0 else mirrored(code, G, N, D, order, -ratio, -less))
 
 
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+@CODES
+@APART
+@ORDERS
+def test_many_rows(order, ratio, less, code, dtype):
+    for G, N, D in ((4, 40, 128), (2, 70, 64), (3, 50, 256)):
+        check(code, dtype, G, N, True, problem(code, G, N, D, order, ratio, abs(less), seed=D) if ratio > 0 else mirrored(code, G, N, D, order, -ratio, -less))
+
+
 def mirrored(code, G, N, D, order, ratio, less):
     """The same with the kinds' blocks of 16 in turn within every step."""
     q, K, V, K_scale, V_scale = problem(code, G, N, D, order, ratio, less, seed=D)
@@ -101,7 +110,7 @@ def mirrored(code, G, N, D, order, ratio, less):
     return q, K[:, :, rows], V[:, :, rows], K_scale[:, :, turn], V_scale[:, :, turn]
 
 
-@pytest.mark.parametrize("G,N", [(2, 2)], ids=["few"])
+@pytest.mark.parametrize("G,N", [(2, 2), (4, 40)], ids=["few", "many"])
 @pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
 @CODES
 @ORDERS
