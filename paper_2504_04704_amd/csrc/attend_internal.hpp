@@ -41,9 +41,9 @@ struct AttendArgs {
   int32_t part_ld;  // D, rounded up to 4
   int32_t rows;    // of a unit
   int32_t row_tiles, splits;
-  int32_t part_splits, part_first;  // pieces of a unit, and the first of them that is this kernel's: `splits` and 0 but for rows behind ones in 8 bits
   Divide by_tiles, by_splits, by_n, by_h, by_g, by_rows;  // row_tiles, splits, N, H, G, rows
   float scale;  // times log2 e for the 16-bit types
+  int32_t part_splits, part_first;  // pieces of a unit, and the first of them that is this kernel's: `splits` and 0 but for rows behind ones in 8 bits
 };
 
 // Launch shape, a pure function of the parameters: rows of a tile, tiles of a unit, pieces the cache is cut into.

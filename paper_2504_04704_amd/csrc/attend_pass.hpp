@@ -249,18 +249,35 @@ constexpr int kAttendWaves = DP > 128 ? 1 : 2;
 template <int DT, int DP, int RT>
 constexpr bool kQueryInLds = DT == LAGKV_F32 && DP == 128 && RT == 2;
 
-// What a workgroup does, with AttendShape's MAIN bytes of LDS.
-template <int DT, int DP, int RT, int WAVES, bool PICK>
-__device__ __forceinline__ void attend_body(const AttendArgs& a, const WorkItem& w, char* lds) {
+// The kernels are also those of lagkv_attend_quantized's tail and new tokens: `Part` says what else a workgroup does.  (What follows is a kernel's own text, and not a
+// function of two kernels': as one it had twice the scalars spilled, read back lane by lane in the loops, and took up to 3 % longer.)
+struct RowsAlone {
+  using Args = AttendArgs;
+  static constexpr bool ALONE = true;
+  static __device__ __forceinline__ const AttendArgs& rows(const Args& a) { return a; }
+};
+
+template <int DT, int DP, int RT, int WAVES, bool PICK, typename Part>
+__global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend_kernel(const typename Part::Args args) {
   using E = AElem<DT>;
   using Sh = AttendShape<DT, DP, RT, WAVES>;
   constexpr int PER = Sh::PER, NC = Sh::NC, CPR = Sh::CPR, SUBS = E::SUBS, KT = Sh::KT, ROWS = Sh::ROWS, THREADS = WAVES * 64;
   constexpr int LDV = Sh::LDV, LDO = Sh::LDO, DT16 = DP / 16, NV = SUBS * NC, VROWS = 64 / CPR;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float sh_ml[WAVES][ROWS][2];
   __shared__ int32_t sh_parent[kMaxTree];
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
 
+  fetch_arguments<typename Part::Args>();
+  const AttendArgs& a = Part::rows(args);
+  uint32_t group = blockIdx.x;
+  if constexpr (!Part::ALONE) {
+    if (group < args.groups) return Part::go(args, lds);
+    group -= args.groups;
+  }
+  const WorkItem w = work_item(a, group);
+  if (!w.any) return;
   const uint32_t stream = PICK ? a.by_n.of((uint32_t)w.unit) : (uint32_t)w.unit, bu = a.by_h.of(stream);
   const int n_fixed = PICK ? (int)((uint32_t)w.unit - stream * a.N) : 0;
   const int64_t b = bu, h = stream - bu * a.H;
@@ -659,8 +676,9 @@ __device__ __forceinline__ void attend_body(const AttendArgs& a, const WorkItem&
     // the slots' channels: `dup` leading ones of a slice are the slice before's
     const int slot = quad * 4, begin = slot / PER * PER;
     const int base = begin < a.D ? slice_at(slot / PER, a.D, PER) : 0, dup = begin - base, within = slot - begin;
-    if (a.part_splits > 1) {
-      const int64_t at = (w.unit * a.part_splits + a.part_first + w.split) * a.rows + r;
+    const int pieces = Part::ALONE ? a.splits : a.part_splits;
+    if (pieces > 1) {
+      const int64_t at = (w.unit * pieces + (Part::ALONE ? 0 : a.part_first) + w.split) * a.rows + r;
       if (slices && begin < a.D) {
         *(f32x4*)(a.part_o + at * a.part_ld + slot) = v;
       } else if (begin < a.D) {
@@ -703,18 +721,10 @@ __device__ __forceinline__ void attend_body(const AttendArgs& a, const WorkItem&
 }
 
 template <int DT, int DP, int RT, int WAVES, bool PICK>
-__global__ __launch_bounds__(WAVES * 64, (kAttendWaves<DT, DP, RT>)) void attend_kernel(const AttendArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  fetch_arguments<AttendArgs>();
-  const WorkItem w = work_item(a);
-  if (w.any) attend_body<DT, DP, RT, WAVES, PICK>(a, w, lds);
-}
-
-template <int DT, int DP, int RT, int WAVES, bool PICK>
 hipError_t launch_attend_one(const AttendArgs& a, hipStream_t s) {
   const int64_t groups = (a.units * a.splits + 7) / 8 * 8 * a.row_tiles;
   constexpr size_t lds = AttendShape<DT, DP, RT, WAVES>::MAIN;
-  auto kernel = attend_kernel<DT, DP, RT, WAVES, PICK>;
+  auto kernel = attend_kernel<DT, DP, RT, WAVES, PICK, RowsAlone>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;

@@ -85,18 +85,6 @@ struct WideState {
   f32x16 o[DP / 32];
   float m, l;
 };
-template <int DP>
-__device__ __forceinline__ WideState<DP> no_rows_yet() {
-  WideState<DP> x;
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x.o[d][i] = 0.f;
-  x.m = -INFINITY;
-  x.l = 0.f;
-  return x;
-}
-
 // Steps of a unit's rows, up to what a tile of ROWS query rows sees of the new tokens.
 template <int DP, int ROWS>
 __device__ __forceinline__ int attend_wide_steps(const AttendArgs& a, const WorkItem& w) {
@@ -109,22 +97,29 @@ __device__ __forceinline__ int attend_wide_steps(const AttendArgs& a, const Work
   return (int)((len + KT - 1) / KT) + (seen_new + KT - 1) / KT;
 }
 
-// What a workgroup does, with two buffers of [K rows][V rows] in LDS: from a state on that `before` steps of its unit's rows, those of the piece
-// among them, have left.
-template <int DT, int DP, int WAVES>
-__device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const WorkItem& w, char* wide_lds, int before, const WideState<DP>& from) {
+// (RowsAlone, or a Part that has gone over other rows first: from its state on that `before` steps of the unit's rows, those of the piece among them, have left.)
+template <int DT, int DP, int WAVES, typename Part>
+__global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_kernel(const typename Part::Args args) {
   using E = AElem<DT>;
   using W = Wide<DT>;
   using Sh = WideShape<DP>;
   constexpr int KT = Sh::KT, CPR = Sh::CPR, LDK = Sh::LDK, LDV = Sh::LDV, THREADS = WAVES * 64, ROWS = WAVES * 32;
   constexpr int HALVES = KT / 32, KS = DP / 16, DT32 = DP / 32, PASSES = KT * CPR / THREADS;
   static_assert(KT * CPR % THREADS == 0, "");
+  extern __shared__ __attribute__((aligned(16))) char wide_lds[];  // two buffers of [K rows][V rows]
   __shared__ int32_t sh_parent[kMaxTree];
   __shared__ uint32_t sh_mask[ROWS * (kMaxTree / 32)];
   __shared__ int sh_odd[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int late = wave >> 2;  // (of the half of eight wavefronts that is a phase behind)
 
+  fetch_arguments<typename Part::Args>();
+  const AttendArgs& a = Part::rows(args);
+  const WorkItem w = work_item(a);
+  if (!w.any) return;
+  int before = 0;
+  WideState<DP> from;
+  if constexpr (!Part::ALONE) from = Part::go(args, w, wide_lds, attend_wide_steps<DP, ROWS>(a, w), before);
   const uint32_t bu = a.by_h.of((uint32_t)w.unit);
   const int64_t b = bu, h = (uint32_t)w.unit - bu * a.H;
   const int row0 = w.tile * ROWS, row1 = min(row0 + ROWS, a.rows);
@@ -134,8 +129,11 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const Work
   const int token0 = (int)a.by_g.of(row0), last_token = (int)a.by_g.of(row1 - 1), tokens = last_token - token0 + 1;
   const int seen_new = a.n_new > 0 ? (a.parents ? a.n_new : last_token + 1) : 0;
   const int steps = cache_steps + (seen_new + KT - 1) / KT;
-  const int all = before + steps, step0 = max((int)((int64_t)all * w.split / a.splits) - before, 0);
-  const int step1 = max((int)((int64_t)all * (w.split + 1) / a.splits) - before, 0);
+  int step0 = (int)((int64_t)(before + steps) * w.split / a.splits), step1 = (int)((int64_t)(before + steps) * (w.split + 1) / a.splits);
+  if constexpr (!Part::ALONE) {
+    step0 = max(step0 - before, 0);
+    step1 = max(step1 - before, 0);
+  }
   const int n = step1 - step0;
 
   const int words = (seen_new + 31) / 32;
@@ -257,11 +255,13 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const Work
     return bits;
   };
 
-  float m = from.m, l = from.l;  // m in units of base 2
+  float m = Part::ALONE ? -INFINITY : from.m, l = Part::ALONE ? 0.f : from.l;  // m in units of base 2
   f32x16 o[DT32], s[HALVES];
   u32v4 p[2 * HALVES], pl[2 * HALVES];  // P, in steps of 16 rows: its leading bits, and the rest
 #pragma unroll
-  for (int d = 0; d < DT32; ++d) o[d] = from.o[d];
+  for (int d = 0; d < DT32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = Part::ALONE ? 0.f : from.o[d][i];
 
   // Scores of step i and outputs of step i - 1, in one stream of products.  (Before the first step P and V are 0; behind the
   // last the scores are not used.)
@@ -397,8 +397,8 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const Work
   if (!mine) return;
   l = sum_across_32(l);
   const bool whole = a.D % 8 == 0;
-  if (a.part_splits > 1) {
-    const int64_t at = (w.unit * a.part_splits + a.part_first + w.split) * a.rows + r;
+  if (a.splits > 1) {
+    const int64_t at = (w.unit * a.splits + w.split) * a.rows + r;
     float* po = a.part_o + at * a.part_ld;
 #pragma unroll
     for (int d = 0; d < DT32; ++d)
@@ -454,18 +454,10 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const Work
 }
 
 template <int DT, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_kernel(const AttendArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char wide_lds[];
-  fetch_arguments<AttendArgs>();
-  const WorkItem w = work_item(a);
-  if (w.any) attend_wide_body<DT, DP, WAVES>(a, w, wide_lds, 0, no_rows_yet<DP>());
-}
-
-template <int DT, int DP, int WAVES>
 hipError_t launch_wide_as(const AttendArgs& a, hipStream_t s) {
   const int64_t groups = (a.units * a.splits + 7) / 8 * 8 * a.row_tiles;
   constexpr size_t lds = 2 * WideShape<DP>::BUF;
-  auto kernel = attend_wide_kernel<DT, DP, WAVES>;
+  auto kernel = attend_wide_kernel<DT, DP, WAVES, RowsAlone>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;

@@ -502,22 +502,20 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 
 // The pieces of rows in 8 bits and, by attend_pass.hpp's way, those of the tail and the new tokens: workgroups of one launch.
 template <int DT, int CODE, int DP, int RT>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attend_quant_kernel(const QuantBoth a) {
-  extern __shared__ __attribute__((aligned(16))) char quant_lds[];
-  fetch_arguments<QuantBoth>();
-  if (blockIdx.x < a.groups) {
+struct BesideCodes {
+  using Args = QuantBoth;
+  static constexpr bool ALONE = false;
+  static __device__ __forceinline__ const AttendArgs& rows(const Args& a) { return a.rows; }
+  static __device__ __forceinline__ void go(const Args& a, char* lds) {
     const WorkItem w = work_item(a.codes);
-    if (w.any) attend_quant_body<DT, CODE, DP, RT>(a.codes, w, quant_lds);
-  } else {
-    const WorkItem w = work_item(a.rows, blockIdx.x - a.groups);
-    if (w.any) attend_body<DT, DP, RT, 4, false>(a.rows, w, quant_lds);
+    if (w.any) attend_quant_body<DT, CODE, DP, RT>(a.codes, w, lds);
   }
-}
+};
 
 template <int DT, int CODE, int DP, int RT>
 hipError_t launch_quant_as(const QuantBoth& a, int64_t groups, hipStream_t s) {
   constexpr int of_codes = QuantShape<DP, RT>::MAIN, of_rows = AttendShape<DT, DP, RT, 4>::MAIN, lds = of_codes > of_rows ? of_codes : of_rows;
-  auto kernel = attend_quant_kernel<DT, CODE, DP, RT>;
+  auto kernel = attend_kernel<DT, DP, RT, 4, false, BesideCodes<DT, CODE, DP, RT>>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;

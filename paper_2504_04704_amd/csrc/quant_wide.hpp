@@ -382,24 +382,23 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 }
 
 // A piece goes over the rows in 8 bits, the tail and the new tokens as one line of steps: its workgroup does what of it is in 8 bits, and goes
-// on with the rest.  (With workgroups apart, as in attend_quant_kernel, 290 query rows of 128 streams x 508 rows and 8 took 62 us in place of
+// on with the rest.  (With workgroups apart, as in BesideCodes, 290 query rows of 128 streams x 508 rows and 8 took 62 us in place of
 // 48: every piece of a query row is 4 bytes a channel, written and read.)
 template <int DT, int CODE, int DP>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_quant_wide_kernel(const QuantBoth a) {
-  extern __shared__ __attribute__((aligned(16))) char wide_lds[];
-  fetch_arguments<QuantBoth>();
-  const WorkItem w = work_item(a.rows);
-  if (!w.any) return;
-  int steps;
-  const WideState<DP> x = attend_quant_wide_body<DT, CODE, DP>(a.codes, w, wide_lds, attend_wide_steps<DP, 128>(a.rows, w), steps);
-  attend_wide_body<DT, DP, 4>(a.rows, w, wide_lds, steps, x);
-}
+struct AfterCodes {
+  using Args = QuantBoth;
+  static constexpr bool ALONE = false;
+  static __device__ __forceinline__ const AttendArgs& rows(const Args& a) { return a.rows; }
+  static __device__ __forceinline__ WideState<DP> go(const Args& a, const WorkItem& w, char* lds, int others, int& steps) {
+    return attend_quant_wide_body<DT, CODE, DP>(a.codes, w, lds, others, steps);
+  }
+};
 
 template <int DT, int CODE, int DP>
 hipError_t launch_quant_wide_as(const QuantBoth& a, int64_t groups, hipStream_t s) {
   static_assert(QuantWideShape<DP>::BUF == WideShape<DP>::BUF, "");
   constexpr int lds = 2 * QuantWideShape<DP>::BUF;
-  auto kernel = attend_quant_wide_kernel<DT, CODE, DP>;
+  auto kernel = attend_wide_kernel<DT, DP, 4, AfterCodes<DT, CODE, DP>>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
