@@ -720,11 +720,13 @@ def _quant_params(x: Quantized, dtype) -> QuantParams:
     return p
 
 
-def quantize(K: torch.Tensor, V: torch.Tensor, block: int, code: torch.dtype = torch.int8, lengths: Optional[torch.Tensor] = None,
+def quantize(K: torch.Tensor, V: torch.Tensor, block: int, code: Optional[torch.dtype] = None, lengths: Optional[torch.Tensor] = None,
              start: int = 0, out: Optional[Quantized] = None) -> Quantized:
-    """lagkv_quantize: rows K, V [B,H,T,D] as codes (torch.int8 or torch.float8_e4m3fn) with a scale for each block of `block`
-    rows and head.  With `start` and `out` only the blocks from that of row `start` on are written; rows behind lengths[b] are left
-    as they are."""
+    """lagkv_quantize: rows K, V [B,H,T,D] as codes (torch.int8 or torch.float8_e4m3fn; those of `out`, or int8, where it is not said)
+    with a scale for each block of `block` rows and head.  With `start` and `out` only the blocks from that of row `start` on are
+    written; rows behind lengths[b] are left as they are."""
+    if out is not None and code is not None and code != out.K.dtype:
+        raise ValueError(f"out holds codes of {out.K.dtype}, not {code}")
     if _native is not None and out is not None and out.block == block:
         rc = _native.go_over(False, out.K, out.V, out.K_scale, out.V_scale, block, K, V, lengths, start)
         if rc >= 0:
@@ -740,6 +742,7 @@ def quantize(K: torch.Tensor, V: torch.Tensor, block: int, code: torch.dtype = t
     B, H, T, D = K.shape
     start = min(start, T)
     if out is None:
+        code = torch.int8 if code is None else code
         if code not in _CODES:
             raise TypeError(f"codes: unsupported dtype {code}")
         if start > 0:
