@@ -1091,6 +1091,13 @@ class QuantizedCache:
                  track_positions: bool = True, launch: int = 0):
         """`capacity`: rows in 8 bits; `window`: rows of the others (a call needs room for what is held there, fewer than block +
         2 L rows, and for its new ones; S + 4 L + block where it is not given)."""
+        # (what the operators would refuse of the first rows that become final is refused here)
+        if code not in _CODES:
+            raise TypeError(f"codes: unsupported dtype {code}")
+        block = index(block)
+        _int32("QuantizedCache", B, H, D, block)
+        p = QuantParams(B=B, H=H, G=1, D=D, dtype=_DTYPES[dtype], code=_CODES[code], block=block, T=capacity, scale=1.0)
+        _check(load().lagkv_attend_quantized_plan(C.byref(p), C.byref(AttendPlanT()), C.byref(AttendPlanT())), "QuantizedCache")
         self.rows = Quantized.empty(B, H, capacity, D, block, code, device)
         self.n = 0  # rows held in 8 bits
         self.pos = torch.empty((B, H, capacity), dtype=torch.int32, device=device) if track_positions else None
