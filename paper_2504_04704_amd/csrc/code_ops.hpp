@@ -11,7 +11,8 @@ template <int CODE>
 struct Code;
 template <>
 struct Code<LAGKV_CODE_INT8> {
-  // Four codes as binary16: with 128 added, a code is the low byte of a number between 1024 and 1279.
+  // Four codes as binary16: with 128 added, a code is the low byte of a number between 1024 and 1279 (a way from bytes to binary16 published by Kim et al.,
+  // "Who Says Elephants Can't Run", 2022).
   static __device__ __forceinline__ void to_half(uint32_t w, uint32_t& lo, uint32_t& hi) {
     const uint32_t u = w ^ 0x80808080u;
     const f16x2 k = {(_Float16)1152.f, (_Float16)1152.f};

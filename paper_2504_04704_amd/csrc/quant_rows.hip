@@ -3,8 +3,9 @@
 // With a = max |x| over a block, code = 127 x / a rounded (int8) or x / 2^e rounded to 4 mantissa bits (e4m3).  The block is
 // read once and waits in registers for its maximum: a wavefront or a workgroup of four takes a block, eight channels of a row a
 // lane at a time.  Bound by memory, at three bytes an element of 16 bits: 32 x 8 streams of 33536 rows with 128 channels, bf16 to int8,
-// blocks of 64, 1057 us (6.2 TB/s; a large copy reaches 5.1); 4 x 8 streams back to bf16 138 us (5.8 TB/s).  The vector
-// units are then busy too, with the exact quotients of int8, but e4m3, which has half as many instructions, takes no less.
+// blocks of 64, 1057 us (6.2 TB/s; a large copy reaches 5.1).  The vector units are then busy too, with the exact quotients of int8, but e4m3, which has half as
+// many instructions, takes no less.  4 x 8 streams back to bf16 138 to 142 us (6.0 to 5.8 TB/s), to fp32 314 (4.4).  A block of more than 16384 numbers is read
+// twice: 256 streams x 16384 rows of 256 channels in blocks of 128 rows 1433 us (4.5 TB/s), of 64 1066 (6.0).
 #include "code_ops.hpp"
 #include "lagkv_internal.hpp"
 #include "quant_internal.hpp"
@@ -305,14 +306,15 @@ void launch_quantize_as(const CodeArgs& a, hipStream_t s) {
   else if (n <= 256 * 8) quantize_kernel<DT, CODE, 4, 8, false, FAR><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
   else quantize_kernel<DT, CODE, 4, 4, true, false><<<groups_of<1>(a), dim3(256), 0, s>>>(a);
 }
-// Codes are stored past the caches, and rows beyond what these hold (256 MB) are read past them: 8 x 32 streams x 33536 rows, 128 channels of bf16
-// to int8, 1057 us in place of 1161 (the stores alone: 1131).  32 streams x 8192 rows, 268 MB, 60 in place of 71; rows of 65 MB in
+// Codes are stored past the caches, and rows that fill these (256 MiB) are read past them: 8 x 32 streams x 33536 rows, 128 channels of bf16
+// to int8, 1057 us in place of 1161 (the stores alone: 1131).  At 256 MiB, 64 streams x 8192 rows of 128 channels in bf16 take 65 us in place of 71 (e4m3 68
+// and 72), 32 of them in fp32 59 in place of 61; rows of 65 MB in
 // fp32, which the caches may still hold, would take 30 us in place of 24, and ones that are read again 117 in place of 107.  Rows on
 // their way back are stored as usual: past the caches the call itself takes 114 us in place of 135 at 512 MB, but with the one that
 // reads them 318 in place of 311.
 template <int DT, int CODE>
 hipError_t launch_quantize_of(const CodeArgs& a, hipStream_t s) {
-  const bool far = (double)a.units * a.block * a.D * AElem<DT>::SIZE > 268435456.0;
+  const bool far = (double)a.units * a.block * a.D * AElem<DT>::SIZE >= 268435456.0;
   if (far) launch_quantize_as<DT, CODE, true>(a, s);
   else launch_quantize_as<DT, CODE, false>(a, s);
   return hipGetLastError();
