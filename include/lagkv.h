@@ -468,10 +468,9 @@ int lagkv_attend_quantized_plan(const lagkv_quant_params* p, lagkv_attend_plan_t
  * tokens' own rows (K_new, V_new, parents, as there).  Lengths below 0 or above T and R count as 0, T and R; NULL: all.
  * out, lse, and what is no number: as of lagkv_attend.  (A row of the cache is none with a scale or, in e4m3, a code that is none; scales
  * are neither negative nor infinite.)
- * Codes go into the products as they are, which binary16 holds, and scales into logits and weights in fp32.  A query row goes in
- * as binary16 times a power of two: in bf16 and fp16 as it is (bf16: what is below 2^-14 of the row's largest off by up to 2^-25 of
- * it), in fp32 as two such numbers (off by up to 2^-23 of the largest).  Weights, times their rows' scales, go in as
- * two numbers of binary16 (22 bits).
+ * Codes go into the products as they are, which binary16 and bf16 hold, and scales into logits and weights in fp32.  A query row goes in
+ * as it is: fp32 as three numbers of bf16, which are all of its bits, and only what is below 2^-126 of the row's largest may be lost.  Weights,
+ * times their rows' scales, go in as two numbers of binary16 (22 bits).
  * They are relative to a query row's largest product of a weight and its scale, in whatever order and however far apart scales come; a scale of V
  * counts as 0 below 2^-125 of the largest before it.
  * The rest as of lagkv_attend: logits, sums and products in fp32, no atomics, its limits on sizes; LAGKV_ESHAPE from 2^26 query

@@ -2,7 +2,8 @@
 //
 // With codes k_t, v_t and their blocks' scales s_t, r_t the logits are x_t = scale s_t q.k_t and the outputs sum (p_t r_t) v_t: a
 // scale is a factor of a logit and of a weight, and the products take the codes as they are.  Binary16 holds them (whole numbers up to 128,
-// and numbers of 4 mantissa bits from 2^-9 to 448), so both products go to the matrix cores in that type, whatever that of Q.
+// and numbers of 4 mantissa bits from 2^-9 to 448), and so does bf16: the products with V go to the matrix cores in the first, with q in its own type (fp32: as three
+// numbers of bf16).
 //
 // A wavefront takes every fourth step of 64 cache rows (32 where 64 do not fit the registers) for all query rows of its workgroup; K's codes become
 // numbers in the registers that they are loaded into, V's on their way into LDS.  Scales are those of sixteen rows that
@@ -107,7 +108,8 @@ struct QuerySlots {
     return m;
   }
 };
-// The power of two, near a row's largest magnitude, that is taken out of the row where it is put into binary16; and its inverse.
+// The power of two, near a row's largest magnitude, that is taken out of the row before the products (which might leave fp32's range otherwise); and its inverse.
+// What is 2^-126 of the largest and more goes in as it is.
 struct QueryUnit {
   float unit, by;
   __device__ __forceinline__ explicit QueryUnit(float most) {
@@ -117,10 +119,11 @@ struct QueryUnit {
   }
 };
 
-// A lane's part of a query row as binary16: eight slots of each of 2 * NC, times a power of two (of fp32 the rest as well).
+// A lane's part of a query row: eight slots of each of 2 * NC, of bf16 and fp32 times a power of two.  fp32 is three numbers of bf16, each the leading bits of what
+// the ones before it leave.
 template <int DT, int NC>
 struct Query {
-  static constexpr int PARTS = DT == LAGKV_F32 ? 2 : 1;
+  static constexpr int PARTS = DT == LAGKV_F32 ? 3 : 1;
   u32v4 part[PARTS][2 * NC];
   float unit;  // that power's inverse
   __device__ __forceinline__ void load(const char* p, int grp, int D, bool there) {
@@ -144,28 +147,34 @@ struct Query {
       for (int j = 0; j < 2 * NC; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float x = raw[j].at(2 * i) * u.by, y = raw[j].at(2 * i + 1) * u.by;
-          const uint32_t hi = AElem<LAGKV_F16>::pack(x, y);
-          part[0][j][i] = hi;
-          if constexpr (PARTS == 2) {
-            const f32x2 back = __builtin_convertvector(__builtin_bit_cast(f16x2, hi), f32x2);
-            // (nothing is left of an infinity, and not NaN)
-            part[1][j][i] = AElem<LAGKV_F16>::pack(fabsf(x) < INFINITY ? x - back.x : 0.f, fabsf(y) < INFINITY ? y - back.y : 0.f);
+          uint32_t x = __float_as_uint(raw[j].at(2 * i) * u.by), y = __float_as_uint(raw[j].at(2 * i + 1) * u.by);
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k) {
+            part[k][j][i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            if (k + 1 == PARTS) break;
+            // (nothing is left of an infinity or of what is no number, which the first part is)
+            auto rest = [](uint32_t v) {
+              const float all = __uint_as_float(v), lead = __uint_as_float(v & 0xffff0000u);
+              return __float_as_uint(fabsf(all) < INFINITY ? all - lead : 0.f);
+            };
+            x = rest(x);
+            y = rest(y);
           }
         }
     }
   }
 };
 
-template <int CODE>
-__device__ __forceinline__ void half_of(u32v4 w, u32v4& lo, u32v4& hi) {
+// Sixteen codes as eight numbers twice, of binary16 or bf16.
+template <int CODE, int DT>
+__device__ __forceinline__ void numbers_of(u32v4 w, u32v4& lo, u32v4& hi) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     uint32_t a, b;
-    Code<CODE>::to_half(w[i], a, b);
+    codes_as<CODE, DT>(w[i], a, b);
     lo[2 * i] = a;
     lo[2 * i + 1] = b;
-    Code<CODE>::to_half(w[2 + i], a, b);
+    codes_as<CODE, DT>(w[2 + i], a, b);
     hi[2 * i] = a;
     hi[2 * i + 1] = b;
   }
@@ -270,7 +279,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
       // (a row that is not there: its codes may be no numbers)
       if (!whole && first + i * VROWS + vrow >= len) vf[i] = u32v4{0, 0, 0, 0};
       u32v4 lo, hi;
-      half_of<CODE>(vf[i], lo, hi);
+      numbers_of<CODE, LAGKV_F16>(vf[i], lo, hi);
       char* at = vl + (i * VROWS + vrow) * LDV + vslice * 32;
       *(u32v4*)at = lo;
       *(u32v4*)(at + 16) = hi;
@@ -291,13 +300,13 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         u32v4 k[2];
-        half_of<CODE>(kf[s][c], k[0], k[1]);
+        numbers_of<CODE, kKeyType<DT>>(kf[s][c], k[0], k[1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int part = 0; part < Query<DT, NC>::PARTS; ++part) p[rt][s] = F::mma(k[i], q[rt].part[part][c * 2 + i], p[rt][s]);
+            for (int part = 0; part < Query<DT, NC>::PARTS; ++part) p[rt][s] = AElem<kKeyType<DT>>::mma(k[i], q[rt].part[part][c * 2 + i], p[rt][s]);
       }
       x_scale[s] = ks[s] * a.scale;
     }

@@ -1,5 +1,5 @@
 // Attention of many query rows over rows in 8 bits (lagkv_attend_quantized of 16-bit types; when it is taken, quant_plan_of says).
-// attend_wide.hpp's way, by workgroups of four wavefronts with 32 query rows each, with quant_attend.hpp's numbers: the rows in LDS are binary16,
+// attend_wide.hpp's way, by workgroups of four wavefronts with 32 query rows each, with quant_attend.hpp's numbers: the rows in LDS are of 16 bits,
 // made of codes on the way from the registers that they are loaded into, and the scales of a step lie beside them.  (Eight wavefronts, 256 query rows, in
 // two phases as there were the better ones of 14 in 100 of 528 shapes, by 4 % in the mean.)
 //
@@ -29,7 +29,7 @@ struct QuantWideShape {
 // rows in 8 bits are.  `others`: steps of the rows behind them.
 template <int DT, int CODE, int DP>
 __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs& a, const WorkItem& w, char* wide_lds, int others, int& steps) {
-  using F = AElem<LAGKV_F16>;
+  constexpr int KEY = kKeyType<DT>;
   using W = Wide<LAGKV_F16>;
   using Sh = QuantWideShape<DP>;
   constexpr int KT = Sh::KT, SUBS = Sh::SUBS, CPR = Sh::CPR, LDK = Sh::LDK, LDV = Sh::LDV, THREADS = 256, ROWS = 128;
@@ -94,12 +94,12 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
   auto load_v = [&](int i) { load_rows(i, vp, vb, vr); };
   auto k_at = [&](int i) { return wide_lds + (i & 1) * (KT * LDK); };
   auto v_at = [&](int i) { return wide_lds + 2 * KT * LDK + (i & 1) * (KT * LDV); };
-  auto store = [&](const u32v4 (&from)[PASSES], char* to, int ld) {
+  auto store = [&](const u32v4 (&from)[PASSES], char* to, int ld, auto type) {
     to += lrow * ld + lslice * 16;
 #pragma unroll
     for (int k = 0; k < PASSES; ++k) {
       u32v4 lo, hi;
-      half_of<CODE>(from[k], lo, hi);
+      numbers_of<CODE, decltype(type)::value>(from[k], lo, hi);
       *(u32v4*)(to + k * LROWS * ld) = lo;
       *(u32v4*)(to + k * LROWS * ld + CPR * 16) = hi;
     }
@@ -148,7 +148,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
           return u32v4{y.x, y.y, z.x, z.y};
         },
         [&](int j, u32v4 f) {
-          if (j < NS) s[j % HALVES] = W::mma(f, q[j < NS ? j / HALVES : 0], s[j % HALVES]);
+          if (j < NS) s[j % HALVES] = Wide<KEY>::mma(f, q[j < NS ? j / HALVES : 0], s[j % HALVES]);
           else {
 #pragma unroll
             for (int k = 0; k < PP; ++k) o[(j - NS) % DT32] = W::mma(f, p[(j - NS) / DT32][k], o[(j - NS) % DT32]);
@@ -159,7 +159,8 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
           const int word = j / 2 % 4, pass_now = j / 8 % PASSES;
           const bool of_k = j / 8 >= PASSES;
           uint32_t x, y;
-          Code<CODE>::to_half(of_k ? kr[pass_now][word] : vr[pass_now][word], x, y);
+          if (of_k) codes_as<CODE, KEY>(kr[pass_now][word], x, y);
+          else codes_as<CODE, LAGKV_F16>(vr[pass_now][word], x, y);
           eight_now[word % 2 * 2] = x;
           eight_now[word % 2 * 2 + 1] = y;
           if (word % 2 == 1) {
@@ -313,12 +314,12 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
         u32v4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          v[i] = (DT == LAGKV_F16 ? raw[k].w[i] : F::pack(raw[k].at(2 * i) * u.by, raw[k].at(2 * i + 1) * u.by)) ^ flip;
+          v[i] = (DT == LAGKV_F16 ? raw[k].w[i] : __builtin_amdgcn_perm(__float_as_uint(raw[k].at(2 * i + 1) * u.by), __float_as_uint(raw[k].at(2 * i) * u.by), 0x07060302u)) ^ flip;
         asm volatile("" : "+v"(v));
         q[k] = v;
       }
     }
-    store(kr, k_at(0), LDK);
+    store(kr, k_at(0), LDK, std::integral_constant<int, KEY>());
     store_scales(0);
     load_k(1);
     __syncthreads();
@@ -334,8 +335,8 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
       for (int i = 0; i <= n; ++i) {
         if (i < n) {
           if (i >= n_whole) clear_v(i);
-          store(vr, v_at(i), LDV);
-          store(kr, k_at(i + 1), LDK);
+          store(vr, v_at(i), LDV, std::integral_constant<int, LAGKV_F16>());
+          store(kr, k_at(i + 1), LDK, std::integral_constant<int, KEY>());
           load_next(i);
         }
         __syncthreads();
