@@ -174,9 +174,9 @@ double quant_narrow_shape(const lagkv_quant_params* p, const QuantForm& f, int64
 }
 
 // The kernel of many rows: tiles of 128, and the pieces of all rows.
-// Of both: over 3268 shapes (17 to 4000 query rows of 1 to 256 streams, 64 to 256 channels, 64 to 65536 rows in 8 bits and up to 2048 behind them, some
-// with lengths that differ; bf16 and fp16) the choice takes 2.1 % longer in the mean than the best form and pieces of up to 128 that were measured: half of them
-// at most 0.1 %, nine in ten 8 %.
+// Of both: over 4417 shapes (1 to 4000 query rows of 1 to 256 streams, 64 to 256 channels, 64 to 65536 rows in 8 bits and up to 2048 behind them, some
+// with lengths that differ; all types) the choice takes 2.4 % longer in the mean than the best form and pieces of up to 128 that were measured: half of them
+// at most 0.1 %, nine in ten 9 %.
 double quant_wide_shape(const lagkv_quant_params* p, int64_t units, int64_t rows, int* pieces) {
   const int64_t kt = p->D > 128 ? 32 : 64, steps = (p->T + kt - 1) / kt + (p->R + kt - 1) / kt + (p->N + kt - 1) / kt;
   const int64_t tiles = (rows + 127) / 128, places = p->D > 128 ? 32 : 64;

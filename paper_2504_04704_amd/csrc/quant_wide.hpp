@@ -8,10 +8,11 @@
 //
 // Codes become numbers behind the products, one word at a time, and a wavefront that multiplies goes before the other workgroup's on its SIMD,
 // whose weights then fill the cycles between products: without either 212 us in place of 183, with one of them alone 209 and 205 (256
-// query rows of 32 streams x 33536 rows, 128 channels, bf16, int8).  Given to the wavefront that makes weights, priority gains 2 us.
+// query rows of 32 streams x 33536 rows, 128 channels, bf16, int8; weights as one number, as in the next comparisons).  Given to the wavefront that
+// makes weights, priority gains 2 us.
 //
-// Bound by the vector instructions (some 260 a step and wavefront) and the matrix cores (32 products of 32 cycles) together, and by what two
-// wavefronts on a SIMD cannot overlap of them: 0.77 Pflop/s.
+// Bound by the vector instructions (some 320 a step and wavefront, 62 % of the cycles) and the matrix cores (48 products of 32 cycles, 59 %) together, of which two
+// wavefronts on a SIMD overlap a part: 209 to 212 us for those rows in e4m3, 0.67 Pflop/s (a product with V counted once).
 #pragma once
 #include "attend_wide.hpp"
 #include "quant_attend.hpp"
