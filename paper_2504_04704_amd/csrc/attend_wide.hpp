@@ -85,6 +85,7 @@ struct WideState {
   f32x16 o[DP / 32];
   float m, l;
 };
+
 // Steps of a unit's rows, up to what a tile of ROWS query rows sees of the new tokens.
 template <int DP, int ROWS>
 __device__ __forceinline__ int attend_wide_steps(const AttendArgs& a, const WorkItem& w) {
