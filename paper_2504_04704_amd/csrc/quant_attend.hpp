@@ -8,8 +8,8 @@
 // A wavefront takes every fourth step of 64 cache rows (32 where 64 do not fit the registers) for all query rows of its workgroup; K's codes become
 // numbers in the registers that they are loaded into, V's on their way into LDS.  Scales are those of sixteen rows that
 // lie in one block.  Weights times scales go in as two numbers of binary16 (split_weights).  They are exponentials of logits with their scale's
-// logarithm, relative to the largest of these (m), so that it does not matter how far apart scales are, nor which of them comes first; the weights' sum,
-// without the scales, is relative to a reference of its own (R, WeightSum).
+// logarithm, relative to the largest of these, so that it does not matter how far apart scales are, nor which of them comes first; the weights' sum is without the
+// scales (see Sums).
 //
 // Each piece of a cache leaves its maximum, sum and outputs; launch_attend_join joins them with those of the tail and the new tokens, which
 // other workgroups of the same launch have gone over.
@@ -30,23 +30,27 @@ constexpr int kNoBase = -1000;  // (any scale is inf beside it)
 constexpr float kNearBase = 16.f;
 __device__ __forceinline__ float log_scale(float s, int base) { return fmaxf(__builtin_amdgcn_logf(__builtin_ldexpf(s, -base)), -INFINITY); }
 
-// The sum of a query row's weights, relative to exp(R), R a logit near the largest.  The weights that go into the products have their scales in them: sum(exp(x + s - m)) over
-// sixteen rows of a scale exp(s) is brought back by exp(m - R - s).  That is done up to 2^kFar; beyond, those products may have left the range of fp32 while their weights
-// are a large part of the sum, and these are worked out by themselves.  (m is that of a row whose logit R is not below and whose s is kNearBase + 1 at most: from
-// s = -kFarBelow on the factor is no larger.)
+// What a query row's sums are relative to.  R is a logit near the largest: l = sum exp(x - R) over its rows.  The weights in the products have their row's scale exp(s) in them, and
+// are relative to exp(R + a), a the largest x - R + s: o = sum exp(x - R + s - a) v.  (R and a by themselves: their sum would lose a where R is large.)  l is made of the same exponentials,
+// of sixteen rows of a scale times exp(a - s).  That is done up to 2^kFar; beyond, those may have left the range of fp32 while they are a large part of the sum,
+// and are worked out by themselves.  (a is of a row whose logit R is not below and whose s is kNearBase + 1 at most: from s = -kFarBelow on the factor is no larger.)
 constexpr float kFar = 64.f, kFarBelow = kFar - kNearBase - 1.f;
-struct WeightSum {
-  float R, l, from_m;  // (the last: m - R in base 2, or something below all numbers that matter where there are no rows of m, or none at all)
+constexpr float kNoLogit = -3.40282347e38f, kNoWeight = -1e30f;  // R and a where there are none yet: less than any, but numbers
+struct Sums {
+  float R = kNoLogit, l = 0.f, a = kNoWeight;  // a in base 2
   __device__ __forceinline__ void raise(float to, float unit) {
     if (to > R) {
-      l *= __builtin_amdgcn_exp2f((R - to) * unit);
+      const float down = (R - to) * unit;
+      l *= __builtin_amdgcn_exp2f(down);
+      a = fmaxf(a + down, kNoWeight);
       R = to;
     }
   }
-  __device__ __forceinline__ void with(float m, float unit) { from_m = fmaxf((m - R) * unit, -1e30f); }
+  // R as it is joined with others': what is no number, or saw nothing, has -inf
+  __device__ __forceinline__ float reference() const { return R == kNoLogit ? -INFINITY : R; }
 };
 
-// 2^(x + more) as a factor of what may be as far from 1 as it is.
+// 2^(x + more), as a factor of what may be as far from 1 as it is.
 struct Power {
   float f;
   int e;
@@ -183,6 +187,7 @@ __device__ __forceinline__ void numbers_of(u32v4 w, u32v4& lo, u32v4& hi) {
 // What a workgroup does with a piece of the rows in 8 bits.
 template <int DT, int CODE, int DP, int RT>
 __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const WorkItem& w, char* quant_lds) {
+#pragma clang fp contract(off)  // (a logit is rounded before R, one of them, is taken from it: where logits are large, the rounding is more than a weight's exponent holds)
   using E = AElem<DT>;
   using F = AElem<LAGKV_F16>;
   using Sh = QuantShape<DP, RT>;
@@ -258,17 +263,13 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     const int r = row0 + rt * 16 + col, rr = r < row1 ? r : row0, n = (int)a.by_g.of(rr);
     q[rt].load(a.Q + b * a.qsb + (h * a.G + rr - n * a.G) * a.qsh + (int64_t)n * a.qsn, grp, a.D, r < row1);
   }
-  float m[RT];        // of logits with their scale's logarithm: what o is relative to
-  WeightSum sum[RT];  // (of this lane's cache rows)
+  Sums sum[RT];  // (l of this lane's cache rows)
   f32x4 o[RT][DT16];
   int base = kNoBase;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = -INFINITY;
-    sum[rt] = WeightSum{-INFINITY, 0.f, -1e30f};
+  for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int d = 0; d < DT16; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
 
   for (; step < step1; step += WAVES) {
     const bool more = step + WAVES < step1, whole = (step + 1) * KT <= len;
@@ -314,7 +315,6 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     if (more) load_k(step + WAVES);
     __builtin_amdgcn_sched_barrier(0);
 
-    constexpr float LOG2 = E::UNIT == 1.f ? 1.f : 0.693147180559945f;  // 1 in base 2, in units of the logits
     float most_of, least_of;
     auto logs = [&] {
 #pragma unroll
@@ -332,10 +332,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
       for (int s = 0; s < SUBS; ++s) most = fmaxf(most, scale[s]);
       const int now = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        m[rt] -= (float)(now - base) * LOG2;
-        sum[rt].with(m[rt], E::UNIT);
-      }
+      for (int rt = 0; rt < RT; ++rt) sum[rt].a = fmaxf(sum[rt].a - (float)(now - base), kNoWeight);
       base = now;
       logs();
     }
@@ -353,52 +350,47 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
           for (int i = 0; i < 4; ++i)
             if (first + s * 16 + grp * 4 + i >= len) p[rt][s][i] = -INFINITY;
       }
-      float top = -INFINITY;
+      float most[SUBS];
 #pragma unroll
-      for (int s = 0; s < SUBS; ++s) {
-        float x = p[rt][s][0];
-#pragma unroll
-        for (int i = 1; i < 4; ++i) x = fmaxf(x, p[rt][s][i]);
-        top = fmaxf(top, __builtin_fmaf(of[s], LOG2, x));
-      }
-      top = max_across_32(max_across_16(top));
-      if (__any(top > m[rt])) {
+      for (int s = 0; s < SUBS; ++s) most[s] = fmaxf(fmaxf(p[rt][s][0], p[rt][s][1]), fmaxf(p[rt][s][2], p[rt][s][3]));
+      auto largest = [&] {
         float x = -INFINITY;
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s)
+        for (int s = 0; s < SUBS; ++s) x = fmaxf(x, __builtin_fmaf(most[s] - sum[rt].R, E::UNIT, of[s]));
+        return max_across_32(max_across_16(x));
+      };
+      float top = largest();
+      if (__any(top > sum[rt].a)) {
+        float x = most[0];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x = fmaxf(x, p[rt][s][i]);
+        for (int s = 1; s < SUBS; ++s) x = fmaxf(x, most[s]);
         x = max_across_32(max_across_16(x));
-        if (top > m[rt]) {
-          const float keep = __builtin_amdgcn_exp2f((m[rt] - top) * E::UNIT);
+        if (top > sum[rt].a) sum[rt].raise(x, E::UNIT);
+        top = largest();
+        if (top > sum[rt].a) {
+          const float keep = __builtin_amdgcn_exp2f(sum[rt].a - top);
 #pragma unroll
           for (int d = 0; d < DT16; ++d) o[rt][d] *= keep;
-          m[rt] = top;
-          sum[rt].raise(x, E::UNIT);
-          sum[rt].with(m[rt], E::UNIT);
+          sum[rt].a = top;
         }
       }
-      const float at = m[rt] == -INFINITY ? 0.f : m[rt];
       uint32_t apart = 0;  // sixteens whose weights are summed by themselves
       if (__builtin_expect(far_scales, 0)) {
         float x = -INFINITY, none = 0.f;
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
           none += scale[s];
-          if (sum[rt].from_m - of[s] > kFar) {
+          if (sum[rt].a - of[s] > kFar) {
             apart |= 1u << s;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x = fmaxf(x, p[rt][s][i]);
+            x = fmaxf(x, most[s]);
           }
         }
         sum[rt].raise(max_across_32(max_across_16(x)), E::UNIT);
-        sum[rt].with(m[rt], E::UNIT);
-        const float R = sum[rt].R == -INFINITY ? 0.f : sum[rt].R;
 #pragma unroll
         for (int s = 0; s < SUBS; ++s)
           if (apart >> s & 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[rt].l += __builtin_amdgcn_exp2f(__builtin_fmaf(p[rt][s][i] - R, E::UNIT, kQuantLift));
+            for (int i = 0; i < 4; ++i) sum[rt].l += __builtin_amdgcn_exp2f(__builtin_fmaf(p[rt][s][i] - sum[rt].R, E::UNIT, kQuantLift));
           }
         // (a scale that is no number: neither are the outputs)
         if (none != none) {
@@ -413,17 +405,17 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // (the difference first: its rounding is that of a number near zero)
-          p[rt][s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[rt][s][i] - at, E::UNIT, of[s] + kQuantLift));
+          p[rt][s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[rt][s][i] - sum[rt].R, E::UNIT, of[s] - sum[rt].a + kQuantLift));
           y[s] += p[rt][s][i];
         }
       }
       if (__builtin_expect(far_scales, 0)) {
 #pragma unroll
         for (int s = 0; s < SUBS; ++s)
-          if (!(apart >> s & 1)) sum[rt].l = __builtin_fmaf(y[s], __builtin_amdgcn_exp2f(sum[rt].from_m - of[s]), sum[rt].l);
+          if (!(apart >> s & 1)) sum[rt].l = __builtin_fmaf(y[s], __builtin_amdgcn_exp2f(sum[rt].a - of[s]), sum[rt].l);
       } else {
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s) sum[rt].l = __builtin_fmaf(y[s], __builtin_amdgcn_exp2f(sum[rt].from_m - of[s]), sum[rt].l);
+        for (int s = 0; s < SUBS; ++s) sum[rt].l = __builtin_fmaf(y[s], __builtin_amdgcn_exp2f(sum[rt].a - of[s]), sum[rt].l);
       }
 #pragma unroll
       for (int s = 0; s < SUBS; ++s)
@@ -455,7 +447,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (grp == 0) {
-      sh_ml[wave][rt * 16 + col][0] = sum[rt].R;
+      sh_ml[wave][rt * 16 + col][0] = sum[rt].reference();
       sh_ml[wave][rt * 16 + col][1] = l;
     }
   }
@@ -467,7 +459,7 @@ __device__ __forceinline__ void attend_quant_body(const QuantArgs& a, const Work
 #pragma unroll
     for (int x = 0; x < WAVES; ++x) top = fmaxf(top, sh_ml[x][rt * 16 + col][0]);
     const bool none = sh_ml[wave][rt * 16 + col][1] == 0.f;  // (what is no number has a reference of -inf too, and is not dropped)
-    const Power of(fmaxf((m[rt] - top) * E::UNIT, -1e30f), base + LIFT);
+    const Power of(fmaxf(sum[rt].a + (sum[rt].R - top) * E::UNIT, kNoWeight), base + LIFT);
 #pragma unroll
     for (int d = 0; d < DT16; ++d) {
       f32x4 y;

@@ -19,6 +19,8 @@
 
 namespace lagkv {
 
+constexpr float kLargeLogit = 0x1p16f;  // in base 2
+
 template <int DP>
 struct QuantWideShape {
   static constexpr int KT = DP > 128 ? 32 : 64, SUBS = KT / 16, CPR = DP / 16;
@@ -116,8 +118,8 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
   };
 
   float c = 0.f;                   // what a query row's products are multiplied by, without the cache rows' scales
-  float m = -INFINITY;             // of logits in base 2 with their scale's logarithm: what o is relative to
-  WeightSum sum = {-INFINITY, 0.f, -1e30f};
+  Sums sum;                        // (l of this half's cache rows)
+  float k_most = 0.f;              // a scale of K with which logits may be large
   int base = kNoBase;
   f32x16 o[DT32];
   constexpr int PP = kWeightParts;
@@ -170,6 +172,12 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
           }
         });
   };
+  // (Rounded by itself, as R was, which is one of them: of logits so large that fp32 does not hold their fractions the difference is to be that of two rounded ones.)
+  auto logit = [](float product, float by) {
+    float x = product * by;
+    asm("" : "+v"(x));
+    return x;
+  };
   auto weights = [&](int i, f32x16 (&s)[HALVES], auto part) {
     const f32x4 ks = *(const f32x4*)sh_scale[i & 1][0], vs = *(const f32x4*)sh_scale[i & 1][1];
     const int left = decltype(part)::value ? len - (step0 + i) * KT : KT;
@@ -195,43 +203,50 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
       for (int u = 0; u < SUBS; ++u) by[u] = by[u] < 1e-30f ? 1e-30f : by[u];
     }
-    bool far_scales = false;
-    if (__builtin_expect(__any(fmaxf(most_of - kNearBase, -kFarBelow - least_of) > 0.f), 0)) {
-      if (__any(most_of > kNearBase)) {
-        float most = 0.f;
-#pragma unroll
-        for (int u = 0; u < SUBS; ++u) most = fmaxf(most, u * 16 < left ? vs[u] : 0.f);
-        const int now = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
-        m -= (float)(now - base);
-        sum.with(m, 1.f);
-        base = now;
-        logs();
-      }
-      far_scales = __any(least_of < -kFarBelow);
-    }
-    float top = -INFINITY;
+    float xs[SUBS];  // the largest logit of each scale's rows (by is not negative)
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
       float x = s[u / 2][u % 2 * 8];
 #pragma unroll
       for (int e = 1; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e]);
-      top = fmaxf(top, __builtin_fmaf(x, by[u], of[u]));
+      xs[u] = logit(x, by[u]);
     }
-    top = max_across_32(top);
-    if (__any(top > m + W::SLACK)) {
+    bool far_scales = false, large = false;
+    float most_k = ks[0];
+#pragma unroll
+    for (int u = 1; u < SUBS; ++u) most_k = fmaxf(most_k, ks[u]);
+    if (__builtin_expect(__any(!(most_of <= kNearBase && least_of >= -kFarBelow && most_k < k_most)), 0)) {
+      large = __any(!(most_k < k_most));
+      if (__any(most_of > kNearBase)) {
+        float most = 0.f;
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) most = fmaxf(most, u * 16 < left ? vs[u] : 0.f);
+        const int now = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
+        sum.a = fmaxf(sum.a - (float)(now - base), kNoWeight);
+        base = now;
+        logs();
+      }
+      far_scales = __any(least_of < -kFarBelow);
+    }
+    auto largest = [&] {
       float x = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u)
+      for (int u = 0; u < SUBS; ++u) x = fmaxf(x, xs[u] - sum.R + of[u]);
+      return max_across_32(x);
+    };
+    float top = largest();
+    if (__any(top > sum.a + W::SLACK)) {
+      float x = xs[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e] * by[u]);
+      for (int u = 1; u < SUBS; ++u) x = fmaxf(x, xs[u]);
       x = max_across_32(x);
-      if (top > m) {
-        const float keep = __builtin_amdgcn_exp2f(m - top);
+      if (top > sum.a) sum.raise(x, 1.f);
+      top = largest();
+      if (top > sum.a) {
+        const float keep = __builtin_amdgcn_exp2f(sum.a - top);
 #pragma unroll
         for (int d = 0; d < DT32; ++d) o[d] *= keep;
-        m = top;
-        sum.raise(x, 1.f);
-        sum.with(m, 1.f);
+        sum.a = top;
       }
     }
     uint32_t apart = 0;  // sixteens whose weights are summed by themselves
@@ -240,20 +255,17 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
       for (int u = 0; u < SUBS; ++u) {
         none += u * 16 < left ? vs[u] : 0.f;
-        if (sum.from_m - of[u] > kFar) {
+        if (sum.a - of[u] > kFar) {
           apart |= 1u << u;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x = fmaxf(x, s[u / 2][u % 2 * 8 + e] * by[u]);
+          x = fmaxf(x, xs[u]);
         }
       }
       sum.raise(max_across_32(x), 1.f);
-      sum.with(m, 1.f);
-      const float R = (sum.R == -INFINITY ? 0.f : sum.R) - W::LIFT;
 #pragma unroll
       for (int u = 0; u < SUBS; ++u)
         if (apart >> u & 1) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum.l += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][u % 2 * 8 + e], by[u], -R));
+          for (int e = 0; e < 8; ++e) sum.l += __builtin_amdgcn_exp2f(logit(s[u / 2][u % 2 * 8 + e], by[u]) - sum.R + W::LIFT);
         }
       // (a scale that is no number: neither are the outputs)
       if (none != none) {
@@ -261,32 +273,36 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
         for (int d = 0; d < DT32; ++d) o[d] *= none;
       }
     }
-    const float at = m == -INFINITY ? 0.f : m - W::LIFT;
     float total[SUBS];
+    auto exponentials = [&](auto weight_of) {
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u) {
-      const float less = at - of[u];
-      float sum0 = 0.f, sum1 = 0.f;
+      for (int u = 0; u < SUBS; ++u) {
+        float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][u % 2 * 8 + e], by[u], -less));
-        const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u / 2][u % 2 * 8 + e + 1], by[u], -less));
-        sum0 += y;
-        sum1 += z;
-        uint32_t part[PP];
-        split_weights(y, z, part);
+        for (int e = 0; e < 8; e += 2) {
+          const float y = weight_of(u, s[u / 2][u % 2 * 8 + e]), z = weight_of(u, s[u / 2][u % 2 * 8 + e + 1]);
+          sum0 += y;
+          sum1 += z;
+          uint32_t part[PP];
+          split_weights(y, z, part);
 #pragma unroll
-        for (int k = 0; k < PP; ++k) p[u][k][e / 2] = part[k];
+          for (int k = 0; k < PP; ++k) p[u][k][e / 2] = part[k];
+        }
+        total[u] = sum0 + sum1;
       }
-      total[u] = sum0 + sum1;
-    }
+    };
+    float more[SUBS];
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) more[u] = of[u] - (sum.a - W::LIFT) - (large ? 0.f : sum.R);
+    if (__builtin_expect(large, 0)) exponentials([&](int u, float x) { return __builtin_amdgcn_exp2f(logit(x, by[u]) - sum.R + more[u]); });
+    else exponentials([&](int u, float x) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, by[u], more[u])); });
     if (__builtin_expect(far_scales, 0)) {
 #pragma unroll
       for (int u = 0; u < SUBS; ++u)
-        if (!(apart >> u & 1)) sum.l = __builtin_fmaf(total[u], __builtin_amdgcn_exp2f(sum.from_m - of[u]), sum.l);
+        if (!(apart >> u & 1)) sum.l = __builtin_fmaf(total[u], __builtin_amdgcn_exp2f(sum.a - of[u]), sum.l);
     } else {
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) sum.l = __builtin_fmaf(total[u], __builtin_amdgcn_exp2f(sum.from_m - of[u]), sum.l);
+      for (int u = 0; u < SUBS; ++u) sum.l = __builtin_fmaf(total[u], __builtin_amdgcn_exp2f(sum.a - of[u]), sum.l);
     }
   };
 
@@ -302,12 +318,15 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
     // here, behind the first rows' loads.)
     {
       const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-      float most = 0.f;
+      float most = 0.f, size = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         raw[k].own(eight(2 * k + half), a.D, mine);
         if constexpr (DT != LAGKV_F16) most = raw[k].most(most);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) size += fabsf(raw[k].at(e));
       }
+      k_most = kLargeLogit / (sum_across_32(size) * fabsf(a.scale) * (CODE == LAGKV_CODE_INT8 ? 128.f : 448.f));
       const QueryUnit u(max_across_32(most));
       c = fabsf(a.scale) * (DT == LAGKV_F16 ? 1.f : u.unit);
 #pragma unroll
@@ -364,7 +383,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
   // Relative to the sum's reference, with the type's factor in place of this kernel's, and channels where attend_wide_body has them.  (A last slice of sixteen that
   // is no whole one has the row's last eight channels, of which there are at most eight of its own, as its second half.)
   constexpr int LIFT = (int)(Wide<DT>::LIFT - W::LIFT);
-  const Power of(fmaxf(m - sum.R, -1e30f), base + LIFT);
+  const Power of(sum.a, base + LIFT);
   WideState<DP> x;
 #pragma unroll
   for (int i = 0; i < DP / 8; ++i) {
@@ -378,7 +397,7 @@ __device__ __forceinline__ WideState<DP> attend_quant_wide_body(const QuantArgs&
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.o[slice / 2][slice % 2 * 8 + e] = x.o[slice / 2][slice % 2 * 8 + 4 + e];
     }
-  x.m = sum.R;
+  x.m = sum.reference();
   x.l = __builtin_ldexpf(sum.l, LIFT);
   return x;
 }
