@@ -325,7 +325,7 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
     top = max_across_32(top) * c;
-    if (__any(top > m + W::SLACK)) {
+    if (__any(top - m > W::SLACK)) {
       const float now = fmaxf(m, top);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
       m = now;
@@ -333,22 +333,34 @@ __global__ __launch_bounds__(WAVES * 64, DP <= 128 ? 2 : 1) void attend_wide_ker
 #pragma unroll
       for (int d = 0; d < DT32; ++d) o[d] *= keep;
     }
-    const float at = m == -INFINITY ? 0.f : m - W::LIFT;
-    float sum0 = 0.f, sum1 = 0.f;
+    auto exponentials = [&](auto weight_of) {
+      float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-    for (int t = 0; t < HALVES; ++t)
+      for (int t = 0; t < HALVES; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], c, -at));
-        const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e + 1], c, -at));
-        sum0 += y;
-        sum1 += z;
-        uint32_t hi, lo;
-        E::split(y, z, hi, lo);
-        p[t * 2 + e / 8][e % 8 / 2] = hi;
-        pl[t * 2 + e / 8][e % 8 / 2] = lo;
-      }
-    l += sum0 + sum1;
+        for (int e = 0; e < 16; e += 2) {
+          const float y = weight_of(s[t][e]), z = weight_of(s[t][e + 1]);
+          sum0 += y;
+          sum1 += z;
+          uint32_t hi, lo;
+          E::split(y, z, hi, lo);
+          p[t * 2 + e / 8][e % 8 / 2] = hi;
+          pl[t * 2 + e / 8][e % 8 / 2] = lo;
+        }
+      l += sum0 + sum1;
+    };
+    const float at = m == -INFINITY ? 0.f : m;
+    if (__builtin_expect(__any(fabsf(at) > 0x1p16f), 0)) {
+      // (so large that fp32 soon does not hold their fractions: m is a rounded logit, and so is to be what it is taken from)
+      exponentials([&](float x) {
+        float y = x * c;
+        asm("" : "+v"(y));
+        return __builtin_amdgcn_exp2f(y - at + W::LIFT);
+      });
+    } else {
+      const float less = at - W::LIFT;
+      exponentials([&](float x) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, -less)); });
+    }
   };
 
   if (n > 0) {
