@@ -15,7 +15,7 @@
 // other workgroups of the same launch have gone over.
 //
 // Bound by memory where there are rows enough: one token each of 32 requests, 8 heads of 128 channels (bf16, up to 8128 rows in int8 and 256 behind them)
-// 87 to 90 us, 5.0 TB/s, and 4 for the join; where there are few, by latency: one request's 4032 rows 10.6 us and 2.5.
+// 85 to 90 us, 5.0 TB/s, and 4 for the join; where there are few, by latency: one request's 4032 rows 10.7 us and 2.5 to 3.
 #pragma once
 #include "code_ops.hpp"
 #include "quant_internal.hpp"

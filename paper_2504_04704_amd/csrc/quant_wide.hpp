@@ -11,8 +11,8 @@
 // query rows of 32 streams x 33536 rows, 128 channels, bf16, int8; weights as one number, as in the next comparisons).  Given to the wavefront that
 // makes weights, priority gains 2 us.
 //
-// Bound by the vector instructions (some 320 a step and wavefront, 62 % of the cycles) and the matrix cores (48 products of 32 cycles, 59 %) together, of which two
-// wavefronts on a SIMD overlap a part: 209 to 212 us for those rows in e4m3, 0.67 Pflop/s (a product with V counted once).
+// Bound by the vector instructions (some 335 a step and wavefront, 64 % of the cycles) and the matrix cores (48 products of 32 cycles, 59 %) together, of which two
+// wavefronts on a SIMD overlap a part: 217 to 221 us for those rows in e4m3, 0.65 Pflop/s (a product with V counted once).
 #pragma once
 #include "attend_wide.hpp"
 #include "quant_attend.hpp"
